@@ -310,6 +310,40 @@ int kvp_decode(const kvp_decode_desc* d, const int32_t* donor, float scale, cons
                const int32_t* lengths, void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws,
                size_t ws_bytes, kvp_stream_t stream);
 
+/* Appending any number of tokens, with the rotary positions applied on the way (the paper has no counterpart: prompts enter the
+ * cache behind kvp_attn_fwd, and the sequences of a batch stand at positions of their own).  T rows of new tokens; sequence b
+ * has rows first[b] .. first[b+1]-1 (first: DEVICE int32 [B+1], non-decreasing), at positions lengths[b] - n .. lengths[b] - 1,
+ * n of them; lengths include them.  first == NULL: one token a sequence, T == B.  Tokens at positions outside
+ * [0, max_pages*page_size) and rows outside all sequences are left out: nothing of theirs is written (so a place of a padded
+ * batch has length 0).
+ *   k_new[l], v_new[l]  [T,Hkv,dh], owners only; q[l], q_out[l]  [T,Hq,dh], every layer, or both arrays NULL.
+ *   theta               pairs (x[2i], x[2i+1]) of K and q are rotated by position * theta^(-2i/dh), as kvp_rope does; 0: they
+ *                       are not.  q_out[l] receives the rotated queries and may be q[l].
+ *   k_cache[l], v_cache[l]  as kvp_cache_append, bf16, where k_scale and v_scale are NULL.  Otherwise the cache is held in 8 bits:
+ *     [n_pages][Hkv][page_size][dh] e4m3 numbers, and k_scale[l], v_scale[l] [n_pages][Hkv][page_size/16], one byte for each
+ *     block of 16 tokens and KV head: a number stands for itself times 2^(byte - 127).  An append takes for a block the smallest
+ *     exponent >= -100 with amax <= 448 * 2^exponent over its new tokens (after the rotation, in fp32; each element is rounded
+ *     once).  In a block that older tokens began the exponent does not fall below theirs, and where it rises, their numbers are
+ *     multiplied by the power of two between and rounded again.  A block whose first token is new has no older ones, whatever
+ *     it held.  What is not finite is stored as NaN and does not count for the exponent.  Bytes are 27 to 247 (others are read as
+ *     the nearer of the two).
+ * No two sequences may append into the same block.  dtype (KVP_F32: q, q_out, k_new, v_new are fp32) and the rest of d as for
+ * kvp_decode; num_splits is not read. */
+int kvp_cache_append_tokens(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float theta,
+                            const void* const* q, void* const* q_out, const void* const* k_new, const void* const* v_new,
+                            void* const* k_cache, void* const* v_cache, uint8_t* const* k_scale, uint8_t* const* v_scale,
+                            const int32_t* block_table, const int32_t* lengths, kvp_stream_t stream);
+
+/* kvp_decode over the cache held in 8 bits.  The arguments, groups of layers and rules of num_splits are kvp_decode's, with the
+ * scales beside the pools; a workspace of kvp_decode8_workspace_bytes serves every layer range.  Differences: a sequence of
+ * length 0 (or below) has output 0 and LSE -infinity, lengths above max_pages*page_size are taken as that; the probabilities
+ * are rounded to 11 bits (f16), not 8.  Slots at and behind a sequence's length are not read. */
+size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor);
+int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q,
+                const void* const* k_cache, const void* const* v_cache, const uint8_t* const* k_scale,
+                const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths, void* const* o,
+                float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, kvp_stream_t stream);
+
 /* kvp_decode without a workspace argument and without any allocation (the paper has no counterpart:
  * this is a packaging variant of kvp_decode, same arithmetic, same outputs).
  *

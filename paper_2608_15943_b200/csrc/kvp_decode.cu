@@ -24,21 +24,15 @@
 // element: 16 sequences of 4096 tokens 61 -> 50 (the copy rate takes 41), 8 of 8K-16K in two groups 141 -> 128 (113), one
 // of 65536 74 -> 49 (41), 2 of 16K in eight groups 172 -> 170, 3 of 3000 in six groups at dh 64 26.8 -> 27.1, 4 of 128K
 // at 32 KV heads 1192 -> 1177 (1313), 32 of 16K-32K in six groups 2767 -> 2687.
-#include <math.h>
-
-#include <algorithm>
 #include <mutex>
 
-#include "kvp_deal.h"
-#include "kvp_host.h"
-#include "kvp_sm100.cuh"
+#include "kvp_decode_list.cuh"
 
 namespace kvp {
 namespace {
 
 constexpr int DEC_WARPS = 4;
 constexpr int DEC_THREADS = DEC_WARPS * 32;
-constexpr int GRAN = 16;           // tokens per ring stage
 constexpr int DEC_STAGES = 3;      // granules per warp in the ring
 template <int DH>
 constexpr int DEC_CTAS_PER_SM = DH == 128 ? 2 : 4;   // as many as shared memory holds
@@ -49,8 +43,6 @@ constexpr int DEC_CTAS_PER_SM = DH == 128 ? 2 : 4;   // as many as shared memory
 // granules a warp, 2.12e-3 so, 0.6 % slower.  Against the largest of each granule by itself: 1.94e-3, 1.2 % slower.)
 constexpr int REFERENCE_GRANULES = 16;
 constexpr float REFERENCE_DROP = 8.f;
-constexpr int MAX_DEC_GROUPS = 64, FEW_DEC_GROUPS = 8;   // a launch of few groups has a parameter block of 1 KB, not 8: 0.6 us less to launch
-constexpr int MAX_MEMBERS = 4;     // layers of a donor group served by one pass (rows = members * G <= 16)
 
 __device__ int g_dec_status;
 
@@ -64,95 +56,17 @@ struct DecGroup {
   int pad;
 };
 
-struct DecSizes {
-  const int32_t* block_table;  // [B, max_pages]
-  const int32_t* lengths;      // [B]
-  float* part_o;               // [pieces][rows][DH]
-  float* part_ml;              // [pieces][rows][2]
-  int rows;                    // query rows of the largest group
-  int n_groups, B, Hq, Hkv, page_size, max_pages, n_pages;
-  int fit;                     // blocks that fit on the device
-  int max_shares;              // most shares of the list
-  int by_units;                // the lists are short at any length: whole units are dealt out, no sums are formed
-  int num_splits;              // > 0: the caller's split count instead; a block is one (unit, split)
-  int io_f32;                  // queries are read and outputs written as fp32 (rounded to bf16 on load / widened on store)
-  float scale_log2;
-};
 template <int NG>
 struct DecParams : DecSizes {
   DecGroup grp[NG];
 };
 
-__device__ __forceinline__ int clamp_length(const DecSizes& p, int len) { return min(max(len, 1), p.max_pages * p.page_size); }
-__device__ __forceinline__ int clamped_length(const DecSizes& p, int b) { return clamp_length(p, p.lengths[b]); }
-__device__ __forceinline__ int granules_of(int len) { return (len + GRAN - 1) / GRAN; }
-
-// Over the batch, formed by one warp: granules (of one KV head) of the sequences before b_before, of all, and of the longest.
-// len0: the length (unclamped) of the lane's sequence among the first 32.
-__device__ __forceinline__ void sum_granules(const DecSizes& p, int len0, int b_before, int& before, int& all, int& longest) {
-  const int lane = threadIdx.x & 31;
-  int sum = 0, most = 0, first = 0;
-  for (int b = lane; b < p.B; b += 32) {
-    const int n = granules_of(clamp_length(p, b < 32 ? len0 : p.lengths[b]));
-    sum += n;
-    most = max(most, n);
-    first += b < b_before ? n : 0;
-  }
-  all = __reduce_add_sync(0xffffffffu, sum);
-  longest = __reduce_max_sync(0xffffffffu, most);
-  before = b_before > 0 ? __reduce_add_sync(0xffffffffu, first) : 0;
-}
-// The lengths of the first 32 sequences, one a lane, before the kernels ahead have finished (through L2: no line of them may
-// stay in L1, later loads must see what those kernels write).  What was worked out from them holds if they are still the same
-// behind the wait, and is worked out again if not: the lengths of a step are in place long before.  Batches of more than 32
-// only look behind it.  (From the wait to a block's first data went 4.2 to 6 us, most of it this arithmetic out of a cold
-// instruction cache.  Append, decode and merge, us: 8 sequences of 8K-16K in four layers 133.4 -> 130.0, 15 of 2K-4K in six
-// 40.5 -> 37.0, 8 of 12K in five 67.3 -> 63.3, 28 of 1000 in three 30.4 -> 28.3.)
-__device__ __forceinline__ int early_length(const DecSizes& p) {
-  const int lane = threadIdx.x & 31;
-  return lane < p.B ? __ldcg(p.lengths + lane) : 0;
-}
-// The first T mod n of n shares of a list of T granules hold one more than the others.
-struct Dealt {
-  uint32_t q, r;
-  __device__ __forceinline__ Dealt(long long total, uint32_t n) : q(uint32_t(div_places(total, n))), r(uint32_t(total - (long long)q * n)) {}
-  __device__ __forceinline__ long long begin(uint32_t i) const { return (long long)i * q + min(i, r); }
-  __device__ __forceinline__ uint32_t size(uint32_t i) const { return q + (i < r ? 1u : 0u); }
-  __device__ __forceinline__ int share_of(long long g) const {
-    const long long longer = (long long)r * (q + 1);
-    return g < longer ? int(div_places(g, q + 1)) : int(r + div_places(g - longer, q));
-  }
-};
-
-// 16-byte asynchronous copy; with src_bytes == 0 nothing is read and the destination is filled with zeros
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float fast_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// ln(l 2^m), with the sum of the two logarithms and the constant kept to twice the precision before the only rounding
-__device__ __forceinline__ float log_sum(float m, float l) {
-  const float t = log2f(l), s = m + t, b = s - m;
-  const float low = (m - (s - b)) + (t - b);          // s + low == m + t
-  constexpr double kLn2 = 0.693147180559945309417;
-  constexpr float hi = float(kLn2), lo = float(kLn2 - double(hi));
-  return fmaf(s, hi, fmaf(s, lo, low * hi));
 }
 
 // Ring stage layout: GRAN rows of DH bf16 (DH*2 bytes per row) for K, then the same for V.  The
@@ -605,131 +519,6 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
   cp_async_wait<0>();
 }
 
-// Merges the pieces of the units that more than one share holds and writes bf16 outputs and LSE.  Eight warps per block;
-// `wpr` of them share a row of a unit (one where a unit has few pieces, eight where it has many), each lane four
-// columns.  Bound: latency; the pieces are in L2.
-constexpr int COMBINE_THREADS = 256;
-template <int DH, int NG>
-__global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const __grid_constant__ DecParams<NG> p, int wpr) {
-  constexpr int LANES = DH / 4;               // lanes per piece and row
-  constexpr int PER_WARP = 32 / LANES;        // pieces a warp takes at a time
-  __shared__ float s_m[COMBINE_THREADS / 32], s_l[COMBINE_THREADS / 32];
-  __shared__ float4 s_o[COMBINE_THREADS / 32][LANES];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rows_per_block = (COMBINE_THREADS / 32) / wpr;
-  const int G = p.Hq / p.Hkv;
-  const int unit = blockIdx.x;
-  const int hk = unit % p.Hkv, b = unit / p.Hkv % p.B, gi = unit / p.Hkv / p.B;
-  const DecGroup& grp = p.grp[gi];
-  const int R = grp.n_members * G;
-  const int row = blockIdx.y * rows_per_block + warp / wpr;
-  grid_dep_launch();
-  int w0 = 0, w1 = 0;                         // shares (or splits) that hold the unit
-  if (p.num_splits > 0) {
-    w0 = unit * p.num_splits;
-    w1 = w0 + p.num_splits - 1;
-    grid_dep_wait();
-  } else {
-    int len0 = 0;
-    for (bool behind = p.B > 32;; behind = true) {
-      if (behind) grid_dep_wait();
-      const int now = early_length(p);
-      if (behind && p.B <= 32 && __all_sync(0xffffffffu, now == len0)) break;
-      len0 = now;
-      int before, all, longest;
-      sum_granules(p, len0, b, before, all, longest);
-      const long long granules = (long long)all * p.Hkv * p.n_groups;
-      if (dealt_by_units(DH, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit)) {
-        w0 = w1 = 0;                          // finished by the blocks that held them
-      } else {
-        const int len = b < 32 ? __shfl_sync(0xffffffffu, len0, b) : p.lengths[b];
-        const int rest = unit_rest(DH, granules, p.fit), ng = granules_of(clamp_length(p, len));
-        const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
-        const int n = shares_for(DH, p.fit, p.max_shares, total);
-        const long long first = gi * per_group + ((long long)before + (long long)b * rest) * p.Hkv + (long long)hk * (ng + rest);
-        const Dealt dealt(total, n);
-        w0 = dealt.share_of(first);
-        w1 = dealt.share_of(first + ng - 1);
-      }
-      if (behind) break;
-    }
-    if (w0 == w1) return;                     // finished by the block that had the share
-  }
-  if (blockIdx.y * rows_per_block >= R) return;
-  const int sub = lane / LANES, col = (lane % LANES) * 4;
-  float m = -INFINITY, l = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < R) {
-    constexpr int UNROLL = 4;                 // pieces in flight per lane
-    const int step = wpr * PER_WARP;
-    for (int w = w0 + (warp % wpr) * PER_WARP + sub; w <= w1; w += step * UNROLL) {
-      float2 ml[UNROLL];
-      float4 o[UNROLL];
-#pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int wu = w + u * step;
-        ml[u] = make_float2(-INFINITY, 0.f);
-        if (wu <= w1) {
-          const size_t piece = p.num_splits > 0 ? size_t(wu) : size_t(wu) * 2 + (wu == w0 ? 1 : 0);
-          ml[u] = *reinterpret_cast<const float2*>(p.part_ml + (piece * p.rows + row) * 2);
-          o[u] = *reinterpret_cast<const float4*>(p.part_o + (piece * p.rows + row) * DH + col);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        if (ml[u].x == -INFINITY) continue;   // an empty split
-        const float mn = fmaxf(m, ml[u].x);
-        const float fa = m == -INFINITY ? 0.f : fast_exp2(m - mn), fb = fast_exp2(ml[u].x - mn);
-        acc.x = acc.x * fa + o[u].x * fb;
-        acc.y = acc.y * fa + o[u].y * fb;
-        acc.z = acc.z * fa + o[u].z * fb;
-        acc.w = acc.w * fa + o[u].w * fb;
-        l = l * fa + ml[u].y * fb;
-        m = mn;
-      }
-    }
-  }
-  auto merge = [&](float om, float ol, const float4& oo) {
-    if (om == -INFINITY) return;
-    const float mn = fmaxf(m, om);
-    const float fa = m == -INFINITY ? 0.f : fast_exp2(m - mn), fb = fast_exp2(om - mn);
-    acc.x = acc.x * fa + oo.x * fb;
-    acc.y = acc.y * fa + oo.y * fb;
-    acc.z = acc.z * fa + oo.z * fb;
-    acc.w = acc.w * fa + oo.w * fb;
-    l = l * fa + ol * fb;
-    m = mn;
-  };
-  if (PER_WARP == 2) {                        // the two halves of the warp hold different pieces
-    const float om = __shfl_xor_sync(0xffffffffu, m, 16), ol = __shfl_xor_sync(0xffffffffu, l, 16);
-    const float4 oo = make_float4(__shfl_xor_sync(0xffffffffu, acc.x, 16), __shfl_xor_sync(0xffffffffu, acc.y, 16),
-                                  __shfl_xor_sync(0xffffffffu, acc.z, 16), __shfl_xor_sync(0xffffffffu, acc.w, 16));
-    merge(om, ol, oo);
-  }
-  if (wpr > 1) {                              // the block's warps hold pieces of one row (uniform: every thread arrives)
-    if (lane < LANES) s_o[warp][lane] = acc;
-    if (lane == 0) {
-      s_m[warp] = m;
-      s_l[warp] = l;
-    }
-    __syncthreads();
-    if (warp % wpr != 0) return;
-    for (int k = 1; k < wpr; ++k) merge(s_m[warp + k], s_l[warp + k], s_o[warp + k][lane % LANES]);
-  }
-  if (row < R && lane < LANES) {
-    const int mem = row / G;
-    const size_t head = size_t(b) * p.Hq + hk * G + row % G;
-    const float inv = 1.f / l;
-    const uint2 v = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));   // rounded to bf16 either way
-    if (p.io_f32)
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(grp.o[mem]) + head * DH + col) =
-          make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-    else
-      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(grp.o[mem]) + head * DH + col) = v;
-    if (lane == 0) grp.lse[mem][head] = log_sum(m, l);
-  }
-}
-
 // Owners write the new token's K and V rows into their pages.
 struct AppendLayer {
   const void *k_new, *v_new;           // [B,Hkv,dh] bf16, or fp32 when new_f32 (rounded to bf16 as it is stored)
@@ -796,87 +585,7 @@ cudaError_t launch_append(const AppendParams<MAX_DEC_GROUPS>& all, int n, cudaSt
   return launch_kernel(append_kernel<NG>, dim3(all.B, n), 128, 0, stream, 1, p);
 }
 
-int check_desc(const kvp_decode_desc* d) {
-  if (d == nullptr) return KVP_ERR_INVALID_ARG;
-  if (d->L < 1 || d->B < 1 || d->Hq < 1 || d->Hkv < 1 || d->max_pages < 1 || d->n_pages < 1 || d->num_splits < 0)
-    return KVP_ERR_INVALID_ARG;
-  if (d->dtype != KVP_BF16 && d->dtype != KVP_F32) return KVP_ERR_UNSUPPORTED;
-  if ((d->dh != 64 && d->dh != 128) || d->Hq % d->Hkv != 0 || d->Hq / d->Hkv > 16 || d->page_size < GRAN ||
-      d->page_size % GRAN != 0)
-    return KVP_ERR_UNSUPPORTED;
-  return KVP_OK;
-}
-
-// Sub-groups of at most min(MAX_MEMBERS, 16 / G) layers that share a donor inside [begin, end).
-struct SubGroup {
-  int owner;
-  int members[MAX_MEMBERS];
-  int n;
-};
-
-int build_groups(const kvp_decode_desc* d, const int32_t* donor, int begin, int end, SubGroup* out, int max_out) {
-  const int G = d->Hq / d->Hkv;
-  int per = 16 / G;
-  if (per > MAX_MEMBERS) per = MAX_MEMBERS;
-  int n_out = 0;
-  for (int own = 0; own < d->L; ++own) {
-    if (donor[own] != own) continue;
-    SubGroup cur;
-    cur.owner = own;
-    cur.n = 0;
-    for (int l = begin > own ? begin : own; l < end; ++l) {
-      if (donor[l] != own) continue;
-      cur.members[cur.n++] = l;
-      if (cur.n == per) {
-        if (n_out == max_out) return -1;
-        out[n_out++] = cur;
-        cur.n = 0;
-      }
-    }
-    if (cur.n > 0) {
-      if (n_out == max_out) return -1;
-      out[n_out++] = cur;
-    }
-  }
-  return n_out;
-}
-
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
-// Pieces and their bytes.  When the library chooses: two for each share of the list at its longest; with the
-// caller's split count: one for every (unit, split).  One launch holds at most MAX_DEC_GROUPS sub-groups and launches
-// reuse the space.
-int blocks_that_fit(int dh) { return sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>); }
-size_t piece_bytes(const kvp_decode_desc* d, size_t pieces, int rows) {
-  return align256(pieces * rows * d->dh * 4) + align256(pieces * rows * 2 * 4);
-}
-long long longest_unit(const kvp_decode_desc* d) { return (long long)d->max_pages * d->page_size / GRAN; }
-long long longest_list(const kvp_decode_desc* d, int n_groups) { return (long long)n_groups * d->B * d->Hkv * longest_unit(d); }
-struct Scratch {
-  int max_shares = 0, rows = 0;
-  size_t pieces = 0, bytes = 0;
-};
-// limit > 0: fewer shares until the pieces fit into that many bytes
-Scratch plan_scratch(const kvp_decode_desc* d, const SubGroup* subs, int n_sub, size_t limit) {
-  Scratch s;
-  const int per_launch = n_sub < MAX_DEC_GROUPS ? n_sub : MAX_DEC_GROUPS;
-  for (int i = 0; i < n_sub; ++i) s.rows = std::max(s.rows, subs[i].n * (d->Hq / d->Hkv));
-  const int fit = blocks_that_fit(d->dh);
-  const long long longest = longest_list(d, per_launch);
-  s.max_shares = shares_for(d->dh, fit, fit * max_rounds(d->dh), longest + (long long)per_launch * d->B * d->Hkv * unit_rest(d->dh, longest, fit));
-  for (;;) {
-    s.pieces = d->num_splits > 0 ? size_t(per_launch) * d->B * d->Hkv * d->num_splits : size_t(s.max_shares) * 2;
-    s.bytes = piece_bytes(d, s.pieces, s.rows);
-    if (limit == 0 || s.bytes <= limit || d->num_splits > 0 || s.max_shares == 1) return s;
-    s.max_shares = (s.max_shares + 1) / 2;
-  }
-}
-// bytes for decoding layers [begin, end); 0 when the request cannot be served at all
-size_t decode_scratch_bytes(const kvp_decode_desc* d, const int32_t* donor, int begin, int end) {
-  static thread_local SubGroup tmp[4096];
-  const int n_sub = build_groups(d, donor, begin, end, tmp, 4096);
-  return n_sub <= 0 ? 0 : plan_scratch(d, tmp, n_sub, 0).bytes;
-}
+DealBy deal_by(int dh) { return {dh, sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>)}; }
 
 int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                 const void* const* v_cache, const int32_t* block_table, const int32_t* lengths, void* const* o,
@@ -901,7 +610,7 @@ using namespace kvp;
 
 extern "C" size_t kvp_decode_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor) {
   if (check_desc(d) != KVP_OK || donor == nullptr) return 0;
-  return decode_scratch_bytes(d, donor, 0, d->L);
+  return decode_scratch_bytes(d, donor, 0, d->L, deal_by(d->dh));
 }
 
 extern "C" int kvp_cache_append(const kvp_decode_desc* d, const int32_t* donor, const void* const* k_new,
@@ -956,7 +665,7 @@ cudaError_t launch_decode(const DecParams<MAX_DEC_GROUPS>& all, dim3 grid, dim3 
   e = launch_kernel(decode_kernel<DH, NG>, grid, DEC_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
-    e = launch_kernel(decode_combine_kernel<DH, NG>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+    e = launch_kernel(decode_combine_kernel<DH, DH, false, DecParams<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 
@@ -975,7 +684,7 @@ int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, con
   static thread_local SubGroup subs[4096];
   const int n_sub = build_groups(d, donor, layer_begin, layer_end, subs, 4096);
   if (n_sub < 0) return KVP_ERR_UNSUPPORTED;
-  const Scratch sc_plan = plan_scratch(d, subs, n_sub, limit);
+  const Scratch sc_plan = plan_scratch(d, subs, n_sub, limit, deal_by(d->dh));
   if (ws == nullptr || ws_bytes < sc_plan.bytes || !aligned16(ws)) return KVP_ERR_WORKSPACE;
   const size_t po_bytes = align256(sc_plan.pieces * sc_plan.rows * d->dh * 4);
 
@@ -991,7 +700,7 @@ int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, con
   p.max_pages = d->max_pages;
   p.n_pages = d->n_pages;
   p.rows = sc_plan.rows;
-  p.fit = blocks_that_fit(d->dh);
+  p.fit = deal_by(d->dh).fit;
   p.max_shares = sc_plan.max_shares;
   p.num_splits = d->num_splits;
   p.io_f32 = d->dtype == KVP_F32;
@@ -1099,7 +808,7 @@ extern "C" int kvp_decode_static(const kvp_decode_desc* d, const int32_t* donor,
   if (layer_begin < 0 || layer_end > d->L || layer_begin >= layer_end) return KVP_ERR_INVALID_ARG;
   // only the donor groups that the layer range touches need room, so a narrower range can fit where all layers do not
   // (when the library deals the rows out, it does so in fewer shares until their pieces fit)
-  const size_t need = decode_scratch_bytes(d, donor, layer_begin, layer_end);
+  const size_t need = decode_scratch_bytes(d, donor, layer_begin, layer_end, deal_by(d->dh));
   if (need == 0) return KVP_ERR_UNSUPPORTED;
   if (d->num_splits > 0 && need > size_t(KVP_DECODE_STATIC_SCRATCH_BYTES)) return KVP_ERR_STATIC_SCRATCH;
   void* scratch = nullptr;

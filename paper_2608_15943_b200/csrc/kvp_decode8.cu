@@ -1,0 +1,711 @@
+// Split-KV decode attention over the shared paged cache held in 8 bits (kvp_cache8.h): half the bytes of the bf16 cache, and the
+// same list of K/V rows dealt out to blocks (kvp_decode.cu describes it), the same groups of layers, the same merge.
+//
+// With half the bytes a granule of 16 tokens and one KV head (4 KB at dh 128) has to pass an SM in about 170 cycles to keep HBM
+// busy, so the design is about instructions a granule:
+//  - K and V are the A operand of mma.sync m16n8k16 (f16 in, fp32 accumulate) and the query rows its N: up to 8 rows cost half the
+//    products that they cost as its M, and the scores of a granule are 4 registers a lane.  S^T = K Q^T, O^T += V^T P^T.
+//  - e4m3 numbers become f16 exactly, two an instruction.  Which element of a row is which k of a product is free as long as both
+//    operands agree, so a lane reads K 16 bytes at a time and its words are its operands.  Tokens are matched to the rows of S^T so
+//    that the V numbers of four tokens that a lane needs lie in four of its own 16-byte words, two byte permutes away.
+//  - Queries are scaled by a power of two a row into f16's range (the largest to 2^14): exact for all bf16 elements down to 2^-31 of
+//    the row's largest, and rounded by at most 2^-39 of it below.  The scale of K joins the factor of the scores.
+//  - The scale of V is a power of two: P is multiplied by 2^(e + M - R) with a reference R of the accumulators beside the
+//    reference M of the sum.  Both rise only when a value would leave f16's upper range, so that no maximum is exchanged between
+//    lanes in nearly all granules: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
+//  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
+#include "kvp_cache8.cuh"
+#include "kvp_decode_list.cuh"
+
+namespace kvp {
+namespace {
+
+constexpr int D8_WARPS = 4, D8_THREADS = D8_WARPS * 32;
+constexpr int D8_KEY = 64;                        // granules of 4 KB (dh 128), as those of the bf16 cache at dh 64 are
+template <int NB>
+constexpr int D8_CTAS = NB == 1 ? 4 : 3;          // per SM, by registers and shared memory
+template <int DH, int NB>
+constexpr int D8_STAGES = (NB == 1 ? 3 : 4) * (DH == 128 ? 1 : 2);   // granules of a warp in the ring
+constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
+constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
+
+struct Dec8Group {
+  const uint8_t *k_cache, *v_cache;               // [n_pages][Hkv][page_size][dh] e4m3
+  const uint8_t *k_scale, *v_scale;               // [n_pages][Hkv][page_size / 16]
+  const void* q[MAX_MEMBERS];
+  void* o[MAX_MEMBERS];
+  float* lse[MAX_MEMBERS];
+  int n_members;
+  int pad;
+};
+template <int NG>
+struct Dec8Params : DecSizes {
+  Dec8Group grp[NG];
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+
+// Ring stage: 16 rows of DH bytes of K, then of V.  16-byte chunks are permuted inside lines of 128 bytes so that both reads are
+// free of bank conflicts: K's (lanes of a phase: rows 4i and 4i + 1, four chunks of each) and V's (rows i, i + 4, i + 8, i + 12, two
+// chunks of each).
+template <int DH>
+__device__ __forceinline__ uint32_t ring8_off(int row, int chunk) {
+  if (DH == 128) return uint32_t(row) * 128 + (uint32_t(chunk ^ ((row >> 2 & 3) << 1) ^ ((row & 1) << 2)) << 4);
+  return uint32_t(row >> 1) * 128 + (uint32_t(((row & 1) << 2 | chunk) ^ ((row >> 2 & 3) << 1)) << 4);
+}
+
+template <int DH, int NB, int NG>
+__global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
+  constexpr int TILE_BYTES = GRAN * DH, STAGE_BYTES = 2 * TILE_BYTES, STAGES = D8_STAGES<DH, NB>;
+  constexpr int CHUNKS = DH / 16;                  // 16-byte chunks of a row
+  constexpr int CP_PER_LANE = TILE_BYTES / 16 / 32;
+  constexpr int HALVES = DH / 64;                  // 16-byte words of a K row that a lane takes
+  constexpr int MB = DH / 16;                      // m-blocks of O^T; a lane has DH / 8 consecutive elements of a row
+
+  extern __shared__ __align__(128) uint8_t dsmem[];
+  __shared__ float2 s_o[D8_WARPS - 1][MB * 32];    // four rows of the results that warp 0 merges into its own
+  __shared__ float2 s_ml[D8_WARPS - 1][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  const int G = p.Hq / p.Hkv;
+
+  // ---- the block's place in the list ----
+  struct Cursor {
+    int grp, b, hk, gran, ng, seen;                // seen: tokens of the sequence (0: none, in one granule)
+    int id;                                        // the unit's number, where units are dealt out
+  };
+  Cursor c;
+  int todo;                                        // places of the block's share of the list still to do
+  const bool caller_splits = p.num_splits > 0;
+  const int cap = p.max_pages * p.page_size;
+  auto set_length = [&](Cursor& x, int len) {
+    x.seen = min(max(len, 0), cap);
+    x.ng = granules_of(max(x.seen, 1));
+  };
+  auto go_to_unit = [&](Cursor& x, int id) {       // (past the last unit: grp >= n_groups)
+    x.id = id;
+    x.hk = id % p.Hkv;
+    x.b = id / p.Hkv % p.B;
+    x.grp = id / p.Hkv / p.B;
+    x.gran = 0;
+    set_length(x, p.lengths[x.b]);
+  };
+  bool by_units = p.by_units != 0;
+  int rest = 0;                                    // places behind the granules of a unit
+  auto find_place = [&](int len0) -> bool {        // from the lengths; false: the block has none
+    int before, all, longest;
+    sum_granules(p, len0, 0, before, all, longest);
+    const long long granules = (long long)all * p.Hkv * p.n_groups;
+    by_units = dealt_by_units(D8_KEY, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit);
+    rest = by_units ? 0 : unit_rest(D8_KEY, granules, p.fit);
+    if (by_units) return true;
+    const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
+    const int n_shares = shares_for(D8_KEY, p.fit, p.max_shares, total);
+    if (blockIdx.x >= n_shares) return false;
+    const Dealt dealt(total, n_shares);
+    long long at = dealt.begin(blockIdx.x);
+    todo = int(dealt.size(blockIdx.x));
+    c.id = 0;
+    c.grp = int(div_places(at, per_group));
+    at -= c.grp * per_group;                       // inside the group: find the sequence, 32 lengths at a time
+    for (int b0 = 0;; b0 += 32) {
+      const bool is_one = b0 + lane < p.B;
+      const int len = !is_one ? 0 : b0 == 0 ? len0 : p.lengths[b0 + lane];
+      const int mine = is_one ? granules_of(clamp_length(p, len)) + rest : 0;
+      int upto = mine;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, s);
+        if (lane >= s) upto += v;
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, at < (long long)upto * p.Hkv);
+      if (hit != 0u) {
+        const int src = __ffs(hit) - 1;
+        at -= (long long)__shfl_sync(0xffffffffu, upto - mine, src) * p.Hkv;
+        c.b = b0 + src;
+        set_length(c, __shfl_sync(0xffffffffu, len, src));
+        break;
+      }
+      at -= (long long)__shfl_sync(0xffffffffu, upto, 31) * p.Hkv;
+    }
+    c.hk = int(at) / (c.ng + rest);                // (a sequence's places of all KV heads fit 32 bits)
+    c.gran = int(at) % (c.ng + rest);
+    return true;
+  };
+  bool placed = true;
+  if (caller_splits || by_units) {
+    grid_dep_wait();
+  } else {
+    int len0 = 0;
+    for (bool behind = p.B > 32;; behind = true) {
+      if (behind) grid_dep_wait();
+      const int now = early_length(p);
+      if (behind && p.B <= 32 && __all_sync(0xffffffffu, now == len0)) break;
+      len0 = now;
+      placed = find_place(len0);
+      if (behind) break;
+    }
+  }
+  if (!placed) return;
+  if (caller_splits) {
+    const int split = blockIdx.x % p.num_splits;
+    go_to_unit(c, blockIdx.x / p.num_splits);
+    const int per = (c.ng + p.num_splits - 1) / p.num_splits;
+    c.gran = min(c.ng, split * per);
+    todo = min(c.ng - c.gran, per);
+  } else if (by_units) {
+    if (blockIdx.x >= p.n_groups * p.B * p.Hkv) return;
+    go_to_unit(c, blockIdx.x);
+    todo = c.ng;
+  }
+  auto next_piece = [&](Cursor& x, int& left) {    // past the end: grp >= n_groups
+    left -= min(left, x.ng + rest - x.gran);
+    if (left > 0) {
+      x.gran = 0;
+      if (++x.hk == p.Hkv) {
+        x.hk = 0;
+        if (++x.b == p.B) {
+          x.b = 0;
+          ++x.grp;
+        }
+        set_length(x, p.lengths[x.b]);
+      }
+    } else if (by_units && !caller_splits && x.id + int(gridDim.x) < p.n_groups * p.B * p.Hkv) {
+      go_to_unit(x, x.id + gridDim.x);
+      left = x.ng;
+    } else {
+      x.grp = p.n_groups;
+    }
+  };
+  if (c.gran >= c.ng && !caller_splits) {          // the share begins behind the granules of a unit
+    next_piece(c, todo);
+    if (c.grp >= p.n_groups) return;
+  }
+
+  // ---- copies: a cursor of their own, STAGES - 1 of this warp's granules ahead of the arithmetic ----
+  const uint32_t ring = smem_u32(dsmem) + warp * STAGES * STAGE_BYTES;
+  Cursor f = c;
+  int f_todo = todo;
+  int f_left;                                      // granules of the piece from this warp's next one on (<= 0: none)
+  const int gran_per_page = p.page_size / GRAN;
+  const Dec8Group* f_grp = &p.grp[0];
+  const int32_t* bt = nullptr;                     // block-table entry of the page the next granule is in,
+  int in_page = 0, f_tok = 0;                      // its place there, and its first token
+  size_t page_block = 0;                           // blocks of 16 tokens before this KV head's of that page
+  int stage_in = 0;
+  uint32_t scales[STAGES];                         // of the granules in the ring, K's byte and V's above it
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) scales[s] = 0;
+  auto enter_page = [&]() {
+    const int page = min(max(*bt, 0), p.n_pages - 1);
+    page_block = (size_t(page) * p.Hkv + f.hk) * gran_per_page;
+  };
+  auto enter_piece = [&]() {
+    f_left = min(f_todo, f.ng - f.gran) - warp;
+    if (f_left <= 0) return;
+    const int gran = f.gran + warp, col = gran / gran_per_page;
+    f_grp = &p.grp[f.grp];
+    bt = p.block_table + size_t(f.b) * p.max_pages + col;
+    in_page = gran - col * gran_per_page;
+    f_tok = gran * GRAN;
+    enter_page();
+  };
+  auto issue_next = [&]() -> uint32_t {
+    uint32_t scale = 0;
+    while (f_left <= 0 && f.grp < p.n_groups) {
+      next_piece(f, f_todo);
+      if (f.grp < p.n_groups) enter_piece();
+    }
+    if (f_left > 0) {
+      const size_t block = page_block + in_page;
+      const uint8_t* const ksrc = f_grp->k_cache + block * TILE_BYTES;
+      const uint8_t* const vsrc = f_grp->v_cache + block * TILE_BYTES;
+      const uint32_t dst = ring + stage_in * STAGE_BYTES;
+      if (f.seen > 0) scale = uint32_t(f_grp->k_scale[block]) | uint32_t(f_grp->v_scale[block]) << 8;
+#pragma unroll
+      for (int i = 0; i < CP_PER_LANE; ++i) {
+        const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
+        const uint32_t off = ring8_off<DH>(row, chunk);
+        const uint32_t nbytes = f_tok + row < f.seen ? 16u : 0u;   // slots never appended may hold anything: zeros instead
+        cp_async16(dst + off, ksrc + idx * 16, nbytes);
+        cp_async16(dst + TILE_BYTES + off, vsrc + idx * 16, nbytes);
+      }
+      if (++stage_in == STAGES) stage_in = 0;
+      f_left -= D8_WARPS;
+      f_tok += D8_WARPS * GRAN;
+      in_page += D8_WARPS;
+      if (in_page >= gran_per_page && f_left > 0) {
+        const int pages = in_page / gran_per_page;
+        bt += pages;
+        in_page -= pages * gran_per_page;
+        enter_page();
+      }
+    }
+    cp_async_commit();
+    return scale;
+  };
+  enter_piece();
+
+  // ---- queries: B operand, row n of the group in lanes g = n mod 8 ----
+  uint32_t qb[HALVES * 4][NB][2];
+  float q_factor[NB][2];                           // of the scores of rows 8 nb + 2 t + h
+  auto load_queries = [&]() {
+    const Dec8Group& grp = p.grp[c.grp];
+    const int R = grp.n_members * G;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int n = nb * 8 + g;
+      float v[HALVES * 16];
+      if (n < R) {
+        const size_t at = (size_t(c.b) * p.Hq + c.hk * G + n % G) * DH;
+        const void* const q = grp.q[n / G];
+#pragma unroll
+        for (int e = 0; e < HALVES * 4; ++e) {
+          const size_t four = at + (e >> 2) * 64 + t * 16 + (e & 3) * 4;
+          uint2 w;
+          if (p.io_f32) {
+            const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(q) + four);
+            w = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+          } else {
+            w = *reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(q) + four);
+          }
+          v[4 * e] = __uint_as_float(w.x << 16);
+          v[4 * e + 1] = __uint_as_float(w.x & 0xffff0000u);
+          v[4 * e + 2] = __uint_as_float(w.y << 16);
+          v[4 * e + 3] = __uint_as_float(w.y & 0xffff0000u);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < HALVES * 16; ++e) v[e] = 0.f;
+      }
+      float amax = 0.f;
+#pragma unroll
+      for (int e = 0; e < HALVES * 16; ++e) amax = fmaxf(amax, fabsf(v[e]));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const int lg = max(int(__float_as_uint(amax) >> 23) - 127, -100);      // (128: infinite, left so)
+      const float up = __uint_as_float(power_bits(lg < 128 ? 14 - lg : 0));
+      const float down = __uint_as_float(power_bits(lg < 128 ? lg - 14 : 0)) * p.scale_log2;
+#pragma unroll
+      for (int e = 0; e < HALVES * 4; ++e) {
+        qb[e][nb][0] = pack_f16(v[4 * e] * up, v[4 * e + 1] * up);
+        qb[e][nb][1] = pack_f16(v[4 * e + 2] * up, v[4 * e + 3] * up);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) q_factor[nb][h] = __shfl_sync(0xffffffffu, down, (2 * t + h) * 4);
+    }
+  };
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) scales[s] = issue_next();
+  load_queries();
+
+  const int tok_g = (g >> 1) * 4 + (g & 1);        // token of the granule that row g of S^T is; row g + 8: two more
+  int stage_out = 0;
+  do {
+    // ---- one unit, or this block's piece of it ----
+    const Dec8Group& grp = p.grp[c.grp];
+    const int R = grp.n_members * G;
+    const int n_here = min(todo, c.ng - c.gran);
+    const bool from_start = c.gran == 0, to_end = c.gran + n_here == c.ng;
+
+    float oacc[MB][NB][4];
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) oacc[m][nb][0] = oacc[m][nb][1] = oacc[m][nb][2] = oacc[m][nb][3] = 0.f;
+    float sum[NB][2], M[NB][2], Rf[NB][2];         // of rows 8 nb + 2 t + h: sum against M (this lane's tokens), reference of oacc
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sum[nb][h] = 0.f;
+        M[nb][h] = Rf[nb][h] = -1e30f;             // (finite: below every score, and no infinity minus infinity)
+      }
+
+    for (int i = warp; i < n_here; i += D8_WARPS) {
+      cp_async_wait<STAGES - 2>();
+      __syncwarp();
+      scales[STAGES - 1] = issue_next();           // into the stage freed by the previous granule
+      const uint32_t here = scales[0];
+#pragma unroll
+      for (int s = 0; s + 1 < STAGES; ++s) scales[s] = scales[s + 1];
+      const uint32_t sK = ring + stage_out * STAGE_BYTES, sV = sK + TILE_BYTES;
+      if (++stage_out == STAGES) stage_out = 0;
+      const float k_scale = __uint_as_float(power_bits(exponent_of_byte(here & 0xffu)));
+      const float v_exp = float(exponent_of_byte(here >> 8));
+
+      // ---- S^T[16 tokens, rows] = K Q^T, even and odd k-steps apart ----
+      float s2[2][NB][4];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s2[0][nb][u] = s2[1][nb][u] = 0.f;
+#pragma unroll
+      for (int hf = 0; hf < HALVES; ++hf) {
+        const uint4 ka = lds16(sK + ring8_off<DH>(tok_g, hf * 4 + t)), kb = lds16(sK + ring8_off<DH>(tok_g + 2, hf * 4 + t));
+        const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(wa[w])), e4m3x2_to_f16x2(uint16_t(wb[w])), e4m3x2_to_f16x2(uint16_t(wa[w] >> 16)),
+                                 e4m3x2_to_f16x2(uint16_t(wb[w] >> 16))};
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma_f16(s2[w & 1][nb], a, qb[hf * 4 + w][nb][0], qb[hf * 4 + w][nb][1]);
+        }
+      }
+      // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
+      const int left = c.seen - (c.gran + i) * GRAN;   // visible tokens from this granule on
+      float x[NB][4];
+      bool over = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float factor = q_factor[nb][h] * k_scale;
+          x[nb][h] = (s2[0][nb][h] + s2[1][nb][h]) * factor;
+          x[nb][2 + h] = (s2[0][nb][2 + h] + s2[1][nb][2 + h]) * factor;
+          if (left < GRAN) {
+            if (tok_g >= left) x[nb][h] = -INFINITY;
+            if (tok_g + 2 >= left) x[nb][2 + h] = -INFINITY;
+          }
+          const float most = fmaxf(x[nb][h], x[nb][2 + h]);
+          over = over || most > M[nb][h] + SUM_TOP || most + v_exp > Rf[nb][h] + P_TOP;
+        }
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float most = fmaxf(x[nb][h], x[nb][2 + h]);
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+            if (most > M[nb][h] + SUM_TOP) {
+              sum[nb][h] *= fast_exp2(M[nb][h] - most);
+              M[nb][h] = most;
+            }
+            if (most + v_exp > Rf[nb][h] + P_TOP) {
+              const float to = most + v_exp - P_NEW, factor = fast_exp2(Rf[nb][h] - to);
+              Rf[nb][h] = to;
+#pragma unroll
+              for (int m = 0; m < MB; ++m) {
+                oacc[m][nb][h] *= factor;
+                oacc[m][nb][2 + h] *= factor;
+              }
+            }
+          }
+      }
+      uint32_t pb[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float w[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = fast_exp2(x[nb][h] - M[nb][h]), p1 = fast_exp2(x[nb][2 + h] - M[nb][h]);
+          sum[nb][h] += p0 + p1;
+          const float to_v = fast_exp2(fminf(v_exp + (M[nb][h] - Rf[nb][h]), 126.f));
+          w[h] = p0 * to_v;
+          w[2 + h] = p1 * to_v;
+        }
+        pb[nb][0] = transpose_8x8(pack_f16(w[0], w[1]));
+        pb[nb][1] = transpose_8x8(pack_f16(w[2], w[3]));
+      }
+      // ---- O^T[DH, rows] += V^T P^T: this lane's elements of tokens 4t .. 4t + 3 ----
+      constexpr int VW = DH / 32;                  // words of a token that a lane takes
+      uint32_t vw[4][VW];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (DH == 128) {
+          const uint4 v = lds16(sV + ring8_off<DH>(4 * t + k, g));
+          vw[k][0] = v.x, vw[k][1] = v.y, vw[k][2] = v.z, vw[k][3] = v.w;
+        } else {
+          const uint2 v = lds8(sV + ring8_off<DH>(4 * t + k, g >> 1) + (g & 1) * 8);
+          vw[k][0] = v.x, vw[k][1] = v.y;
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {           // elements 4w + 2hi and the one behind it
+          const uint32_t a01 = __byte_perm(vw[0][w], vw[1][w], hi ? 0x7362 : 0x5140), a23 = __byte_perm(vw[2][w], vw[3][w], hi ? 0x7362 : 0x5140);
+          const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(a01)), e4m3x2_to_f16x2(uint16_t(a01 >> 16)), e4m3x2_to_f16x2(uint16_t(a23)),
+                                 e4m3x2_to_f16x2(uint16_t(a23 >> 16))};
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma_f16(oacc[2 * w + hi][nb], a, pb[nb][0], pb[nb][1]);
+        }
+      }
+      __syncwarp();  // every lane is done with this stage before it is refilled
+    }
+    const Cursor here = c;
+    next_piece(c, todo);
+    const bool last = c.grp >= p.n_groups;
+    if (last) grid_dep_launch();   // this warp's loads are out, the others' within a granule
+    else load_queries();
+
+    // ---- everything against M; no term at all: M = -infinity ----
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) sum[nb][h] += __shfl_xor_sync(0xffffffffu, sum[nb][h], s);
+        const float to_m = fast_exp2(fminf(Rf[nb][h] - M[nb][h], 126.f));
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          oacc[m][nb][h] *= to_m;
+          oacc[m][nb][2 + h] *= to_m;
+        }
+        if (sum[nb][h] == 0.f) M[nb][h] = -INFINITY;
+      }
+    // ---- warp 0 merges the results of the others into its own, four rows at a time ----
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (8 * nb + h >= R) break;
+        __syncthreads();   // warp 0 is done with the previous ones
+        if (warp > 0) {
+#pragma unroll
+          for (int m = 0; m < MB; ++m) s_o[warp - 1][m * 32 + lane] = make_float2(oacc[m][nb][h], oacc[m][nb][2 + h]);
+          s_ml[warp - 1][lane] = make_float2(M[nb][h], sum[nb][h]);
+        }
+        __syncthreads();
+        if (warp == 0) {
+          float2 om[D8_WARPS - 1];
+          float mn = M[nb][h];
+#pragma unroll
+          for (int w = 0; w < D8_WARPS - 1; ++w) {
+            om[w] = s_ml[w][lane];
+            mn = fmaxf(mn, om[w].x);
+          }
+          const float fa = M[nb][h] == -INFINITY ? 0.f : fast_exp2(M[nb][h] - mn);
+          M[nb][h] = mn;
+          sum[nb][h] *= fa;
+#pragma unroll
+          for (int m = 0; m < MB; ++m) {
+            oacc[m][nb][h] *= fa;
+            oacc[m][nb][2 + h] *= fa;
+          }
+#pragma unroll
+          for (int w = 0; w < D8_WARPS - 1; ++w) {
+            const float fb = om[w].x == -INFINITY ? 0.f : fast_exp2(om[w].x - mn);
+            sum[nb][h] += om[w].y * fb;
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+              const float2 v = s_o[w][m * 32 + lane];
+              oacc[m][nb][h] += v.x * fb;
+              oacc[m][nb][2 + h] += v.y * fb;
+            }
+          }
+        }
+      }
+    if (warp != 0) {
+      // (warp 0 alone goes on to store)
+    } else if (!caller_splits && from_start && to_end) {
+      // ---- the whole unit: normalise and store DH / 8 consecutive elements a lane ----
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = nb * 8 + 2 * t + h;
+          if (row < R) {
+            const size_t head = size_t(here.b) * p.Hq + here.hk * G + row % G, at = head * DH + g * (DH / 8);
+            const bool none = sum[nb][h] == 0.f;
+            const float inv = none ? 0.f : 1.f / sum[nb][h];
+            uint32_t v[MB];
+#pragma unroll
+            for (int m = 0; m < MB; ++m) v[m] = pack_bf16(oacc[m][nb][h] * inv, oacc[m][nb][2 + h] * inv);   // rounded to bf16 either way
+#pragma unroll
+            for (int m = 0; m < MB; m += 4) {
+              if (p.io_f32) {
+                float4* const o = reinterpret_cast<float4*>(reinterpret_cast<float*>(grp.o[row / G]) + at + 2 * m);
+                o[0] = make_float4(__uint_as_float(v[m] << 16), __uint_as_float(v[m] & 0xffff0000u), __uint_as_float(v[m + 1] << 16), __uint_as_float(v[m + 1] & 0xffff0000u));
+                o[1] = make_float4(__uint_as_float(v[m + 2] << 16), __uint_as_float(v[m + 2] & 0xffff0000u), __uint_as_float(v[m + 3] << 16), __uint_as_float(v[m + 3] & 0xffff0000u));
+              } else {
+                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(grp.o[row / G]) + at + 2 * m) = make_uint4(v[m], v[m + 1], v[m + 2], v[m + 3]);
+              }
+            }
+            if (g == 0) grp.lse[row / G][head] = none ? -INFINITY : log_sum(M[nb][h], sum[nb][h]);
+          }
+        }
+    } else {
+      // ---- a piece: the first of a share, or the last one if that starts a unit ----
+      const size_t piece = caller_splits ? size_t(blockIdx.x) : size_t(blockIdx.x) * 2 + (from_start ? 1 : 0);
+      float* const po = p.part_o + piece * p.rows * DH;
+      float* const pml = p.part_ml + piece * p.rows * 2;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = nb * 8 + 2 * t + h;
+          if (row < R) {
+#pragma unroll
+            for (int m = 0; m < MB; m += 2)
+              *reinterpret_cast<float4*>(po + row * DH + g * (DH / 8) + 2 * m) = make_float4(oacc[m][nb][h], oacc[m][nb][2 + h], oacc[m + 1][nb][h], oacc[m + 1][nb][2 + h]);
+            if (g == 0) *reinterpret_cast<float2*>(pml + row * 2) = make_float2(M[nb][h], sum[nb][h]);
+          }
+        }
+    }
+    if (last) break;
+  } while (true);
+  cp_async_wait<0>();
+}
+
+DealBy deal8_by(int rows) { return {D8_KEY, sm_count() * (rows <= 8 ? D8_CTAS<1> : D8_CTAS<2>)}; }
+// query rows of the largest group of a call
+int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
+  int rows = 0;
+  for (int i = 0; i < n; ++i) rows = std::max(rows, subs[i].n * (d->Hq / d->Hkv));
+  return rows;
+}
+
+template <int DH, int NB, int NG>
+cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
+  constexpr int smem = D8_WARPS * D8_STAGES<DH, NB> * 2 * GRAN * DH;
+  cudaError_t e = allow_smem<decode8_kernel<DH, NB, NG>>(smem);
+  if (e != cudaSuccess) return e;
+  Dec8Params<NG> p;
+  static_cast<DecSizes&>(p) = all;
+  std::copy(all.grp, all.grp + all.n_groups, p.grp);
+  timing_before(KVP_KERNEL_DECODE, stream);
+  e = launch_kernel(decode8_kernel<DH, NB, NG>, grid, D8_THREADS, smem, stream, 1, p);
+  timing_after(KVP_KERNEL_DECODE, stream);
+  if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
+    e = launch_kernel(decode_combine_kernel<DH, D8_KEY, true, Dec8Params<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+  return e;
+}
+template <int DH, int NB>
+cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& p, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
+  return p.n_groups <= FEW_DEC_GROUPS ? launch_decode8<DH, NB, FEW_DEC_GROUPS>(p, grid, combine_grid, wpr, stream)
+                                      : launch_decode8<DH, NB, MAX_DEC_GROUPS>(p, grid, combine_grid, wpr, stream);
+}
+
+int check_desc8(const kvp_decode_desc* d) {
+  const int rc = check_desc(d);
+  if (rc != KVP_OK) return rc;
+  return (long long)d->max_pages * d->page_size > 0x7fffffffLL - GRAN ? KVP_ERR_UNSUPPORTED : KVP_OK;
+}
+
+}  // namespace
+}  // namespace kvp
+
+using namespace kvp;
+
+extern "C" size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor) {
+  if (check_desc8(d) != KVP_OK || donor == nullptr) return 0;
+  for (int l = 0; l < d->L; ++l)
+    if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return 0;
+  // of any layer range: one that leaves out members of the largest groups may have fewer rows, and more blocks that fit
+  return std::max(decode_scratch_bytes(d, donor, 0, d->L, deal8_by(8)), decode_scratch_bytes(d, donor, 0, d->L, deal8_by(16)));
+}
+
+extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
+                           const void* const* v_cache, const uint8_t* const* k_scale, const uint8_t* const* v_scale, const int32_t* block_table,
+                           const int32_t* lengths, void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes,
+                           kvp_stream_t stream_) {
+  const int rc = check_desc8(d);
+  if (rc != KVP_OK) return rc;
+  if (donor == nullptr || q == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr || v_scale == nullptr ||
+      block_table == nullptr || lengths == nullptr || o == nullptr || lse == nullptr || !(scale >= 0.f && scale < INFINITY))
+    return KVP_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end > d->L || layer_begin >= layer_end) return KVP_ERR_INVALID_ARG;
+  for (int l = 0; l < d->L; ++l)
+    if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return KVP_ERR_BAD_DONOR;
+  static thread_local SubGroup subs[4096];
+  const int n_sub = build_groups(d, donor, layer_begin, layer_end, subs, 4096);
+  if (n_sub < 0) return KVP_ERR_UNSUPPORTED;
+  for (int i = 0; i < n_sub; ++i) {      // all of them before anything is launched
+    const int own = subs[i].owner;
+    if (k_cache[own] == nullptr || v_cache[own] == nullptr || k_scale[own] == nullptr || v_scale[own] == nullptr) return KVP_ERR_INVALID_ARG;
+    if (!aligned16(k_cache[own]) || !aligned16(v_cache[own])) return KVP_ERR_UNSUPPORTED;
+    for (int m = 0; m < subs[i].n; ++m) {
+      const int l = subs[i].members[m];
+      if (q[l] == nullptr || o[l] == nullptr || lse[l] == nullptr) return KVP_ERR_INVALID_ARG;
+      if (!aligned16(q[l]) || !aligned16(o[l]) || (reinterpret_cast<uintptr_t>(lse[l]) & 3u) != 0) return KVP_ERR_UNSUPPORTED;
+    }
+  }
+  const DealBy by = deal8_by(most_rows(d, subs, n_sub));
+  const Scratch plan = plan_scratch(d, subs, n_sub, 0, by);
+  if (ws == nullptr || ws_bytes < plan.bytes || !aligned16(ws)) return KVP_ERR_WORKSPACE;
+
+  Dec8Params<MAX_DEC_GROUPS> p;
+  p.block_table = block_table;
+  p.lengths = lengths;
+  p.part_o = reinterpret_cast<float*>(ws);
+  p.part_ml = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ws) + align256(plan.pieces * plan.rows * d->dh * 4));
+  p.B = d->B;
+  p.Hq = d->Hq;
+  p.Hkv = d->Hkv;
+  p.page_size = d->page_size;
+  p.max_pages = d->max_pages;
+  p.n_pages = d->n_pages;
+  p.rows = plan.rows;
+  p.fit = by.fit;
+  p.max_shares = plan.max_shares;
+  p.num_splits = d->num_splits;
+  p.io_f32 = d->dtype == KVP_F32;
+  p.scale_log2 = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
+
+  for (int s0 = 0; s0 < n_sub; s0 += MAX_DEC_GROUPS) {
+    const int n = std::min(n_sub - s0, MAX_DEC_GROUPS);
+    for (int i = 0; i < n; ++i) {
+      const SubGroup& sg = subs[s0 + i];
+      Dec8Group& g = p.grp[i];
+      g.k_cache = reinterpret_cast<const uint8_t*>(k_cache[sg.owner]);
+      g.v_cache = reinterpret_cast<const uint8_t*>(v_cache[sg.owner]);
+      g.k_scale = k_scale[sg.owner];
+      g.v_scale = v_scale[sg.owner];
+      g.n_members = sg.n;
+      g.pad = 0;
+      for (int m = 0; m < MAX_MEMBERS; ++m) {
+        const int l = sg.members[m < sg.n ? m : 0];
+        g.q[m] = q[l];
+        g.o[m] = o[l];
+        g.lse[m] = lse[l];
+      }
+    }
+    const int rows = most_rows(d, subs + s0, n);
+    const long long units = (long long)n * d->B * d->Hkv;
+    // a block for every share of the longest list; shares go by the lengths on the device, and so does whether whole units
+    // are dealt out instead
+    const long long blocks = d->num_splits > 0 ? units * d->num_splits
+                                               : std::max((long long)plan.max_shares, std::min(units, (long long)p.fit * max_rounds(by.key)));
+    if (units > 0x3fffffffLL || blocks > 0x3fffffffLL) return KVP_ERR_UNSUPPORTED;
+    p.n_groups = n;
+    p.by_units = dealt_by_units(by.key, longest_list(d, n), units, longest_unit(d), p.fit);
+    const long long unit_pieces = d->num_splits > 0 ? d->num_splits : plan.max_shares / units;
+    const int wpr = unit_pieces > 8 ? 8 : 1;   // many pieces a unit: eight warps share those of a row
+    const int rows_per_block = COMBINE_THREADS / 32 / wpr;
+    const dim3 grid(static_cast<unsigned>(blocks)), cgrid(unsigned(units), (rows + rows_per_block - 1) / rows_per_block);
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+    // (the whole call's largest group decides: p.fit goes by it)
+    const cudaError_t e = d->dh == 128 ? (plan.rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
+                                       : (plan.rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
+    if (e != cudaSuccess) return KVP_ERR_CUDA;
+  }
+  return KVP_OK;
+}

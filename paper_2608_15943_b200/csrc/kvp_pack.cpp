@@ -102,6 +102,10 @@ struct Library {
   decltype(&kvp_decode) decode;
 } lib;
 PyTypeObject *shape_type, *desc_type;   // kvp.Shape, kvp.DecodeDesc
+struct CacheLibrary {
+  decltype(&kvp_cache_append_tokens) append_tokens;
+  decltype(&kvp_decode8) decode8;
+} cache_lib;
 
 // bind(addresses of the entry points in the order above, Shape, DecodeDesc)
 PyObject* bind(PyObject*, PyObject* args) {
@@ -118,6 +122,32 @@ PyObject* bind(PyObject*, PyObject* args) {
   shape_type = reinterpret_cast<PyTypeObject*>(Py_NewRef(shape));
   desc_type = reinterpret_cast<PyTypeObject*>(Py_NewRef(desc));
   Py_RETURN_NONE;
+}
+
+// bind_cache(addresses of the two entry points that CacheLibrary lists)
+PyObject* bind_cache(PyObject*, PyObject* list) {
+  constexpr Py_ssize_t n = sizeof(CacheLibrary) / sizeof(void*);
+  if (!PyList_Check(list) || PyList_GET_SIZE(list) != n) return PyErr_Format(PyExc_ValueError, "%zd addresses", n);
+  void* at[n];
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    at[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  memcpy(&cache_lib, at, sizeof(cache_lib));
+  Py_RETURN_NONE;
+}
+
+// Element types of a tensor of the calls that look at their tensors.
+enum Kind { BF16, F32, I32, CODES, SCALES };
+bool is_kind(const at::Tensor& t, Kind k) {
+  const at::ScalarType s = t.scalar_type();
+  switch (k) {
+    case BF16: return s == at::kBFloat16;
+    case F32: return s == at::kFloat;
+    case I32: return s == at::kInt;
+    case CODES: return s == at::kFloat8_e4m3fn || s == at::kByte;
+    default: return s == at::kFloat8_e8m0fnu || s == at::kByte;
+  }
 }
 
 // The arguments of a call, one after the other; `ok` is false as soon as one is not of the plain kind.
@@ -230,6 +260,40 @@ struct Reader {
     if (n < layers) numbers[n] = -1;   // no donor: the map is refused before anything else is read
     else entries = layers;
     return numbers;
+  }
+  // Tensors whose type, size and device the call looks at (contiguous ones).  What does not fit is left to kvp.py, which says so.
+  int device = -2;           // of all of them; -2: not asked for
+  bool fits(PyObject* o, Kind kind, int64_t numel) {
+    ok = ok && THPVariable_CheckExact(o);
+    if (!ok) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    ok = is_kind(t, kind) && t.numel() == numel && t.is_contiguous() && (device == -2 || (t.is_cuda() && t.get_device() == device));
+    return ok;
+  }
+  void* one(Kind kind, int64_t numel) {
+    PyObject* o = next();
+    return fits(o, kind, numel) ? THPVariable_Unpack(o).data_ptr() : nullptr;
+  }
+  // A list over the layers, or (optional) None; of every layer in [begin, end) or of its donor.  Others are not looked at.
+  template <typename T>
+  T* layers_of(Kind kind, int64_t numel, const int32_t* donor, bool owners, bool optional = false, int begin = 0, int end = INT32_MAX) {
+    PyObject* o = next();
+    if (optional && o == Py_None) return nullptr;
+    Py_ssize_t n = 0;
+    PyObject** it = items(o, n);
+    const Py_ssize_t all = std::max(n, entries);
+    ok = ok && used + all <= kRoom;
+    if (!ok) return nullptr;
+    void** const dst = room + used;
+    std::fill(dst, dst + all, nullptr);
+    const Py_ssize_t many = std::min<Py_ssize_t>(n, entries);
+    for (Py_ssize_t l = std::max(begin, 0); l < many && l < end && ok; ++l) {
+      const Py_ssize_t i = owners ? donor[l] : l;
+      if (i < 0 || i >= many || it[i] == Py_None || dst[i] != nullptr) continue;   // (missing ones are the library's to refuse)
+      if (fits(it[i], kind, numel)) dst[i] = THPVariable_Unpack(it[i]).data_ptr();
+    }
+    used += int(all);
+    return reinterpret_cast<T*>(dst);
   }
   struct Space {
     void* p;
@@ -444,12 +508,83 @@ ENTRY(decode) {   // desc, donor, scale, q, k_cache, v_cache, block_table, lengt
     return [=] { return lib.decode(d, donor, scale, q, kc, vc, table, lengths, o, lse, begin, end, ws.p, ws.n, stream); };
   });
 }
+ENTRY(cache_append_tokens) {   // desc, donor, k_new, v_new, k_cache, v_cache, block_table, lengths, first, theta, q, q_out, k_scale, v_scale, device, stream
+  return run(args, n, 16, [&](Reader& r) {
+    r.ok = r.ok && cache_lib.append_tokens != nullptr;
+    r.device = r.ok && PyLong_CheckExact(args[14]) ? int(PyLong_AsLong(args[14])) : -2;
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    // the number of tokens: of the first layer's keys (the first layer is always an owner)
+    int64_t T = 0;
+    if (r.ok && r.left > 0 && PyList_CheckExact(*r.a) && PyList_GET_SIZE(*r.a) > 0 && THPVariable_CheckExact(PyList_GET_ITEM(*r.a, 0))) {
+      const at::Tensor& k0 = THPVariable_Unpack(PyList_GET_ITEM(*r.a, 0));
+      r.ok = k0.dim() > 0 && k0.size(0) <= INT32_MAX;
+      T = r.ok ? k0.size(0) : 0;
+    } else {
+      r.ok = false;
+    }
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    const Kind io = z.dtype == KVP_F32 ? F32 : BF16;
+    const bool bits8 = r.ok && args[12] != Py_None;
+    const int64_t kv = T * z.Hkv * z.dh, qs = T * z.Hq * z.dh, rows = int64_t(z.n_pages) * z.Hkv * z.page_size;
+    In kn = r.layers_of<const void* const>(io, kv, donor, true), vn = r.layers_of<const void* const>(io, kv, donor, true);
+    Out kc = r.layers_of<void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true), vc = r.layers_of<void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true);
+    auto* table = static_cast<const int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<const int32_t*>(r.one(I32, z.B));
+    const int32_t* first = nullptr;
+    if (r.left > 0 && *r.a == Py_None) r.next();
+    else first = static_cast<const int32_t*>(r.one(I32, int64_t(z.B) + 1));
+    const float theta = float(r.real());
+    In q = r.layers_of<const void* const>(io, qs, donor, false, true);
+    Out q_out = r.layers_of<void* const>(io, qs, donor, false, true);
+    typedef uint8_t* const* Scale;
+    Scale ks = r.layers_of<uint8_t* const>(SCALES, rows / 16, donor, true, true), vs = r.layers_of<uint8_t* const>(SCALES, rows / 16, donor, true, true);
+    r.integer();
+    const kvp_stream_t stream = r.stream();
+    return [=] { return cache_lib.append_tokens(d, donor, int32_t(T), first, theta, q, q_out, kn, vn, kc, vc, ks, vs, table, lengths, stream); };
+  });
+}
+ENTRY(decode8) {   // desc, donor, scale, q, k_cache, v_cache, k_scale, v_scale, block_table, lengths, o, lse, layer_begin, layer_end or None, ws, device, stream
+  return run(args, n, 17, [&](Reader& r) {
+    r.ok = r.ok && cache_lib.decode8 != nullptr;
+    r.device = r.ok && PyLong_CheckExact(args[15]) ? int(PyLong_AsLong(args[15])) : -2;
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    const float scale = float(r.real());
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    r.ok = r.ok && PyLong_CheckExact(args[12]) && (args[13] == Py_None || PyLong_CheckExact(args[13]));
+    const long begin = r.ok ? PyLong_AsLong(args[12]) : 0, end = r.ok && args[13] != Py_None ? PyLong_AsLong(args[13]) : z.L;
+    if (r.ok && (begin < 0 || begin >= end || end > z.L)) r.ok = false;   // (kvp.py's to refuse)
+    const int b = int(begin), e = int(end);
+    const Kind io = z.dtype == KVP_F32 ? F32 : BF16;
+    const int64_t qs = int64_t(z.B) * z.Hq * z.dh, rows = int64_t(z.n_pages) * z.Hkv * z.page_size;
+    In q = r.layers_of<const void* const>(io, qs, donor, false, false, b, e);
+    In kc = r.layers_of<const void* const>(CODES, rows * z.dh, donor, true, false, b, e), vc = r.layers_of<const void* const>(CODES, rows * z.dh, donor, true, false, b, e);
+    typedef const uint8_t* const* Scale;
+    Scale ks = r.layers_of<const uint8_t* const>(SCALES, rows / 16, donor, true, false, b, e), vs = r.layers_of<const uint8_t* const>(SCALES, rows / 16, donor, true, false, b, e);
+    auto* table = static_cast<const int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<const int32_t*>(r.one(I32, z.B));
+    Out o = r.layers_of<void* const>(io, qs, donor, false, false, b, e);
+    OutF lse = r.layers_of<float* const>(F32, int64_t(z.B) * z.Hq, donor, false, false, b, e);
+    r.next();
+    r.next();
+    if (r.ok && r.left > 0 && *r.a != Py_None && THPVariable_CheckExact(*r.a)) {
+      const at::Tensor& w = THPVariable_Unpack(*r.a);
+      r.ok = w.is_contiguous() && (r.device == -2 || (w.is_cuda() && w.get_device() == r.device));
+    }
+    const Reader::Space ws = r.workspace();
+    r.next();
+    const kvp_stream_t stream = r.stream();
+    return [=] { return cache_lib.decode8(d, donor, scale, q, kc, vc, ks, vs, table, lengths, o, lse, b, e, ws.p, ws.n, stream); };
+  });
+}
 #define METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(fn)), METH_FASTCALL, nullptr}
 
-PyMethodDef methods[] = {{"pointers", pointers, METH_VARARGS, nullptr}, {"donors", donors, METH_O, nullptr}, {"bind", bind, METH_VARARGS, nullptr},
+PyMethodDef methods[] = {{"pointers", pointers, METH_VARARGS, nullptr}, {"donors", donors, METH_O, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr},
                          METHOD("gemm", gemm), METHOD("rmsnorm", rmsnorm), METHOD("rope", rope), METHOD("swiglu", zip<false>), METHOD("add", zip<true>),
                          METHOD("proj_fwd", proj_fwd), METHOD("proj_bwd", proj_bwd), METHOD("out_proj_fwd", out_proj_fwd), METHOD("out_proj_bwd", out_proj_bwd),
                          METHOD("attn_fwd", attn_fwd), METHOD("attn_bwd", attn_bwd), METHOD("cache_append", cache_append), METHOD("decode", decode),
+                         METHOD("cache_append_tokens", cache_append_tokens), METHOD("decode8", decode8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pack", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <math.h>
+#include <stdint.h>
 
 namespace kvp {
 
@@ -15,6 +16,14 @@ inline void rope_frequencies(double theta, int dh, float* hi, float* lo, int str
     hi[i * stride] = float(f);
     lo[i * stride] = float(f - (long double)hi[i * stride]);
   }
+}
+
+// The same frequencies in turns a position, as 64-bit fractions of a turn: a position's angle is the product modulo 2^64, which
+// leaves no more of an error than pos * 2^-57 turns (the ratio's roundings; the first frequency, pos * 2^-65).
+inline void rope_turns(double theta, int dh, uint64_t* turns) {
+  const long double ratio = powl((long double)theta, -2.0L / dh);
+  long double f = 0.159154943091895335768883763372514362L * 18446744073709551616.0L;   // 2^64 / (2 pi)
+  for (int i = 0; i < dh / 2; ++i, f *= ratio) turns[i] = uint64_t(f + 0.5L);
 }
 
 }  // namespace kvp

@@ -33,7 +33,8 @@ EXPORTS = ["kvp_status_string", "kvp_device_status", "kvp_launch_count", "kvp_se
            "kvp_timing_events_used", "kvp_plan", "kvp_layer_flops", "kvp_sim_1f1b", "kvp_workspace_bytes",
            "kvp_proj_fwd", "kvp_proj_bwd", "kvp_proj_bwd_range", "kvp_out_proj_fwd", "kvp_out_proj_bwd", "kvp_attn_fwd", "kvp_attn_bwd",
            "kvp_gemm", "kvp_rmsnorm", "kvp_rope", "kvp_swiglu", "kvp_add", "kvp_decode_workspace_bytes", "kvp_cache_append",
-           "kvp_decode", "kvp_decode_static", "kvp_selftest_bounded_wait"]
+           "kvp_decode", "kvp_decode_static", "kvp_selftest_bounded_wait",
+           "kvp_cache_append_tokens", "kvp_decode8", "kvp_decode8_workspace_bytes"]
 
 
 class KvpError(RuntimeError):
@@ -511,3 +512,121 @@ def decode_static(desc, donor, q, k_cache, v_cache, block_table, lengths, o, lse
                                  _ptr_array(v_cache, n), block_table.data_ptr(), lengths.data_ptr(), _ptr_array(o, n),
                                  _ptr_array(lse, n), layer_begin, desc.L if layer_end is None else layer_end, _stream()),
            "kvp_decode_static")
+
+
+# ------------------------------------------------------------------------------------------
+# tokens with rotary positions into the paged cache; the cache held in 8 bits
+# ------------------------------------------------------------------------------------------
+CACHE_BLOCK = 16     # tokens that share a scale
+lib.kvp_cache_append_tokens.restype = C.c_int
+lib.kvp_cache_append_tokens.argtypes = [C.POINTER(DecodeDesc), C.c_void_p, C.c_int32, C.c_void_p, C.c_float] + [_PP] * 8 + [C.c_void_p] * 3
+lib.kvp_decode8_workspace_bytes.restype = C.c_size_t
+lib.kvp_decode8_workspace_bytes.argtypes = [C.POINTER(DecodeDesc), C.c_void_p]
+lib.kvp_decode8.restype = C.c_int
+lib.kvp_decode8.argtypes = [C.POINTER(DecodeDesc), C.c_void_p, C.c_float] + [_PP] * 5 + [C.c_void_p, C.c_void_p] + [_PP] * 2 + \
+    [C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+_pack.bind_cache([C.cast(getattr(lib, "kvp_" + n), C.c_void_p).value for n in ("cache_append_tokens", "decode8")])
+
+_I32, _CODES, _SCALES = (torch.int32,), (torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8)
+
+
+def _call_device() -> int:
+    """Device that a call runs on (-2: there is none, and the library refuses the call or fails to launch)."""
+    if torch.cuda.is_initialized():
+        return _device()
+    return 0 if torch.cuda.is_available() else -2
+
+
+def _fit(what: str, t, dtypes, numel: int, device: int) -> None:
+    """The library sees pointers alone: what a tensor has to be besides is looked at here."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what} is {t.dtype}: {' or '.join(map(str, dtypes))} is wanted")
+    if t.numel() != numel:
+        raise ValueError(f"{what} has {t.numel()} elements {tuple(t.shape)}: {numel} are wanted")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} has strides {t.stride()}: a contiguous tensor is wanted")
+    if device != -2 and (not t.is_cuda or t.get_device() != device):
+        raise ValueError(f"{what} is on {t.device}: the call runs on cuda:{device}")
+
+
+def _fit_layers(what, ts, dtypes, numel, layers, device) -> None:
+    for l in layers:
+        if l < len(ts) and ts[l] is not None:      # (missing ones are the library's to refuse)
+            _fit(f"{what}[{l}]", ts[l], dtypes, numel, device)
+
+
+def _layer_range(desc, donor, begin=0, end=None):
+    """Layers of a call and their donors, as far as the map is one (the library refuses it otherwise)."""
+    n = min(max(desc.L, 0), len(donor))
+    layers = range(max(begin, 0), n if end is None else min(end, n))
+    return layers, sorted({int(donor[l]) for l in layers if 0 <= int(donor[l]) <= l})
+
+
+def _io(desc):
+    return (torch.float32,) if desc.dtype == F32 else (torch.bfloat16,)
+
+
+def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table, lengths, first=None, theta=0.0, q=None, q_out=None,
+                        k_scale=None, v_scale=None):
+    """kvp_cache_append_tokens: the rows k_new[l], v_new[l] [T, Hkv, dh] (owner layers) go into the pages of their sequences, K
+    rotated by the token's position where theta is not 0, and q[l] [T, Hq, dh] rotated by the same positions goes to q_out[l].
+    Sequence b has rows first[b] .. first[b+1]-1 (int32 [B + 1]; None: one token each, T == B) at the positions before lengths[b].
+    With k_scale, v_scale (uint8 or float8_e8m0fnu [n_pages, Hkv, page_size / 16]) the cache holds float8_e4m3fn numbers.
+    Tensors are contiguous, of the documented sizes, on the current device: ValueError otherwise."""
+    device = _call_device()
+    status = _pack.cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table, lengths, first, theta, q, q_out, k_scale, v_scale,
+                                       device, _stream())
+    if status is not NotImplemented:
+        return _check(status, "kvp_cache_append_tokens")
+    layers, owners = _layer_range(desc, donor)
+    T = next((int(t.shape[0]) if t.dim() else 0 for t in k_new if t is not None), 0)
+    rows, io = desc.n_pages * desc.Hkv * desc.page_size, _io(desc)
+    held = (torch.bfloat16,) if k_scale is None else _CODES
+    for what, ts, dtypes, numel, of in (("k_new", k_new, io, T * desc.Hkv * desc.dh, owners), ("v_new", v_new, io, T * desc.Hkv * desc.dh, owners),
+                                        ("k_cache", k_cache, held, rows * desc.dh, owners), ("v_cache", v_cache, held, rows * desc.dh, owners),
+                                        ("q", q, io, T * desc.Hq * desc.dh, layers), ("q_out", q_out, io, T * desc.Hq * desc.dh, layers),
+                                        ("k_scale", k_scale, _SCALES, rows // CACHE_BLOCK, owners), ("v_scale", v_scale, _SCALES, rows // CACHE_BLOCK, owners)):
+        if ts is not None:
+            _fit_layers(what, ts, dtypes, numel, of, device)
+    for what, t, numel in (("block_table", block_table, desc.B * desc.max_pages), ("lengths", lengths, desc.B), ("first", first, desc.B + 1)):
+        if t is not None:
+            _fit(what, t, _I32, numel, device)
+    d, n = _map(desc, donor)
+    array = lambda ts: None if ts is None else _ptr_array(ts, n)
+    _check(lib.kvp_cache_append_tokens(C.byref(desc), d, T, _ptr(first), float(theta), array(q), array(q_out), array(k_new), array(v_new),
+                                       array(k_cache), array(v_cache), array(k_scale), array(v_scale), _ptr(block_table), _ptr(lengths), _stream()),
+           "kvp_cache_append_tokens")
+
+
+def decode8_workspace_bytes(desc: DecodeDesc, donor) -> int:
+    """kvp_decode8_workspace_bytes: enough for any layer range."""
+    d, entries = _map(desc, donor)
+    return int(lib.kvp_decode8_workspace_bytes(C.byref(desc), d)) if entries else 0
+
+
+def decode8(desc, donor, q, k_cache, v_cache, k_scale, v_scale, block_table, lengths, o, lse, ws, scale=0.0, layer_begin=0, layer_end=None):
+    """kvp_decode8: decode attention over the cache held in 8 bits, as cache_append_tokens with scales leaves it.  Arguments as for
+    decode; a sequence of length 0 has output 0 and LSE -infinity.  Tensors are contiguous, of the documented sizes, on the
+    current device: ValueError otherwise."""
+    device = _call_device()
+    status = _pack.decode8(desc, donor, scale, q, k_cache, v_cache, k_scale, v_scale, block_table, lengths, o, lse, layer_begin, layer_end, ws, device,
+                           _stream())
+    if status is not NotImplemented:
+        return _check(status, "kvp_decode8")
+    end = desc.L if layer_end is None else int(layer_end)
+    layers, owners = _layer_range(desc, donor, int(layer_begin), end)
+    rows, io = desc.n_pages * desc.Hkv * desc.page_size, _io(desc)
+    for what, ts, dtypes, numel, of in (("q", q, io, desc.B * desc.Hq * desc.dh, layers), ("o", o, io, desc.B * desc.Hq * desc.dh, layers),
+                                        ("lse", lse, (torch.float32,), desc.B * desc.Hq, layers),
+                                        ("k_cache", k_cache, _CODES, rows * desc.dh, owners), ("v_cache", v_cache, _CODES, rows * desc.dh, owners),
+                                        ("k_scale", k_scale, _SCALES, rows // CACHE_BLOCK, owners), ("v_scale", v_scale, _SCALES, rows // CACHE_BLOCK, owners)):
+        _fit_layers(what, ts, dtypes, numel, of, device)
+    _fit("block_table", block_table, _I32, desc.B * desc.max_pages, device)
+    _fit("lengths", lengths, _I32, desc.B, device)
+    if ws is not None:
+        _fit("ws", ws, (ws.dtype,), ws.numel(), device)
+    d, n = _map(desc, donor)
+    p, size = _ws(ws)
+    _check(lib.kvp_decode8(C.byref(desc), d, float(scale), _ptr_array(q, n), _ptr_array(k_cache, n), _ptr_array(v_cache, n), _ptr_array(k_scale, n),
+                           _ptr_array(v_scale, n), block_table.data_ptr(), lengths.data_ptr(), _ptr_array(o, n), _ptr_array(lse, n), int(layer_begin), end, p,
+                           size, _stream()), "kvp_decode8")
