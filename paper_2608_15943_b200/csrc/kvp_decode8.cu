@@ -1,18 +1,19 @@
 // Split-KV decode attention over the shared paged cache held in 8 bits (kvp_cache8.h): half the bytes of the bf16 cache, and the
 // same list of K/V rows dealt out to blocks (kvp_decode.cu describes it), the same groups of layers, the same merge.
 //
-// With half the bytes a granule of 16 tokens and one KV head (4 KB at dh 128) has to pass an SM in about 170 cycles to keep HBM
-// busy, so the design is about instructions a granule:
+// With half the bytes a warp's step of 32 tokens of one KV head (8 KB at dh 128) has to pass an SM in about 340 cycles to keep HBM
+// busy, so the design is about instructions a step:
 //  - K and V are the A operand of mma.sync m16n8k16 (f16 in, fp32 accumulate) and the query rows its N: up to 8 rows cost half the
 //    products that they cost as its M, and the scores of a granule are 4 registers a lane.  S^T = K Q^T, O^T += V^T P^T.
-//  - e4m3 numbers become f16 exactly, two an instruction.  Which element of a row is which k of a product is free as long as both
-//    operands agree, so a lane reads K 16 bytes at a time and its words are its operands.  Tokens are matched to the rows of S^T so
-//    that the V numbers of four tokens that a lane needs lie in four of its own 16-byte words, two byte permutes away.
+//  - e4m3 numbers become f16 exactly, two an instruction.  (mma.sync takes e4m3 as it is, but converts it itself at twice the
+//    instructions.)  Which element of a row is which k of a product is free as long as both operands agree, so a lane reads K 16 bytes
+//    at a time and its words are its operands; V comes transposed from ldmatrix .b8, four tokens of an element a word, and the
+//    rows of S^T are matched to those tokens.
 //  - Queries are scaled by a power of two a row into f16's range (the largest to 2^14): exact for all bf16 elements down to 2^-31 of
 //    the row's largest, and rounded by at most 2^-39 of it below.  The scale of K joins the factor of the scores.
 //  - The scale of V is a power of two: P is multiplied by 2^(e + M - R) with a reference R of the accumulators beside the
 //    reference M of the sum.  Both rise only when a value would leave f16's upper range, so that no maximum is exchanged between
-//    lanes in nearly all granules: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
+//    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
 #include "kvp_cache8.cuh"
 #include "kvp_decode_list.cuh"
@@ -21,11 +22,15 @@ namespace kvp {
 namespace {
 
 constexpr int D8_WARPS = 4, D8_THREADS = D8_WARPS * 32;
-constexpr int D8_KEY = 64;                        // granules of 4 KB (dh 128), as those of the bf16 cache at dh 64 are
-template <int NB>
-constexpr int D8_CTAS = NB == 1 ? 4 : 3;          // per SM, by registers and shared memory
-template <int DH, int NB>
-constexpr int D8_STAGES = (NB == 1 ? 3 : 4) * (DH == 128 ? 1 : 2);   // granules of a warp in the ring
+constexpr int STEP = 2 * GRAN;                    // tokens of a step of a warp: two granules, each with scales of its own
+#ifndef V_STAGES
+#define V_STAGES 2
+#define V_CTAS 3
+#endif
+template <int DH>
+constexpr int D8_STAGES = DH == 128 ? V_STAGES : 3;   // steps of a warp in the ring
+template <int DH>
+constexpr int D8_CTAS = DH == 128 ? V_CTAS : 4;   // per SM, as many as shared memory holds
 constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
@@ -54,38 +59,47 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Two matrices of 16 rows of 16 bytes (row addresses in lanes 0 to 15 and 16 to 31), transposed: register 2m + i of lane (g, t) holds
+// columns g + 8i of rows 4t .. 4t + 3 of matrix m.
+__device__ __forceinline__ void ldsm_b8_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
+}
+// 16-byte asynchronous copy
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ uint4 lds16(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ uint2 lds8(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-  return v;
-}
 
-// Ring stage: 16 rows of DH bytes of K, then of V.  16-byte chunks are permuted inside lines of 128 bytes so that both reads are
-// free of bank conflicts: K's (lanes of a phase: rows 4i and 4i + 1, four chunks of each) and V's (rows i, i + 4, i + 8, i + 12, two
-// chunks of each).
+// Ring stage: 32 rows of DH bytes of K, then of V.  16-byte chunks are permuted inside lines of 128 bytes so that reads are free of
+// bank conflicts: K's lanes of a phase want four chunks of rows 4i and 4i + 1, V's eight rows of ldmatrix the same chunk of each.
 template <int DH>
-__device__ __forceinline__ uint32_t ring8_off(int row, int chunk) {
-  if (DH == 128) return uint32_t(row) * 128 + (uint32_t(chunk ^ ((row >> 2 & 3) << 1) ^ ((row & 1) << 2)) << 4);
-  return uint32_t(row >> 1) * 128 + (uint32_t(((row & 1) << 2 | chunk) ^ ((row >> 2 & 3) << 1)) << 4);
+__device__ __forceinline__ uint32_t k_off(int row, int chunk) {
+  if (DH == 128) return uint32_t(row) * 128 + (uint32_t(chunk ^ ((row & 1) << 2)) << 4);
+  return uint32_t(row) * 64 + (uint32_t(chunk) << 4);
+}
+template <int DH>
+__device__ __forceinline__ uint32_t v_off(int row, int chunk) {
+  if (DH == 128) return uint32_t(row) * 128 + (uint32_t(chunk ^ (row & 7)) << 4);
+  return uint32_t(row >> 1) * 128 + (uint32_t((row & 1) << 2 | (chunk ^ (row >> 1 & 3))) << 4);
 }
 
 template <int DH, int NB, int NG>
-__global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
-  constexpr int TILE_BYTES = GRAN * DH, STAGE_BYTES = 2 * TILE_BYTES, STAGES = D8_STAGES<DH, NB>;
+__global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
+  constexpr int GRAN_BYTES = GRAN * DH, TILE_BYTES = 2 * GRAN_BYTES, STAGE_BYTES = 2 * TILE_BYTES, STAGES = D8_STAGES<DH>;
   constexpr int CHUNKS = DH / 16;                  // 16-byte chunks of a row
-  constexpr int CP_PER_LANE = TILE_BYTES / 16 / 32;
+  constexpr int CP_PER_LANE = GRAN_BYTES / 16 / 32;
   constexpr int HALVES = DH / 64;                  // 16-byte words of a K row that a lane takes
-  constexpr int MB = DH / 16;                      // m-blocks of O^T; a lane has DH / 8 consecutive elements of a row
+  constexpr int KSTEPS = DH / 16;
+  constexpr int MB = DH / 16;                      // m-blocks of O^T
 
   extern __shared__ __align__(128) uint8_t dsmem[];
   __shared__ float2 s_o[D8_WARPS - 1][MB * 32];    // four rows of the results that warp 0 merges into its own
@@ -121,11 +135,11 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
     int before, all, longest;
     sum_granules(p, len0, 0, before, all, longest);
     const long long granules = (long long)all * p.Hkv * p.n_groups;
-    by_units = dealt_by_units(D8_KEY, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit);
-    rest = by_units ? 0 : unit_rest(D8_KEY, granules, p.fit);
+    by_units = dealt_by_units(DH, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit);
+    rest = by_units ? 0 : unit_rest(DH, granules, p.fit);
     if (by_units) return true;
     const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
-    const int n_shares = shares_for(D8_KEY, p.fit, p.max_shares, total);
+    const int n_shares = shares_for(DH, p.fit, p.max_shares, total);
     if (blockIdx.x >= n_shares) return false;
     const Dealt dealt(total, n_shares);
     long long at = dealt.begin(blockIdx.x);
@@ -207,72 +221,89 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
     if (c.grp >= p.n_groups) return;
   }
 
-  // ---- copies: a cursor of their own, STAGES - 1 of this warp's granules ahead of the arithmetic ----
+  // ---- copies: a cursor of their own, STAGES - 1 of this warp's steps ahead of the arithmetic ----
   const uint32_t ring = smem_u32(dsmem) + warp * STAGES * STAGE_BYTES;
   Cursor f = c;
   int f_todo = todo;
-  int f_left;                                      // granules of the piece from this warp's next one on (<= 0: none)
+  int f_left;                                      // steps of the piece from this warp's next one on (<= 0: none)
   const int gran_per_page = p.page_size / GRAN;
   const Dec8Group* f_grp = &p.grp[0];
-  const int32_t* bt = nullptr;                     // block-table entry of the page the next granule is in,
-  int in_page = 0, f_tok = 0;                      // its place there, and its first token
+  const int32_t* bt = nullptr;                     // block-table entry of the page the next step begins in,
+  int in_page = 0, f_live = 0;                     // its granule there; tokens of the piece from there on
   size_t page_block = 0;                           // blocks of 16 tokens before this KV head's of that page
   int stage_in = 0;
-  uint32_t scales[STAGES];                         // of the granules in the ring, K's byte and V's above it
-#pragma unroll
-  for (int s = 0; s < STAGES; ++s) scales[s] = 0;
-  auto enter_page = [&]() {
-    const int page = min(max(*bt, 0), p.n_pages - 1);
-    page_block = (size_t(page) * p.Hkv + f.hk) * gran_per_page;
-  };
+  auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
   auto enter_piece = [&]() {
-    f_left = min(f_todo, f.ng - f.gran) - warp;
+    const int n = min(f_todo, f.ng - f.gran);
+    f_left = (n + 1) / 2 - warp;
     if (f_left <= 0) return;
-    const int gran = f.gran + warp, col = gran / gran_per_page;
+    const int gran = f.gran + 2 * warp, col = gran / gran_per_page;
     f_grp = &p.grp[f.grp];
     bt = p.block_table + size_t(f.b) * p.max_pages + col;
     in_page = gran - col * gran_per_page;
-    f_tok = gran * GRAN;
-    enter_page();
+    f_live = min(f.seen, (f.gran + n) * GRAN) - gran * GRAN;
+    page_block = block_of(*bt);
   };
-  auto issue_next = [&]() -> uint32_t {
-    uint32_t scale = 0;
+  struct Scales {
+    uint32_t k[2], v[2];                           // bytes of a step's granules
+  };
+  Scales scales[STAGES];
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) scales[s] = {{0, 0}, {0, 0}};
+  auto issue_next = [&](Scales& sc) {
     while (f_left <= 0 && f.grp < p.n_groups) {
       next_piece(f, f_todo);
       if (f.grp < p.n_groups) enter_piece();
     }
     if (f_left > 0) {
-      const size_t block = page_block + in_page;
-      const uint8_t* const ksrc = f_grp->k_cache + block * TILE_BYTES;
-      const uint8_t* const vsrc = f_grp->v_cache + block * TILE_BYTES;
+      const size_t block0 = page_block + in_page;
+      size_t block1 = block0;
+      if (f_live > GRAN) block1 = in_page + 1 < gran_per_page ? block0 + 1 : block_of(bt[1]);
       const uint32_t dst = ring + stage_in * STAGE_BYTES;
-      if (f.seen > 0) scale = uint32_t(f_grp->k_scale[block]) | uint32_t(f_grp->v_scale[block]) << 8;
+      sc.k[0] = f_grp->k_scale[block0];
+      sc.v[0] = f_grp->v_scale[block0];
+      sc.k[1] = f_grp->k_scale[block1];
+      sc.v[1] = f_grp->v_scale[block1];
 #pragma unroll
-      for (int i = 0; i < CP_PER_LANE; ++i) {
-        const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
-        const uint32_t off = ring8_off<DH>(row, chunk);
-        const uint32_t nbytes = f_tok + row < f.seen ? 16u : 0u;   // slots never appended may hold anything: zeros instead
-        cp_async16(dst + off, ksrc + idx * 16, nbytes);
-        cp_async16(dst + TILE_BYTES + off, vsrc + idx * 16, nbytes);
+      for (int h = 0; h < 2; ++h) {
+        const size_t at = (h ? block1 : block0) * GRAN_BYTES + lane * 16;
+        const uint8_t* const ksrc = f_grp->k_cache + at;
+        const uint8_t* const vsrc = f_grp->v_cache + at;
+        if (f_live >= (h + 1) * GRAN) {
+#pragma unroll
+          for (int i = 0; i < CP_PER_LANE; ++i) {
+            const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
+            cp_async16(dst + k_off<DH>(row, chunk), ksrc + i * 512);
+            cp_async16(dst + TILE_BYTES + v_off<DH>(row, chunk), vsrc + i * 512);
+          }
+        } else {                                   // slots never appended may hold anything: zeros instead
+#pragma unroll
+          for (int i = 0; i < CP_PER_LANE; ++i) {
+            const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
+            const uint32_t nbytes = row < f_live ? 16u : 0u;
+            cp_async16(dst + k_off<DH>(row, chunk), ksrc + i * 512, nbytes);
+            cp_async16(dst + TILE_BYTES + v_off<DH>(row, chunk), vsrc + i * 512, nbytes);
+          }
+        }
       }
       if (++stage_in == STAGES) stage_in = 0;
       f_left -= D8_WARPS;
-      f_tok += D8_WARPS * GRAN;
-      in_page += D8_WARPS;
+      f_live -= D8_WARPS * STEP;
+      in_page += D8_WARPS * 2;
       if (in_page >= gran_per_page && f_left > 0) {
-        const int pages = in_page / gran_per_page;
-        bt += pages;
-        in_page -= pages * gran_per_page;
-        enter_page();
+        do {
+          in_page -= gran_per_page;
+          ++bt;
+        } while (in_page >= gran_per_page);
+        page_block = block_of(*bt);
       }
     }
     cp_async_commit();
-    return scale;
   };
   enter_piece();
 
   // ---- queries: B operand, row n of the group in lanes g = n mod 8 ----
-  uint32_t qb[HALVES * 4][NB][2];
+  uint32_t qb[KSTEPS][NB][2];
   float q_factor[NB][2];                           // of the scores of rows 8 nb + 2 t + h
   auto load_queries = [&]() {
     const Dec8Group& grp = p.grp[c.grp];
@@ -312,7 +343,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
       const float up = __uint_as_float(power_bits(lg < 128 ? 14 - lg : 0));
       const float down = __uint_as_float(power_bits(lg < 128 ? lg - 14 : 0)) * p.scale_log2;
 #pragma unroll
-      for (int e = 0; e < HALVES * 4; ++e) {
+      for (int e = 0; e < KSTEPS; ++e) {
         qb[e][nb][0] = pack_f16(v[4 * e] * up, v[4 * e + 1] * up);
         qb[e][nb][1] = pack_f16(v[4 * e + 2] * up, v[4 * e + 3] * up);
       }
@@ -322,10 +353,10 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
   };
 
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) scales[s] = issue_next();
+  for (int s = 0; s < STAGES - 1; ++s) issue_next(scales[s]);
   load_queries();
 
-  const int tok_g = (g >> 1) * 4 + (g & 1);        // token of the granule that row g of S^T is; row g + 8: two more
+  const int tok_g = (g >> 1) * 4 + (g & 1);        // token of a granule that row g of its S^T is; row g + 8: two more
   int stage_out = 0;
   do {
     // ---- one unit, or this block's piece of it ----
@@ -339,7 +370,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
     for (int m = 0; m < MB; ++m)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) oacc[m][nb][0] = oacc[m][nb][1] = oacc[m][nb][2] = oacc[m][nb][3] = 0.f;
-    float sum[NB][2], M[NB][2], Rf[NB][2];         // of rows 8 nb + 2 t + h: sum against M (this lane's tokens), reference of oacc
+    float sum[NB][2], M[NB][2], Rf[NB][2];         // of rows 8 nb + 2 t + h: sum of this lane's terms, against M; reference of oacc
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -348,68 +379,87 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
         M[nb][h] = Rf[nb][h] = -1e30f;             // (finite: below every score, and no infinity minus infinity)
       }
 
-    for (int i = warp; i < n_here; i += D8_WARPS) {
+    const int tokens = min(c.seen, (c.gran + n_here) * GRAN) - c.gran * GRAN;   // that the piece sees (0: none)
+    for (int i = warp; 2 * i < n_here; i += D8_WARPS) {
       cp_async_wait<STAGES - 2>();
       __syncwarp();
-      scales[STAGES - 1] = issue_next();           // into the stage freed by the previous granule
-      const uint32_t here = scales[0];
-#pragma unroll
-      for (int s = 0; s + 1 < STAGES; ++s) scales[s] = scales[s + 1];
+      issue_next(scales[STAGES - 1]);              // into the stage freed by the previous step
       const uint32_t sK = ring + stage_out * STAGE_BYTES, sV = sK + TILE_BYTES;
       if (++stage_out == STAGES) stage_out = 0;
-      const float k_scale = __uint_as_float(power_bits(exponent_of_byte(here & 0xffu)));
-      const float v_exp = float(exponent_of_byte(here >> 8));
 
-      // ---- S^T[16 tokens, rows] = K Q^T, even and odd k-steps apart ----
-      float s2[2][NB][4];
+      // ---- S^T[32 tokens, rows] = K Q^T, even and odd k-steps apart ----
+      float s2[2][NB][2][4];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int m = 0; m < 2; ++m) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s2[0][nb][u] = s2[1][nb][u] = 0.f;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int hf = 0; hf < HALVES; ++hf) {
-        const uint4 ka = lds16(sK + ring8_off<DH>(tok_g, hf * 4 + t)), kb = lds16(sK + ring8_off<DH>(tok_g + 2, hf * 4 + t));
-        const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+          for (int u = 0; u < 4; ++u) s2[m][nb][0][u] = s2[m][nb][1][u] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(wa[w])), e4m3x2_to_f16x2(uint16_t(wb[w])), e4m3x2_to_f16x2(uint16_t(wa[w] >> 16)),
-                                 e4m3x2_to_f16x2(uint16_t(wb[w] >> 16))};
+        for (int hf = 0; hf < HALVES; ++hf) {
+          const uint4 ka = lds16(sK + k_off<DH>(m * GRAN + tok_g, hf * 4 + t)), kb = lds16(sK + k_off<DH>(m * GRAN + tok_g + 2, hf * 4 + t));
+          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma_f16(s2[w & 1][nb], a, qb[hf * 4 + w][nb][0], qb[hf * 4 + w][nb][1]);
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(wa[w])), e4m3x2_to_f16x2(uint16_t(wb[w])), e4m3x2_to_f16x2(uint16_t(wa[w] >> 16)),
+                                   e4m3x2_to_f16x2(uint16_t(wb[w] >> 16))};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_f16(s2[m][nb][w & 1], a, qb[hf * 4 + w][nb][0], qb[hf * 4 + w][nb][1]);
+          }
         }
       }
       // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
-      const int left = c.seen - (c.gran + i) * GRAN;   // visible tokens from this granule on
-      float x[NB][4];
+      const int left = tokens - i * STEP;          // visible tokens from this step on
+      float x[2][NB][4], v_exp[2];
       bool over = false;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const float k_scale = __uint_as_float(power_bits(exponent_of_byte(scales[0].k[m])));
+        v_exp[m] = float(exponent_of_byte(scales[0].v[m]));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float factor = q_factor[nb][h] * k_scale;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) x[m][nb][2 * u + h] = (s2[m][nb][0][2 * u + h] + s2[m][nb][1][2 * u + h]) * factor;
+          }
+      }
+      if (left < STEP) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            if (m * GRAN + tok_g + 2 * u >= left) {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) x[m][nb][2 * u] = x[m][nb][2 * u + 1] = -INFINITY;
+            }
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float factor = q_factor[nb][h] * k_scale;
-          x[nb][h] = (s2[0][nb][h] + s2[1][nb][h]) * factor;
-          x[nb][2 + h] = (s2[0][nb][2 + h] + s2[1][nb][2 + h]) * factor;
-          if (left < GRAN) {
-            if (tok_g >= left) x[nb][h] = -INFINITY;
-            if (tok_g + 2 >= left) x[nb][2 + h] = -INFINITY;
-          }
-          const float most = fmaxf(x[nb][h], x[nb][2 + h]);
-          over = over || most > M[nb][h] + SUM_TOP || most + v_exp > Rf[nb][h] + P_TOP;
+          const float m0 = fmaxf(x[0][nb][h], x[0][nb][2 + h]), m1 = fmaxf(x[1][nb][h], x[1][nb][2 + h]);
+          over = over || fmaxf(m0, m1) > M[nb][h] + SUM_TOP || fmaxf(m0 + v_exp[0], m1 + v_exp[1]) > Rf[nb][h] + P_TOP;
         }
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float most = fmaxf(x[nb][h], x[nb][2 + h]);
+            const float m0 = fmaxf(x[0][nb][h], x[0][nb][2 + h]), m1 = fmaxf(x[1][nb][h], x[1][nb][2 + h]);
+            float most = fmaxf(m0, m1), top = fmaxf(m0 + v_exp[0], m1 + v_exp[1]);
 #pragma unroll
-            for (int s = 4; s < 32; s <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+            for (int s = 4; s < 32; s <<= 1) {
+              most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+            }
             if (most > M[nb][h] + SUM_TOP) {
               sum[nb][h] *= fast_exp2(M[nb][h] - most);
               M[nb][h] = most;
             }
-            if (most + v_exp > Rf[nb][h] + P_TOP) {
-              const float to = most + v_exp - P_NEW, factor = fast_exp2(Rf[nb][h] - to);
+            if (top > Rf[nb][h] + P_TOP) {
+              const float to = top - P_NEW, factor = fast_exp2(Rf[nb][h] - to);
               Rf[nb][h] = to;
 #pragma unroll
               for (int m = 0; m < MB; ++m) {
@@ -419,45 +469,38 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
             }
           }
       }
-      uint32_t pb[NB][2];
+      uint32_t pb[2][NB][2];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float w[4];
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float p0 = fast_exp2(x[nb][h] - M[nb][h]), p1 = fast_exp2(x[nb][2 + h] - M[nb][h]);
-          sum[nb][h] += p0 + p1;
-          const float to_v = fast_exp2(fminf(v_exp + (M[nb][h] - Rf[nb][h]), 126.f));
-          w[h] = p0 * to_v;
-          w[2 + h] = p1 * to_v;
+        for (int nb = 0; nb < NB; ++nb) {
+          float w[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float p0 = fast_exp2(x[m][nb][h] - M[nb][h]), p1 = fast_exp2(x[m][nb][2 + h] - M[nb][h]);
+            sum[nb][h] += p0 + p1;
+            const float to_v = fast_exp2(fminf(v_exp[m] + (M[nb][h] - Rf[nb][h]), 126.f));
+            w[h] = p0 * to_v;
+            w[2 + h] = p1 * to_v;
+          }
+          pb[m][nb][0] = transpose_8x8(pack_f16(w[0], w[1]));
+          pb[m][nb][1] = transpose_8x8(pack_f16(w[2], w[3]));
         }
-        pb[nb][0] = transpose_8x8(pack_f16(w[0], w[1]));
-        pb[nb][1] = transpose_8x8(pack_f16(w[2], w[3]));
-      }
-      // ---- O^T[DH, rows] += V^T P^T: this lane's elements of tokens 4t .. 4t + 3 ----
-      constexpr int VW = DH / 32;                  // words of a token that a lane takes
-      uint32_t vw[4][VW];
+      // ---- O^T[DH, rows] += V^T P^T ----
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if constexpr (DH == 128) {
-          const uint4 v = lds16(sV + ring8_off<DH>(4 * t + k, g));
-          vw[k][0] = v.x, vw[k][1] = v.y, vw[k][2] = v.z, vw[k][3] = v.w;
-        } else {
-          const uint2 v = lds8(sV + ring8_off<DH>(4 * t + k, g >> 1) + (g & 1) * 8);
-          vw[k][0] = v.x, vw[k][1] = v.y;
-        }
-      }
+      for (int m = 0; m < MB; ++m) {
+        uint32_t v[4];
+        ldsm_b8_t(sV + v_off<DH>(lane, m), v);
 #pragma unroll
-      for (int w = 0; w < VW; ++w) {
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(v[2 * k])), e4m3x2_to_f16x2(uint16_t(v[2 * k + 1])), e4m3x2_to_f16x2(uint16_t(v[2 * k] >> 16)),
+                                 e4m3x2_to_f16x2(uint16_t(v[2 * k + 1] >> 16))};
 #pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {           // elements 4w + 2hi and the one behind it
-          const uint32_t a01 = __byte_perm(vw[0][w], vw[1][w], hi ? 0x7362 : 0x5140), a23 = __byte_perm(vw[2][w], vw[3][w], hi ? 0x7362 : 0x5140);
-          const uint32_t a[4] = {e4m3x2_to_f16x2(uint16_t(a01)), e4m3x2_to_f16x2(uint16_t(a01 >> 16)), e4m3x2_to_f16x2(uint16_t(a23)),
-                                 e4m3x2_to_f16x2(uint16_t(a23 >> 16))};
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma_f16(oacc[2 * w + hi][nb], a, pb[nb][0], pb[nb][1]);
+          for (int nb = 0; nb < NB; ++nb) mma_f16(oacc[m][nb], a, pb[k][nb][0], pb[k][nb][1]);
         }
       }
+#pragma unroll
+      for (int s = 0; s + 1 < STAGES; ++s) scales[s] = scales[s + 1];
       __syncwarp();  // every lane is done with this stage before it is refilled
     }
     const Cursor here = c;
@@ -526,31 +569,31 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
     if (warp != 0) {
       // (warp 0 alone goes on to store)
     } else if (!caller_splits && from_start && to_end) {
-      // ---- the whole unit: normalise and store DH / 8 consecutive elements a lane ----
+      // ---- the whole unit: normalise and store; a lane has elements 16 m + g and 16 m + g + 8, of which lanes g and g ^ 1 make pairs ----
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+          if (8 * nb + h >= R) break;
           const int row = nb * 8 + 2 * t + h;
-          if (row < R) {
-            const size_t head = size_t(here.b) * p.Hq + here.hk * G + row % G, at = head * DH + g * (DH / 8);
-            const bool none = sum[nb][h] == 0.f;
-            const float inv = none ? 0.f : 1.f / sum[nb][h];
-            uint32_t v[MB];
+          const size_t head = size_t(here.b) * p.Hq + here.hk * G + row % G;
+          const bool none = sum[nb][h] == 0.f, odd = (g & 1) != 0;
+          const float inv = none ? 0.f : 1.f / sum[nb][h];
+          void* const o = row < R ? grp.o[row / G] : nullptr;
 #pragma unroll
-            for (int m = 0; m < MB; ++m) v[m] = pack_bf16(oacc[m][nb][h] * inv, oacc[m][nb][2 + h] * inv);   // rounded to bf16 either way
-#pragma unroll
-            for (int m = 0; m < MB; m += 4) {
-              if (p.io_f32) {
-                float4* const o = reinterpret_cast<float4*>(reinterpret_cast<float*>(grp.o[row / G]) + at + 2 * m);
-                o[0] = make_float4(__uint_as_float(v[m] << 16), __uint_as_float(v[m] & 0xffff0000u), __uint_as_float(v[m + 1] << 16), __uint_as_float(v[m + 1] & 0xffff0000u));
-                o[1] = make_float4(__uint_as_float(v[m + 2] << 16), __uint_as_float(v[m + 2] & 0xffff0000u), __uint_as_float(v[m + 3] << 16), __uint_as_float(v[m + 3] & 0xffff0000u));
-              } else {
-                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(grp.o[row / G]) + at + 2 * m) = make_uint4(v[m], v[m + 1], v[m + 2], v[m + 3]);
-              }
+          for (int m = 0; m < MB; ++m) {
+            const float lo = oacc[m][nb][h] * inv, hi = oacc[m][nb][2 + h] * inv;
+            const float other = __shfl_xor_sync(0xffffffffu, odd ? lo : hi, 4);
+            const uint32_t v = odd ? pack_bf16(other, hi) : pack_bf16(lo, other);   // rounded to bf16 either way: one set of results
+            const size_t at = head * DH + m * 16 + (odd ? g + 7 : g);
+            if (row < R) {
+              if (p.io_f32)
+                *reinterpret_cast<float2*>(reinterpret_cast<float*>(o) + at) = make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+              else
+                *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(o) + at) = v;
             }
-            if (g == 0) grp.lse[row / G][head] = none ? -INFINITY : log_sum(M[nb][h], sum[nb][h]);
           }
+          if (row < R && g == 0) grp.lse[row / G][head] = none ? -INFINITY : log_sum(M[nb][h], sum[nb][h]);
         }
     } else {
       // ---- a piece: the first of a share, or the last one if that starts a unit ----
@@ -564,8 +607,10 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
           const int row = nb * 8 + 2 * t + h;
           if (row < R) {
 #pragma unroll
-            for (int m = 0; m < MB; m += 2)
-              *reinterpret_cast<float4*>(po + row * DH + g * (DH / 8) + 2 * m) = make_float4(oacc[m][nb][h], oacc[m][nb][2 + h], oacc[m + 1][nb][h], oacc[m + 1][nb][2 + h]);
+            for (int m = 0; m < MB; ++m) {
+              po[row * DH + m * 16 + g] = oacc[m][nb][h];
+              po[row * DH + m * 16 + g + 8] = oacc[m][nb][2 + h];
+            }
             if (g == 0) *reinterpret_cast<float2*>(pml + row * 2) = make_float2(M[nb][h], sum[nb][h]);
           }
         }
@@ -575,7 +620,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<NB>) decode8_kernel(const 
   cp_async_wait<0>();
 }
 
-DealBy deal8_by(int rows) { return {D8_KEY, sm_count() * (rows <= 8 ? D8_CTAS<1> : D8_CTAS<2>)}; }
+DealBy deal8_by(int dh) { return {dh, sm_count() * (dh == 128 ? D8_CTAS<128> : D8_CTAS<64>)}; }
 // query rows of the largest group of a call
 int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
   int rows = 0;
@@ -585,7 +630,7 @@ int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
 
 template <int DH, int NB, int NG>
 cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
-  constexpr int smem = D8_WARPS * D8_STAGES<DH, NB> * 2 * GRAN * DH;
+  constexpr int smem = D8_WARPS * D8_STAGES<DH> * 2 * STEP * DH;
   cudaError_t e = allow_smem<decode8_kernel<DH, NB, NG>>(smem);
   if (e != cudaSuccess) return e;
   Dec8Params<NG> p;
@@ -595,7 +640,7 @@ cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim
   e = launch_kernel(decode8_kernel<DH, NB, NG>, grid, D8_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
-    e = launch_kernel(decode_combine_kernel<DH, D8_KEY, true, Dec8Params<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+    e = launch_kernel(decode_combine_kernel<DH, DH, true, Dec8Params<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 template <int DH, int NB>
@@ -619,8 +664,7 @@ extern "C" size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const in
   if (check_desc8(d) != KVP_OK || donor == nullptr) return 0;
   for (int l = 0; l < d->L; ++l)
     if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return 0;
-  // of any layer range: one that leaves out members of the largest groups may have fewer rows, and more blocks that fit
-  return std::max(decode_scratch_bytes(d, donor, 0, d->L, deal8_by(8)), decode_scratch_bytes(d, donor, 0, d->L, deal8_by(16)));
+  return decode_scratch_bytes(d, donor, 0, d->L, deal8_by(d->dh));
 }
 
 extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
@@ -648,7 +692,7 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
       if (!aligned16(q[l]) || !aligned16(o[l]) || (reinterpret_cast<uintptr_t>(lse[l]) & 3u) != 0) return KVP_ERR_UNSUPPORTED;
     }
   }
-  const DealBy by = deal8_by(most_rows(d, subs, n_sub));
+  const DealBy by = deal8_by(d->dh);
   const Scratch plan = plan_scratch(d, subs, n_sub, 0, by);
   if (ws == nullptr || ws_bytes < plan.bytes || !aligned16(ws)) return KVP_ERR_WORKSPACE;
 
@@ -702,9 +746,8 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     const int rows_per_block = COMBINE_THREADS / 32 / wpr;
     const dim3 grid(static_cast<unsigned>(blocks)), cgrid(unsigned(units), (rows + rows_per_block - 1) / rows_per_block);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-    // (the whole call's largest group decides: p.fit goes by it)
-    const cudaError_t e = d->dh == 128 ? (plan.rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
-                                       : (plan.rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
+    const cudaError_t e = d->dh == 128 ? (rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
+                                       : (rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
     if (e != cudaSuccess) return KVP_ERR_CUDA;
   }
   return KVP_OK;
