@@ -23,14 +23,17 @@ namespace {
 
 constexpr int D8_WARPS = 4, D8_THREADS = D8_WARPS * 32;
 constexpr int STEP = 2 * GRAN;                    // tokens of a step of a warp: two granules, each with scales of its own
-#ifndef V_STAGES
-#define V_STAGES 2
+#ifndef V_CTAS
 #define V_CTAS 3
+#define V_SLOTS 4
+#define V_CTAS64 4
+#define V_SLOTS64 6
 #endif
-template <int DH>
-constexpr int D8_STAGES = DH == 128 ? V_STAGES : 3;   // steps of a warp in the ring
-template <int DH>
-constexpr int D8_CTAS = DH == 128 ? V_CTAS : 4;   // per SM, as many as shared memory holds
+// CTAs per SM, and tiles (32 tokens of K or of V) of a warp in the ring.
+template <int DH, int NB>
+constexpr int D8_CTAS = DH == 128 ? (NB == 1 ? V_CTAS : 2) : NB == 1 ? V_CTAS64 : 3;
+template <int DH, int NB>
+constexpr int D8_SLOTS = DH == 128 ? (NB == 1 ? V_SLOTS : 6) : V_SLOTS64;
 constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
@@ -93,8 +96,8 @@ __device__ __forceinline__ uint32_t v_off(int row, int chunk) {
 }
 
 template <int DH, int NB, int NG>
-__global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
-  constexpr int GRAN_BYTES = GRAN * DH, TILE_BYTES = 2 * GRAN_BYTES, STAGE_BYTES = 2 * TILE_BYTES, STAGES = D8_STAGES<DH>;
+__global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
+  constexpr int GRAN_BYTES = GRAN * DH, TILE_BYTES = 2 * GRAN_BYTES, SLOTS = D8_SLOTS<DH, NB>, DEPTH = SLOTS / 2;
   constexpr int CHUNKS = DH / 16;                  // 16-byte chunks of a row
   constexpr int CP_PER_LANE = GRAN_BYTES / 16 / 32;
   constexpr int HALVES = DH / 64;                  // 16-byte words of a K row that a lane takes
@@ -221,8 +224,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
     if (c.grp >= p.n_groups) return;
   }
 
-  // ---- copies: a cursor of their own, STAGES - 1 of this warp's steps ahead of the arithmetic ----
-  const uint32_t ring = smem_u32(dsmem) + warp * STAGES * STAGE_BYTES;
+  // ---- copies: a cursor of their own; K_i, V_i, K_i+1, ... of this warp's steps go round a ring of tiles, all but one of them ahead of
+  // the arithmetic: V_i+DEPTH-1 is asked for when K_i is there, K_i+DEPTH as soon as K_i has been read ----
+  const uint32_t ring = smem_u32(dsmem) + warp * SLOTS * TILE_BYTES;
   Cursor f = c;
   int f_todo = todo;
   int f_left;                                      // steps of the piece from this warp's next one on (<= 0: none)
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
   const int32_t* bt = nullptr;                     // block-table entry of the page the next step begins in,
   int in_page = 0, f_live = 0;                     // its granule there; tokens of the piece from there on
   size_t page_block = 0;                           // blocks of 16 tokens before this KV head's of that page
-  int stage_in = 0;
+  int slot_in = 0, slot_out = 0;                   // in pairs: K's tile and V's behind it
   auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
   auto enter_piece = [&]() {
     const int n = min(f_todo, f.ng - f.gran);
@@ -247,46 +251,50 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
   struct Scales {
     uint32_t k[2], v[2];                           // bytes of a step's granules
   };
-  Scales scales[STAGES];
+  Scales scales[DEPTH + 1];
 #pragma unroll
-  for (int s = 0; s < STAGES; ++s) scales[s] = {{0, 0}, {0, 0}};
-  auto issue_next = [&](Scales& sc) {
+  for (int s = 0; s <= DEPTH; ++s) scales[s] = {{0, 0}, {0, 0}};
+  // V's granules of the step whose K was asked for last, and how many tokens of it are to be read (-1: no step)
+  const uint8_t *v_src0 = nullptr, *v_src1 = nullptr;
+  int v_live = -1;
+  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool is_v) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* const src = h ? src1 : src0;
+      if (live >= (h + 1) * GRAN) {
+#pragma unroll
+        for (int i = 0; i < CP_PER_LANE; ++i) {
+          const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
+          cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), src + i * 512);
+        }
+      } else {                                     // slots never appended may hold anything: zeros instead
+#pragma unroll
+        for (int i = 0; i < CP_PER_LANE; ++i) {
+          const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
+          cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), src + i * 512, row < live ? 16u : 0u);
+        }
+      }
+    }
+  };
+  auto issue_k = [&](Scales& sc) {
     while (f_left <= 0 && f.grp < p.n_groups) {
       next_piece(f, f_todo);
       if (f.grp < p.n_groups) enter_piece();
     }
+    v_live = -1;
     if (f_left > 0) {
       const size_t block0 = page_block + in_page;
       size_t block1 = block0;
       if (f_live > GRAN) block1 = in_page + 1 < gran_per_page ? block0 + 1 : block_of(bt[1]);
-      const uint32_t dst = ring + stage_in * STAGE_BYTES;
       sc.k[0] = f_grp->k_scale[block0];
       sc.v[0] = f_grp->v_scale[block0];
       sc.k[1] = f_grp->k_scale[block1];
       sc.v[1] = f_grp->v_scale[block1];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const size_t at = (h ? block1 : block0) * GRAN_BYTES + lane * 16;
-        const uint8_t* const ksrc = f_grp->k_cache + at;
-        const uint8_t* const vsrc = f_grp->v_cache + at;
-        if (f_live >= (h + 1) * GRAN) {
-#pragma unroll
-          for (int i = 0; i < CP_PER_LANE; ++i) {
-            const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
-            cp_async16(dst + k_off<DH>(row, chunk), ksrc + i * 512);
-            cp_async16(dst + TILE_BYTES + v_off<DH>(row, chunk), vsrc + i * 512);
-          }
-        } else {                                   // slots never appended may hold anything: zeros instead
-#pragma unroll
-          for (int i = 0; i < CP_PER_LANE; ++i) {
-            const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
-            const uint32_t nbytes = row < f_live ? 16u : 0u;
-            cp_async16(dst + k_off<DH>(row, chunk), ksrc + i * 512, nbytes);
-            cp_async16(dst + TILE_BYTES + v_off<DH>(row, chunk), vsrc + i * 512, nbytes);
-          }
-        }
-      }
-      if (++stage_in == STAGES) stage_in = 0;
+      const size_t at0 = block0 * GRAN_BYTES + lane * 16, at1 = block1 * GRAN_BYTES + lane * 16;
+      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, false);
+      v_src0 = f_grp->v_cache + at0;
+      v_src1 = f_grp->v_cache + at1;
+      v_live = max(f_live, 0);
       f_left -= D8_WARPS;
       f_live -= D8_WARPS * STEP;
       in_page += D8_WARPS * 2;
@@ -297,6 +305,13 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
         } while (in_page >= gran_per_page);
         page_block = block_of(*bt);
       }
+    }
+    cp_async_commit();
+  };
+  auto issue_v = [&]() {
+    if (v_live >= 0) {
+      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, true);
+      if (++slot_in == DEPTH) slot_in = 0;
     }
     cp_async_commit();
   };
@@ -353,11 +368,13 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
   };
 
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) issue_next(scales[s]);
+  for (int s = 0; s < DEPTH; ++s) {
+    issue_k(scales[s]);
+    if (s + 1 < DEPTH) issue_v();
+  }
   load_queries();
 
   const int tok_g = (g >> 1) * 4 + (g & 1);        // token of a granule that row g of its S^T is; row g + 8: two more
-  int stage_out = 0;
   do {
     // ---- one unit, or this block's piece of it ----
     const Dec8Group& grp = p.grp[c.grp];
@@ -381,11 +398,11 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
 
     const int tokens = min(c.seen, (c.gran + n_here) * GRAN) - c.gran * GRAN;   // that the piece sees (0: none)
     for (int i = warp; 2 * i < n_here; i += D8_WARPS) {
-      cp_async_wait<STAGES - 2>();
+      cp_async_wait<SLOTS - 2>();
       __syncwarp();
-      issue_next(scales[STAGES - 1]);              // into the stage freed by the previous step
-      const uint32_t sK = ring + stage_out * STAGE_BYTES, sV = sK + TILE_BYTES;
-      if (++stage_out == STAGES) stage_out = 0;
+      issue_v();                                   // into the place of the previous step's
+      const uint32_t sK = ring + slot_out * 2 * TILE_BYTES, sV = sK + TILE_BYTES;
+      if (++slot_out == DEPTH) slot_out = 0;
 
       // ---- S^T[32 tokens, rows] = K Q^T, even and odd k-steps apart ----
       float s2[2][NB][2][4];
@@ -408,6 +425,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
           }
         }
       }
+      __syncwarp();                                // every lane has read K
+      issue_k(scales[DEPTH]);
       // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
       const int left = tokens - i * STEP;          // visible tokens from this step on
       float x[2][NB][4], v_exp[2];
@@ -487,6 +506,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
           pb[m][nb][1] = transpose_8x8(pack_f16(w[2], w[3]));
         }
       // ---- O^T[DH, rows] += V^T P^T ----
+      cp_async_wait<SLOTS - 1>();
+      __syncwarp();
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         uint32_t v[4];
@@ -500,8 +521,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
         }
       }
 #pragma unroll
-      for (int s = 0; s + 1 < STAGES; ++s) scales[s] = scales[s + 1];
-      __syncwarp();  // every lane is done with this stage before it is refilled
+      for (int s = 0; s < DEPTH; ++s) scales[s] = scales[s + 1];
+      // (every lane is done with V before it is refilled: the barrier at the top)
     }
     const Cursor here = c;
     next_piece(c, todo);
@@ -620,7 +641,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH>) decode8_kernel(const 
   cp_async_wait<0>();
 }
 
-DealBy deal8_by(int dh) { return {dh, sm_count() * (dh == 128 ? D8_CTAS<128> : D8_CTAS<64>)}; }
+DealBy deal8_by(int dh, int rows) {
+  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>)};
+}
 // query rows of the largest group of a call
 int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
   int rows = 0;
@@ -630,7 +653,7 @@ int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
 
 template <int DH, int NB, int NG>
 cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
-  constexpr int smem = D8_WARPS * D8_STAGES<DH> * 2 * STEP * DH;
+  constexpr int smem = D8_WARPS * D8_SLOTS<DH, NB> * STEP * DH;
   cudaError_t e = allow_smem<decode8_kernel<DH, NB, NG>>(smem);
   if (e != cudaSuccess) return e;
   Dec8Params<NG> p;
@@ -664,7 +687,8 @@ extern "C" size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const in
   if (check_desc8(d) != KVP_OK || donor == nullptr) return 0;
   for (int l = 0; l < d->L; ++l)
     if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return 0;
-  return decode_scratch_bytes(d, donor, 0, d->L, deal8_by(d->dh));
+  // of any layer range: one that leaves out members of the largest groups may have fewer rows, and more blocks that fit
+  return std::max(decode_scratch_bytes(d, donor, 0, d->L, deal8_by(d->dh, 8)), decode_scratch_bytes(d, donor, 0, d->L, deal8_by(d->dh, 16)));
 }
 
 extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
@@ -692,7 +716,7 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
       if (!aligned16(q[l]) || !aligned16(o[l]) || (reinterpret_cast<uintptr_t>(lse[l]) & 3u) != 0) return KVP_ERR_UNSUPPORTED;
     }
   }
-  const DealBy by = deal8_by(d->dh);
+  const DealBy by = deal8_by(d->dh, most_rows(d, subs, n_sub));
   const Scratch plan = plan_scratch(d, subs, n_sub, 0, by);
   if (ws == nullptr || ws_bytes < plan.bytes || !aligned16(ws)) return KVP_ERR_WORKSPACE;
 
@@ -746,8 +770,8 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     const int rows_per_block = COMBINE_THREADS / 32 / wpr;
     const dim3 grid(static_cast<unsigned>(blocks)), cgrid(unsigned(units), (rows + rows_per_block - 1) / rows_per_block);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-    const cudaError_t e = d->dh == 128 ? (rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
-                                       : (rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
+    const cudaError_t e = d->dh == 128 ? (plan.rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
+                                       : (plan.rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
     if (e != cudaSuccess) return KVP_ERR_CUDA;
   }
   return KVP_OK;
