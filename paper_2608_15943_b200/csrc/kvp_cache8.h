@@ -22,10 +22,11 @@ KVP_HD inline int scale_exponent(uint32_t amax_bits) {
   return e < LEAST_SCALE ? LEAST_SCALE : e;
 }
 // A byte that no append wrote is taken as the nearest that one could have written.
-KVP_HD inline int exponent_of_byte(uint32_t byte) {
-  const int e = int(byte) - 127;
-  return e < LEAST_SCALE ? LEAST_SCALE : e > MOST_SCALE ? MOST_SCALE : e;
+KVP_HD inline uint32_t scale_byte(uint32_t byte) {
+  const uint32_t least = uint32_t(LEAST_SCALE + 127), most = uint32_t(MOST_SCALE + 127), b = byte < least ? least : byte;
+  return b > most ? most : b;
 }
+KVP_HD inline int exponent_of_byte(uint32_t byte) { return int(scale_byte(byte)) - 127; }
 // Bits of 2^e as a float; e below the smallest normal number's is taken as that (used for factors below 2^-20, where a number
 // of the cache becomes 0 either way).
 KVP_HD inline uint32_t power_bits(int e) { return uint32_t((e < -126 ? -126 : e) + 127) << 23; }

@@ -23,18 +23,17 @@ namespace {
 
 constexpr int D8_WARPS = 4, D8_THREADS = D8_WARPS * 32;
 constexpr int STEP = 2 * GRAN;                    // tokens of a step of a warp: two granules, each with scales of its own
-#ifndef V_CTAS
-#define V_CTAS 3
-#define V_SLOTS 4
-#define V_CTAS64 4
-#define V_SLOTS64 6
-#endif
-// CTAs per SM, and tiles (32 tokens of K or of V) of a warp in the ring.
+// CTAs per SM, and tiles (32 tokens of K or of V) of a warp in the ring.  (dh 128, two CTAs and six tiles: 32 sequences of 16K-32K in
+// six groups 1424 us instead of 1403; dh 64, six tiles: 256 of 100-300 tokens 45.5 instead of 43.9.)
 template <int DH, int NB>
-constexpr int D8_CTAS = DH == 128 ? (NB == 1 ? V_CTAS : 2) : NB == 1 ? V_CTAS64 : 3;
+constexpr int D8_CTAS = DH == 128 ? (NB == 1 ? 3 : 2) : NB == 1 ? 4 : 3;
 template <int DH, int NB>
-constexpr int D8_SLOTS = DH == 128 ? (NB == 1 ? V_SLOTS : 6) : V_SLOTS64;
+constexpr int D8_SLOTS = DH == 128 && NB == 2 ? 6 : 4;
 constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
+// Where whole units are dealt out and there are so many units for a block that fits, a warp takes a unit alone: nothing is merged.
+// (us, four warps a unit -> so: 128 sequences of 50 to 400 tokens, 8 KV heads, six groups 116 -> 71, 64 of 1 to 64 at dh 64 27.6 ->
+// 12.8; but 32 of 200 to 400 in two groups, 1.2 units a block, 17.3 -> 18.5, 58 of 1 to 700 in four, 1.6, 21 -> 25.)
+constexpr int LONE_UNITS = 2;
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
 struct Dec8Group {
@@ -133,12 +132,13 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     set_length(x, p.lengths[x.b]);
   };
   bool by_units = p.by_units != 0;
+  const int units = p.n_groups * p.B * p.Hkv;
   int rest = 0;                                    // places behind the granules of a unit
   auto find_place = [&](int len0) -> bool {        // from the lengths; false: the block has none
     int before, all, longest;
     sum_granules(p, len0, 0, before, all, longest);
     const long long granules = (long long)all * p.Hkv * p.n_groups;
-    by_units = dealt_by_units(DH, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit);
+    by_units = dealt_by_units(DH, granules, units, longest, p.fit);
     rest = by_units ? 0 : unit_rest(DH, granules, p.fit);
     if (by_units) return true;
     const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
@@ -189,6 +189,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     }
   }
   if (!placed) return;
+  const bool lone = by_units && !caller_splits && units >= LONE_UNITS * p.fit;
+  int first_step = warp, team = D8_WARPS;          // of a piece: this warp's first step, and how many warps take its steps in turn
   if (caller_splits) {
     const int split = blockIdx.x % p.num_splits;
     go_to_unit(c, blockIdx.x / p.num_splits);
@@ -196,10 +198,16 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     c.gran = min(c.ng, split * per);
     todo = min(c.ng - c.gran, per);
   } else if (by_units) {
-    if (blockIdx.x >= p.n_groups * p.B * p.Hkv) return;
-    go_to_unit(c, blockIdx.x);
+    if (lone) {
+      first_step = 0;
+      team = 1;
+    }
+    const int id = lone ? int(blockIdx.x) * D8_WARPS + warp : int(blockIdx.x);
+    if (id >= units) return;
+    go_to_unit(c, id);
     todo = c.ng;
   }
+  const int unit_step = int(gridDim.x) * (lone ? D8_WARPS : 1);
   auto next_piece = [&](Cursor& x, int& left) {    // past the end: grp >= n_groups
     left -= min(left, x.ng + rest - x.gran);
     if (left > 0) {
@@ -212,8 +220,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
         }
         set_length(x, p.lengths[x.b]);
       }
-    } else if (by_units && !caller_splits && x.id + int(gridDim.x) < p.n_groups * p.B * p.Hkv) {
-      go_to_unit(x, x.id + gridDim.x);
+    } else if (by_units && !caller_splits && x.id + unit_step < units) {
+      go_to_unit(x, x.id + unit_step);
       left = x.ng;
     } else {
       x.grp = p.n_groups;
@@ -239,44 +247,40 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
   auto enter_piece = [&]() {
     const int n = min(f_todo, f.ng - f.gran);
-    f_left = (n + 1) / 2 - warp;
+    f_left = (n + 1) / 2 - first_step;
     if (f_left <= 0) return;
-    const int gran = f.gran + 2 * warp, col = gran / gran_per_page;
+    const int gran = f.gran + 2 * first_step, col = gran / gran_per_page;
     f_grp = &p.grp[f.grp];
     bt = p.block_table + size_t(f.b) * p.max_pages + col;
     in_page = gran - col * gran_per_page;
     f_live = min(f.seen, (f.gran + n) * GRAN) - gran * GRAN;
     page_block = block_of(*bt);
   };
-  struct Scales {
-    uint32_t k[2], v[2];                           // bytes of a step's granules
-  };
-  Scales scales[DEPTH + 1];
+  // Scales of the steps in the ring: a lane has the byte of one granule (lane & 3: K's and V's of the first, of the second).
+  uint32_t scales[DEPTH + 1];
 #pragma unroll
-  for (int s = 0; s <= DEPTH; ++s) scales[s] = {{0, 0}, {0, 0}};
+  for (int s = 0; s <= DEPTH; ++s) scales[s] = 0;
   // V's granules of the step whose K was asked for last, and how many tokens of it are to be read (-1: no step)
   const uint8_t *v_src0 = nullptr, *v_src1 = nullptr;
   int v_live = -1;
-  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool is_v) {
+  // the tile of a step: 32 rows in a run from src0, or (split) 16 from either
+  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool split, bool is_v) {
+    if (!split) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint8_t* const src = h ? src1 : src0;
-      if (live >= (h + 1) * GRAN) {
+      for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
+        const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
+        cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), src0 + i * 512);
+      }
+    } else {                                       // slots never appended may hold anything: zeros instead
 #pragma unroll
-        for (int i = 0; i < CP_PER_LANE; ++i) {
-          const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
-          cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), src + i * 512);
-        }
-      } else {                                     // slots never appended may hold anything: zeros instead
-#pragma unroll
-        for (int i = 0; i < CP_PER_LANE; ++i) {
-          const int idx = i * 32 + lane, row = h * GRAN + idx / CHUNKS, chunk = idx % CHUNKS;
-          cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), src + i * 512, row < live ? 16u : 0u);
-        }
+      for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
+        const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
+        cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), (i < CP_PER_LANE ? src0 : src1) + i % CP_PER_LANE * 512, row < live ? 16u : 0u);
       }
     }
   };
-  auto issue_k = [&](Scales& sc) {
+  bool v_split = false;
+  auto issue_k = [&](uint32_t& scale) {
     while (f_left <= 0 && f.grp < p.n_groups) {
       next_piece(f, f_todo);
       if (f.grp < p.n_groups) enter_piece();
@@ -284,20 +288,19 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     v_live = -1;
     if (f_left > 0) {
       const size_t block0 = page_block + in_page;
-      size_t block1 = block0;
-      if (f_live > GRAN) block1 = in_page + 1 < gran_per_page ? block0 + 1 : block_of(bt[1]);
-      sc.k[0] = f_grp->k_scale[block0];
-      sc.v[0] = f_grp->v_scale[block0];
-      sc.k[1] = f_grp->k_scale[block1];
-      sc.v[1] = f_grp->v_scale[block1];
+      const bool in_a_row = in_page + 1 < gran_per_page;
+      size_t block1 = block0 + 1;
+      if (!in_a_row || f_live <= GRAN) block1 = f_live > GRAN ? block_of(bt[1]) : block0;
+      scale = (lane & 1 ? f_grp->v_scale : f_grp->k_scale)[lane & 2 ? block1 : block0];
       const size_t at0 = block0 * GRAN_BYTES + lane * 16, at1 = block1 * GRAN_BYTES + lane * 16;
-      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, false);
+      v_split = !in_a_row || f_live < STEP;
+      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, v_split, false);
       v_src0 = f_grp->v_cache + at0;
       v_src1 = f_grp->v_cache + at1;
       v_live = max(f_live, 0);
-      f_left -= D8_WARPS;
-      f_live -= D8_WARPS * STEP;
-      in_page += D8_WARPS * 2;
+      f_left -= team;
+      f_live -= team * STEP;
+      in_page += team * 2;
       if (in_page >= gran_per_page && f_left > 0) {
         do {
           in_page -= gran_per_page;
@@ -310,7 +313,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   };
   auto issue_v = [&]() {
     if (v_live >= 0) {
-      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, true);
+      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, v_split, true);
       if (++slot_in == DEPTH) slot_in = 0;
     }
     cp_async_commit();
@@ -387,17 +390,17 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     for (int m = 0; m < MB; ++m)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) oacc[m][nb][0] = oacc[m][nb][1] = oacc[m][nb][2] = oacc[m][nb][3] = 0.f;
-    float sum[NB][2], M[NB][2], Rf[NB][2];         // of rows 8 nb + 2 t + h: sum of this lane's terms, against M; reference of oacc
+    float M[NB][2], Rf[NB][2];                     // of rows 8 nb + 2 t + h: reference of the sum, reference of oacc (exponents as bytes)
+    uint64_t sum2[NB], minus_M[NB], M_to_R[NB];    // sums of this lane's terms, -M and M - R, both rows of the lane side by side
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        sum[nb][h] = 0.f;
-        M[nb][h] = Rf[nb][h] = -1e30f;             // (finite: below every score, and no infinity minus infinity)
-      }
+    for (int nb = 0; nb < NB; ++nb) {
+      M[nb][0] = M[nb][1] = Rf[nb][0] = Rf[nb][1] = -1e30f;   // (finite: below every score, and no infinity minus infinity)
+      sum2[nb] = M_to_R[nb] = 0;
+      minus_M[nb] = pack_f2(1e30f, 1e30f);
+    }
 
     const int tokens = min(c.seen, (c.gran + n_here) * GRAN) - c.gran * GRAN;   // that the piece sees (0: none)
-    for (int i = warp; 2 * i < n_here; i += D8_WARPS) {
+    for (int i = first_step; 2 * i < n_here; i += team) {
       cp_async_wait<SLOTS - 2>();
       __syncwarp();
       issue_v();                                   // into the place of the previous step's
@@ -429,81 +432,102 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       issue_k(scales[DEPTH]);
       // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
       const int left = tokens - i * STEP;          // visible tokens from this step on
-      float x[2][NB][4], v_exp[2];
+      const uint32_t scale = scale_byte(scales[0]);
+      uint64_t factor[2][NB], x[2][NB][2];         // x - M
+      float v_exp[2];
+      uint64_t to_v[2][NB];                        // e + M - R
       bool over = false;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const float k_scale = __uint_as_float(power_bits(exponent_of_byte(scales[0].k[m])));
-        v_exp[m] = float(exponent_of_byte(scales[0].v[m]));
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float factor = q_factor[nb][h] * k_scale;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) x[m][nb][2 * u + h] = (s2[m][nb][0][2 * u + h] + s2[m][nb][1][2 * u + h]) * factor;
-          }
-      }
-      if (left < STEP) {
+      auto scores = [&]() {
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-            if (m * GRAN + tok_g + 2 * u >= left) {
+          for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) x[m][nb][2 * u] = x[m][nb][2 * u + 1] = -INFINITY;
-            }
-      }
+            for (int u = 0; u < 2; ++u) x[m][nb][u] = ffma2(pack_f2(s2[m][nb][0][2 * u], s2[m][nb][0][2 * u + 1]), factor[m][nb], minus_M[nb]);
+            to_v[m][nb] = fadd2(pack_f2(v_exp[m], v_exp[m]), M_to_R[nb]);
+          }
+        if (left < STEP) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+          for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float m0 = fmaxf(x[0][nb][h], x[0][nb][2 + h]), m1 = fmaxf(x[1][nb][h], x[1][nb][2 + h]);
-          over = over || fmaxf(m0, m1) > M[nb][h] + SUM_TOP || fmaxf(m0 + v_exp[0], m1 + v_exp[1]) > Rf[nb][h] + P_TOP;
+            for (int u = 0; u < 2; ++u)
+              if (m * GRAN + tok_g + 2 * u >= left) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) x[m][nb][u] = pack_f2(-INFINITY, -INFINITY);
+              }
         }
-      if (__any_sync(0xffffffffu, over)) {
+      };
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const float k_scale = __uint_as_float(__shfl_sync(0xffffffffu, scale, 2 * m) << 23);
+        v_exp[m] = __uint_as_float(0x4b000000u | __shfl_sync(0xffffffffu, scale, 2 * m + 1)) - 8388608.f;      // (2^23 + byte - 2^23)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          factor[m][nb] = fmul2(pack_f2(q_factor[nb][0], q_factor[nb][1]), pack_f2(k_scale, k_scale));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s2[m][nb][0][u] += s2[m][nb][1][u];
+        }
+      }
+      scores();
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
+          over = over || fmaxf(f2_lo(x[m][nb][0]), f2_lo(x[m][nb][1])) > fminf(SUM_TOP, P_TOP - f2_lo(to_v[m][nb])) ||
+                 fmaxf(f2_hi(x[m][nb][0]), f2_hi(x[m][nb][1])) > fminf(SUM_TOP, P_TOP - f2_hi(to_v[m][nb]));
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float m0 = fmaxf(x[0][nb][h], x[0][nb][2 + h]), m1 = fmaxf(x[1][nb][h], x[1][nb][2 + h]);
-            float most = fmaxf(m0, m1), top = fmaxf(m0 + v_exp[0], m1 + v_exp[1]);
+            float y[2];                            // largest score of each granule
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              y[m] = -INFINITY;
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+                if (m * GRAN + tok_g + 2 * u < left) y[m] = fmaxf(y[m], s2[m][nb][0][2 * u + h] * (h ? f2_hi(factor[m][nb]) : f2_lo(factor[m][nb])));
+            }
+            float most = fmaxf(y[0], y[1]), top = fmaxf(y[0] + v_exp[0], y[1] + v_exp[1]);
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
               most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
             }
             if (most > M[nb][h] + SUM_TOP) {
-              sum[nb][h] *= fast_exp2(M[nb][h] - most);
+              const float factor_s = fast_exp2(M[nb][h] - most);
+              sum2[nb] = h ? pack_f2(f2_lo(sum2[nb]), f2_hi(sum2[nb]) * factor_s) : pack_f2(f2_lo(sum2[nb]) * factor_s, f2_hi(sum2[nb]));
               M[nb][h] = most;
             }
             if (top > Rf[nb][h] + P_TOP) {
-              const float to = top - P_NEW, factor = fast_exp2(Rf[nb][h] - to);
+              const float to = top - P_NEW, factor_o = fast_exp2(Rf[nb][h] - to);
               Rf[nb][h] = to;
 #pragma unroll
               for (int m = 0; m < MB; ++m) {
-                oacc[m][nb][h] *= factor;
-                oacc[m][nb][2 + h] *= factor;
+                oacc[m][nb][h] *= factor_o;
+                oacc[m][nb][2 + h] *= factor_o;
               }
             }
           }
+          minus_M[nb] = pack_f2(-M[nb][0], -M[nb][1]);
+          M_to_R[nb] = pack_f2(M[nb][0] - Rf[nb][0], M[nb][1] - Rf[nb][1]);
+        }
+        scores();
       }
       uint32_t pb[2][NB][2];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          float w[4];
+          const uint64_t f = pack_f2(fast_exp2(fminf(f2_lo(to_v[m][nb]), 126.f)), fast_exp2(fminf(f2_hi(to_v[m][nb]), 126.f)));
+          uint64_t pr[2];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float p0 = fast_exp2(x[m][nb][h] - M[nb][h]), p1 = fast_exp2(x[m][nb][2 + h] - M[nb][h]);
-            sum[nb][h] += p0 + p1;
-            const float to_v = fast_exp2(fminf(v_exp[m] + (M[nb][h] - Rf[nb][h]), 126.f));
-            w[h] = p0 * to_v;
-            w[2 + h] = p1 * to_v;
+          for (int u = 0; u < 2; ++u) {
+            pr[u] = pack_f2(fast_exp2(f2_lo(x[m][nb][u])), fast_exp2(f2_hi(x[m][nb][u])));
+            const uint64_t w = fmul2(pr[u], f);
+            pb[m][nb][u] = transpose_8x8(pack_f16(f2_lo(w), f2_hi(w)));
           }
-          pb[m][nb][0] = transpose_8x8(pack_f16(w[0], w[1]));
-          pb[m][nb][1] = transpose_8x8(pack_f16(w[2], w[3]));
+          sum2[nb] = fadd2(sum2[nb], fadd2(pr[0], pr[1]));
         }
       // ---- O^T[DH, rows] += V^T P^T ----
       cp_async_wait<SLOTS - 1>();
@@ -531,13 +555,15 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     else load_queries();
 
     // ---- everything against M; no term at all: M = -infinity ----
+    float sum[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        sum[nb][h] = h ? f2_hi(sum2[nb]) : f2_lo(sum2[nb]);
 #pragma unroll
         for (int s = 4; s < 32; s <<= 1) sum[nb][h] += __shfl_xor_sync(0xffffffffu, sum[nb][h], s);
-        const float to_m = fast_exp2(fminf(Rf[nb][h] - M[nb][h], 126.f));
+        const float to_m = fast_exp2(fminf(Rf[nb][h] - 127.f - M[nb][h], 126.f));
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           oacc[m][nb][h] *= to_m;
@@ -550,7 +576,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (8 * nb + h >= R) break;
+        if (8 * nb + h >= R || lone) break;
         __syncthreads();   // warp 0 is done with the previous ones
         if (warp > 0) {
 #pragma unroll
@@ -587,8 +613,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           }
         }
       }
-    if (warp != 0) {
-      // (warp 0 alone goes on to store)
+    if (first_step != 0) {
+      // (the piece's first warp alone goes on to store)
     } else if (!caller_splits && from_start && to_end) {
       // ---- the whole unit: normalise and store; a lane has elements 16 m + g and 16 m + g + 8, of which lanes g and g ^ 1 make pairs ----
 #pragma unroll
