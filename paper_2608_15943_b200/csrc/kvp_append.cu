@@ -1,10 +1,12 @@
 // Appending any number of tokens to the paged cache: K rotated by the token's position on the way in, the queries of the same
 // tokens rotated beside it, and K and V stored as bf16 or in 8 bits (kvp_cache8.h).  One launch for up to 64 layers.
 //
-// Bound: HBM for prompts (every element is read and written once: 16-byte loads, a warp's all in flight before the first is
-// used), latency for token steps (lengths -> block table -> store).  Positions are per sequence, so the angle is formed on the
-// device: pos times the frequency as a 64-bit fraction of a turn, whose wrap-around is the range reduction; sine and cosine are
-// taken of its upper 32 bits as a float, and what that float leaves off is applied as a first-order correction.
+// Bound: HBM for prompts (every element is read and written once, 16 bytes a load), latency for token steps.  Positions are per
+// sequence, so the angle is formed on the device: pos times the frequency as a 64-bit fraction of a turn, whose wrap-around is the
+// range reduction; sine and cosine are taken of its upper 32 bits as a float, and what that float leaves off is applied as a
+// first-order correction.
+// Measured (us; in brackets the bytes at the copy rate): prompts of 12000 tokens, four layers, queries with them, bf16 170 (165);
+// 30400 tokens behind begun blocks into 8 bits 433 (390); 32 tokens of eight layers, device time in a graph, 4.5 bf16, 4.8 in 8 bits.
 #include <math.h>
 
 #include <algorithm>
@@ -16,11 +18,20 @@
 namespace kvp {
 namespace {
 
-constexpr int APP_THREADS = 256, APP_WARPS = APP_THREADS / 32;
+constexpr int APP_THREADS = 256;
+// Blocks per SM, by registers.  (Token kernel with five, whose last blocks wait for the others: 32 tokens of eight layers 5.4 us instead
+// of 4.5.  Runs of 30400 tokens in four layers: dh 64 with four 149 us instead of 136; dh 128 with five, which spills, 462 instead of 433.)
+constexpr int ONES_AN_SM = 6, RUNS_A_WAVE = 4;
+template <int DH, bool ONE_WAVE>
+constexpr int RUNS_AN_SM = DH == 64 && !ONE_WAVE ? 5 : RUNS_A_WAVE;
+// Heads that a block of runs has in flight.  (K's and V's in 8 bits: with four, registers spill.)
+template <bool BITS8>
+constexpr int KV_HEADS = BITS8 ? 2 : 4;
+constexpr int Q_HEADS = 4;
 constexpr int MANY_LAYERS = 64, FEW_LAYERS = 8;    // a launch of few layers has a parameter block of 1 KB, not 5
 
 struct AppLayer {
-  const void* q;                 // [T,Hq,dh] bf16 or (io_f32) fp32; null: no queries
+  const void* q;                 // [T,Hq,dh] bf16 or (F32) fp32; null: no queries
   void* q_out;
   const void *k_new, *v_new;     // [T,Hkv,dh]; null: a consumer
   void *k_cache, *v_cache;       // [n_pages][Hkv][page_size][dh], bf16 or e4m3
@@ -31,7 +42,8 @@ struct AppSizes {
   const int32_t* lengths;        // [B]
   const int32_t* first;          // [B + 1], or null: one token a sequence
   int B, T, Hq, Hkv, page_size, max_pages, n_pages;
-  int io_f32, rotate;
+  int rotate;
+  int kv_slices, q_slices;       // of runs: blocks that share K's and V's heads of a block of positions, and its query heads (0: the same blocks do both)
   uint64_t turns[64];            // rope_turns
 };
 template <int NL>
@@ -40,8 +52,9 @@ struct AppParams : AppSizes {
 };
 
 // eight consecutive elements as bf16
-__device__ __forceinline__ uint4 load_eight(const void* base, size_t at, int f32) {
-  if (f32) {
+template <bool F32>
+__device__ __forceinline__ uint4 load_eight(const void* base, size_t at) {
+  if constexpr (F32) {
     const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
     const float4 a = p[0], b = p[1];
     return make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
@@ -49,9 +62,10 @@ __device__ __forceinline__ uint4 load_eight(const void* base, size_t at, int f32
   return *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(base) + at);
 }
 // eight floats rounded to bf16, stored as such or widened
-__device__ __forceinline__ void store_eight(void* base, size_t at, int f32, const float (&f)[8]) {
+template <bool F32>
+__device__ __forceinline__ void store_eight(void* base, size_t at, const float (&f)[8]) {
   const uint4 v = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-  if (f32) {
+  if constexpr (F32) {
     float4* p = reinterpret_cast<float4*>(reinterpret_cast<float*>(base) + at);
     auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
     auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
@@ -105,41 +119,59 @@ __device__ __forceinline__ uint2 quantise(const float (&f)[8], int e) {
 }
 
 // One token a sequence.  A head row of DH elements is DH / 8 lanes; a CTA takes 256 / (DH / 8) of the rows of one token and layer
-// (K heads, V heads, query heads).  The rows are asked for before the lengths are there.
-template <int DH, bool BITS8, int NL>
-__global__ void __launch_bounds__(APP_THREADS) append_one_kernel(const __grid_constant__ AppParams<NL> p) {
+// (K heads, V heads, query heads).  The length, the page and the angles are worked out before the kernels ahead have finished
+// (through L2: no line may stay in L1) and again behind the wait if the length or the page is not the same there, so that one
+// latency lies between the wait and the stores: the rows, the length, the page and the block's scale are asked for at once.
+template <int DH, bool BITS8, bool F32, int NL>
+__global__ void __launch_bounds__(APP_THREADS, ONES_AN_SM) append_one_kernel(const __grid_constant__ AppParams<NL> p) {
   constexpr int LANES = DH / 8;
   const AppLayer& at = p.at[blockIdx.y];
   const int b = blockIdx.x, c = threadIdx.x % LANES;
-  int row = blockIdx.z * (APP_THREADS / LANES) + threadIdx.x / LANES;
+  const int row = blockIdx.z * (APP_THREADS / LANES) + threadIdx.x / LANES;
   grid_dep_launch();
-  grid_dep_wait();
   const int kv_rows = at.k_new != nullptr ? 2 * p.Hkv : 0, rows = kv_rows + (at.q != nullptr ? p.Hq : 0);
-  if (blockIdx.z * (APP_THREADS / LANES) >= rows) return;          // (the whole block)
   const bool there = row < rows;
   const bool is_q = row >= kv_rows, is_v = !is_q && row >= p.Hkv;
   const int head = is_q ? row - kv_rows : is_v ? row - p.Hkv : row, heads = is_q ? p.Hq : p.Hkv;
   const size_t in = (size_t(b) * heads + head) * DH + c * 8;
-  uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-  if (there) raw = load_eight(is_q ? at.q : is_v ? at.v_new : at.k_new, in, p.io_f32);
-  const int pos = p.lengths[b] - 1;
-  if (pos < 0 || pos >= p.max_pages * p.page_size) return;         // (the whole block)
-  const int page = p.block_table[size_t(b) * p.max_pages + pos / p.page_size];
-  const bool stored = there && !is_q && page >= 0 && page < p.n_pages;
-  const int slot = pos % p.page_size, older = pos % CACHE_BLOCK;
-  const size_t block = (size_t(stored ? page : 0) * p.Hkv + (is_q ? 0 : head)) * (p.page_size / CACHE_BLOCK) + slot / CACHE_BLOCK;
-  uint8_t* const scale = BITS8 ? (is_v ? at.v_scale : at.k_scale) : nullptr;
-  int e_old = LEAST_SCALE;
-  if (BITS8 && stored && older > 0) e_old = exponent_of_byte(scale[block]);
-  float f[8];
-  widen(raw, f);
-  if (p.rotate && !is_v && there) {
-    float2 cs[4];
+  const int cap = p.max_pages * p.page_size;
+  float2 cs[4];
+  auto angles = [&](int pos) {
+    if (!p.rotate) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k) cs[k] = turn_of(p.turns[c * 4 + k], pos);
-    turn_pairs(f, cs);
+  };
+  auto page_at = [&](int pos) { return pos >= 0 && pos < cap ? __ldcg(p.block_table + size_t(b) * p.max_pages + pos / p.page_size) : -1; };
+  uint8_t* const scale = BITS8 ? (is_v ? at.v_scale : at.k_scale) : nullptr;
+  auto block_of = [&](int page, int pos) {
+    return (size_t(page) * p.Hkv + head) * (p.page_size / CACHE_BLOCK) + pos % p.page_size / CACHE_BLOCK;
+  };
+  auto scale_at = [&](int page, int pos) -> int {        // exponent of a block that older tokens began
+    const bool begun = BITS8 && there && !is_q && page >= 0 && page < p.n_pages && pos % CACHE_BLOCK > 0;
+    return begun ? exponent_of_byte(scale[block_of(page, pos)]) : LEAST_SCALE;
+  };
+  int pos = __ldcg(p.lengths + b) - 1;
+  int page = page_at(pos);
+  angles(pos);
+  grid_dep_wait();
+  uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+  if (there) raw = load_eight<F32>(is_q ? at.q : is_v ? at.v_new : at.k_new, in);
+  const int pos_now = p.lengths[b] - 1, page_now = page_at(pos);
+  int e_old = scale_at(page, pos);
+  if (pos_now != pos || page_now != page) {              // (the whole block)
+    pos = pos_now;
+    page = page_at(pos);
+    angles(pos);
+    e_old = scale_at(page, pos);
   }
-  if (there && is_q) store_eight(at.q_out, in, p.io_f32, f);
+  if (pos < 0 || pos >= cap) return;                     // (the whole block)
+  const bool stored = there && !is_q && page >= 0 && page < p.n_pages;
+  const int older = pos % CACHE_BLOCK;
+  const size_t block = stored ? block_of(page, pos) : 0;
+  float f[8];
+  widen(raw, f);
+  if (p.rotate && !is_v) turn_pairs(f, cs);
+  if (there && is_q) store_eight<F32>(at.q_out, in, f);
   void* const cache = is_v ? at.v_cache : at.k_cache;
   const size_t first_elem = block * CACHE_BLOCK * DH + c * 8;      // of the block's first token
   if constexpr (BITS8) {
@@ -160,163 +192,225 @@ __global__ void __launch_bounds__(APP_THREADS) append_one_kernel(const __grid_co
       if (c == 0) scale[block] = uint8_t(e + 127);
     }
   } else if (stored) {
-    store_eight(cache, first_elem + older * DH, 0, f);
+    store_eight<false>(cache, first_elem + older * DH, f);
   }
 }
 
 // Runs of tokens of every sequence.  A CTA takes one block of 16 positions of a sequence that new tokens fall into, in one layer
-// (and every gridDim.z-th head): it finds its block by a prefix sum over the sequences, forms the 16 rows' sines and cosines
-// once, and its warps take the heads in turn, a warp all 16 rows of one, so that the largest magnitude of a block and head and
-// the rounding to its scale stay in registers.
-template <int DH, bool BITS8, int NL>
-__global__ void __launch_bounds__(APP_THREADS, 2) append_runs_kernel(const __grid_constant__ AppParams<NL> p) {
-  constexpr int LANES = DH / 8, ROWS = 32 / LANES, ITERS = CACHE_BLOCK / ROWS;   // lanes a row, rows at a time
-  __shared__ float2 s_turn[CACHE_BLOCK][DH / 2];
-  __shared__ int s_sum[APP_WARPS], s_found[2];
+// (and where there is room, some of its heads).  A thread keeps one row and one slice of eight elements and goes through the heads,
+// so that its sines and cosines stay in registers.  In 8 bits the largest magnitude of a block and head is exchanged through
+// shared memory.  (A warp for all 16 rows of a head instead, with the angles in shared memory: prompts 211 and 492 us.  All blocks
+// found by a search over the sequences: 64 runs of 4 tokens 22 us instead of 8.5.)
+template <int DH, bool BITS8, bool F32, bool ONE_WAVE, int NL>
+__global__ void __launch_bounds__(APP_THREADS, RUNS_AN_SM<DH, ONE_WAVE>) append_runs_kernel(const __grid_constant__ AppParams<NL> p) {
+  constexpr int LANES = DH / 8, TEAM = CACHE_BLOCK * LANES, TEAMS = APP_THREADS / TEAM, TEAM_WARPS = TEAM / 32, HEADS = KV_HEADS<BITS8>, FLY = HEADS / TEAMS, Q_FLY = Q_HEADS / TEAMS;
+  __shared__ uint32_t s_amax[2][TEAMS][FLY][TEAM_WARPS];
+  __shared__ int2 s_found;
   const AppLayer& at = p.at[blockIdx.y];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int team = threadIdx.x / TEAM, r = threadIdx.x % TEAM / LANES, c = threadIdx.x % LANES;
   const int cap = p.max_pages * p.page_size;
-  grid_dep_wait();
-  // positions of sequence b that its new tokens take: [lo, hi); rows of T outside [0, T) do not exist
-  auto span = [&](int b, int& lo, int& hi) {
-    const long long r0 = p.first[b], r1 = p.first[b + 1], len = p.lengths[b], to_pos = len - r1;   // position of row r: r + to_pos
-    lo = int(min((long long)cap, max(0LL, max(r0, 0LL) + to_pos)));
-    hi = int(min((long long)cap, max(0LL, min(r1, (long long)p.T) + to_pos)));
+  if (ONE_WAVE) grid_dep_launch();
+
+  // The sequence and its block of positions: the first B blocks of the grid take the first one of each sequence, the others look
+  // theirs up among the rest.
+  int b = -1, base = 0;                            // sequence, the block's first position
+  int r_lo = 0, r_hi = 0, row0 = 0;                // its rows that are new, and the row of T that its first one would be
+  struct Ends {
+    int r0, r1, len;
   };
-  if (threadIdx.x == 0) s_found[0] = -1;
-  int before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += APP_THREADS) {
-    const int b = b0 + threadIdx.x;
-    int n = 0;
-    if (b < p.B) {
-      int lo, hi;
-      span(b, lo, hi);
-      if (hi > lo) n = (hi - 1) / CACHE_BLOCK - lo / CACHE_BLOCK + 1;
-    }
-    int upto = n;
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, upto, s);
-      if (lane >= s) upto += v;
-    }
-    if (lane == 31) s_sum[warp] = upto;
+  auto load = [&](int i) { return i < p.B ? Ends{__ldcg(p.first + i), __ldcg(p.first + i + 1), __ldcg(p.lengths + i)} : Ends{0, 0, 0}; };
+  auto span = [&](const Ends& e, int& l, int& h, long long& tp) {   // rows of T outside [0, T) do not exist
+    tp = (long long)e.len - e.r1;
+    l = int(min((long long)cap, max(0LL, max((long long)e.r0, 0LL) + tp)));
+    h = int(min((long long)cap, max(0LL, min((long long)e.r1, (long long)p.T) + tp)));
+  };
+  auto take = [&](int seq, int nth) {              // its nth block, if it has one
+    int lo, hi;
+    long long to_pos;
+    span(load(seq), lo, hi, to_pos);
+    base = (lo / CACHE_BLOCK + nth) * CACHE_BLOCK;
+    b = base < hi && lo < hi ? seq : -1;
+    r_lo = max(lo - base, 0);
+    r_hi = min(hi - base, CACHE_BLOCK);
+    row0 = int(base - to_pos);
+  };
+  auto locate = [&]() {
+    if (int(blockIdx.x) < p.B) return take(blockIdx.x, 0);
     __syncthreads();
-    int ahead = before;
+    if (threadIdx.x == 0) s_found = int2{-1, 0};
+    __syncwarp();
+    if (warp == 0) {
+      int before = 0;
+      Ends e = load(lane);
+      for (int b0 = 0; b0 < p.B; b0 += 32) {
+        Ends next = e;
+        if (b0 + 32 < p.B) next = load(b0 + 32 + lane);
+        int l, h;
+        long long tp;
+        span(e, l, h, tp);
+        const int n = h > l ? (h - 1) / CACHE_BLOCK - l / CACHE_BLOCK : 0;   // blocks behind the first
+        int upto = n;
 #pragma unroll
-    for (int w = 0; w < APP_WARPS; ++w) {
-      ahead += w < warp ? s_sum[w] : 0;
-      before += s_sum[w];
-    }
-    const int unit = int(blockIdx.x) - ahead;
-    if (unit < upto && unit >= upto - n) {
-      s_found[0] = b;
-      s_found[1] = unit - (upto - n);
+        for (int s = 1; s < 32; s <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, s);
+          if (lane >= s) upto += v;
+        }
+        const int unit = int(blockIdx.x) - p.B - before;
+        if (unit < upto && unit >= upto - n) s_found = int2{b0 + lane, unit - (upto - n) + 1};
+        if (__any_sync(0xffffffffu, unit < upto)) break;
+        before += __shfl_sync(0xffffffffu, upto, 31);
+        e = next;
+      }
     }
     __syncthreads();
-    if (s_found[0] >= 0) break;
+    b = -1;
+    if (s_found.x >= 0) take(s_found.x, s_found.y);
+  };
+  float2 cs[4];
+  auto angles = [&]() {
+    if (!p.rotate) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) cs[k] = turn_of(p.turns[c * 4 + k], base + r);
+  };
+  // As in decode, where all blocks come up at once: from what is there before the kernels ahead have finished, and again behind the
+  // wait; the angles are kept if the place is still the same.
+  if constexpr (ONE_WAVE) {
+    for (int behind = 0, angles_of = -1; behind < 2; ++behind) {   // (one copy of the code)
+      if (behind != 0) grid_dep_wait();
+      locate();
+      if (b >= 0 && base != angles_of) angles();
+      angles_of = b >= 0 ? base : -1;
+    }
+  } else {
+    grid_dep_wait();
+    locate();
+    if (b >= 0) angles();
   }
-  if (s_found[0] < 0) {
-    grid_dep_launch();
+  if (b < 0) {
+    if (!ONE_WAVE) grid_dep_launch();
     return;
   }
-  const int b = s_found[0];
-  int lo, hi;
-  span(b, lo, hi);
-  const int base = (lo / CACHE_BLOCK + s_found[1]) * CACHE_BLOCK;   // the block's first position
-  const int r_lo = max(lo - base, 0), r_hi = min(hi - base, CACHE_BLOCK);   // its rows that are new
-  const long long row0 = (long long)base - p.lengths[b] + p.first[b + 1];   // row of T at `base` (may be negative)
+  const bool mine = r >= r_lo && r < r_hi;             // this thread's row is new
+  const int older = r_lo;                              // rows of the block that older tokens have
   const int page = p.block_table[size_t(b) * p.max_pages + base / p.page_size];
-  if (p.rotate) {
-    for (int i = threadIdx.x; i < CACHE_BLOCK * (DH / 2); i += APP_THREADS) s_turn[i / (DH / 2)][i % (DH / 2)] = turn_of(p.turns[i % (DH / 2)], base + i / (DH / 2));
-  }
-  __syncthreads();
-  const int rr = lane / LANES, c = lane % LANES;
-  const int kv_rows = at.k_new != nullptr ? 2 * p.Hkv : 0, rows = kv_rows + (at.q != nullptr ? p.Hq : 0);
-  const bool paged = page >= 0 && page < p.n_pages;
-  for (int row = int(blockIdx.z) * APP_WARPS + warp; row < rows; row += int(gridDim.z) * APP_WARPS) {
-    const bool is_q = row >= kv_rows, is_v = !is_q && row >= p.Hkv;
-    if (!is_q && !paged) continue;
-    const int head = is_q ? row - kv_rows : is_v ? row - p.Hkv : row, heads = is_q ? p.Hq : p.Hkv;
-    const void* const src = is_q ? at.q : is_v ? at.v_new : at.k_new;
-    auto in = [&](int r) { return (size_t(row0 + r) * heads + head) * DH + c * 8; };
-    uint4 raw[ITERS];
+  const size_t row = size_t(row0 + r);                 // of T (where the row is new)
+  const bool does_kv = int(blockIdx.z) < p.kv_slices, does_q = p.q_slices == 0 || !does_kv;
+
+  if (does_kv && at.k_new != nullptr && page >= 0 && page < p.n_pages) {
+    // groups of HEADS K heads, then of V heads
+    const int groups = (p.Hkv + HEADS - 1) / HEADS, per_page = p.page_size / CACHE_BLOCK;
+    const size_t page_block = size_t(page) * p.Hkv * per_page + base % p.page_size / CACHE_BLOCK;
+    int buf = 0;
+    for (int group = blockIdx.z; group < 2 * groups; group += p.kv_slices, buf ^= 1) {
+      const bool is_v = group >= groups;
+      const int head = (is_v ? group - groups : group) * HEADS + team;         // and every TEAMS-th behind it
+      const int heads = (p.Hkv - head + TEAMS - 1) / TEAMS;                    // that there are of those (or fewer than one)
+      const size_t block = page_block + size_t(head) * per_page, next_block = size_t(TEAMS) * per_page;
+      uint8_t* const scale = BITS8 ? (is_v ? at.v_scale : at.k_scale) + block : nullptr;
+      const size_t in = (row * p.Hkv + head) * DH + c * 8;
+      uint4 raw[FLY];
+      uint32_t held[FLY];                          // scales of a block that older tokens began
 #pragma unroll
-    for (int i = 0; i < ITERS; ++i) {
-      const int r = i * ROWS + rr;
-      raw[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (r >= r_lo && r < r_hi) raw[i] = load_eight(src, in(r), p.io_f32);
-    }
-    auto rotated = [&](int i, float (&f)[8]) {
-      widen(raw[i], f);
-      if (p.rotate && !is_v) {
-        float2 cs[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) cs[k] = s_turn[i * ROWS + rr][c * 4 + k];
-        turn_pairs(f, cs);
-      }
-    };
-    const size_t block = (size_t(is_q ? 0 : page) * p.Hkv + head) * (p.page_size / CACHE_BLOCK) + base % p.page_size / CACHE_BLOCK;
-    void* const cache = is_v ? at.v_cache : at.k_cache;
-    const size_t first_elem = block * CACHE_BLOCK * DH + c * 8;
-    if (BITS8 && !is_q) {
-      uint8_t* const scale = is_v ? at.v_scale : at.k_scale;
-      uint8_t* const codes = reinterpret_cast<uint8_t*>(cache) + first_elem;
-      const int e_old = r_lo > 0 ? exponent_of_byte(scale[block]) : LEAST_SCALE;
-      float f[ITERS][8];
-      uint32_t amax = 0;
-#pragma unroll
-      for (int i = 0; i < ITERS; ++i) {
-        rotated(i, f[i]);
-        amax = max(amax, finite_amax(f[i]));
-      }
-      amax = __reduce_max_sync(0xffffffffu, amax);
-      const int e = max(e_old, scale_exponent(amax));
-      if (r_lo > 0 && e > e_old) {
-        const float factor = __uint_as_float(power_bits(e_old - e));
-        for (int r = rr; r < r_lo; r += ROWS) {
-          uint2* const w = reinterpret_cast<uint2*>(codes + r * DH);
-          *w = make_uint2(rescale_e4m3(w->x, factor), rescale_e4m3(w->y, factor));
+      for (int u = 0; u < FLY; ++u) {
+        raw[u] = make_uint4(0u, 0u, 0u, 0u);
+        held[u] = 0;
+        if (u < heads) {
+          if (mine) raw[u] = load_eight<F32>(is_v ? at.v_new : at.k_new, in + u * TEAMS * DH);
+          if (BITS8 && older > 0) held[u] = scale[u * next_block];
         }
       }
+      auto turned = [&](int u, float (&f)[8]) {
+        widen(raw[u], f);
+        if (p.rotate && !is_v) turn_pairs(f, cs);
+      };
+      if constexpr (BITS8) {
 #pragma unroll
-      for (int i = 0; i < ITERS; ++i) {
-        const int r = i * ROWS + rr;
-        if (r >= r_lo && r < r_hi) *reinterpret_cast<uint2*>(codes + r * DH) = quantise(f[i], e);
+        for (int u = 0; u < FLY; ++u) {            // (rotated again below: kept, four heads' floats would leave room for three blocks an SM)
+          float f[8];
+          turned(u, f);
+          const uint32_t m = __reduce_max_sync(0xffffffffu, finite_amax(f));
+          if (lane == 0) s_amax[buf][team][u][warp % TEAM_WARPS] = m;
+        }
+        __syncthreads();
       }
-      __syncwarp();                                                // (every lane has read the old scale)
-      if (lane == 0) scale[block] = uint8_t(e + 127);
-    } else {
+      const size_t elem = (block * CACHE_BLOCK + r) * DH + c * 8, next_elem = next_block * CACHE_BLOCK * DH;
 #pragma unroll
-      for (int i = 0; i < ITERS; ++i) {
-        const int r = i * ROWS + rr;
+      for (int u = 0; u < FLY; ++u) {
+        if (u >= heads) break;
+        void* const cache = is_v ? at.v_cache : at.k_cache;
         float f[8];
-        rotated(i, f);
-        if (r >= r_lo && r < r_hi) {
-          if (is_q) store_eight(at.q_out, in(r), p.io_f32, f);
-          else store_eight(cache, first_elem + r * DH, 0, f);
+        turned(u, f);
+        if constexpr (BITS8) {
+          uint32_t amax = 0;
+#pragma unroll
+          for (int w = 0; w < TEAM_WARPS; ++w) amax = max(amax, s_amax[buf][team][u][w]);
+          const int e_old = older > 0 ? exponent_of_byte(held[u]) : LEAST_SCALE, e = max(e_old, scale_exponent(amax));
+          uint2* const codes = reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(cache) + elem + u * next_elem);
+          if (mine) {
+            finite_amax(f);
+            *codes = quantise(f, e);
+          } else if (r < older && e > e_old) {
+            const float factor = __uint_as_float(power_bits(e_old - e));
+            *codes = make_uint2(rescale_e4m3(codes->x, factor), rescale_e4m3(codes->y, factor));
+          }
+          if (threadIdx.x % TEAM == 0) scale[u * next_block] = uint8_t(e + 127);   // (all have read the old one)
+        } else {
+          if (mine) store_eight<false>(cache, elem + u * next_elem, f);
         }
       }
     }
   }
-  grid_dep_launch();
+  if (does_q && at.q != nullptr && mine) {
+    const int first = int(blockIdx.z) - (p.q_slices == 0 ? 0 : p.kv_slices), step = p.q_slices == 0 ? p.kv_slices : p.q_slices;
+    for (int head = first * Q_HEADS + team; head < p.Hq; head += step * Q_HEADS) {
+      const size_t in = (row * p.Hq + head) * DH + c * 8;
+      const int heads = (p.Hq - head + TEAMS - 1) / TEAMS;
+      uint4 raw[Q_FLY];
+#pragma unroll
+      for (int u = 0; u < Q_FLY; ++u)
+        if (u < heads) raw[u] = load_eight<F32>(at.q, in + u * TEAMS * DH);
+#pragma unroll
+      for (int u = 0; u < Q_FLY; ++u) {
+        if (u >= heads) break;
+        float f[8];
+        widen(raw[u], f);
+        if (p.rotate) turn_pairs(f, cs);
+        store_eight<F32>(at.q_out, in + u * TEAMS * DH, f);
+      }
+    }
+  }
+  if (!ONE_WAVE) grid_dep_launch();
 }
 
-template <bool BITS8, int NL>
+template <bool BITS8, bool F32, int NL>
 cudaError_t launch_tokens(const AppParams<MANY_LAYERS>& all, int n, int dh, cudaStream_t stream) {
   AppParams<NL> p;
   static_cast<AppSizes&>(p) = all;
   std::copy(all.at, all.at + n, p.at);
-  const int rows = 2 * all.Hkv + all.Hq;
   if (all.first == nullptr) {
+    const int rows = 2 * all.Hkv + all.Hq;
     const int per = APP_THREADS / (dh / 8);
-    return launch_kernel(dh == 128 ? append_one_kernel<128, BITS8, NL> : append_one_kernel<64, BITS8, NL>, dim3(all.B, n, (rows + per - 1) / per), APP_THREADS,
+    return launch_kernel(dh == 128 ? append_one_kernel<128, BITS8, F32, NL> : append_one_kernel<64, BITS8, F32, NL>, dim3(all.B, n, (rows + per - 1) / per), APP_THREADS,
                          0, stream, 1, p);
   }
-  // blocks that n >= 1 tokens fall into: at most n, and at most (n + 14) / 16 + 1
-  const long long live = std::min(all.B, all.T), most = std::min((long long)all.T, (all.T + 30 * live) / CACHE_BLOCK);
-  const int slices = int(std::max(1LL, std::min((long long)(rows + APP_WARPS - 1) / APP_WARPS, 2LL * sm_count() / std::max(1LL, most * n))));
-  return launch_kernel(dh == 128 ? append_runs_kernel<128, BITS8, NL> : append_runs_kernel<64, BITS8, NL>, dim3(unsigned(most), n, slices), APP_THREADS, 0, stream,
-                       1, p);
+  // a block of the grid for each sequence, and for each block of positions behind the first that n tokens fall into: (n + 14) / 16
+  const long long most = all.B + (all.T + 14LL * std::min(all.B, all.T)) / CACHE_BLOCK;
+  // Where there is room for them, blocks of their own for the queries, and heads over several blocks, four each.
+  const int room = int(std::min(64LL, ((long long)RUNS_A_WAVE * sm_count() + most * n - 1) / (most * n)));
+  const int kv = 2 * ((all.Hkv + KV_HEADS<BITS8> - 1) / KV_HEADS<BITS8>), q = all.at[0].q != nullptr ? (all.Hq + Q_HEADS - 1) / Q_HEADS : 0;
+  p.kv_slices = std::max(1, std::min(kv, q > 0 ? room * 2 * kv / (2 * kv + q) : room));
+  p.q_slices = q > 0 ? std::max(0, std::min(q, room - p.kv_slices)) : 0;
+  const dim3 grid(unsigned(most), n, p.kv_slices + p.q_slices);
+  const bool one_wave = most * n * grid.z <= (long long)RUNS_A_WAVE * sm_count();
+  auto* const kernel = one_wave ? (dh == 128 ? append_runs_kernel<128, BITS8, F32, true, NL> : append_runs_kernel<64, BITS8, F32, true, NL>)
+                                : (dh == 128 ? append_runs_kernel<128, BITS8, F32, false, NL> : append_runs_kernel<64, BITS8, F32, false, NL>);
+  return launch_kernel(kernel, grid, APP_THREADS, 0, stream, 1, p);
+}
+
+template <bool BITS8, bool F32>
+cudaError_t launch_tokens(const AppParams<MANY_LAYERS>& p, int n, int dh, cudaStream_t stream) {
+  return n <= FEW_LAYERS ? launch_tokens<BITS8, F32, FEW_LAYERS>(p, n, dh, stream) : launch_tokens<BITS8, F32, MANY_LAYERS>(p, n, dh, stream);
 }
 
 }  // namespace
@@ -364,7 +458,6 @@ extern "C" int kvp_cache_append_tokens(const kvp_decode_desc* d, const int32_t* 
   p.page_size = d->page_size;
   p.max_pages = d->max_pages;
   p.n_pages = d->n_pages;
-  p.io_f32 = d->dtype == KVP_F32;
   p.rotate = theta != 0.f;
   if (p.rotate) rope_turns(double(theta), d->dh, p.turns);
   int n = 0;
@@ -376,8 +469,9 @@ extern "C" int kvp_cache_append_tokens(const kvp_decode_desc* d, const int32_t* 
                    owner ? v_cache[l] : nullptr, owner && bits8 ? k_scale[l] : nullptr, owner && bits8 ? v_scale[l] : nullptr};
     }
     if (n == MANY_LAYERS || (l == d->L && n > 0)) {
-      const cudaError_t e = n <= FEW_LAYERS ? (bits8 ? launch_tokens<true, FEW_LAYERS>(p, n, d->dh, stream) : launch_tokens<false, FEW_LAYERS>(p, n, d->dh, stream))
-                                            : (bits8 ? launch_tokens<true, MANY_LAYERS>(p, n, d->dh, stream) : launch_tokens<false, MANY_LAYERS>(p, n, d->dh, stream));
+      const bool f32 = d->dtype == KVP_F32;
+      const cudaError_t e = bits8 ? (f32 ? launch_tokens<true, true>(p, n, d->dh, stream) : launch_tokens<true, false>(p, n, d->dh, stream))
+                                  : (f32 ? launch_tokens<false, true>(p, n, d->dh, stream) : launch_tokens<false, false>(p, n, d->dh, stream));
       if (e != cudaSuccess) return KVP_ERR_CUDA;
       n = 0;
     }

@@ -530,11 +530,12 @@ _pack.bind_cache([C.cast(getattr(lib, "kvp_" + n), C.c_void_p).value for n in ("
 _I32, _CODES, _SCALES = (torch.int32,), (torch.float8_e4m3fn, torch.uint8), (torch.float8_e8m0fnu, torch.uint8)
 
 
-def _call_device() -> int:
-    """Device that a call runs on (-2: there is none, and the library refuses the call or fails to launch)."""
-    if torch.cuda.is_initialized():
-        return _device()
-    return 0 if torch.cuda.is_available() else -2
+def _call_place():
+    """Device that a call runs on (-2: there is none, and the library refuses the call or fails to launch) and its stream."""
+    if _raw_stream is not None and torch.cuda.is_initialized():
+        device = _device()
+        return device, _raw_stream(device)
+    return (_device() if torch.cuda.is_available() else -2), _stream()
 
 
 def _fit(what: str, t, dtypes, numel: int, device: int) -> None:
@@ -573,9 +574,9 @@ def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table
     Sequence b has rows first[b] .. first[b+1]-1 (int32 [B + 1]; None: one token each, T == B) at the positions before lengths[b].
     With k_scale, v_scale (uint8 or float8_e8m0fnu [n_pages, Hkv, page_size / 16]) the cache holds float8_e4m3fn numbers.
     Tensors are contiguous, of the documented sizes, on the current device: ValueError otherwise."""
-    device = _call_device()
+    device, stream = _call_place()
     status = _pack.cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table, lengths, first, theta, q, q_out, k_scale, v_scale,
-                                       device, _stream())
+                                       device, stream)
     if status is not NotImplemented:
         return _check(status, "kvp_cache_append_tokens")
     layers, owners = _layer_range(desc, donor)
@@ -594,7 +595,7 @@ def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table
     d, n = _map(desc, donor)
     array = lambda ts: None if ts is None else _ptr_array(ts, n)
     _check(lib.kvp_cache_append_tokens(C.byref(desc), d, T, _ptr(first), float(theta), array(q), array(q_out), array(k_new), array(v_new),
-                                       array(k_cache), array(v_cache), array(k_scale), array(v_scale), _ptr(block_table), _ptr(lengths), _stream()),
+                                       array(k_cache), array(v_cache), array(k_scale), array(v_scale), _ptr(block_table), _ptr(lengths), stream),
            "kvp_cache_append_tokens")
 
 
@@ -608,9 +609,9 @@ def decode8(desc, donor, q, k_cache, v_cache, k_scale, v_scale, block_table, len
     """kvp_decode8: decode attention over the cache held in 8 bits, as cache_append_tokens with scales leaves it.  Arguments as for
     decode; a sequence of length 0 has output 0 and LSE -infinity.  Tensors are contiguous, of the documented sizes, on the
     current device: ValueError otherwise."""
-    device = _call_device()
+    device, stream = _call_place()
     status = _pack.decode8(desc, donor, scale, q, k_cache, v_cache, k_scale, v_scale, block_table, lengths, o, lse, layer_begin, layer_end, ws, device,
-                           _stream())
+                           stream)
     if status is not NotImplemented:
         return _check(status, "kvp_decode8")
     end = desc.L if layer_end is None else int(layer_end)
@@ -629,4 +630,4 @@ def decode8(desc, donor, q, k_cache, v_cache, k_scale, v_scale, block_table, len
     p, size = _ws(ws)
     _check(lib.kvp_decode8(C.byref(desc), d, float(scale), _ptr_array(q, n), _ptr_array(k_cache, n), _ptr_array(v_cache, n), _ptr_array(k_scale, n),
                            _ptr_array(v_scale, n), block_table.data_ptr(), lengths.data_ptr(), _ptr_array(o, n), _ptr_array(lse, n), int(layer_begin), end, p,
-                           size, _stream()), "kvp_decode8")
+                           size, stream), "kvp_decode8")
