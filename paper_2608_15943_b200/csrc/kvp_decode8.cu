@@ -30,10 +30,12 @@ constexpr int D8_CTAS = DH == 128 ? (NB == 1 ? 3 : 2) : NB == 1 ? 4 : 3;
 template <int DH, int NB>
 constexpr int D8_SLOTS = DH == 128 && NB == 2 ? 6 : 4;
 constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
-// Where whole units are dealt out and there are so many units for a block that fits, a warp takes a unit alone: nothing is merged.
-// (us, four warps a unit -> so: 128 sequences of 50 to 400 tokens, 8 KV heads, six groups 116 -> 71, 64 of 1 to 64 at dh 64 27.6 ->
-// 12.8; but 32 of 200 to 400 in two groups, 1.2 units a block, 17.3 -> 18.5, 58 of 1 to 700 in four, 1.6, 21 -> 25.)
+// Where whole units are dealt out, two warps take one if there are as many units as blocks that fit, and one takes it alone (nothing is
+// merged) if there are so many times as many.  (us, four warps -> two: 58 sequences of 1 to 700 tokens, 4 KV heads at dh 64, four groups,
+// 1.6 units a block 20.6 -> 18.8; 32 of 200 to 400, two groups, 1.2 units 17.9 -> 15.0; 80 of 1 to 900 at dh 64, 1.1 units 18.1 -> 19.4.
+// Four -> one: 128 of 50 to 400, 8 KV heads, six groups 116 -> 71, 64 of 1 to 64 at dh 64 27.6 -> 12.8; but the 58 above 21 -> 25.)
 constexpr int LONE_UNITS = 2;
+static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
 struct Dec8Group {
@@ -189,8 +191,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     }
   }
   if (!placed) return;
-  const bool lone = by_units && !caller_splits && units >= LONE_UNITS * p.fit;
-  int first_step = warp, team = D8_WARPS;          // of a piece: this warp's first step, and how many warps take its steps in turn
+  // teams of 4, 2 or 1 warps take the steps of a piece in turn
+  const int log_team = !by_units || caller_splits || units < p.fit ? 2 : units < LONE_UNITS * p.fit ? 1 : 0;
+  const int team = 1 << log_team, first_step = warp & (team - 1);
   if (caller_splits) {
     const int split = blockIdx.x % p.num_splits;
     go_to_unit(c, blockIdx.x / p.num_splits);
@@ -198,16 +201,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     c.gran = min(c.ng, split * per);
     todo = min(c.ng - c.gran, per);
   } else if (by_units) {
-    if (lone) {
-      first_step = 0;
-      team = 1;
-    }
-    const int id = lone ? int(blockIdx.x) * D8_WARPS + warp : int(blockIdx.x);
+    const int id = (int(blockIdx.x) * D8_WARPS + warp) >> log_team;
     if (id >= units) return;
     go_to_unit(c, id);
     todo = c.ng;
   }
-  const int unit_step = int(gridDim.x) * (lone ? D8_WARPS : 1);
+  const int unit_step = int(gridDim.x) << (2 - log_team);
   auto next_piece = [&](Cursor& x, int& left) {    // past the end: grp >= n_groups
     left -= min(left, x.ng + rest - x.gran);
     if (left > 0) {
@@ -571,25 +570,26 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
         }
         if (sum[nb][h] == 0.f) M[nb][h] = -INFINITY;
       }
-    // ---- warp 0 merges the results of the others into its own, four rows at a time ----
+    // ---- the team's first warp merges the results of the others into its own, four rows at a time ----
+    auto team_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + (warp >> log_team)), "r"(32 << log_team) : "memory"); };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (8 * nb + h >= R || lone) break;
-        __syncthreads();   // warp 0 is done with the previous ones
-        if (warp > 0) {
+        if (8 * nb + h >= R || team == 1) break;
+        team_sync();       // its first warp is done with the previous ones
+        if (first_step > 0) {
 #pragma unroll
           for (int m = 0; m < MB; ++m) s_o[warp - 1][m * 32 + lane] = make_float2(oacc[m][nb][h], oacc[m][nb][2 + h]);
           s_ml[warp - 1][lane] = make_float2(M[nb][h], sum[nb][h]);
         }
-        __syncthreads();
-        if (warp == 0) {
+        team_sync();
+        if (first_step == 0) {
           float2 om[D8_WARPS - 1];
           float mn = M[nb][h];
 #pragma unroll
           for (int w = 0; w < D8_WARPS - 1; ++w) {
-            om[w] = s_ml[w][lane];
+            om[w] = w < team - 1 ? s_ml[warp + w][lane] : make_float2(-INFINITY, 0.f);
             mn = fmaxf(mn, om[w].x);
           }
           const float fa = M[nb][h] == -INFINITY ? 0.f : fast_exp2(M[nb][h] - mn);
@@ -602,11 +602,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           }
 #pragma unroll
           for (int w = 0; w < D8_WARPS - 1; ++w) {
+            if (w >= team - 1) break;
             const float fb = om[w].x == -INFINITY ? 0.f : fast_exp2(om[w].x - mn);
             sum[nb][h] += om[w].y * fb;
 #pragma unroll
             for (int m = 0; m < MB; ++m) {
-              const float2 v = s_o[w][m * 32 + lane];
+              const float2 v = s_o[warp + w][m * 32 + lane];
               oacc[m][nb][h] += v.x * fb;
               oacc[m][nb][2 + h] += v.y * fb;
             }
