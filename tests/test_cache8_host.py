@@ -219,3 +219,61 @@ def test_a_workspace_serves_every_layer_range(kvp):
                 got = kvp.lib.kvp_decode8(C.byref(desc), kvp._donors(donor), 0.0, *[(C.c_void_p * L)(*[4096] * L)] * 5, 4096, 4096,
                                           *[(C.c_void_p * L)(*[4096] * L)] * 2, a, b, 4096, need, None)
                 assert got == kvp.ERR_CUDA, (donor, a, b)       # every check passed, the workspace's among them
+
+
+# ---------------------------------------------------------------------------------------------
+# what the native calls hand over
+# ---------------------------------------------------------------------------------------------
+FORMS = {"cache_append_tokens": "SDipfAAAAAAAAppp", "decode8": "SDfAAAAAppAAiiplp"}
+TYPES = dict(i=C.c_int, l=C.c_size_t, f=C.c_float, p=C.c_void_p, S=C.c_void_p, D=C.c_void_p, A=C.c_void_p)
+
+
+def test_both_paths_hand_over_the_same(monkeypatch):
+    """Sizes, pointers and null arrays reach the library alike by the native and the ctypes path; unusual lists go by the latter."""
+    from paper_2608_15943_b200 import kvp
+    if torch.cuda.is_available():
+        pytest.skip("host tensors")
+    seen, keep = [], []
+    for name, form in FORMS.items():
+        def called(*args, name=name, form=form):
+            layers = C.cast(args[0], C.POINTER(C.c_int32))[0]
+            read = {"S": lambda v: C.string_at(v, C.sizeof(kvp.DecodeDesc)), "D": lambda v: C.string_at(v, 4 * layers),
+                    "A": lambda v: v and C.string_at(v, 8 * layers)}
+            seen.append([name] + [read.get(k, lambda v: v)(v) for k, v in zip(form, args)])
+            return 0
+        keep.append(C.CFUNCTYPE(C.c_int, *[TYPES[k] for k in form])(called))
+        monkeypatch.setattr(kvp.lib, "kvp_" + name, keep[-1])
+    real = kvp._pack
+    original = [C.cast(getattr(C.CDLL(kvp.LIB_PATH), "kvp_" + n), C.c_void_p).value for n in FORMS]
+    monkeypatch.setattr(kvp, "_call_place", lambda: (-2, 0x7f0000001238))
+    none = types.SimpleNamespace(cache_append_tokens=lambda *a: NotImplemented, decode8=lambda *a: NotImplemented, pointers=real.pointers, donors=real.donors)
+    real.bind_cache([C.cast(cb, C.c_void_p).value for cb in keep])
+    try:
+        first = torch.tensor([0, 1, 2], dtype=torch.int32)
+        calls = [tokens_call(kvp, **o) for o in ({}, dict(bits8=False), dict(dtype=1), dict(q=None, q_out=None, theta=0.0), dict(first=first), dict(T=7, first=first),
+                                                 dict(donor=(0, 1), k_new=[torch.zeros(2, 2, 64, dtype=torch.bfloat16)] * 2, L=2))]
+        calls += [decode_call(kvp, **o) for o in ({}, dict(dtype=1), dict(scale=0.25, layer_begin=1), dict(layer_end=1), dict(splits=4))]
+        for call in calls:
+            del seen[:]
+            monkeypatch.setattr(kvp, "_pack", real)
+            call()
+            monkeypatch.setattr(kvp, "_pack", none)
+            call()
+            a, b = seen
+            for k, x, y in zip("." + FORMS[a[0]], a, b):
+                if k != "A":
+                    assert x == y, (a[0], k)
+                    continue
+                assert (x is None) == (y is None)
+                for i in range(0, len(x or b""), 8):      # (the native path hands over what the call looks at alone)
+                    assert x[i:i + 8] in (y[i:i + 8], bytes(8))
+        monkeypatch.setattr(kvp, "_pack", real)
+
+        class Sub(torch.Tensor):
+            pass
+        del seen[:]
+        tokens_call(kvp, lengths=torch.ones(2, dtype=torch.int32).as_subclass(Sub))()
+        decode_call(kvp, scale=0)()
+        assert len(seen) == 2
+    finally:
+        real.bind_cache(original)

@@ -182,6 +182,26 @@ def test_many_sequences_and_layers(kvp, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dh,Hq,Hkv,page", [(64, 9, 3, 48), (128, 10, 5, 128)])
+def test_long_runs(kvp, bits, dh, Hq, Hkv, page):
+    """More blocks of positions than are on the device at once; heads that do not fill a group."""
+    c = Cache(kvp, 2, [0, 1], [3001, 1, 2500, 4000], [0, 77, 5, 130], Hq, Hkv, dh, page, bits)
+    before = c.snapshot()
+    c.call()
+    c.check(before, 10000.0)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_prompt_among_single_tokens(kvp, bits):
+    """A mixed batch: 70 sequences with a token each and one with 500, whose later blocks are looked up behind all the others."""
+    new = [1] * 45 + [500] + [1] * 25
+    c = Cache(kvp, 2, [0, 0], new, [i % 37 for i in range(71)], 8, 2, 128, 16, bits)
+    before = c.snapshot()
+    c.call()
+    c.check(before, 10000.0)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("one", [False, True])
 def test_without_queries_and_in_place(kvp, bits, one):
     args = (kvp, 2, [0, 0], [1, 1, 1], [4, 0, 30], 4, 2, 64, 16, bits)
@@ -368,6 +388,29 @@ def test_lengths_of_the_step_ahead(kvp):
         torch.cuda.synchronize()
     x, y = c.snapshot(), ref.snapshot()
     assert all(np.array_equal(u, w) for name in ("k_cache", "v_cache", "k_scale", "v_scale") for u, w in zip(x[name], y[name]))
+
+
+@pytest.mark.parametrize("B", [3, 40])
+def test_places_written_by_the_kernel_ahead(kvp, B):
+    """Lengths, first rows and pages are looked at before the kernels ahead have finished; what those write counts."""
+    new = [1 + i % 5 for i in range(B)]
+    args = (kvp, 1, [0], new, [7 * i % 50 for i in range(B)], 4, 2, 64, 16, 8)
+    c, ref = Cache(*args, spare=4), Cache(*args, spare=4)
+    k_new, v_new, k_cache, v_cache, table, lengths = c.lists()
+    first = c.first.cuda()
+    right = (table.clone(), lengths.clone(), first.clone())
+    big = torch.zeros(64 << 20, device="cuda")
+    table.fill_(0), lengths.fill_(5), first.copy_(torch.arange(B + 1, dtype=torch.int32))
+    torch.cuda.synchronize()
+    big.add_(1.0)                                             # keeps the device busy ahead of the copies
+    for x, y in zip((table, lengths, first), right):
+        x.copy_(y)
+    kvp.cache_append_tokens(c.desc, [0], k_new, v_new, k_cache, v_cache, table, lengths, first=first, theta=10000.0, q=c.q, q_out=c.q_out, k_scale=c.k_scale,
+                            v_scale=c.v_scale)
+    ref.call()
+    torch.cuda.synchronize()
+    x, y = c.snapshot(), ref.snapshot()
+    assert all(u is None or np.array_equal(u, w) for name in x for u, w in zip(x[name], y[name]))
 
 
 def test_same_as_rope_and_append(kvp):

@@ -140,6 +140,54 @@ def test_against_64_bits(kvp, donor, lens, Hq, Hkv, dh, page, io):
     c.check(*c.run())
 
 
+MANY = [
+    ([0, 0], 128, 8, 8, 128, 16, 90),                         # units for single warps, several each: rows of one n-block
+    ([0, 0, 2], 160, 36, 4, 64, 32, 150),                     # the same with 9 rows: two n-blocks
+    ([0, 0], 80, 12, 6, 128, 64, 200),                        # two warps a unit
+    ([0], 110, 72, 6, 64, 48, 130),                           # the same with 12 rows
+    ([0], 35, 32, 16, 128, 128, 300),
+]
+
+
+@pytest.mark.parametrize("donor,B,Hq,Hkv,dh,page,most", MANY)
+def test_many_short_sequences(kvp, donor, B, Hq, Hkv, dh, page, most):
+    """Whole units dealt out to one, two or four warps; empty places, lengths of one and of whole blocks among them."""
+    r = np.random.default_rng(B)
+    lens = [int(x) for x in r.integers(0, most, B)]
+    lens[::9], lens[1::11], lens[2::13] = [0] * len(lens[::9]), [1] * len(lens[1::11]), [most // 16 * 16] * len(lens[2::13])
+    c = Case(kvp, donor, lens, Hq, Hkv, dh, page)
+    o, lse = c.run()
+    c.check(o, lse)
+    again, lse2 = c.run()
+    assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
+
+
+def test_values_that_are_not_finite(kvp):
+    """NaN among the visible keys of a KV head reaches its queries' outputs and LSE and no others; among the values, its element."""
+    c = Case(kvp, [0], [500, 40], 4, 2, 128, 16, poison=False)
+    p = int(c.bt[0, 7])
+    c.pools[0][0].view(torch.uint8)[p, 1, 3, 5] = 0x7f
+    c.pools[1][0].view(torch.uint8)[int(c.bt[1, 1]), 0, 2, 9] = 0xff
+    o, lse = c.run()
+    ro, rl, to, tl = exact(c.q[0], c.pools, c.scales, c.bt, c.lens, 16, 128 ** -0.5, 0)
+    bad = torch.zeros(2, 4, 128, dtype=torch.bool, device="cuda")
+    bad[0, 2:], bad[1, :2, 9] = True, True
+    assert torch.equal(torch.isnan(o[0]), bad) and ((o[0].double() - ro).abs() <= to)[~bad].all()
+    assert torch.isnan(lse[0][0, 2:]).all() and torch.isfinite(lse[0][0, :2]).all() and torch.isfinite(lse[0][1]).all()
+    c.q[0][1, 0, 0] = float("nan")                            # a query: its own row
+    o, lse = c.run()
+    assert torch.isnan(o[0][1, 0]).all() and torch.isfinite(o[0][1, 1, :9]).all() and torch.isnan(lse[0][1, 0])
+
+
+def test_another_device_is_refused_and_the_current_one_serves(kvp):
+    if torch.cuda.device_count() < 2:
+        pytest.skip("needs a second device")
+    c = Case(kvp, [0], [100], 4, 1, 64, 16)
+    o, lse, ws = c.outputs()
+    with torch.cuda.device(1), pytest.raises(ValueError):
+        kvp.decode8(c.desc, c.donor, c.q, *c.lists, c.table, c.lengths, o, lse, ws)
+
+
 @pytest.mark.parametrize("splits", [1, 3, 8, 70])
 @pytest.mark.parametrize("dh", [64, 128])
 def test_the_callers_splits(kvp, splits, dh):
