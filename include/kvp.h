@@ -80,7 +80,7 @@ int kvp_selftest_bounded_wait_pair(void* scratch, size_t scratch_bytes, kvp_stre
 /* Benchmark bookkeeping.  kvp_launch_count: kernels launched by this library since it was loaded.
  * kvp_set_timing_events: record the caller's CUDA events (HOST arrays of n cudaEvent_t, created by
  * the caller) immediately before and after each of the next n launches of one kernel
- * (0 GEMM, 1 attention forward, 2 attention backward, 3 decode, 4 the backward's helper passes: Delta, accumulator clear, dQ conversion, one pair per group of launches, the first alone up to 128 tokens); n == 0 switches it off.
+ * (0 GEMM, 1 attention forward, 2 attention backward, 3 decode (over either cache), 4 the backward's helper passes: Delta, accumulator clear, dQ conversion, one pair per group of launches, the first alone up to 128 tokens); n == 0 switches it off.
  * kvp_timing_events_used: how many pairs have been recorded since.  Not thread-safe. */
 unsigned long long kvp_launch_count(void);
 int kvp_set_timing_events(int kernel, void** starts, void** stops, int n);
@@ -327,6 +327,7 @@ int kvp_decode(const kvp_decode_desc* d, const int32_t* donor, float scale, cons
  *     multiplied by the power of two between and rounded again.  A block whose first token is new has no older ones, whatever
  *     it held.  What is not finite is stored as NaN and does not count for the exponent.  Bytes are 27 to 247 (others are read as
  *     the nearer of the two).
+ *     Scales may lie at any address.
  * No two sequences may append into the same block.  dtype (KVP_F32: q, q_out, k_new, v_new are fp32) and the rest of d as for
  * kvp_decode; num_splits is not read. */
 int kvp_cache_append_tokens(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float theta,

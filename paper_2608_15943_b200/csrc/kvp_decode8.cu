@@ -2,11 +2,11 @@
 // same list of K/V rows dealt out to blocks (kvp_decode.cu describes it), the same groups of layers, the same merge.
 //
 // With half the bytes a warp's step of 32 tokens of one KV head (8 KB at dh 128) has to pass an SM in about 340 cycles to keep HBM
-// busy, so the design is about instructions a step:
+// busy, so the design is about instructions a step and bytes in flight:
 //  - K and V are the A operand of mma.sync m16n8k16 (f16 in, fp32 accumulate) and the query rows its N: up to 8 rows cost half the
 //    products that they cost as its M, and the scores of a granule are 4 registers a lane.  S^T = K Q^T, O^T += V^T P^T.
-//  - e4m3 numbers become f16 exactly, two an instruction.  (mma.sync takes e4m3 as it is, but converts it itself at twice the
-//    instructions.)  Which element of a row is which k of a product is free as long as both operands agree, so a lane reads K 16 bytes
+//  - e4m3 numbers become f16 exactly, two an instruction.  (mma.sync takes e4m3 as it is, but converts it itself: half
+//    as many instructions again, 32 sequences of 16K-32K tokens in six groups 1930 us instead of 1420.)  Which element of a row is which k of a product is free as long as both operands agree, so a lane reads K 16 bytes
 //    at a time and its words are its operands; V comes transposed from ldmatrix .b8, four tokens of an element a word, and the
 //    rows of S^T are matched to those tokens.
 //  - Queries are scaled by a power of two a row into f16's range (the largest to 2^14): exact for all bf16 elements down to 2^-31 of
@@ -14,7 +14,11 @@
 //  - The scale of V is a power of two: P is multiplied by 2^(e + M - R) with a reference R of the accumulators beside the
 //    reference M of the sum.  Both rise only when a value would leave f16's upper range, so that no maximum is exchanged between
 //    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
+//  - A warp has a ring of tiles, K's and V's apart, each filled again as soon as it has been read: 12 KB in flight of 16.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
+// Measured (us; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 (1477), 4 of 128K at 32 KV heads 600
+// (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
+// merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 18 (6.5): the longest unit's steps, 1 us each.
 #include "kvp_cache8.cuh"
 #include "kvp_decode_list.cuh"
 
@@ -106,7 +110,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   constexpr int MB = DH / 16;                      // m-blocks of O^T
 
   extern __shared__ __align__(128) uint8_t dsmem[];
-  __shared__ float2 s_o[D8_WARPS - 1][MB * 32];    // four rows of the results that warp 0 merges into its own
+  __shared__ float2 s_o[D8_WARPS - 1][MB * 32];    // four rows of the results that a team's first warp merges into its own
   __shared__ float2 s_ml[D8_WARPS - 1][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
