@@ -338,7 +338,8 @@ int kvp_cache_append_tokens(const kvp_decode_desc* d, const int32_t* donor, int3
 /* kvp_decode over the cache held in 8 bits.  The arguments, groups of layers and rules of num_splits are kvp_decode's, with the
  * scales beside the pools; a workspace of kvp_decode8_workspace_bytes serves every layer range.  Differences: a sequence of
  * length 0 (or below) has output 0 and LSE -infinity, lengths above max_pages*page_size are taken as that; the probabilities
- * are rounded to 11 bits (f16), not 8.  Slots at and behind a sequence's length are not read. */
+ * are rounded to 11 bits (f16), not 8.  Slots at and behind a sequence's length are not read.
+ * Drafted tokens of a sequence are entries of a batch of their own: the same pages, each with the length up to its token. */
 size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor);
 int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q,
                 const void* const* k_cache, const void* const* v_cache, const uint8_t* const* k_scale,

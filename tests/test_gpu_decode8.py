@@ -420,6 +420,20 @@ def test_a_prompt_then_tokens(kvp):
     assert kvp.device_status() == kvp.OK
 
 
+def test_drafted_tokens_as_a_batch(kvp):
+    """Entries that share their pages: each token of a run sees what lies before it, as calls of their own would."""
+    runs, old, Hq, Hkv, dh, page = [4, 1, 3], [30, 100, 13], 8, 2, 128, 16
+    c = Case(kvp, [0, 0], [n + o for n, o in zip(runs, old)], Hq, Hkv, dh, page)
+    of = [b for b, n in enumerate(runs) for _ in range(n)]
+    lens = [o + 1 + i for n, o in zip(runs, old) for i in range(n)]
+    d = Case(kvp, [0, 0], [1] * len(of), Hq, Hkv, dh, page)
+    d.pools, d.scales, d.bt, d.lens = c.pools, c.scales, c.bt[of].contiguous(), lens
+    d.lists = c.lists
+    d.table, d.lengths = d.bt.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    d.desc = kvp.DecodeDesc(2, len(of), Hq, Hkv, dh, page, d.bt.shape[1], c.desc.n_pages)
+    d.check(*d.run())
+
+
 def test_tensors_of_the_host_are_refused(kvp):
     c = Case(kvp, [0], [16, 3], 4, 2, 64, 16)
     o, lse, ws = c.outputs()
