@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   const Dec8Group* f_grp = &p.grp[0];
   const int32_t* bt = nullptr;                     // block-table entry of the page the next step begins in,
   int in_page = 0, f_live = 0;                     // its granule there; tokens of the piece from there on
-  size_t page_block = 0;                           // blocks of 16 tokens before this KV head's of that page
+  int page = 0;                                    // that entry, looked at when its step is asked for: a load ahead of it
   int slot_in = 0, slot_out = 0;                   // in pairs: K's tile and V's behind it
   auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
   auto enter_piece = [&]() {
@@ -257,12 +257,13 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     bt = p.block_table + size_t(f.b) * p.max_pages + col;
     in_page = gran - col * gran_per_page;
     f_live = min(f.seen, (f.gran + n) * GRAN) - gran * GRAN;
-    page_block = block_of(*bt);
+    page = *bt;
   };
   // Scales of the steps in the ring: a lane has the byte of one granule (lane & 3: K's and V's of the first, of the second).
-  uint32_t scales[DEPTH + 1];
+  // (Moved up a step behind the load, or the move would wait for it.)
+  uint32_t scales[DEPTH];
 #pragma unroll
-  for (int s = 0; s <= DEPTH; ++s) scales[s] = 0;
+  for (int s = 0; s < DEPTH; ++s) scales[s] = 0;
   // V's granules of the step whose K was asked for last, and how many tokens of it are to be read (-1: no step)
   const uint8_t *v_src0 = nullptr, *v_src1 = nullptr;
   int v_live = -1;
@@ -290,7 +291,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     }
     v_live = -1;
     if (f_left > 0) {
-      const size_t block0 = page_block + in_page;
+      const size_t block0 = block_of(page) + in_page;
       const bool in_a_row = in_page + 1 < gran_per_page;
       size_t block1 = block0 + 1;
       if (!in_a_row || f_live <= GRAN) block1 = f_live > GRAN ? block_of(bt[1]) : block0;
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           in_page -= gran_per_page;
           ++bt;
         } while (in_page >= gran_per_page);
-        page_block = block_of(*bt);
+        page = *bt;
       }
     }
     cp_async_commit();
@@ -432,10 +433,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
         }
       }
       __syncwarp();                                // every lane has read K
-      issue_k(scales[DEPTH]);
+      const uint32_t scale = scale_byte(scales[0]);
+#pragma unroll
+      for (int s = 0; s + 1 < DEPTH; ++s) scales[s] = scales[s + 1];
+      issue_k(scales[DEPTH - 1]);
       // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
       const int left = tokens - i * STEP;          // visible tokens from this step on
-      const uint32_t scale = scale_byte(scales[0]);
       uint64_t factor[2][NB], x[2][NB][2];         // x - M
       float v_exp[2];
       uint64_t to_v[2][NB];                        // e + M - R
@@ -547,8 +550,6 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           for (int nb = 0; nb < NB; ++nb) mma_f16(oacc[m][nb], a, pb[k][nb][0], pb[k][nb][1]);
         }
       }
-#pragma unroll
-      for (int s = 0; s < DEPTH; ++s) scales[s] = scales[s + 1];
       // (every lane is done with V before it is refilled: the barrier at the top)
     }
     const Cursor here = c;
