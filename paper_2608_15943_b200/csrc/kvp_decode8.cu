@@ -34,11 +34,14 @@ constexpr int D8_CTAS = DH == 128 ? (NB == 1 ? 3 : 2) : NB == 1 ? 4 : 3;
 template <int DH, int NB>
 constexpr int D8_SLOTS = DH == 128 && NB == 2 ? 6 : 4;
 constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight of V in f16; of the one that raises the reference
-// Where whole units are dealt out, two warps take one if there are as many units as blocks that fit, and one takes it alone (nothing is
-// merged) if there are so many times as many.  (us, four warps -> two: 58 sequences of 1 to 700 tokens, 4 KV heads at dh 64, four groups,
-// 1.6 units a block 20.6 -> 18.8; 32 of 200 to 400, two groups, 1.2 units 17.9 -> 15.0; 80 of 1 to 900 at dh 64, 1.1 units 18.1 -> 19.4.
-// Four -> one: 128 of 50 to 400, 8 KV heads, six groups 116 -> 71, 64 of 1 to 64 at dh 64 27.6 -> 12.8; but the 58 above 21 -> 25.)
-constexpr int LONE_UNITS = 2;
+// Where whole units are dealt out, four warps take one if there are fewer than blocks that fit.  From there to as many as warps that fit the
+// length decides: with a limit on the steps of a warp, the smallest (in parts of the longest unit's) that fits the device, a unit gets
+// one, two or four warps.  Above, or with batches larger than LENGTH_WORDS warps look at together, two warps a unit up to
+// LONE_UNITS units a block, then one (nothing is merged).
+// (us, by the number of units alone -> so: 58 sequences of 1 to 700 tokens, 4 KV heads at dh 64, four groups 17.0 -> 13.7; 80 of 1 to 900, 2
+// KV heads 18.6 -> 14.2; at dh 128 25 of 1 to 1000, 8 KV heads, three groups 29.3 -> 23.0; 30 of 600 to 700, 4 KV heads, four groups 21.7 ->
+// 20.8; at dh 64 70 of 100 to 200, nearly as many units as warps, 14.3 -> 14.5.  Four -> one: 128 of 50 to 400, 8 KV heads, six groups 116 -> 71.)
+constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
@@ -129,24 +132,126 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     x.seen = min(max(len, 0), cap);
     x.ng = granules_of(max(x.seen, 1));
   };
-  auto go_to_unit = [&](Cursor& x, int id) {       // (past the last unit: grp >= n_groups)
+  auto set_unit = [&](Cursor& x, int id) {
     x.id = id;
     x.hk = id % p.Hkv;
     x.b = id / p.Hkv % p.B;
     x.grp = id / p.Hkv / p.B;
     x.gran = 0;
+  };
+  auto go_to_unit = [&](Cursor& x, int id) {
+    set_unit(x, id);
     set_length(x, p.lengths[x.b]);
   };
   bool by_units = p.by_units != 0;
   const int units = p.n_groups * p.B * p.Hkv;
   int rest = 0;                                    // places behind the granules of a unit
-  auto find_place = [&](int len0) -> bool {        // from the lengths; false: the block has none
-    int before, all, longest;
-    sum_granules(p, len0, 0, before, all, longest);
-    const long long granules = (long long)all * p.Hkv * p.n_groups;
-    by_units = dealt_by_units(DH, granules, units, longest, p.fit);
-    rest = by_units ? 0 : unit_rest(DH, granules, p.fit);
-    if (by_units) return true;
+  // teams of 4, 2 or 1 warps take the steps of a unit or a piece in turn
+  const int plain_team = units < p.fit ? 2 : units < LONE_UNITS * p.fit ? 1 : 0;
+  int log_team = caller_splits ? 2 : plain_team;
+  const bool by_length = units >= p.fit && units < D8_WARPS * p.fit && p.B <= 32 * LENGTH_WORDS;
+  const bool read_all = p.by_units != 0 && by_length;                // lengths of the whole batch, not of its first 32 sequences
+  const bool read_one = p.by_units != 0 && !by_length && p.B > 32;
+  int len[LENGTH_WORDS] = {};                      // of sequence 32 i + lane
+  auto find_unit = [&]() -> bool {
+    if (by_length && blockIdx.x >= p.fit) return false;   // (no more are needed)
+    if (by_length && !read_all) {
+#pragma unroll
+      for (int i = 1; i < LENGTH_WORDS; ++i) len[i] = 32 * i + lane < p.B ? p.lengths[32 * i + lane] : 0;
+    }
+    auto begin_unit = [&]() {                      // (lengths may have been read early: none may come through L1 before the wait)
+      int mine = 0;
+      if (by_length || p.B <= 32) {
+#pragma unroll
+        for (int i = 0; i < LENGTH_WORDS; ++i) {
+          const int v = __shfl_sync(0xffffffffu, len[i], c.b & 31);
+          if (c.b >> 5 == i) mine = v;
+        }
+      } else {
+        mine = p.lengths[c.b];
+      }
+      set_length(c, mine);
+      todo = c.ng;
+      return true;
+    };
+    if (by_length) {
+      int steps[LENGTH_WORDS], longest = 0;        // of sequence 32 i + lane
+#pragma unroll
+      for (int i = 0; i < LENGTH_WORDS; ++i) {
+        const int b = 32 * i + lane;
+        steps[i] = b < p.B ? (granules_of(clamp_length(p, len[i])) + 1) / 2 : 0;
+        longest = max(longest, steps[i]);
+      }
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      const int per_seq = p.Hkv * p.n_groups;
+      int most = 0, of4 = 0, of2 = 0, of1 = 0;     // steps of a warp, units of each kind of team
+      auto fits = [&](int parts) -> bool {
+        most = (longest * parts + LENGTH_PARTS - 1) / LENGTH_PARTS;
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < LENGTH_WORDS; ++i) n += (steps[i] > 2 * most ? 1u << 16 : 0u) + (steps[i] > most ? 1u : 0u);
+        n = __reduce_add_sync(0xffffffffu, n);
+        of1 = (p.B - int(n & 0xffffu)) * per_seq;
+        of2 = int((n & 0xffffu) - (n >> 16)) * per_seq;
+        of4 = int(n >> 16) * per_seq;
+        return of4 + (of2 + 1) / 2 + (of1 + 3) / 4 <= p.fit;
+      };
+      int parts = LENGTH_PARTS >> (plain_team + 1);
+      while (!fits(parts)) ++parts;                // (ends: twice as many parts are the plain teams, which fit)
+      int u = blockIdx.x, n = of4;                 // the team's unit among those of its kind, the longest first
+      int above = 2 * most, upto = longest;
+      log_team = 2;
+      if (u >= of4) {
+        u = (u - of4) * 2;
+        n = of2;
+        above = most;
+        upto = 2 * most;
+        log_team = 1;
+        if (u >= of2) {
+          u = (u - (of2 + 1) / 2 * 2) * 2;
+          n = of1;
+          above = 0;
+          upto = most;
+          log_team = 0;
+        }
+      }
+      u += warp >> log_team;
+      if (u >= n) return false;
+      int nth = u / per_seq;
+      const int r = u - nth * per_seq;
+#pragma unroll
+      for (int i = 0; i < LENGTH_WORDS; ++i) {
+        const bool is_one = steps[i] > above && steps[i] <= upto;
+        const uint32_t kind = __ballot_sync(0xffffffffu, is_one);
+        const uint32_t hit = __ballot_sync(0xffffffffu, is_one && __popc(kind & ((1u << lane) - 1)) == nth);
+        if (hit != 0u) c.b = 32 * i + __ffs(hit) - 1;
+        nth -= __popc(kind);
+      }
+      c.id = units;                                // no other unit comes behind it
+      c.hk = r % p.Hkv;
+      c.grp = r / p.Hkv;
+      c.gran = 0;
+      return begin_unit();
+    }
+    log_team = plain_team;
+    const int id = (int(blockIdx.x) * D8_WARPS + warp) >> log_team;
+    if (id >= units) return false;
+    set_unit(c, id);
+    return begin_unit();
+  };
+  auto find_place = [&]() -> bool {                // from the lengths; false: the block (or the team) has none
+    const int len0 = len[0];
+    int all = 0;
+    long long granules = 0;
+    if (!p.by_units) {
+      int before, longest;
+      sum_granules(p, len0, 0, before, all, longest);
+      granules = (long long)all * p.Hkv * p.n_groups;
+      by_units = dealt_by_units(DH, granules, units, longest, p.fit);
+      rest = by_units ? 0 : unit_rest(DH, granules, p.fit);
+    }
+    if (by_units) return find_unit();
+    log_team = 2;
     const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
     const int n_shares = shares_for(DH, p.fit, p.max_shares, total);
     if (blockIdx.x >= n_shares) return false;
@@ -181,22 +286,25 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     return true;
   };
   bool placed = true;
-  if (caller_splits || by_units) {
+  if (caller_splits || read_one) {
     grid_dep_wait();
   } else {
-    int len0 = 0;
-    for (bool behind = p.B > 32;; behind = true) {
+    const bool early = (p.B <= 32 || read_all) && blockIdx.x < p.fit;   // (what starts later than that starts behind the wait)
+    for (bool behind = !early;; behind = true) {
       if (behind) grid_dep_wait();
-      const int now = early_length(p);
-      if (behind && p.B <= 32 && __all_sync(0xffffffffu, now == len0)) break;
-      len0 = now;
-      placed = find_place(len0);
+      bool same = true;
+#pragma unroll
+      for (int i = 0; i < LENGTH_WORDS; ++i) {
+        const int b = 32 * i + lane, now = b < p.B && (i == 0 || read_all) ? __ldcg(p.lengths + b) : 0;
+        same = same && now == len[i];
+        len[i] = now;
+      }
+      if (behind && early && __all_sync(0xffffffffu, same)) break;
+      placed = find_place();
       if (behind) break;
     }
   }
   if (!placed) return;
-  // teams of 4, 2 or 1 warps take the steps of a piece in turn
-  const int log_team = !by_units || caller_splits || units < p.fit ? 2 : units < LONE_UNITS * p.fit ? 1 : 0;
   const int team = 1 << log_team, first_step = warp & (team - 1);
   if (caller_splits) {
     const int split = blockIdx.x % p.num_splits;
@@ -204,7 +312,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     const int per = (c.ng + p.num_splits - 1) / p.num_splits;
     c.gran = min(c.ng, split * per);
     todo = min(c.ng - c.gran, per);
-  } else if (by_units) {
+  } else if (read_one) {
     const int id = (int(blockIdx.x) * D8_WARPS + warp) >> log_team;
     if (id >= units) return;
     go_to_unit(c, id);
@@ -676,6 +784,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 DealBy deal8_by(int dh, int rows) {
   return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>)};
 }
+// Blocks for whole units.  (One too many costs: it has to be started before the next kernel's.  34 sequences of 50 to 60 tokens in six groups 11.7 us instead of 8.3.)
+long long blocks_by_units(long long units, int B, int fit) {
+  if (units < fit) return units;
+  if (units < (long long)D8_WARPS * fit && B <= 32 * LENGTH_WORDS) return fit;
+  return units < (long long)LONE_UNITS * fit ? (units + 1) / 2 : (units + D8_WARPS - 1) / D8_WARPS;
+}
 // query rows of the largest group of a call
 int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
   int rows = 0;
@@ -792,11 +906,13 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     const long long units = (long long)n * d->B * d->Hkv;
     // a block for every share of the longest list; shares go by the lengths on the device, and so does whether whole units
     // are dealt out instead
-    const long long blocks = d->num_splits > 0 ? units * d->num_splits
-                                               : std::max((long long)plan.max_shares, std::min(units, (long long)p.fit * max_rounds(by.key)));
-    if (units > 0x3fffffffLL || blocks > 0x3fffffffLL) return KVP_ERR_UNSUPPORTED;
     p.n_groups = n;
     p.by_units = dealt_by_units(by.key, longest_list(d, n), units, longest_unit(d), p.fit);
+    const long long most_blocks = (long long)p.fit * max_rounds(by.key);
+    const long long blocks = d->num_splits > 0 ? units * d->num_splits
+                             : p.by_units      ? std::min(blocks_by_units(units, d->B, p.fit), most_blocks)
+                                               : std::max((long long)plan.max_shares, std::min(units, most_blocks));
+    if (units > 0x3fffffffLL || blocks > 0x3fffffffLL) return KVP_ERR_UNSUPPORTED;
     const long long unit_pieces = d->num_splits > 0 ? d->num_splits : plan.max_shares / units;
     const int wpr = unit_pieces > 8 ? 8 : 1;   // many pieces a unit: eight warps share those of a row
     const int rows_per_block = COMBINE_THREADS / 32 / wpr;

@@ -162,6 +162,31 @@ def test_many_short_sequences(kvp, donor, B, Hq, Hkv, dh, page, most):
     assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
 
 
+BY_LENGTH = [
+    ([0, 1], 32, 8, 8, 128, 16, (1, 700)),                    # between one and two units a block: teams of four, two and one
+    ([0, 1, 2, 3], 31, 16, 16, 64, 32, (0, 300)),             # between two and four
+    ([0, 1], 128, 8, 2, 128, 48, (0, 400)),                   # the longest batch that is looked at whole
+    ([0, 1, 1], 127, 4, 4, 64, 16, (10, 900)),
+    ([0, 1], 129, 8, 2, 128, 16, (0, 200)),                   # and one beyond it
+    ([0, 0, 0, 0], 100, 16, 4, 128, 32, (0, 500)),            # sixteen rows
+    ([0, 1, 2], 50, 8, 4, 128, 16, (200, 200)),               # nobody longer than the others
+    ([0, 1, 2], 50, 8, 4, 64, 16, (0, 0)),
+    ([0, 1, 2, 3], 97, 4, 4, 128, 16, (1, 33)),               # one step or two
+]
+
+
+@pytest.mark.parametrize("columns", [1, 2000])                # with the wide table the lengths alone say that units are short
+@pytest.mark.parametrize("donor,B,Hq,Hkv,dh,page,lens", BY_LENGTH)
+def test_teams_go_by_the_length(kvp, donor, B, Hq, Hkv, dh, page, lens, columns):
+    r = np.random.default_rng(B)
+    lens = [int(x) for x in r.integers(lens[0], lens[1] + 1, B)]
+    c = Case(kvp, donor, lens, Hq, Hkv, dh, page, columns=columns)
+    o, lse = c.run()
+    c.check(o, lse)
+    again, lse2 = c.run()
+    assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
+
+
 def test_values_that_are_not_finite(kvp):
     """NaN among the visible keys of a KV head reaches its queries' outputs and LSE and no others; among the values, its element."""
     c = Case(kvp, [0], [500, 40], 4, 2, 128, 16, poison=False)
@@ -339,6 +364,29 @@ def test_lengths_written_by_the_kernel_ahead(kvp):
             assert ((o[0].double() - ro).abs() <= to).all()
             some = torch.isfinite(rl)
             assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("B,Hkv", [(30, 16), (100, 8)])
+def test_lengths_written_ahead_of_teams(kvp, B, Hkv):
+    """The same where the lengths of the whole batch say which team a unit gets."""
+    r = np.random.default_rng(B)
+    first, second = ([int(x) for x in r.integers(0, 350, B)] for _ in range(2))
+    second[0], first[-1] = 700, 650
+    c = Case(kvp, [0], [max(a, b) for a, b in zip(first, second)], Hkv, Hkv, 128, 16, poison=False)
+    want = [exact(c.q[0], c.pools, c.scales, c.bt, lens, 16, 128 ** -0.5, 0) for lens in (first, second)]
+    on_device = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (first, second)]
+    runs = [c.outputs() for _ in range(8)]
+    big = torch.zeros(64 << 20, device="cuda")
+    for i, (o, lse, ws) in enumerate(runs):
+        big.add_(1.0)
+        c.lengths.copy_(on_device[i % 2])
+        kvp.decode8(c.desc, c.donor, c.q, *c.lists, c.table, c.lengths, o, lse, ws)
+    torch.cuda.synchronize()
+    for i, (o, lse, _) in enumerate(runs):
+        ro, rl, to, tl = want[i % 2]
+        assert ((o[0].double() - ro).abs() <= to).all()
+        some = torch.isfinite(rl)
+        assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all()
 
 
 def test_beyond_32_bits(kvp):
