@@ -585,7 +585,7 @@ cudaError_t launch_append(const AppendParams<MAX_DEC_GROUPS>& all, int n, cudaSt
   return launch_kernel(append_kernel<NG>, dim3(all.B, n), 128, 0, stream, 1, p);
 }
 
-DealBy deal_by(int dh) { return {dh, sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>)}; }
+DealBy deal_by(int dh) { return {dh, sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>), max_rounds(dh)}; }
 
 int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                 const void* const* v_cache, const int32_t* block_table, const int32_t* lengths, void* const* o,

@@ -19,6 +19,8 @@
 // Measured (us; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 (1477), 4 of 128K at 32 KV heads 600
 // (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
 // merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 18 (6.5): the longest unit's steps, 1 us each.
+#include <type_traits>
+
 #include "kvp_cache8.cuh"
 #include "kvp_decode_list.cuh"
 
@@ -44,6 +46,42 @@ constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight 
 constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
+
+// Shares of the list: up to five a block that fits, as kvp_deal.h cuts them.  Where that would be more, up to FINEST, the blocks that fit
+// get a large one each first, and then as many of the size that all would have had (SMALL_ROUNDS a block) as even out when
+// they end: fewer blocks are started, and a table far wider than the lengths leaves fewer without work.
+// (us, all alike, up to sixteen -> so: 4 of 128K at 32 KV heads 595 -> 581, 32 of 16K-32K in six groups 1378 -> 1371; in a table for 32000 tokens
+// 16 of 2000 to 5000 in two groups 48.1 -> 44.6, 34 of 50 to 60 in six 28.2 -> 17.9.)
+constexpr int SMALL_ROUNDS = 4, FINEST = max_rounds(128);
+static_assert(SMALL_ROUNDS + 1 == max_rounds(64), "rounds of either head size");
+struct LargeFirst {
+  Dealt head;                                      // shares ahead of the small ones, or all
+  long long in_head;                               // places there
+  uint32_t n_head, small;
+  static __device__ __forceinline__ int rounds(const DecSizes& p, long long total) {
+    return int(max(1LL, min((long long)FINEST, div_places(total, (long long)p.fit * long_share(128)))));
+  }
+  static __device__ __forceinline__ int shares(const DecSizes& p, long long total) {
+    long long n = total / MIN_SHARE;
+    if (n > p.fit) n = (long long)p.fit * min(rounds(p, total), SMALL_ROUNDS + 1);
+    return int(max(1LL, min(n, (long long)p.max_shares)));
+  }
+  __device__ __forceinline__ LargeFirst(const DecSizes& p, long long total, int n) : head(total, n), in_head(total), n_head(n), small(0) {
+    if (n != (SMALL_ROUNDS + 1) * p.fit) return;
+    const int r = rounds(p, total);
+    if (r <= SMALL_ROUNDS + 1) return;
+    small = uint32_t(div_places(total, (long long)p.fit * r));
+    n_head = p.fit;
+    in_head = total - (long long)SMALL_ROUNDS * p.fit * small;
+    head = Dealt(in_head, n_head);
+  }
+  __device__ __forceinline__ long long begin(uint32_t i) const { return i < n_head ? head.begin(i) : in_head + (long long)(i - n_head) * small; }
+  __device__ __forceinline__ uint32_t size(uint32_t i) const { return i < n_head ? head.size(i) : small; }
+  __device__ __forceinline__ int share_of(long long g) const { return g < in_head ? head.share_of(g) : int(n_head + div_places(g - in_head, small)); }
+};
+// (at dh 64 five a block are as many as there may be, and all alike are as fast)
+template <int DH>
+using Deal8 = std::conditional_t<DH == 128, LargeFirst, EvenDeal<DH>>;
 
 struct Dec8Group {
   const uint8_t *k_cache, *v_cache;               // [n_pages][Hkv][page_size][dh] e4m3
@@ -253,9 +291,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     if (by_units) return find_unit();
     log_team = 2;
     const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
-    const int n_shares = shares_for(DH, p.fit, p.max_shares, total);
+    const int n_shares = Deal8<DH>::shares(p, total);
     if (blockIdx.x >= n_shares) return false;
-    const Dealt dealt(total, n_shares);
+    const Deal8<DH> dealt(p, total, n_shares);
     long long at = dealt.begin(blockIdx.x);
     todo = int(dealt.size(blockIdx.x));
     c.id = 0;
@@ -782,7 +820,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 }
 
 DealBy deal8_by(int dh, int rows) {
-  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>)};
+  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>), SMALL_ROUNDS + 1};
 }
 // Blocks for whole units.  (One too many costs: it has to be started before the next kernel's.  34 sequences of 50 to 60 tokens in six groups 11.7 us instead of 8.3.)
 long long blocks_by_units(long long units, int B, int fit) {
@@ -809,7 +847,7 @@ cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim
   e = launch_kernel(decode8_kernel<DH, NB, NG>, grid, D8_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
-    e = launch_kernel(decode_combine_kernel<DH, DH, true, Dec8Params<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+    e = launch_kernel(decode_combine_kernel<DH, DH, true, Dec8Params<NG>, Deal8<DH>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 template <int DH, int NB>
@@ -908,7 +946,7 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     // are dealt out instead
     p.n_groups = n;
     p.by_units = dealt_by_units(by.key, longest_list(d, n), units, longest_unit(d), p.fit);
-    const long long most_blocks = (long long)p.fit * max_rounds(by.key);
+    const long long most_blocks = (long long)p.fit * by.rounds;
     const long long blocks = d->num_splits > 0 ? units * d->num_splits
                              : p.by_units      ? std::min(blocks_by_units(units, d->B, p.fit), most_blocks)
                                                : std::max((long long)plan.max_shares, std::min(units, most_blocks));

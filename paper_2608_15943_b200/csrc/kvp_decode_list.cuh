@@ -96,13 +96,20 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return fmaf(s, hi, fmaf(s, lo, low * hi));
 }
 
+// All shares alike
+template <int KEY>
+struct EvenDeal : Dealt {
+  static __device__ __forceinline__ int shares(const DecSizes& p, long long total) { return shares_for(KEY, p.fit, p.max_shares, total); }
+  __device__ __forceinline__ EvenDeal(const DecSizes&, long long total, int n) : Dealt(total, n) {}
+};
+
 // Merges the pieces of the units that more than one share holds and writes bf16 outputs and LSE.  Eight warps per block;
 // `wpr` of them share a row of a unit (one where a unit has few pieces, eight where it has many), each lane four
 // columns.  Bound: latency; the pieces are in L2.
 constexpr int COMBINE_THREADS = 256;
 // KEY: the head size that the rules of kvp_deal.h are asked for (they go by the bytes of a granule).  EMPTY: there may be units
 // without a token, whose pieces have no sum: output 0, LSE -infinity.
-template <int DH, int KEY, bool EMPTY, typename Params>
+template <int DH, int KEY, bool EMPTY, typename Params, typename Deal = EvenDeal<KEY>>
 __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const __grid_constant__ Params p, int wpr) {
   constexpr int LANES = DH / 4;               // lanes per piece and row
   constexpr int PER_WARP = 32 / LANES;        // pieces a warp takes at a time
@@ -138,9 +145,9 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
         const int len = b < 32 ? __shfl_sync(0xffffffffu, len0, b) : p.lengths[b];
         const int rest = unit_rest(KEY, granules, p.fit), ng = granules_of(clamp_length(p, len));
         const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
-        const int n = shares_for(KEY, p.fit, p.max_shares, total);
+        const int n = Deal::shares(p, total);
         const long long first = gi * per_group + ((long long)before + (long long)b * rest) * p.Hkv + (long long)hk * (ng + rest);
-        const Dealt dealt(total, n);
+        const Deal dealt(p, total, n);
         w0 = dealt.share_of(first);
         w1 = dealt.share_of(first + ng - 1);
       }
@@ -276,6 +283,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 struct DealBy {
   int key;   // head size that the rules are asked for
   int fit;   // blocks that fit on the device
+  int rounds;   // shares at most, in as many
 };
 inline size_t piece_bytes(const kvp_decode_desc* d, size_t pieces, int rows) {
   return align256(pieces * rows * d->dh * 4) + align256(pieces * rows * 2 * 4);
@@ -292,7 +300,7 @@ inline Scratch plan_scratch(const kvp_decode_desc* d, const SubGroup* subs, int 
   const int per_launch = n_sub < MAX_DEC_GROUPS ? n_sub : MAX_DEC_GROUPS;
   for (int i = 0; i < n_sub; ++i) s.rows = std::max(s.rows, subs[i].n * (d->Hq / d->Hkv));
   const long long longest = longest_list(d, per_launch);
-  s.max_shares = shares_for(by.key, by.fit, by.fit * max_rounds(by.key), longest + (long long)per_launch * d->B * d->Hkv * unit_rest(by.key, longest, by.fit));
+  s.max_shares = shares_for(by.key, by.fit, by.fit * by.rounds, longest + (long long)per_launch * d->B * d->Hkv * unit_rest(by.key, longest, by.fit));
   for (;;) {
     s.pieces = d->num_splits > 0 ? size_t(per_launch) * d->B * d->Hkv * d->num_splits : size_t(s.max_shares) * 2;
     s.bytes = piece_bytes(d, s.pieces, s.rows);

@@ -389,6 +389,15 @@ def test_lengths_written_ahead_of_teams(kvp, B, Hkv):
         assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all()
 
 
+def test_shares_of_two_sizes(kvp):
+    """A list of more than six shares of 160 granules a block: large ones first, and small ones behind them."""
+    c = Case(kvp, [0, 1, 2, 3], [28500 + 37 * b for b in range(8)] + [1, 0, 700], 8, 8, 128, 128)
+    o, lse = c.run()
+    c.check(o, lse)
+    again, lse2 = c.run()
+    assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
+
+
 def test_beyond_32_bits(kvp):
     """A pool of more than 2^32 numbers: the last pages are found."""
     if torch.cuda.mem_get_info()[0] < 24 << 30:
