@@ -16,9 +16,10 @@
 //    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
 //  - A warp has a ring of tiles, K's and V's apart, each filled again as soon as it has been read: 12 KB in flight of 16.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
-// Measured (us; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 (1477), 4 of 128K at 32 KV heads 600
-// (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
-// merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 18 (6.5): the longest unit's steps, 1 us each.
+// Measured (us; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1380 to 1450 by the board (1477), 4 of 128K at
+// 32 KV heads 580 to 600 (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
+// merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 14 (6.5): the steps of
+// a warp, nearly 1 us each.
 #include <type_traits>
 
 #include "kvp_cache8.cuh"
@@ -47,41 +48,47 @@ constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 
-// Shares of the list: up to five a block that fits, as kvp_deal.h cuts them.  Where that would be more, up to FINEST, the blocks that fit
-// get a large one each first, and then as many of the size that all would have had (SMALL_ROUNDS a block) as even out when
-// they end: fewer blocks are started, and a table far wider than the lengths leaves fewer without work.
-// (us, all alike, up to sixteen -> so: 4 of 128K at 32 KV heads 595 -> 581, 32 of 16K-32K in six groups 1378 -> 1371; in a table for 32000 tokens
-// 16 of 2000 to 5000 in two groups 48.1 -> 44.6, 34 of 50 to 60 in six 28.2 -> 17.9.)
-constexpr int SMALL_ROUNDS = 4, FINEST = max_rounds(128);
-static_assert(SMALL_ROUNDS + 1 == max_rounds(64), "rounds of either head size");
+// Shares of the list at dh 128.  Rounds: how often the blocks that fit could have shares of long_share places.  Below LARGE_FROM, as many
+// shares a block, all alike.  From there on a block gets a large one first, and then come small ones that even out when the blocks end:
+// one an eighth of a block's part, or, in long lists, two a sixteenth of it.  Few blocks are started that way, and a table far
+// wider than the lengths leaves few without work.
+// (us, up to sixteen shares a block, all alike -> so: 64 of 2000 to 20000, 8 KV heads, one group 235 -> 232; the same in five alike 245; 16 rows, 64 of
+// 8000 to 16000 344 in one large and four small -> 321; 32 of 16K-32K in six groups 1380 to 1440, with the eighth 1462, with two sixteenths 1415 where
+// four gave 1420.
+// In a table for 32000 tokens: 16 of 2000 to 5000 in two groups 48.1 -> 43.7, 34 of 50 to 60 in six 28.2 -> 18 to 21.)
+constexpr int LARGE_FROM = 3, LONG_FROM = 12;
 struct LargeFirst {
   Dealt head;                                      // shares ahead of the small ones, or all
   long long in_head;                               // places there
   uint32_t n_head, small;
   static __device__ __forceinline__ int rounds(const DecSizes& p, long long total) {
-    return int(max(1LL, min((long long)FINEST, div_places(total, (long long)p.fit * long_share(128)))));
+    return int(max(1LL, min((long long)LONG_FROM, div_places(total, (long long)p.fit * long_share(128)))));
   }
+  static __device__ __forceinline__ int small_ones(int rounds) { return rounds < LARGE_FROM ? 0 : rounds < LONG_FROM ? 1 : 2; }
   static __device__ __forceinline__ int shares(const DecSizes& p, long long total) {
     long long n = total / MIN_SHARE;
-    if (n > p.fit) n = (long long)p.fit * min(rounds(p, total), SMALL_ROUNDS + 1);
+    if (n > p.fit) {
+      const int r = rounds(p, total);
+      n = (long long)p.fit * (r < LARGE_FROM ? r : 1 + small_ones(r));
+    }
     return int(max(1LL, min(n, (long long)p.max_shares)));
   }
   __device__ __forceinline__ LargeFirst(const DecSizes& p, long long total, int n) : head(total, n), in_head(total), n_head(n), small(0) {
-    if (n != (SMALL_ROUNDS + 1) * p.fit) return;
-    const int r = rounds(p, total);
-    if (r <= SMALL_ROUNDS + 1) return;
-    small = uint32_t(div_places(total, (long long)p.fit * r));
+    if (n <= p.fit) return;
+    const int s = small_ones(rounds(p, total));
+    if (s == 0) return;
+    small = uint32_t(div_places(total, 8LL * s * p.fit));
     n_head = p.fit;
-    in_head = total - (long long)SMALL_ROUNDS * p.fit * small;
+    in_head = total - (long long)s * p.fit * small;
     head = Dealt(in_head, n_head);
   }
   __device__ __forceinline__ long long begin(uint32_t i) const { return i < n_head ? head.begin(i) : in_head + (long long)(i - n_head) * small; }
   __device__ __forceinline__ uint32_t size(uint32_t i) const { return i < n_head ? head.size(i) : small; }
   __device__ __forceinline__ int share_of(long long g) const { return g < in_head ? head.share_of(g) : int(n_head + div_places(g - in_head, small)); }
 };
-// (at dh 64 five a block are as many as there may be, and all alike are as fast)
 template <int DH>
 using Deal8 = std::conditional_t<DH == 128, LargeFirst, EvenDeal<DH>>;
+constexpr int most_rounds(int dh) { return dh == 128 ? 3 : max_rounds(dh); }
 
 struct Dec8Group {
   const uint8_t *k_cache, *v_cache;               // [n_pages][Hkv][page_size][dh] e4m3
@@ -820,7 +827,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 }
 
 DealBy deal8_by(int dh, int rows) {
-  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>), SMALL_ROUNDS + 1};
+  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>), most_rounds(dh)};
 }
 // Blocks for whole units.  (One too many costs: it has to be started before the next kernel's.  34 sequences of 50 to 60 tokens in six groups 11.7 us instead of 8.3.)
 long long blocks_by_units(long long units, int B, int fit) {

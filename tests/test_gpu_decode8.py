@@ -389,9 +389,13 @@ def test_lengths_written_ahead_of_teams(kvp, B, Hkv):
         assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all()
 
 
-def test_shares_of_two_sizes(kvp):
-    """A list of more than six shares of 160 granules a block: large ones first, and small ones behind them."""
-    c = Case(kvp, [0, 1, 2, 3], [28500 + 37 * b for b in range(8)] + [1, 0, 700], 8, 8, 128, 128)
+@pytest.mark.parametrize("donor,Hkv,lens", [
+    ([0, 1, 2, 3], 8, [28500 + 37 * b for b in range(8)] + [1, 0, 700]),          # one small share a block behind the large one
+    ([0, 1, 2, 3], 16, [28500 + 37 * b for b in range(8)] + [1, 0, 700]),         # two
+])
+def test_shares_of_two_sizes(kvp, donor, Hkv, lens):
+    """Lists of six and twelve shares of 160 granules a block: large ones first, and small ones behind them."""
+    c = Case(kvp, donor, lens, Hkv, Hkv, 128, 128)
     o, lse = c.run()
     c.check(o, lse)
     again, lse2 = c.run()
