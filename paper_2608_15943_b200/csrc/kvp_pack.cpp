@@ -518,7 +518,7 @@ ENTRY(cache_append_tokens) {   // desc, donor, k_new, v_new, k_cache, v_cache, b
     int64_t T = 0;
     if (r.ok && r.left > 0 && PyList_CheckExact(*r.a) && PyList_GET_SIZE(*r.a) > 0 && THPVariable_CheckExact(PyList_GET_ITEM(*r.a, 0))) {
       const at::Tensor& k0 = THPVariable_Unpack(PyList_GET_ITEM(*r.a, 0));
-      r.ok = k0.dim() > 0 && k0.size(0) <= INT32_MAX;
+      r.ok = k0.dim() > 0 && k0.size(0) > 0 && k0.size(0) <= INT32_MAX;   // (no rows, or missing ones: kvp.py's to tell)
       T = r.ok ? k0.size(0) : 0;
     } else {
       r.ok = false;

@@ -592,6 +592,8 @@ def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table
     for what, t, numel in (("block_table", block_table, desc.B * desc.max_pages), ("lengths", lengths, desc.B), ("first", first, desc.B + 1)):
         if t is not None:
             _fit(what, t, _I32, numel, device)
+    if T == 0 and any(l >= len(ts) or ts[l] is None for ts in (k_new, v_new) for l in owners):
+        T = -1     # for the library to refuse: by their addresses it cannot tell missing rows from none
     d, n = _map(desc, donor)
     array = lambda ts: None if ts is None else _ptr_array(ts, n)
     _check(lib.kvp_cache_append_tokens(C.byref(desc), d, T, _ptr(first), float(theta), array(q), array(q_out), array(k_new), array(v_new),

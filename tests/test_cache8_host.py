@@ -277,3 +277,18 @@ def test_both_paths_hand_over_the_same(monkeypatch):
         assert len(seen) == 2
     finally:
         real.bind_cache(original)
+
+
+@pytest.mark.parametrize("bits8", [True, False])
+def test_owners_without_rows_are_refused(kvp, bits8):
+    """Runs of tokens whose rows are missing or are None: no number of tokens can be read off them, and nothing would be stored."""
+    runs = dict(T=5, first=torch.tensor([0, 2, 5], dtype=torch.int32), q=None, q_out=None, bits8=bits8)
+    none = torch.zeros(0, 2, 64, dtype=torch.bfloat16)
+    for over in (dict(k_new=[None], v_new=[None]), dict(k_new=[], v_new=[]), dict(k_new=[None, None]), dict(v_new=[None, None], k_new=[none, None]),
+                 dict(k_new=[None, none], v_new=[none, none]), dict(donor=(0, 1), k_new=[none, None], v_new=[none, none], k_cache=None, v_cache=None)):
+        if "k_cache" in over:                                 # an owner above the first one
+            pool = torch.zeros(7, 2, 16, 64, dtype=torch.uint8 if bits8 else torch.bfloat16)
+            scale = torch.zeros(7, 2, 1, dtype=torch.uint8)
+            over.update(k_cache=[pool] * 2, v_cache=[pool] * 2, k_scale=[scale] * 2 if bits8 else None, v_scale=[scale] * 2 if bits8 else None)
+        refused(kvp, tokens_call(kvp, **(runs | over)), kvp.ERR_INVALID_ARG)
+    tokens_call(kvp, **(runs | dict(k_new=[none, None], v_new=[none, None])))()      # rows there are, none of them: nothing to do
