@@ -581,6 +581,8 @@ def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table
         return _check(status, "kvp_cache_append_tokens")
     layers, owners = _layer_range(desc, donor)
     T = next((int(t.shape[0]) if t.dim() else 0 for t in k_new if t is not None), 0)
+    if T == 0 and any(l >= len(ts) or ts[l] is None for ts in (k_new, v_new) for l in owners):
+        _check(ERR_INVALID_ARG, "kvp_cache_append_tokens")     # (by their addresses the library cannot tell missing rows from none)
     rows, io = desc.n_pages * desc.Hkv * desc.page_size, _io(desc)
     held = (torch.bfloat16,) if k_scale is None else _CODES
     for what, ts, dtypes, numel, of in (("k_new", k_new, io, T * desc.Hkv * desc.dh, owners), ("v_new", v_new, io, T * desc.Hkv * desc.dh, owners),
@@ -592,8 +594,6 @@ def cache_append_tokens(desc, donor, k_new, v_new, k_cache, v_cache, block_table
     for what, t, numel in (("block_table", block_table, desc.B * desc.max_pages), ("lengths", lengths, desc.B), ("first", first, desc.B + 1)):
         if t is not None:
             _fit(what, t, _I32, numel, device)
-    if T == 0 and any(l >= len(ts) or ts[l] is None for ts in (k_new, v_new) for l in owners):
-        T = -1     # for the library to refuse: by their addresses it cannot tell missing rows from none
     d, n = _map(desc, donor)
     array = lambda ts: None if ts is None else _ptr_array(ts, n)
     _check(lib.kvp_cache_append_tokens(C.byref(desc), d, T, _ptr(first), float(theta), array(q), array(q_out), array(k_new), array(v_new),
