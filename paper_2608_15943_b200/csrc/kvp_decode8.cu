@@ -47,6 +47,10 @@ constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight 
 constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
+// From this power of V (and of how far M lags the largest score) on the results of a unit or a piece are held against a higher M: the sum
+// of up to 2^SUM_TOP a term times V would leave fp32 where V is 2^112 and more.  With sums below 2^-16 it stays below the largest of V,
+// 2^16 pieces merged.  (Below it 2^64 times the accumulators, at most 2^23 a token, are far from the end.)
+constexpr float LARGE_V = 64.f;
 
 // Shares of the list at dh 128.  Rounds: how often the blocks that fit could have shares of long_share places.  Below LARGE_FROM, as many
 // shares a block, all alike.  From there on a block gets a large one first, and then come small ones that even out when the blocks end:
@@ -720,7 +724,14 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
         sum[nb][h] = h ? f2_hi(sum2[nb]) : f2_lo(sum2[nb]);
 #pragma unroll
         for (int s = 4; s < 32; s <<= 1) sum[nb][h] += __shfl_xor_sync(0xffffffffu, sum[nb][h], s);
-        const float to_m = fast_exp2(fminf(Rf[nb][h] - 127.f - M[nb][h], 126.f));
+        float up = Rf[nb][h] - 127.f - M[nb][h];
+        if (up > LARGE_V) {                        // M rises until the sum is below 2^-16
+          const int raise = int(__float_as_uint(sum[nb][h]) >> 23) - (127 - 17);
+          sum[nb][h] *= __uint_as_float(power_bits(-raise));
+          M[nb][h] += float(raise);
+          up -= float(raise);
+        }
+        const float to_m = fast_exp2(fminf(up, 126.f));
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           oacc[m][nb][h] *= to_m;

@@ -503,3 +503,27 @@ def test_tensors_of_the_host_are_refused(kvp):
         args[at] = x
         with pytest.raises(ValueError):
             kvp.decode8(c.desc, c.donor, *args)
+
+
+@pytest.mark.parametrize("splits", [0, 5])
+@pytest.mark.parametrize("byte", [60, 190, 230, 243, 244, 245, 246])
+@pytest.mark.parametrize("dh,lens", [(64, [40, 3]), (128, [40, 1000]), (128, [20000, 33]), (64, [700] * 20)])
+def test_large_values_behind_rising_scores(kvp, dh, lens, byte, splits):
+    """V up to the end of bf16's range (256 * 2^119 = 2^127), scores that rise by less than the sum's reference allows (12 in the
+    exponent of e, 2^17.3, in steps of at most 2^6) and many terms alike: the sum times V is far beyond fp32, the output, the value itself, is not.
+    (bf16's half step, the weights' half step of 11 bits, fp32 sums.)"""
+    c = Case(kvp, [0], lens, 4, 1, dh, 16, splits=splits)
+    q = c.q[0]
+    q[:] = q[:1, :1]
+    unit = q[0, 0].float() * (dh ** 0.5 / q[0, 0].float().pow(2).sum())
+    c.scales[0][0].fill_(127)
+    c.pools[1][0].copy_(torch.full(c.pools[1][0].shape, 256.0).to(torch.float8_e4m3fn))
+    c.scales[1][0].fill_(byte)
+    for b, n in enumerate(lens):
+        for i in range((n + 15) // 16):                       # 0, 4, 8, 12, 12, ... a block
+            c.pools[0][0][int(c.bt[b, i])] = (unit * 4.0 * min(i, 3)).to(torch.float8_e4m3fn)
+    o, lse = c.run()
+    want = 256.0 * 2.0 ** (byte - 127)
+    assert ((o[0].double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -13)).all()
+    ro, rl, to, tl = exact(q, c.pools, c.scales, c.bt, lens, 16, dh ** -0.5, 0)
+    assert ((lse[0].double() - rl).abs() <= tl).all()
