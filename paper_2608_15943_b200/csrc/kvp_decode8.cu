@@ -11,8 +11,8 @@
 //    rows of S^T are matched to those tokens.
 //  - Queries are scaled by a power of two a row into f16's range (the largest to 2^14): exact for all bf16 elements down to 2^-31 of
 //    the row's largest, and rounded by at most 2^-39 of it below.  The scale of K joins the factor of the scores.
-//  - The scale of V is a power of two: P is multiplied by 2^(e + M - R) with a reference R of the accumulators beside the
-//    reference M of the sum.  Both rise only when a value would leave f16's upper range, so that no maximum is exchanged between
+//  - The scale of V is a power of two: P is multiplied by 2^(e - D) with a reference M + D of the accumulators beside the
+//    reference M of the sum (D is of the powers' size, whatever M is).  Both rise only when a value would leave f16's upper range, so that no maximum is exchanged between
 //    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
 //  - A warp has a ring of tiles, K's and V's apart, each filled again as soon as it has been read: 12 KB in flight of 16.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
@@ -20,6 +20,8 @@
 // 32 KV heads 580 to 600 (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
 // merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 14 (6.5): the steps of
 // a warp, nearly 1 us each.
+#include <float.h>
+
 #include <type_traits>
 
 #include "kvp_cache8.cuh"
@@ -47,6 +49,9 @@ constexpr float P_TOP = 14.f, P_NEW = 8.f;        // log2 of the largest weight 
 constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
+// Beyond this |M| a score is rounded before M comes off it, as the one that became M was: equal scores are then equal terms, and the largest is
+// 2^0.  (A fused product would be off from M by up to 2^-24 |M|, which has to stay far below the reserve of f16's range; below it is the more exact.)
+constexpr float FAR = 65536.f;
 // From this power of V (and of how far M lags the largest score) on the results of a unit or a piece are held against a higher M: the sum
 // of up to 2^SUM_TOP a term times V would leave fp32 where V is 2^112 and more.  With sums below 2^-16 it stays below the largest of V,
 // 2^16 pieces merged.  (Below it 2^64 times the accumulators, at most 2^23 a token, are far from the end.)
@@ -551,13 +556,14 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     for (int m = 0; m < MB; ++m)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) oacc[m][nb][0] = oacc[m][nb][1] = oacc[m][nb][2] = oacc[m][nb][3] = 0.f;
-    float M[NB][2], Rf[NB][2];                     // of rows 8 nb + 2 t + h: reference of the sum, reference of oacc (exponents as bytes)
-    uint64_t sum2[NB], minus_M[NB], M_to_R[NB];    // sums of this lane's terms, -M and M - R, both rows of the lane side by side
+    // of rows 8 nb + 2 t and the next, side by side: sums of this lane's terms; -M, M the reference of the sum; -D, M + D that of oacc
+    // (exponents as bytes)
+    uint64_t sum2[NB], minus_M[NB], minus_D[NB];
+    bool far = false;                              // some |M| is beyond FAR
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      M[nb][0] = M[nb][1] = Rf[nb][0] = Rf[nb][1] = -1e30f;   // (finite: below every score, and no infinity minus infinity)
-      sum2[nb] = M_to_R[nb] = 0;
-      minus_M[nb] = pack_f2(1e30f, 1e30f);
+      sum2[nb] = 0;
+      minus_M[nb] = minus_D[nb] = pack_f2(FLT_MAX, FLT_MAX);   // (no finite score is below M, and no infinity comes off an infinity)
     }
 
     const int tokens = min(c.seen, (c.gran + n_here) * GRAN) - c.gran * GRAN;   // that the piece sees (0: none)
@@ -594,11 +600,11 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 #pragma unroll
       for (int s = 0; s + 1 < DEPTH; ++s) scales[s] = scales[s + 1];
       issue_k(scales[DEPTH - 1]);
-      // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e + M - R) ----
+      // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e - D) ----
       const int left = tokens - i * STEP;          // visible tokens from this step on
       uint64_t factor[2][NB], x[2][NB][2];         // x - M
       float v_exp[2];
-      uint64_t to_v[2][NB];                        // e + M - R
+      uint64_t to_v[2][NB];                        // e - D
       bool over = false;
       auto scores = [&]() {
 #pragma unroll
@@ -607,8 +613,16 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) x[m][nb][u] = ffma2(pack_f2(s2[m][nb][0][2 * u], s2[m][nb][0][2 * u + 1]), factor[m][nb], minus_M[nb]);
-            to_v[m][nb] = fadd2(pack_f2(v_exp[m], v_exp[m]), M_to_R[nb]);
+            to_v[m][nb] = fadd2(pack_f2(v_exp[m], v_exp[m]), minus_D[nb]);
           }
+        if (far) {
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) x[m][nb][u] = fadd2(fmul2(pack_f2(s2[m][nb][0][2 * u], s2[m][nb][0][2 * u + 1]), factor[m][nb]), minus_M[nb]);
+        }
         if (left < STEP) {
 #pragma unroll
           for (int m = 0; m < 2; ++m)
@@ -641,6 +655,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
+          float M[2] = {-f2_lo(minus_M[nb]), -f2_hi(minus_M[nb])}, D[2] = {-f2_lo(minus_D[nb]), -f2_hi(minus_D[nb])};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float y[2];                            // largest score of each granule
@@ -651,20 +666,22 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
               for (int u = 0; u < 2; ++u)
                 if (m * GRAN + tok_g + 2 * u < left) y[m] = fmaxf(y[m], s2[m][nb][0][2 * u + h] * (h ? f2_hi(factor[m][nb]) : f2_lo(factor[m][nb])));
             }
-            float most = fmaxf(y[0], y[1]), top = fmaxf(y[0] + v_exp[0], y[1] + v_exp[1]);
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
-              most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+              y[0] = fmaxf(y[0], __shfl_xor_sync(0xffffffffu, y[0], s));
+              y[1] = fmaxf(y[1], __shfl_xor_sync(0xffffffffu, y[1], s));
             }
-            if (most > M[nb][h] + SUM_TOP) {
-              const float factor_s = fast_exp2(M[nb][h] - most);
+            const float most = fmaxf(y[0], y[1]);
+            if (most > M[h] + SUM_TOP) {
+              const float rise = most - M[h], factor_s = fast_exp2(-rise);
               sum2[nb] = h ? pack_f2(f2_lo(sum2[nb]), f2_hi(sum2[nb]) * factor_s) : pack_f2(f2_lo(sum2[nb]) * factor_s, f2_hi(sum2[nb]));
-              M[nb][h] = most;
+              M[h] = most;
+              D[h] -= rise;                      // (M + D as it was)
             }
-            if (top > Rf[nb][h] + P_TOP) {
-              const float to = top - P_NEW, factor_o = fast_exp2(Rf[nb][h] - to);
-              Rf[nb][h] = to;
+            const float top = fmaxf(y[0] - M[h] + v_exp[0], y[1] - M[h] + v_exp[1]);
+            if (top > D[h] + P_TOP) {
+              const float to = top - P_NEW, factor_o = fast_exp2(D[h] - to);
+              D[h] = to;
 #pragma unroll
               for (int m = 0; m < MB; ++m) {
                 oacc[m][nb][h] *= factor_o;
@@ -672,9 +689,11 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
               }
             }
           }
-          minus_M[nb] = pack_f2(-M[nb][0], -M[nb][1]);
-          M_to_R[nb] = pack_f2(M[nb][0] - Rf[nb][0], M[nb][1] - Rf[nb][1]);
+          minus_M[nb] = pack_f2(-M[0], -M[1]);
+          minus_D[nb] = pack_f2(-D[0], -D[1]);
+          far = far || fmaxf(fabsf(M[0]), fabsf(M[1])) > FAR;
         }
+        far = __any_sync(0xffffffffu, far);
         scores();
       }
       uint32_t pb[2][NB][2];
@@ -716,15 +735,16 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     else load_queries();
 
     // ---- everything against M; no term at all: M = -infinity ----
-    float sum[NB][2];
+    float sum[NB][2], M[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        M[nb][h] = h ? -f2_hi(minus_M[nb]) : -f2_lo(minus_M[nb]);
         sum[nb][h] = h ? f2_hi(sum2[nb]) : f2_lo(sum2[nb]);
 #pragma unroll
         for (int s = 4; s < 32; s <<= 1) sum[nb][h] += __shfl_xor_sync(0xffffffffu, sum[nb][h], s);
-        float up = Rf[nb][h] - 127.f - M[nb][h];
+        float up = -127.f - (h ? f2_hi(minus_D[nb]) : f2_lo(minus_D[nb]));
         if (up > LARGE_V) {                        // M rises until the sum is below 2^-16
           const int raise = int(__float_as_uint(sum[nb][h]) >> 23) - (127 - 17);
           sum[nb][h] *= __uint_as_float(power_bits(-raise));

@@ -527,3 +527,35 @@ def test_large_values_behind_rising_scores(kvp, dh, lens, byte, splits):
     assert ((o[0].double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -13)).all()
     ro, rl, to, tl = exact(q, c.pools, c.scales, c.bt, lens, 16, dh ** -0.5, 0)
     assert ((lse[0].double() - rl).abs() <= tl).all()
+
+
+@pytest.mark.parametrize("splits", [0, 4])
+@pytest.mark.parametrize("dh,lens", [(64, [40, 3, 0]), (128, [40, 1000]), (128, [20000]), (64, [150] * 20)])
+@pytest.mark.parametrize("power", [12, 20, 27, 40, 86, 100, 110, 120])
+def test_scores_far_below_zero(kvp, dh, lens, power, splits):
+    """Every score of a sequence is a negative number of great magnitude, -2^power and below: its weights are as good as any others.
+    All arithmetic is exact but the factor: K = -2^4 in the second half of the blocks and -2^5 in the first, one q element, a power of two.
+    Blocks of V differ by powers of two as well."""
+    c = Case(kvp, [0], lens, 4, 1, dh, 16, splits=splits)
+    k, q = c.pools[0][0], c.q[0]
+    k.zero_()
+    q.zero_()
+    c.scales[1][0].copy_(torch.randint(100, 150, c.scales[1][0].shape, generator=torch.Generator().manual_seed(power), dtype=torch.uint8))
+    q[:, :, 5] = 2.0 ** (power // 2)
+    c.scales[0][0].fill_(127 + power - power // 2)
+    for b, n in enumerate(lens):
+        for i in range((n + 15) // 16):
+            k[int(c.bt[b, i]), :, :, 5] = -16.0 if 2 * i >= (n + 15) // 16 - 1 else -32.0
+    o, lse = c.run(scale=0.25)
+    assert c.kvp.device_status() == c.kvp.OK
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert (o[0][b] == 0).all() and (lse[0][b] == -float("inf")).all()
+            continue
+        blocks = (n + 15) // 16
+        near = [i for i in range(blocks) if 2 * i >= blocks - 1]
+        value = c.pools[1][0][c.bt[b, near].long().cuda(), 0].double() * torch.exp2(c.scales[1][0][c.bt[b, near].long().cuda(), 0].double() - 127)[..., None]
+        value = value.flatten(0, 1)[:n - near[0] * 16]
+        want, size = value.mean(0), value.abs().mean(0)
+        assert ((o[0][b].double() - want).abs() <= 2.0 ** -8 * want.abs() + size * (2.0 ** -11 + 2.0 ** -13)).all()
+        assert (lse[0][b].double() + 2.0 ** (power + 2) - np.log(len(value))).abs().max() <= 2.0 ** -20 * 2.0 ** (power + 2)
