@@ -25,7 +25,7 @@
  *    unchanged) and widens its bf16 results on store, so the arithmetic, and the results, are those of KVP_BF16:
  *    one code path.  The training entry points then keep the bf16 copies in the workspace (kvp_workspace_bytes
  *    accounts for them, also for KVP_OP_PROJ_FWD / KVP_OP_ATTN_FWD, which need none otherwise); the decode entry
- *    points read fp32 queries / new K, V rows and write fp32 outputs directly (the cache itself stays bf16).
+ *    points read fp32 queries / new K, V rows and write fp32 outputs directly (the cache itself stays bf16 or 8 bits).
  *    kvp_out_proj_* and kvp_gemm take bf16 only.
  *  - Supported: dh in {64, 128}; Hq % Hkv == 0; D % 64 == 0; S >= 1.  Anything else returns
  *    KVP_ERR_UNSUPPORTED -- there is no slow path and no CPU fallback.
@@ -281,7 +281,7 @@ typedef struct {
   int32_t max_pages;  /* columns of block_table */
   int32_t n_pages;    /* pages in each owner layer's pool */
   int32_t num_splits; /* KV splits per (sequence, KV head); 0: the library deals the step's K/V rows out evenly */
-  int32_t dtype;      /* KVP_BF16, or KVP_F32: q, k_new, v_new, o are fp32; the cache is bf16 either way */
+  int32_t dtype;      /* KVP_BF16, or KVP_F32: q, k_new, v_new, o are fp32; the cache is the same either way */
 } kvp_decode_desc;
 
 size_t kvp_decode_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor);
@@ -322,8 +322,9 @@ int kvp_decode(const kvp_decode_desc* d, const int32_t* donor, float scale, cons
  *   k_cache[l], v_cache[l]  as kvp_cache_append, bf16, where k_scale and v_scale are NULL.  Otherwise the cache is held in 8 bits:
  *     [n_pages][Hkv][page_size][dh] e4m3 numbers, and k_scale[l], v_scale[l] [n_pages][Hkv][page_size/16], one byte for each
  *     block of 16 tokens and KV head: a number stands for itself times 2^(byte - 127).  An append takes for a block the smallest
- *     exponent >= -100 with amax <= 448 * 2^exponent over its new tokens (after the rotation, in fp32; each element is rounded
- *     once).  In a block that older tokens began the exponent does not fall below theirs, and where it rises, their numbers are
+ *     exponent >= -100 with amax <= 448 * 2^exponent over its new tokens (after the rotation, in fp32; each bf16 element is rounded
+ *     once.  KVP_F32 rows are rounded to bf16 on load as everywhere, before the rotation and before the exponent is formed).
+ *     In a block that older tokens began the exponent does not fall below theirs, and where it rises, their numbers are
  *     multiplied by the power of two between and rounded again.  A block whose first token is new has no older ones, whatever
  *     it held.  What is not finite is stored as NaN and does not count for the exponent.  Bytes are 27 to 247 (others are read as
  *     the nearer of the two).

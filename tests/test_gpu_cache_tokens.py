@@ -435,3 +435,38 @@ def test_host_and_foreign_tensors_are_refused(kvp):
         kw = dict(k_new=k_new, v_new=v_new, k_cache=k_cache, v_cache=v_cache, block_table=table, lengths=lengths, k_scale=c.k_scale, v_scale=c.v_scale) | over
         with pytest.raises(ValueError):
             kvp.cache_append_tokens(c.desc, [0], **kw)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("one", [False, True])
+@pytest.mark.parametrize("theta", [0.0, 10000.0])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_fp32_rows_are_rounded_to_bf16_on_load(kvp, bits, one, theta, dh):
+    """fp32 numbers between those of bf16, ties to either side among them: cache, scales and queries as from the rows rounded to
+    nearest even beforehand, bit for bit, and by the oracle of those.  One row's largest lies between 448 * 2^e and the next bf16."""
+    new, old = ([1, 1, 1], [0, 15, 18]) if one else ([5, 33, 2], [0, 9, 30])
+    a, b = (Cache(kvp, 2, [0, 1], new, old, 4, 2, dh, 16, bits, io) for io in ("f32", "bf16"))
+    g = torch.Generator(device="cuda").manual_seed(7)
+    for x, y in zip(a.q + a.k_new + a.v_new, b.q + b.k_new + b.v_new):
+        step = torch.randint(-65536, 65537, x.shape, generator=g, device="cuda")
+        step[..., ::3] = torch.where(step[..., ::3] > 0, 32768, -32768)          # ties
+        x.view(torch.int32).add_(torch.where(x == 0, 0, step).int())
+        if x.shape[1] == 2:
+            x[0].clamp_(-400, 400)[0, 0] = 448.0 * 2.0 ** 3 * (1 + 2.0 ** -12)
+        y.copy_(x)                                            # to nearest even
+        assert (x != y.float()).float().mean() > 0.9
+        bits_of = x.view(torch.int32).long() & 0xffffffff     # (torch's rounding, by the bits)
+        even = (bits_of + 0x7fff + (bits_of >> 16 & 1)) >> 16
+        assert torch.equal(even, y.view(torch.int16).long() & 0xffff)
+    before = b.snapshot()
+    a.call(theta, one=one)
+    b.call(theta, one=one)
+    b.check(before, theta)
+    x, y = a.snapshot(), b.snapshot()
+    for name in x:
+        for u, w in zip(x[name], y[name]):
+            assert np.array_equal(u, w), name
+    a.guard.check()
+    if bits == 8:
+        row = int(a.table[0, old[0] // 16])
+        assert int(a.v_scale[0][row, 0, old[0] % 16 // 16]) == 127 + 3 and float(a.v_cache[0][row, 0, old[0] % 16, 0]) == 448.0

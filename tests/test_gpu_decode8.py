@@ -559,3 +559,20 @@ def test_scores_far_below_zero(kvp, dh, lens, power, splits):
         want, size = value.mean(0), value.abs().mean(0)
         assert ((o[0][b].double() - want).abs() <= 2.0 ** -8 * want.abs() + size * (2.0 ** -11 + 2.0 ** -13)).all()
         assert (lse[0][b].double() + 2.0 ** (power + 2) - np.log(len(value))).abs().max() <= 2.0 ** -20 * 2.0 ** (power + 2)
+
+
+@pytest.mark.parametrize("dh,Hq,Hkv", [(128, 8, 2), (64, 12, 1)])
+def test_fp32_queries_are_rounded_to_bf16_on_load(kvp, dh, Hq, Hkv):
+    """fp32 queries between the numbers of bf16, ties to either side among them: results as from those rounded to nearest even."""
+    a, b = (Case(kvp, [0, 0], [700, 1, 33], Hq, Hkv, dh, 16, io) for io in ("f32", "bf16"))
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for x, y in zip(a.q, b.q):
+        step = torch.randint(-65536, 65537, x.shape, generator=g, device="cuda")
+        step[..., ::3] = torch.where(step[..., ::3] > 0, 32768, -32768)
+        x.view(torch.int32).add_(torch.where(x == 0, 0, step).int())
+        y.copy_(x)
+        assert (x != y.float()).float().mean() > 0.9
+    (oa, la), (ob, lb) = a.run(), b.run()
+    b.check(ob, lb)
+    for l in range(2):
+        assert torch.equal(oa[l], ob[l].float()) and torch.equal(la[l], lb[l])
