@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from ahead import Ahead
 from guard import Guarded
 from oracle import cache8 as O
 from test_gpu_parity import f64
@@ -470,3 +471,68 @@ def test_fp32_rows_are_rounded_to_bf16_on_load(kvp, bits, one, theta, dh):
     if bits == 8:
         row = int(a.table[0, old[0] // 16])
         assert int(a.v_scale[0][row, 0, old[0] % 16 // 16]) == 127 + 3 and float(a.v_cache[0][row, 0, old[0] % 16, 0]) == 448.0
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_queries_that_are_not_turned_are_the_same_numbers(kvp, bits, io):
+    """theta 0, and position 0 at any theta: q_out is q, exactly, and so is K in bf16; rows of no sequence keep what q_out held."""
+    for new, old, one, theta in (([5, 0, 17, 1], [0, 9, 30, 2], False, 0.0), ([1, 1, 1], [0, 15, 16], True, 0.0), ([1, 1, 1], [0, 0, 0], True, 10000.0),
+                                 ([1, 1], [0, 0], False, 10000.0)):
+        c = Cache(kvp, 2, [0, 0], new, old, 4, 2, 64, 16, bits, io, spare=3)
+        if not one:                                           # the last rows are nobody's
+            c.first = torch.cat([c.first[:-1], c.first[-1:] - 1])
+            c.lengths[-1] -= 1
+        rows = c.T if one else c.T - 1
+        c.call(theta, one=one)
+        torch.cuda.synchronize()
+        for l in range(2):
+            assert torch.equal(c.q_out[l][:rows], c.q[l][:rows]) and (c.q_out[l][rows:] == 7).all()
+        if bits == 16:
+            for b, n in enumerate(c.lengths):
+                for i, p in enumerate(range(n - int(c.first[b + 1] - c.first[b]), n)):
+                    row = int(c.first[b]) + i
+                    page, slot = int(c.table[b, p // 16]), p % 16
+                    assert torch.equal(c.k_cache[0][page, :, slot].float(), c.k_new[0][row].float()) and torch.equal(c.v_cache[0][page, :, slot].float(), c.v_new[0][row].float())
+        c.guard.check()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("form,what", [("one", "lengths"), ("one", "table"), ("one", "all"), ("runs", "lengths"), ("runs", "table"), ("runs", "first"), ("runs", "all")])
+@pytest.mark.parametrize("B", [2, 5])
+def test_places_that_a_kernel_of_the_library_writes(kvp, form, B, what, bits):
+    """Lengths, first rows and pages are looked at before the kernel ahead has finished, while it is writing others: what it writes
+    counts, whichever of them it is that changes.  Each call has a cache of its own, compared with calls behind a finished kernel."""
+    one = form == "one"
+    r = np.random.default_rng(B)
+    new = [1] * B if one else [128 + int(x) for x in r.integers(0, 40, B)]
+    c = Cache(kvp, 2, [0, 0], new, [int(x) for x in r.integers(0 if not one else 130, 40 if not one else 170, B)], 4, 2, 64, 16, bits, spare=256)
+    n_pages, columns = c.desc.n_pages, c.table.shape[1]
+    pages = [128 + torch.from_numpy(r.permutation(n_pages - 128)[:B * columns]).int().view(B, columns) for _ in range(2)]
+    lengths = [torch.tensor(c.lengths), torch.tensor([max(128, n - int(x)) for n, x in zip(c.lengths, r.integers(1, 2 if not one else 30, B))])]
+    first = [c.first, torch.cat([c.first[:1], (c.first[1:] + torch.from_numpy(r.integers(-9, 0, B)).int()).clamp(min=128)])]
+    if B > 2:
+        lengths[1][1] = 0
+    state = lambda i: [x[i if what in (name, "all") else 0] for name, x in (("lengths", lengths), ("table", pages), ("first", first)) if not one or name != "first"]
+    ahead = Ahead(kvp, state(0), state(1))
+    k_new, v_new = c.k_new, c.v_new
+    owned = ("k_cache", "v_cache", "k_scale", "v_scale") if bits == 8 else ("k_cache", "v_cache")
+
+    def call(out, lens, table, f=None):
+        kvp.cache_append_tokens(c.desc, c.donor, k_new, v_new, out["k_cache"], out["v_cache"], table, lens, first=f, theta=10000.0, q=c.q,
+                                q_out=out["q_out"], k_scale=out.get("k_scale"), v_scale=out.get("v_scale"))
+    copies = lambda: {n: [None if x is None else x.clone() for x in getattr(c, n)] for n in owned + ("q_out",)}
+    want, runs = [copies() for _ in range(2)], [copies() for _ in range(8)]
+    for i in (0, 1):
+        there = [x.cuda().int() for x in state(i)]
+        torch.cuda.synchronize()
+        call(want[i], *there)
+        torch.cuda.synchronize()
+    same = lambda x, y: all(u is None or torch.equal(u.view(torch.uint8), w.view(torch.uint8)) for n in x for u, w in zip(x[n], y[n]))
+    assert not same(*want)
+    for i, out in enumerate(runs):
+        ahead.write(i)
+        call(out, *ahead.views)
+    assert kvp.device_status() == kvp.OK
+    for i, out in enumerate(runs):
+        assert same(out, want[i % 2]), i

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from ahead import Ahead
 from guard import Guarded
 from paper_2608_15943_b200 import synth
 
@@ -576,3 +577,47 @@ def test_fp32_queries_are_rounded_to_bf16_on_load(kvp, dh, Hq, Hkv):
     b.check(ob, lb)
     for l in range(2):
         assert torch.equal(oa[l], ob[l].float()) and torch.equal(la[l], lb[l])
+
+
+AHEAD = [  # lengths in turn, Hkv, dh, page, columns of the table behind the longest's
+    ([20000], [777], 1, 128, 128, 1),                         # many shares, few; the merge
+    ([300, 5000, 0], [4000, 0, 129], 2, 128, 16, 1),
+    ([300, 5000, 1100], [4000, 200, 129], 2, 64, 16, 1),
+    ([130] * 32, [130] * 31 + [9000], 2, 64, 16, 1),          # whole units, shares
+    ([130, 300] * 10, [300, 130] * 10, 2, 128, 16, 1),        # whole units, fewer than blocks
+    ([700] * 33, [700] * 32 + [8000], 2, 64, 16, 1),          # more lengths than a warp's lanes: behind the wait alone
+    (30, 16, 128, 16, 1),                                     # teams by the length, lengths of the whole batch
+    (30, 16, 128, 16, 2000),                                  # the same where the lengths alone say that units are short
+    (30, 32, 64, 16, 1),
+    (100, 8, 128, 16, 1),
+    (128, 8, 128, 16, 1),
+    (150, 16, 64, 16, 1),                                     # (more than are looked at)
+]
+
+
+@pytest.mark.parametrize("case", range(len(AHEAD)))
+def test_lengths_that_a_kernel_of_the_library_writes(kvp, case):
+    """Lengths are looked at before the kernel ahead has finished, while it is writing others: what it writes counts, in the deal, in the
+    teams and in the merge."""
+    if len(AHEAD[case]) == 6:
+        first, second, Hkv, dh, page, columns = AHEAD[case]
+    else:
+        B, Hkv, dh, page, columns = AHEAD[case]
+        r = np.random.default_rng(B)
+        first, second = ([int(x) for x in r.integers(128, 350, B)] for _ in range(2))
+        first[3], second[0], first[-1], second[-2] = 0, 700, 650, 0
+    longest = [max(a, b) for a, b in zip(first, second)]
+    c = Case(kvp, [0], longest, Hkv, Hkv, dh, page, poison=False, columns=columns)
+    want = [exact(c.q[0], c.pools, c.scales, c.bt, lens, page, dh ** -0.5, 0) for lens in (first, second)]
+    ahead = Ahead(kvp, [torch.tensor(first)], [torch.tensor(second)])
+    runs = [c.outputs() for _ in range(8)]
+    torch.cuda.synchronize()
+    for i, (o, lse, ws) in enumerate(runs):
+        ahead.write(i)
+        kvp.decode8(c.desc, c.donor, c.q, *c.lists, c.table, ahead.views[0], o, lse, ws)
+    assert kvp.device_status() == kvp.OK
+    for i, (o, lse, _) in enumerate(runs):
+        ro, rl, to, tl = want[i % 2]
+        assert ((o[0].double() - ro).abs() <= to).all(), i
+        some = torch.isfinite(rl)
+        assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all(), i
