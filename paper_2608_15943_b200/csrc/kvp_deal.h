@@ -1,6 +1,8 @@
 // How a decode step's K/V rows are dealt out to blocks, in granules of 16 tokens (no CUDA dependency: the kernels, the host
 // and a host-only test use the same rules).  `total`: granules of all units of the launch; a unit is one (donor group,
-// sequence, KV head); `fit`: blocks that fit on the device.
+// sequence, KV head); `fit`: blocks that fit on the device.  Bytes and times below are those of the bf16 cache.  The 8-bit cache, whose granules
+// have half the bytes, goes by the same numbers of granules: a step of a warp costs it as much (8 sequences of 8K-16K in two groups at dh 128
+// 77 us so, 86 with the limits of dh 64, which has granules of the same bytes).
 #pragma once
 
 #ifdef __CUDACC__

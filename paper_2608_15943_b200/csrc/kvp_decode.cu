@@ -585,7 +585,7 @@ cudaError_t launch_append(const AppendParams<MAX_DEC_GROUPS>& all, int n, cudaSt
   return launch_kernel(append_kernel<NG>, dim3(all.B, n), 128, 0, stream, 1, p);
 }
 
-DealBy deal_by(int dh) { return {dh, sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>), max_rounds(dh)}; }
+DealBy deal_by(int dh) { return {sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> : DEC_CTAS_PER_SM<64>), max_rounds(dh)}; }
 
 int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                 const void* const* v_cache, const int32_t* block_table, const int32_t* lengths, void* const* o,
@@ -665,7 +665,7 @@ cudaError_t launch_decode(const DecParams<MAX_DEC_GROUPS>& all, dim3 grid, dim3 
   e = launch_kernel(decode_kernel<DH, NG>, grid, DEC_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
-    e = launch_kernel(decode_combine_kernel<DH, DH, false, DecParams<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+    e = launch_kernel(decode_combine_kernel<DH, false, DecParams<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 

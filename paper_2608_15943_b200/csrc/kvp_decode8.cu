@@ -858,7 +858,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 }
 
 DealBy deal8_by(int dh, int rows) {
-  return {dh, sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>), most_rounds(dh)};
+  return {sm_count() * (dh == 128 ? (rows <= 8 ? D8_CTAS<128, 1> : D8_CTAS<128, 2>) : rows <= 8 ? D8_CTAS<64, 1> : D8_CTAS<64, 2>), most_rounds(dh)};
 }
 // Blocks for whole units.  (One too many costs: it has to be started before the next kernel's.  34 sequences of 50 to 60 tokens in six groups 11.7 us instead of 8.3.)
 long long blocks_by_units(long long units, int B, int fit) {
@@ -885,7 +885,7 @@ cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim
   e = launch_kernel(decode8_kernel<DH, NB, NG>, grid, D8_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
-    e = launch_kernel(decode_combine_kernel<DH, DH, true, Dec8Params<NG>, Deal8<DH>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
+    e = launch_kernel(decode_combine_kernel<DH, true, Dec8Params<NG>, Deal8<DH>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 template <int DH, int NB>
@@ -983,7 +983,7 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     // a block for every share of the longest list; shares go by the lengths on the device, and so does whether whole units
     // are dealt out instead
     p.n_groups = n;
-    p.by_units = dealt_by_units(by.key, longest_list(d, n), units, longest_unit(d), p.fit);
+    p.by_units = dealt_by_units(d->dh, longest_list(d, n), units, longest_unit(d), p.fit);
     const long long most_blocks = (long long)p.fit * by.rounds;
     const long long blocks = d->num_splits > 0 ? units * d->num_splits
                              : p.by_units      ? std::min(blocks_by_units(units, d->B, p.fit), most_blocks)

@@ -97,9 +97,9 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 }
 
 // All shares alike
-template <int KEY>
+template <int DH>
 struct EvenDeal : Dealt {
-  static __device__ __forceinline__ int shares(const DecSizes& p, long long total) { return shares_for(KEY, p.fit, p.max_shares, total); }
+  static __device__ __forceinline__ int shares(const DecSizes& p, long long total) { return shares_for(DH, p.fit, p.max_shares, total); }
   __device__ __forceinline__ EvenDeal(const DecSizes&, long long total, int n) : Dealt(total, n) {}
 };
 
@@ -107,9 +107,8 @@ struct EvenDeal : Dealt {
 // `wpr` of them share a row of a unit (one where a unit has few pieces, eight where it has many), each lane four
 // columns.  Bound: latency; the pieces are in L2.
 constexpr int COMBINE_THREADS = 256;
-// KEY: the head size that the rules of kvp_deal.h are asked for (they go by the bytes of a granule).  EMPTY: there may be units
-// without a token, whose pieces have no sum: output 0, LSE -infinity.
-template <int DH, int KEY, bool EMPTY, typename Params, typename Deal = EvenDeal<KEY>>
+// EMPTY: there may be units without a token, whose pieces have no sum: output 0, LSE -infinity.
+template <int DH, bool EMPTY, typename Params, typename Deal = EvenDeal<DH>>
 __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const __grid_constant__ Params p, int wpr) {
   constexpr int LANES = DH / 4;               // lanes per piece and row
   constexpr int PER_WARP = 32 / LANES;        // pieces a warp takes at a time
@@ -139,11 +138,11 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
       int before, all, longest;
       sum_granules(p, len0, b, before, all, longest);
       const long long granules = (long long)all * p.Hkv * p.n_groups;
-      if (dealt_by_units(KEY, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit)) {
+      if (dealt_by_units(DH, granules, (long long)p.n_groups * p.B * p.Hkv, longest, p.fit)) {
         w0 = w1 = 0;                          // finished by the blocks that held them
       } else {
         const int len = b < 32 ? __shfl_sync(0xffffffffu, len0, b) : p.lengths[b];
-        const int rest = unit_rest(KEY, granules, p.fit), ng = granules_of(clamp_length(p, len));
+        const int rest = unit_rest(DH, granules, p.fit), ng = granules_of(clamp_length(p, len));
         const long long per_group = ((long long)all + (long long)p.B * rest) * p.Hkv, total = per_group * p.n_groups;
         const int n = Deal::shares(p, total);
         const long long first = gi * per_group + ((long long)before + (long long)b * rest) * p.Hkv + (long long)hk * (ng + rest);
@@ -281,8 +280,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 // caller's split count: one for every (unit, split).  One launch holds at most MAX_DEC_GROUPS sub-groups and launches
 // reuse the space.
 struct DealBy {
-  int key;   // head size that the rules are asked for
-  int fit;   // blocks that fit on the device
+  int fit;      // blocks that fit on the device
   int rounds;   // shares at most, in as many
 };
 inline size_t piece_bytes(const kvp_decode_desc* d, size_t pieces, int rows) {
@@ -300,7 +298,7 @@ inline Scratch plan_scratch(const kvp_decode_desc* d, const SubGroup* subs, int 
   const int per_launch = n_sub < MAX_DEC_GROUPS ? n_sub : MAX_DEC_GROUPS;
   for (int i = 0; i < n_sub; ++i) s.rows = std::max(s.rows, subs[i].n * (d->Hq / d->Hkv));
   const long long longest = longest_list(d, per_launch);
-  s.max_shares = shares_for(by.key, by.fit, by.fit * by.rounds, longest + (long long)per_launch * d->B * d->Hkv * unit_rest(by.key, longest, by.fit));
+  s.max_shares = shares_for(d->dh, by.fit, by.fit * by.rounds, longest + (long long)per_launch * d->B * d->Hkv * unit_rest(d->dh, longest, by.fit));
   for (;;) {
     s.pieces = d->num_splits > 0 ? size_t(per_launch) * d->B * d->Hkv * d->num_splits : size_t(s.max_shares) * 2;
     s.bytes = piece_bytes(d, s.pieces, s.rows);
