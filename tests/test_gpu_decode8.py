@@ -621,3 +621,32 @@ def test_lengths_that_a_kernel_of_the_library_writes(kvp, case):
         assert ((o[0].double() - ro).abs() <= to).all(), i
         some = torch.isfinite(rl)
         assert ((lse[0].double() - rl).abs() <= tl)[some].all() and (lse[0][~some] == -float("inf")).all(), i
+
+
+LISTS = [  # donor, lengths, Hq, Hkv, dh, page
+    # 9 to 16 rows: two blocks an SM fit at dh 128, three at dh 64
+    ([0, 1, 2, 3, 4, 4, 4, 4], [16000 + 37 * b for b in range(4)] + [1, 0, 700], 32, 8, 128, 128),      # three rounds: one small share a block
+    ([0, 1, 2, 3, 4, 4, 4, 4], [57000 + 37 * b for b in range(4)] + [1, 0, 700], 32, 8, 128, 128),      # twelve: two
+    ([0, 0], [5000, 3, 3000, 0, 17] * 2, 64, 8, 128, 32),     # places behind the granules of a unit, fewer than three rounds
+    ([0], [30000, 100, 41000, 5, 33], 128, 8, 128, 64),
+    ([0, 0, 0, 0], [9000, 1, 3000, 0, 500], 32, 8, 64, 16),   # the same at dh 64: one round,
+    ([0, 0, 0, 0], [70000, 80000, 7], 32, 8, 64, 64),         # two,
+    ([0, 1], [100000, 120001, 130000, 60], 128, 8, 64, 128),  # five
+    # up to 8 rows
+    ([0], [5000, 3, 7000, 0, 17], 8, 8, 128, 32),
+    ([0, 1], [60000, 100, 90000, 5], 8, 8, 128, 64),          # two rounds of shares alike
+    ([0, 0], [9000, 1, 3000, 0, 500, 9000], 16, 8, 64, 16),
+    ([0, 1], [60000, 100, 50000, 33], 8, 8, 64, 64),
+    ([0, 1, 2], [100000, 70001, 60000, 60], 24, 8, 64, 128),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LISTS)))
+def test_long_lists(kvp, case):
+    """Lists of K/V rows of every plan: rounds of shares alike, of two sizes, places that stand for a unit's merge; and the same again."""
+    donor, lens, Hq, Hkv, dh, page = LISTS[case]
+    c = Case(kvp, donor, lens, Hq, Hkv, dh, page)
+    o, lse = c.run()
+    c.check(o, lse)
+    again, lse2 = c.run()
+    assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
