@@ -16,10 +16,11 @@
 //    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
 //  - A warp has a ring of tiles, K's and V's apart, each filled again as soon as it has been read: 12 KB in flight of 16.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
-// Measured (us; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1380 to 1450 by the board (1477), 4 of 128K at
-// 32 KV heads 580 to 600 (636): memory.  8 of 8K-16K in two groups 77 (62), of which 75 are left without the softmax: SMs that end up to 5 us apart, 4 of
-// merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 14 (6.5): the steps of
-// a warp, nearly 1 us each.
+// Measured (us, by the board; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 to 1477 (1477), 4 of 128K at
+// 32 KV heads 583 to 626 (636): memory.  8 of 8K-16K in two groups 68 to 78 (62), of which 75 of 77 are left without the softmax: SMs that end up to 5 us
+// apart, 4 of merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 14 to 16 (6.5): the steps of
+// a warp, nearly 1 us each.  16 rows: 32 of 8K-16K in four groups 619 (497), where the same bytes at 8 rows take 481; heads of 64, 16 of 8K-16K in
+// two groups 103 at 8 rows, 130 at 16 (63): a step's latencies one behind the other, two or three warps a scheduler.
 #include <float.h>
 
 #include <type_traits>
@@ -50,7 +51,7 @@ constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 // Beyond this |M| a score is rounded before M comes off it, as the one that became M was: equal scores are then equal terms, and the largest is
-// 2^0.  (A fused product would be off from M by up to 2^-24 |M|, which has to stay far below the reserve of f16's range; below it is the more exact.)
+// 2^0.  (A fused product would be off from M by up to 2^-24 |M|, which has to stay far below the reserve of f16's range; below it is the more exact.)  Its code costs 16 rows 2 %: 32 of 8K-16K in four groups 588 us -> 599.
 constexpr float FAR = 65536.f;
 // From this power of V (and of how far M lags the largest score) on the results of a unit or a piece are held against a higher M: the sum
 // of up to 2^SUM_TOP a term times V would leave fp32 where V is 2^112 and more.  With sums below 2^-16 it stays below the largest of V,
@@ -62,8 +63,8 @@ constexpr float LARGE_V = 64.f;
 // one an eighth of a block's part, or, in long lists, two a sixteenth of it.  Few blocks are started that way, and a table far
 // wider than the lengths leaves few without work.
 // (us, up to sixteen shares a block, all alike -> so: 64 of 2000 to 20000, 8 KV heads, one group 235 -> 232; the same in five alike 245; 16 rows, 64 of
-// 8000 to 16000 344 in one large and four small -> 321; 32 of 16K-32K in six groups 1380 to 1440, with the eighth 1462, with two sixteenths 1415 where
-// four gave 1420.
+// 8000 to 16000 344 in one large and four small -> 321.  One eighth -> two sixteenths, medians of five runs in turn: 32 of 16K-32K in six groups 1472 ->
+// 1455, 64 of 8K-24K in four 1220 -> 1204, 48 of 4K-32K in twelve 3204 -> 3156; 16 rows, 64 of 8K-32K in four 2094 -> 2111.
 // In a table for 32000 tokens: 16 of 2000 to 5000 in two groups 48.1 -> 43.7, 34 of 50 to 60 in six 28.2 -> 18 to 21.)
 constexpr int LARGE_FROM = 3, LONG_FROM = 12;
 struct LargeFirst {
