@@ -51,7 +51,7 @@ constexpr int LONE_UNITS = 2, LENGTH_WORDS = 4, LENGTH_PARTS = 16;
 static_assert(D8_WARPS == 4, "teams of 4, 2 and 1 warps");
 constexpr float SUM_TOP = 16.f;                   // log2 of the largest term of the sum
 // Beyond this |M| a score is rounded before M comes off it, as the one that became M was: equal scores are then equal terms, and the largest is
-// 2^0.  (A fused product would be off from M by up to 2^-24 |M|, which has to stay far below the reserve of f16's range; below it is the more exact.)  Its code costs 16 rows 2 %: 32 of 8K-16K in four groups 588 us -> 599.
+// 2^0.  (A fused product would be off from M by up to 2^-24 |M|, which has to stay far below the reserve of f16's range; below it is the more exact.)
 constexpr float FAR = 65536.f;
 // From this power of V (and of how far M lags the largest score) on the results of a unit or a piece are held against a higher M: the sum
 // of up to 2^SUM_TOP a term times V would leave fp32 where V is 2^112 and more.  With sums below 2^-16 it stays below the largest of V,
@@ -616,13 +616,15 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
             for (int u = 0; u < 2; ++u) x[m][nb][u] = ffma2(pack_f2(s2[m][nb][0][2 * u], s2[m][nb][0][2 * u + 1]), factor[m][nb], minus_M[nb]);
             to_v[m][nb] = fadd2(pack_f2(v_exp[m], v_exp[m]), minus_D[nb]);
           }
-        if (far) {
+        if (__builtin_expect(far, 0)) {            // (in single operations: the assembler fuses a packed product and sum)
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int u = 0; u < 2; ++u) x[m][nb][u] = fadd2(fmul2(pack_f2(s2[m][nb][0][2 * u], s2[m][nb][0][2 * u + 1]), factor[m][nb]), minus_M[nb]);
+              for (int u = 0; u < 2; ++u)
+                x[m][nb][u] = pack_f2(__fadd_rn(__fmul_rn(s2[m][nb][0][2 * u], f2_lo(factor[m][nb])), f2_lo(minus_M[nb])),
+                                      __fadd_rn(__fmul_rn(s2[m][nb][0][2 * u + 1], f2_hi(factor[m][nb])), f2_hi(minus_M[nb])));
         }
         if (left < STEP) {
 #pragma unroll

@@ -650,3 +650,37 @@ def test_long_lists(kvp, case):
     c.check(o, lse)
     again, lse2 = c.run()
     assert all(torch.equal(x, y) for x, y in zip(o + lse, again + lse2))
+
+
+@pytest.mark.parametrize("splits", [0, 4])
+@pytest.mark.parametrize("dh,Hq,lens", [(64, 4, [40, 3, 0]), (128, 4, [32, 1000]), (128, 12, [20000]), (64, 16, [150] * 20), (64, 1, [300])])
+@pytest.mark.parametrize("power", [10, 16, 22, 28, 34, 50, 90])
+def test_scores_of_great_magnitude_that_are_rounded(kvp, dh, Hq, lens, power, splits):
+    """Two keys in turn, whose scores are numbers like any others times 2^power: tokens of the larger one have one weight, the others none.
+    (Every query has an element of 1 or -1 along the keys' difference: scores 2^power and more apart, far more than their errors.)"""
+    c = Case(kvp, [0], lens, Hq, 1, dh, 16, splits=splits)
+    g = torch.Generator(device="cuda").manual_seed(power)
+    two = (torch.randn(2, dh, device="cuda", generator=g) * 64).to(torch.float8_e4m3fn)
+    q, along = torch.randn(Hq, dh, device="cuda", generator=g), torch.nn.functional.normalize(two[0].float() - two[1].float(), dim=0)
+    sign = torch.tensor([1.0, -1.0, -1.0] * Hq, device="cuda")[:Hq, None]
+    q = (q - (q @ along)[:, None] * along + sign * along).bfloat16()
+    y = q.double() @ two.double().T * 2.0 ** -6 * 0.25        # [Hq, 2]
+    assert ((y[:, 0] - y[:, 1]).abs() > 1).all()
+    c.q[0][:] = q * 2.0 ** (power // 2)
+    c.scales[0][0].fill_(127 - 6 + power - power // 2)
+    c.pools[0][0][:, :, 0::2] = two[0]
+    c.pools[0][0][:, :, 1::2] = two[1]
+    o, lse = c.run(scale=0.25)
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert (o[0][b] == 0).all() and (lse[0][b] == -float("inf")).all()
+            continue
+        pages = c.bt[b, :(n + 15) // 16].long().cuda()
+        value = (c.pools[1][0][pages, 0].double() * torch.exp2(c.scales[1][0][pages, 0].double() - 127)[..., None]).flatten(0, 1)[:n]
+        for h in range(Hq):
+            best = int(y[h].argmax()) if n > 1 else 0
+            v = value[best::2]
+            want, size = v.mean(0), v.abs().mean(0)
+            # beside the winners the others weigh e^-1024 at most
+            assert ((o[0][b, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + size * (2.0 ** -11 + 2.0 ** -13)).all(), (b, h)
+            assert abs(float(lse[0][b, h]) - float(y[h, best]) * 2.0 ** power - np.log(len(v))) <= 2.0 ** -16 * float(y[h].abs().max() + 16) * 2.0 ** power
