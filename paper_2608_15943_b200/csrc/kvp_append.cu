@@ -6,7 +6,7 @@
 // range reduction; sine and cosine are taken of its upper 32 bits as a float, and what that float leaves off is applied as a
 // first-order correction.
 // Measured (us; in brackets the bytes at the copy rate): prompts of 12000 tokens, four layers, queries with them, bf16 169 to 171 (165), fp32
-// 329 (308), bf16 without queries 53 (45); 30400 tokens behind begun blocks into 8 bits 437 to 445 (390), without queries 202 (86: the
+// 329 (308), bf16 without queries 53 (45); 30400 tokens behind begun blocks into 8 bits 437 to 445 (390), without queries 203 (86: the
 // barrier and two heads in flight a block); 32 tokens of eight layers, device time in a graph, 4.5 bf16, 4.8 in 8 bits.
 #include <math.h>
 

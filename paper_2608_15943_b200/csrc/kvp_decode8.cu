@@ -16,11 +16,11 @@
 //    lanes in nearly all steps: a vote says whether any lane's scores do.  P in f16 has 11 bits, against bf16's 8.
 //  - A warp has a ring of tiles, K's and V's apart, each filled again as soon as it has been read: 12 KB in flight of 16.
 //  - A length of 0 (an empty place of a padded batch) is one granule without a visible token: output 0, LSE -infinity.
-// Measured (us, by the board; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 to 1477 (1477), 4 of 128K at
-// 32 KV heads 583 to 626 (636): memory.  8 of 8K-16K in two groups 68 to 78 (62), of which 75 of 77 are left without the softmax: SMs that end up to 5 us
+// Measured (us, by the board; in brackets the bytes at the copy rate): 32 sequences of 16K-32K in six groups 1390 to 1500 (1477), 4 of 128K at
+// 32 KV heads 583 to 633 (636): memory.  8 of 8K-16K in two groups 68 to 78 (62), of which 75 of 77 are left without the softmax: SMs that end up to 5 us
 // apart, 4 of merge and 5 from the merge to the next call's first tiles.  58 of 1 to 700 at dh 64 14 to 16 (6.5): the steps of
-// a warp, nearly 1 us each.  16 rows: 32 of 8K-16K in four groups 619 (497), where the same bytes at 8 rows take 481; heads of 64, 16 of 8K-16K in
-// two groups 103 at 8 rows, 130 at 16 (63): a step's latencies one behind the other, two or three warps a scheduler.
+// a warp, nearly 1 us each.  16 rows: 32 of 8K-16K in four groups 605 (497), where the same bytes at 8 rows take 483; heads of 64, 16 of 8K-16K in
+// two groups 106 at 8 rows, 127 at 16 (63): a step's latencies one behind the other, two or three warps a scheduler.
 #include <float.h>
 
 #include <type_traits>
