@@ -80,7 +80,7 @@ int kvp_selftest_bounded_wait_pair(void* scratch, size_t scratch_bytes, kvp_stre
 /* Benchmark bookkeeping.  kvp_launch_count: kernels launched by this library since it was loaded.
  * kvp_set_timing_events: record the caller's CUDA events (HOST arrays of n cudaEvent_t, created by
  * the caller) immediately before and after each of the next n launches of one kernel
- * (0 GEMM, 1 attention forward, 2 attention backward, 3 decode (over either cache), 4 the backward's helper passes: Delta, accumulator clear, dQ conversion, one pair per group of launches, the first alone up to 128 tokens); n == 0 switches it off.
+ * (0 GEMM, 1 attention forward, 2 attention backward, 3 decode (over either cache) and attention of new tokens, 4 the backward's helper passes: Delta, accumulator clear, dQ conversion, one pair per group of launches, the first alone up to 128 tokens); n == 0 switches it off.
  * kvp_timing_events_used: how many pairs have been recorded since.  Not thread-safe. */
 unsigned long long kvp_launch_count(void);
 int kvp_set_timing_events(int kernel, void** starts, void** stops, int n);
@@ -346,6 +346,72 @@ int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, con
                 const void* const* k_cache, const void* const* v_cache, const uint8_t* const* k_scale,
                 const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths, void* const* o,
                 float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, kvp_stream_t stream);
+
+/* Attention of the tokens that kvp_cache_append_tokens has put into the cache (the paper has no counterpart: a prompt may come in
+ * pieces, drafted tokens are verified together, a layer may see a window).  T rows of queries; sequence b has rows first[b] ..
+ * first[b+1]-1 (first: DEVICE int32 [B+1], non-decreasing) at positions lengths[b] - n .. lengths[b] - 1, n of them; first == NULL:
+ * one token a sequence, T == B.  The row at position i sees the cached tokens j <= i of its sequence, its own among them;
+ * with window > 0 those with j > i - window or j < sinks alone (sinks > 0 needs a window).
+ *   q[l], o[l]  [T,Hq,dh]; lse[l]  fp32 [T,Hq], the natural logarithm of the row's sum; layers layer_begin <= l < layer_end, each
+ *   over the pages of its donor, which are read once for all layers of a donor group, up to min(8, 128 / (Hq/Hkv)) of them.
+ * Rows at positions outside [0, max_pages*page_size) and rows outside all sequences are left out: nothing of theirs is written.
+ * Slots at and behind a sequence's length, and tokens that no row of the call sees (pages freed by kvp_pages_trim with the same
+ * window among them), are not relied on: they may hold anything.  What a row does not see has no part in its result, infinite or not.
+ *   k_cache[l], v_cache[l]  as kvp_decode where k_scale and v_scale are NULL, as kvp_decode8 otherwise; numbers of the 8-bit cache
+ *   are taken as bf16 (infinite beyond its range).  A page number outside [0, n_pages) stands for a page of zeros.
+ * scale == 0 means 1/sqrt(dh); it is not negative.  P is rounded to bf16 for the second product, sums are fp32: |V| is to stay below
+ * 2^100.  A row whose scores are all -infinity has output 0 and LSE -infinity.
+ * A call cuts the work by the lengths of the whole batch: equal calls give equal bits, and a sequence's last bits (fp32 summation
+ * order) depend on the other sequences and the layer range.  dtype and the rest of d as for kvp_decode, num_splits is not read;
+ * max_pages*page_size <= 2^30, B <= 16384, n_pages*Hkv*page_size < 2^31 - 64.
+ * Workspace: kvp_attn_chunk_workspace_bytes(d, donor, T), 16-byte aligned; enough for any layer range and any smaller T. */
+size_t kvp_attn_chunk_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor, int32_t T);
+int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float scale, int32_t window,
+                   int32_t sinks, const void* const* q, const void* const* k_cache, const void* const* v_cache,
+                   const uint8_t* const* k_scale, const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths,
+                   void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, kvp_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Pages of the cache, held by any number of sequences (the paper has no counterpart: a serving program gives pages out, shares
+ * those of common prefixes, and takes them back).  Everything is decided on the device, on the caller's stream.
+ *
+ * refs: DEVICE int32 [n_pages], how many places of the block table hold a page; 0: it is free.  Sequence b holds the pages in
+ * places i < ceil(lengths[b] / page_size) of its row of block_table; a place with a number outside [0, n_pages) holds none.  The
+ * caller starts with refs and lengths 0 (or what he has laid out himself, refs counted to match) and changes the three through these
+ * calls alone.  Places that a row gives up become -1; other places behind its length are not looked at.  Free pages are taken from the
+ * lowest number up, and pages that a call frees are free for the next call.  Calls on the same arrays are to follow one another on
+ * a stream; a workspace of kvp_pages_workspace_bytes(d), 16-byte aligned, serves them all, one call at a time.
+ * Of d: L, B, Hkv, dh, page_size, max_pages, n_pages (B <= 16384, Hkv*page_size*dh <= 2^30, max_pages*page_size < 2^31); pools and scales as
+ * in kvp_cache_append_tokens (k_scale and v_scale both NULL for a bf16 cache).  A page is copied whole, in all owner layers.
+ *
+ *   kvp_pages_copy     pages src[i] -> dst[i] (DEVICE int32 [n]).  Entries with a number outside [0, n_pages) and entries onto
+ *                      themselves are left out.  No page may be the target of two entries, nor a target of one and the source of another.
+ *   kvp_pages_fork     row b goes on from what row parent[b] (DEVICE int32 [B]) was before the call: it gives up its pages and holds
+ *                      the parent's, at the parent's length.  parent[b] == b, or outside [-1, B): the row stays; -1: it ends
+ *                      (length 0).  No page is copied: the last one, partly filled, is shared too until one of its rows grows.
+ *   kvp_pages_resize   row b has length new_lengths[b] (DEVICE int32 [B]) from now on.  A row that grows gets pages; a row that shrinks
+ *                      gives up those behind its new length.  A row that grows inside a partly filled page with refs > 1 gets a
+ *                      copy of it, so that an append changes no other row's tokens; only if all who hold the page grow, the lowest
+ *                      of them keeps it.  New pages go to the rows in order, a copy's before those behind it.
+ *                      lacking: DEVICE int32 [1], 0; or the number of pages that are lacking, or -1 where a new length is outside
+ *                      [0, max_pages*page_size]: then nothing is changed.
+ *   kvp_pages_trim     frees the pages that no token from position lengths[b] on sees, with window >= 1 and sinks as in
+ *                      kvp_attn_chunk: those whose tokens are all below lengths[b] - window + 1 and at or above sinks.
+ *   kvp_pages_compact  moves the used pages with the highest numbers, in order, into the free ones below the number of used pages,
+ *                      and renames them in the table, so that pages 0 .. used-1 are the used ones.  used: DEVICE int32 [1]. */
+size_t kvp_pages_workspace_bytes(const kvp_decode_desc* d);
+int kvp_pages_copy(const kvp_decode_desc* d, const int32_t* donor, int32_t n, const int32_t* src, const int32_t* dst, void* const* k_cache,
+                   void* const* v_cache, uint8_t* const* k_scale, uint8_t* const* v_scale, kvp_stream_t stream);
+int kvp_pages_fork(const kvp_decode_desc* d, const int32_t* parent, int32_t* refs, int32_t* block_table, int32_t* lengths, void* ws,
+                   size_t ws_bytes, kvp_stream_t stream);
+int kvp_pages_resize(const kvp_decode_desc* d, const int32_t* donor, const int32_t* new_lengths, int32_t* refs, int32_t* block_table,
+                     int32_t* lengths, int32_t* lacking, void* ws, size_t ws_bytes, void* const* k_cache, void* const* v_cache,
+                     uint8_t* const* k_scale, uint8_t* const* v_scale, kvp_stream_t stream);
+int kvp_pages_trim(const kvp_decode_desc* d, int32_t window, int32_t sinks, int32_t* refs, int32_t* block_table, const int32_t* lengths,
+                   kvp_stream_t stream);
+int kvp_pages_compact(const kvp_decode_desc* d, const int32_t* donor, int32_t* refs, int32_t* block_table, const int32_t* lengths, int32_t* used,
+                      void* ws, size_t ws_bytes, void* const* k_cache, void* const* v_cache, uint8_t* const* k_scale, uint8_t* const* v_scale,
+                      kvp_stream_t stream);
 
 /* kvp_decode without a workspace argument and without any allocation (the paper has no counterpart:
  * this is a packaging variant of kvp_decode, same arithmetic, same outputs).

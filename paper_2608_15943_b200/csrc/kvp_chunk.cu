@@ -1,0 +1,1194 @@
+// Attention of the new tokens of every sequence (one, a few drafted ones, a piece of a prompt) over the shared paged cache they
+// have been appended to, bf16 or 8 bits, with or without a sliding window and first tokens that stay visible.
+//
+// The query rows of a sequence and KV head are laid out token by token: the G heads of a token in each of the layers that
+// share the donor.  128 of them are a tile, two tiles a unit; a unit walks the cached keys that any of its rows sees, 64 a step,
+// and each K/V block that it brings in serves both tiles, all heads and all layers.  The steps of all units form one list, which the
+// CTAs (one an SM) cut into equal shares from the lengths on the device; a unit that ends up in several shares is merged by a
+// second kernel.  So one long context occupies the whole device, and prompts of any lengths leave no SM behind.
+//   warp 0        TMA producer: K and V blocks, page by page (8-bit cache: the codes into a ring of their own, and their scales)
+//   warps 1, 2    tcgen05.mma issuers, one per tile: S = Q K^T into one of two 64-column score buffers, O += P V with P from TMEM
+//   warp 3        gathers the query rows of the next unit, and looks through the V blocks that not every row sees in full
+//   warps 4-11    softmax, a warpgroup per tile, a thread per row; then O out of TMEM to the outputs or to the unit's partial sums
+//   warps 12-15   (8-bit cache only) codes times scales to bf16, which holds every such product exactly
+// Masked places.  A score that a row does not see is -infinity before the maximum.  In V, rows that no row of the unit sees (slots
+// behind the sequence, freed pages before the window: anything may be there) are not read and are zeros in shared memory.  A
+// visible row of V with an infinity or NaN in it must reach the rows that see it and no other, which 0 * NaN in a matrix product
+// does not give: in blocks with any masking such rows are taken out, and the softmax threads add them to O by themselves.
+#include <math.h>
+
+#include <algorithm>
+
+#include "kvp_cache8.cuh"
+#include "kvp_decode_list.cuh"
+#include "kvp_host.h"
+#include "kvp_sm100.cuh"
+
+namespace kvp {
+namespace {
+
+constexpr int TILE = 128;                 // query rows of a tile (TMEM lanes)
+constexpr int STEP = 64;                  // keys per step
+constexpr int BATCH = 8;                  // steps whose pages the producer's lanes hold: four blocks of 16 keys a step
+constexpr int CHUNK_MEMBERS = 8;          // layers of a donor group in one tile
+constexpr int MANY_CHUNK_GROUPS = 16, FEW_CHUNK_GROUPS = 4;
+constexpr uint32_t Q_HALF = TILE * 128;   // one [128 rows x 128 B] block of Q
+constexpr uint32_t KV_HALF = STEP * 128;
+constexpr float kRescaleBy = 8.0f;        // log2: O is rescaled when the maximum has moved by more
+// Places of the list behind the steps of a unit, for its start and its merge; least places of a share.
+constexpr int REST = 3, LEAST_SHARE = 8;
+
+__device__ int g_chunk_status;
+
+template <int DH, bool BITS8>
+struct ChunkSmem {
+  static constexpr int K_STAGES = BITS8 ? (DH == 128 ? 3 : 4) : (DH == 128 ? 5 : 8);
+  static constexpr int V_STAGES = K_STAGES;
+  static constexpr int RAW_STAGES = BITS8 ? (DH == 128 ? 8 : 16) : 0;
+  static constexpr int Q_BYTES = TILE * DH * 2, KV_BYTES = STEP * DH * 2, RAW_BYTES = STEP * DH;
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
+  static constexpr int OFF_V = OFF_K + K_STAGES * KV_BYTES;
+  static constexpr int OFF_RAW = OFF_V + V_STAGES * KV_BYTES;
+  static constexpr int OFF_BAR = OFF_RAW + RAW_STAGES * RAW_BYTES;
+  static constexpr int OFF_BAD = OFF_BAR + 640;                 // [V_STAGES][4] rows of V that are left to the softmax threads
+  static constexpr int OFF_SCALE = OFF_BAD + V_STAGES * 32;     // [RAW_STAGES] four bytes each
+  static constexpr int OFF_SHARE = OFF_SCALE + RAW_STAGES * 4;
+  static constexpr int TOTAL = OFF_SHARE + 64 + 1024;
+  static constexpr int THREADS = BITS8 ? 512 : 384;
+};
+static_assert(ChunkSmem<128, false>::TOTAL <= 232448 && ChunkSmem<128, true>::TOTAL <= 232448, "shared memory of a CTA");
+
+// A unit that more than one share holds, noted by the CTA of its second share
+struct Merge {
+  int g, hk, b, pair;
+  int w0, w1;                              // its shares (w0 < 0: nothing to merge)
+  int pad[2];
+};
+
+struct ChunkSizes {
+  const int32_t *block_table, *lengths, *first;
+  Merge* merges;                           // [shares]
+  float* part_o;                           // [2 * shares][256][DH]
+  float* part_ml;                          // [2 * shares][256][2]
+  int B, T, Hq, Hkv, G, page_size, max_pages, n_pages;
+  int n_groups;
+  int members[MANY_CHUNK_GROUPS];
+  int kind[MANY_CHUNK_GROUPS];             // groups of as many members have the same list: its number
+  int n_kinds, kind_rows[CHUNK_MEMBERS];   // rows of a token in each
+  int window, sinks;                       // window 0: none
+  int box;                                 // keys of a TMA box: 64, 32 or 16
+  int io_f32;
+  float scale_log2;
+};
+struct ChunkGroup {
+  CUtensorMap map_k, map_v;
+  const void* q[CHUNK_MEMBERS];
+  void* o[CHUNK_MEMBERS];
+  float* lse[CHUNK_MEMBERS];
+  const void* v_pool;
+  const uint8_t *k_scale, *v_scale;
+};
+template <int NG>
+struct ChunkParams : ChunkSizes {
+  ChunkGroup grp[NG];
+};
+
+// ---------------------------------------------------------------------------------------------
+// the list of steps
+// ---------------------------------------------------------------------------------------------
+// The rows of a sequence that are computed: tokens before position 0 or behind the table's capacity are left out.
+struct Span {
+  int row0, n;       // rows of q
+  int pos0;          // position of the first
+};
+__device__ __forceinline__ Span span_of(const ChunkSizes& p, int b) {
+  Span s;
+  int end;
+  if (p.first != nullptr) {
+    s.row0 = min(max(p.first[b], 0), p.T);
+    end = min(max(p.first[b + 1], s.row0), p.T);
+  } else {
+    s.row0 = b;
+    end = b + 1;
+  }
+  s.n = end - s.row0;
+  s.pos0 = max(p.lengths[b], 0) - s.n;
+  const int early = max(0, -s.pos0);
+  s.row0 += early;
+  s.n -= early;
+  s.pos0 += early;
+  s.n = max(0, min(s.n, p.max_pages * p.page_size - s.pos0));
+  return s;
+}
+// The keys that a pair of tiles walks
+struct Walked {
+  int pos_first, pos_last_a, pos_last;   // positions of the first row, of tile A's last and of the last
+  int sink_blocks, from;                 // blocks of first tokens, then blocks from `from` on
+  int n, n_a;                            // steps, and those of tile A
+};
+__device__ __forceinline__ int pairs_of(const Span& s, int R) { return int((uint32_t(s.n) * uint64_t(R) + 2 * TILE - 1) / (2 * TILE)); }
+__device__ __forceinline__ Walked walked(const ChunkSizes& p, const Span& s, int R, int pair) {
+  Walked w;
+  const long long row0 = (long long)pair * 2 * TILE;
+  auto token = [&](long long row) { return int(min((long long)s.n - 1, div_places(row, R))); };
+  w.pos_first = s.pos0 + token(row0);
+  w.pos_last_a = s.pos0 + token(row0 + TILE - 1);
+  w.pos_last = s.pos0 + token(row0 + 2 * TILE - 1);
+  const int end_a = w.pos_last_a / STEP + 1, end = w.pos_last / STEP + 1;
+  w.sink_blocks = p.window > 0 ? min((p.sinks + STEP - 1) / STEP, end) : 0;
+  w.from = p.window > 0 ? max(max(0, w.pos_first - p.window + 1) / STEP, w.sink_blocks) : 0;
+  w.n = w.sink_blocks + max(0, end - w.from);
+  w.n_a = min(w.sink_blocks, end_a) + max(0, end_a - w.from);
+  return w;
+}
+// Places of the lane's sequence b (0 behind the last), a warp together.
+__device__ __forceinline__ long long places_of(const ChunkSizes& p, int b, int R) {
+  const int lane = lane_id();
+  Span s{0, 0, 0};
+  if (b < p.B) s = span_of(p, b);
+  const int pairs = pairs_of(s, R);
+  long long sum = 0;
+  const bool few = pairs <= 2;
+  if (few)
+    for (int i = 0; i < pairs; ++i) sum += walked(p, s, R, i).n + REST;
+  for (uint32_t left = __ballot_sync(0xffffffffu, !few); left != 0; left &= left - 1) {
+    const int of = __ffs(left) - 1;
+    const Span t{__shfl_sync(0xffffffffu, s.row0, of), __shfl_sync(0xffffffffu, s.n, of), __shfl_sync(0xffffffffu, s.pos0, of)};
+    const int n = __shfl_sync(0xffffffffu, pairs, of);
+    long long mine = 0;
+    for (int i = lane; i < n; i += 32) mine += walked(p, t, R, i).n + REST;
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if (lane == of) sum = mine;
+  }
+  return sum;
+}
+__device__ __forceinline__ long long warp_scan(long long v) {   // inclusive
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const long long o = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane_id() >= d) v += o;
+  }
+  return v;
+}
+// Where a share begins
+struct Share {
+  int g, hk, b, pair;
+  int off;           // places of the unit that belong to earlier shares
+  int left;          // places of the share
+};
+// Sums over 32 sequences each, then over all before them: sums[kind][i], i <= n32 = ceil(B / 32).  All warps of the block.
+__device__ __forceinline__ void list_sums(const ChunkSizes& p, long long* sums, int n32, int warps) {
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+  for (int i = warp; i < n32 * p.n_kinds; i += warps) {
+    const int kind = i / n32, at = i % n32;
+    long long v = places_of(p, at * 32 + lane, p.kind_rows[kind]);
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (lane == 0) sums[kind * (n32 + 1) + at] = v;
+  }
+  __syncthreads();
+  for (int kind = warp; kind < p.n_kinds; kind += warps) {
+    long long* const s = sums + kind * (n32 + 1);
+    long long before = 0;
+    for (int i0 = 0; i0 < n32; i0 += 32) {
+      const int i = i0 + lane;
+      const long long v = i < n32 ? s[i] : 0, up = warp_scan(v);
+      if (i < n32) s[i] = before + up - v;
+      before += __shfl_sync(0xffffffffu, up, 31);
+    }
+    __syncwarp();
+    if (lane == 0) s[n32] = before;
+  }
+  __syncthreads();
+}
+// The share of this CTA, by one warp; writes the note for the merge.  Returns false where there is none.
+__device__ __forceinline__ bool find_share(const ChunkSizes& p, const long long* sums, int n32, Share& out) {
+  const int lane = lane_id(), w = int(blockIdx.x);
+  long long total = 0;
+  for (int g = 0; g < p.n_groups; ++g) total += sums[p.kind[g] * (n32 + 1) + n32] * p.Hkv;
+  const int n = int(min((long long)gridDim.x, max(total > 0 ? 1ll : 0ll, total / LEAST_SHARE)));
+  Merge note{0, 0, 0, 0, -1, -1, {0, 0}};
+  bool there = w < n;
+  if (there) {
+    const Dealt dealt(total, n);
+    long long at = dealt.begin(w);
+    int g = 0;
+    for (;; ++g) {
+      const long long of_group = sums[p.kind[g] * (n32 + 1) + n32] * p.Hkv;
+      if (at < of_group) break;
+      at -= of_group;
+    }
+    const long long* const s = sums + p.kind[g] * (n32 + 1);
+    const int R = p.kind_rows[p.kind[g]];
+    out.g = g;
+    out.hk = int(div_places(at, s[n32]));
+    at -= out.hk * s[n32];
+    // the last 32 sequences that begin at or before it, then the sequence
+    int i = 0;
+    for (int i0 = 0; i0 < n32; i0 += 32) {
+      const uint32_t before = __ballot_sync(0xffffffffu, i0 + lane < n32 && s[i0 + lane] <= at);
+      if (before == 0) break;
+      i = i0 + 31 - __clz(before);
+    }
+    at -= s[i];
+    const long long mine = places_of(p, i * 32 + lane, R), up = warp_scan(mine);
+    const int of = __ffs(__ballot_sync(0xffffffffu, up > at)) - 1;
+    at -= __shfl_sync(0xffffffffu, up - mine, of);
+    out.b = i * 32 + of;
+    const Span span = span_of(p, out.b);
+    const int pairs = pairs_of(span, R);
+    for (int pair0 = 0;; pair0 += 32) {
+      const int pair = pair0 + lane;
+      const long long cost = pair < pairs ? walked(p, span, R, pair).n + REST : 0, sum = warp_scan(cost);
+      const long long all = __shfl_sync(0xffffffffu, sum, 31);
+      if (at >= all && pair0 + 32 < pairs) {
+        at -= all;
+        continue;
+      }
+      const int first = __ffs(__ballot_sync(0xffffffffu, sum > at)) - 1;
+      at -= __shfl_sync(0xffffffffu, sum - cost, first);
+      out.pair = pair0 + first;
+      break;
+    }
+    out.off = int(at);
+    out.left = int(dealt.size(w));
+    const int steps = walked(p, span, R, out.pair).n;
+    if (w > 0 && out.off > 0 && out.off < steps && dealt.begin(w) - out.off >= dealt.begin(w - 1))
+      note = Merge{out.g, out.hk, out.b, out.pair, w - 1, dealt.share_of(dealt.begin(w) - out.off + steps - 1), {0, 0}};
+  }
+  if (lane == 0) p.merges[w] = note;
+  return there;
+}
+
+// A share's pieces, one after the other; every role walks them by itself.
+struct Piece {
+  int g, hk, b, pair, R;
+  Span span;
+  Walked w;
+  int c0, c1;            // steps of the unit
+  bool whole;            // the unit has no other piece
+  int slot;              // place of its partial sums
+  __device__ __forceinline__ int n() const { return c1 - c0; }
+  __device__ __forceinline__ int n_a() const { return max(0, min(c1, w.n_a) - c0); }
+  __device__ __forceinline__ bool has_b() const { return ((long long)pair * 2 + 1) * TILE < (long long)span.n * R; }
+  __device__ __forceinline__ int n_of(int x) const { return x == 0 ? n_a() : has_b() ? n() : 0; }
+  __device__ __forceinline__ int block(int i) const {       // of the piece's step i
+    const int c = c0 + i;
+    return c < w.sink_blocks ? c : w.from + c - w.sink_blocks;
+  }
+  // not every row of the pair sees all keys of the block
+  __device__ __forceinline__ bool masked(const ChunkSizes& p, int block) const { return masked(p, block, w.pos_first, w.pos_last); }
+  static __device__ __forceinline__ bool masked(const ChunkSizes& p, int block, int pos_first, int pos_last) {
+    const int key = block * STEP;
+    return key + STEP - 1 > pos_first || (p.window > 0 && pos_last - p.window >= key && key + STEP > p.sinks);
+  }
+  // no row of the pair sees any of n keys from `key` on
+  __device__ __forceinline__ bool unseen(const ChunkSizes& p, int key, int n) const {
+    return key > w.pos_last || (p.window > 0 && key + n - 1 <= w.pos_first - p.window && key >= p.sinks);
+  }
+};
+struct Pieces {
+  int g, hk, b, pair, off, left;
+  __device__ __forceinline__ explicit Pieces(const Share& s) : g(s.g), hk(s.hk), b(s.b), pair(s.pair), off(s.off), left(s.left) {}
+  __device__ __forceinline__ bool next(const ChunkSizes& p, Piece& out) {
+    while (left > 0) {
+      out.g = g;
+      out.hk = hk;
+      out.b = b;
+      out.pair = pair;
+      out.R = p.members[g] * p.G;
+      out.span = span_of(p, b);
+      const int pairs = pairs_of(out.span, out.R);
+      if (pair >= pairs) {                 // (a sequence without rows, or the last pair is done)
+        pair = 0;
+        if (++b == p.B) {
+          b = 0;
+          if (++hk == p.Hkv) {
+            hk = 0;
+            ++g;
+          }
+        }
+        continue;
+      }
+      out.w = walked(p, out.span, out.R, pair);
+      out.c0 = off;
+      out.c1 = min(out.w.n, off + left);
+      out.whole = off == 0 && out.c1 == out.w.n;
+      out.slot = 2 * int(blockIdx.x) + (off == 0 ? 1 : 0);
+      left -= min(left, out.w.n + REST - off);
+      off = 0;
+      ++pair;
+      if (out.c0 < out.c1) return true;
+    }
+    return false;
+  }
+};
+
+// ---------------------------------------------------------------------------------------------
+// pieces of the kernel
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t tmem_ld_x1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+  return r;
+}
+// A bounded wait of a whole warp: true in all lanes or in none (the roles that use warp-wide operations go on or leave together).
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); }
+// two e4m3 numbers times 2^e as bf16: exact, but for what is beyond its range
+__device__ __forceinline__ uint32_t widen8(uint32_t two, float power) {
+  const float2 f = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(two)));
+  return pack_bf16(f.x * power, f.y * power);
+}
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) {   // of two bf16 numbers
+  return uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u);
+}
+__device__ __forceinline__ uint32_t not_finite(const uint4& v) { return not_finite(v.x) | not_finite(v.y) | not_finite(v.z) | not_finite(v.w); }
+
+// O of this thread's row += p_j V_j for the keys `left` of a block, from the pool itself.  P is in TMEM by now, as the product takes
+// it; `fresh`: O holds nothing yet.  A warp together.
+template <int DH, bool BITS8>
+__device__ __noinline__ void add_rows(const ChunkSizes& p, const ChunkGroup& grp, int b, int hk, int key0, unsigned long long left, unsigned long long seen,
+                                      uint32_t tm_p, uint32_t tm_o, bool fresh) {
+  for (int h = 0; h < DH / 32; ++h) {
+    uint32_t acc[32];
+    if (fresh) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[i] = 0;
+    } else {
+      tmem_ld_x32(tm_o + h * 32, acc);
+      tmem_ld_wait();
+    }
+    for (unsigned long long rest = left; rest != 0; rest &= rest - 1) {
+      const int j = __ffsll(rest) - 1, key = key0 + j;
+      const uint32_t two = tmem_ld_x1(tm_p + (j >> 1));
+      tmem_ld_wait();
+      const float pj = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+      const int page = p.block_table[size_t(b) * p.max_pages + key / p.page_size];
+      const bool takes = unsigned(page) < unsigned(p.n_pages) && (seen >> j & 1) != 0;
+      const size_t row = takes ? (size_t(page) * p.Hkv + hk) * p.page_size + key % p.page_size : 0;
+      float power = 1.f;
+      if (BITS8) power = __uint_as_float(power_bits(exponent_of_byte(grp.v_scale[row / CACHE_BLOCK])));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        uint32_t v;
+        if (BITS8)
+          v = widen8(reinterpret_cast<const uint16_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i], power);
+        else
+          v = reinterpret_cast<const uint32_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i];
+        if (takes) {
+          acc[2 * i] = __float_as_uint(fmaf(pj, __uint_as_float(v << 16), __uint_as_float(acc[2 * i])));
+          acc[2 * i + 1] = __float_as_uint(fmaf(pj, __uint_as_float(v & 0xffff0000u), __uint_as_float(acc[2 * i + 1])));
+        }
+      }
+      __syncwarp();      // (the next load of TMEM is one of the whole warp)
+    }
+    tmem_st_x32(tm_o + h * 32, acc);
+  }
+  tmem_st_wait();
+}
+
+// ---------------------------------------------------------------------------------------------
+// the kernel
+// ---------------------------------------------------------------------------------------------
+template <int DH, bool BITS8, int NG>
+__global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel(const __grid_constant__ ChunkParams<NG> p) {
+  using L = ChunkSmem<DH, BITS8>;
+  constexpr int KS = L::K_STAGES, VS = L::V_STAGES, RS = L::RAW_STAGES;
+  constexpr int HALVES = DH / 64;      // 64-column (128-byte) blocks of a row
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* const q_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
+  uint64_t* const q_empty = q_full + 1;         // 2 arrivals: both issuing warps are done with the query tiles
+  uint64_t* const k_full = q_empty + 1;         // [KS]
+  uint64_t* const k_empty = k_full + KS;        // [KS]
+  uint64_t* const v_full = k_empty + KS;        // [VS]
+  uint64_t* const v_empty = v_full + VS;        // [VS]
+  uint64_t* const v_fixed = v_empty + VS;       // [VS] warp 3 has looked through the block (8 bits: the converting warps have, at v_full)
+  uint64_t* const s_full = v_fixed + VS;        // [2][2] per tile and score buffer
+  uint64_t* const p_ready = s_full + 4;         // [2][2] (128 arrivals)
+  uint64_t* const pv_done = p_ready + 4;        // [2] one completion per step's product
+  uint64_t* const o_done = pv_done + 2;         // [2] a piece's last product
+  uint64_t* const raw_full = o_done + 2;        // [RS]
+  uint64_t* const raw_empty = raw_full + RS;    // [RS] (128 arrivals)
+  static_assert((2 + 2 * KS + 3 * VS + 12 + 2 * RS) * 8 <= 632, "barriers");
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + 632);
+  unsigned long long* const s_bad = reinterpret_cast<unsigned long long*>(smem + L::OFF_BAD);
+  uint8_t* const s_scale = smem + L::OFF_SCALE;
+  int* const s_share = reinterpret_cast<int*>(smem + L::OFF_SHARE);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int* const err = &g_chunk_status;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 2);
+    for (int i = 0; i < KS; ++i) {
+      mbar_init(&k_full[i], BITS8 ? 128 : 1);
+      mbar_init(&k_empty[i], 2);
+    }
+    for (int i = 0; i < VS; ++i) {
+      mbar_init(&v_full[i], BITS8 ? 128 : 1);
+      mbar_init(&v_empty[i], 2);
+      mbar_init(&v_fixed[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_ready[i], 128);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&pv_done[i], 1);
+      mbar_init(&o_done[i], 1);
+    }
+    for (int i = 0; i < RS; ++i) {
+      mbar_init(&raw_full[i], 1);
+      mbar_init(&raw_empty[i], 128);
+    }
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  {
+    long long* const sums = reinterpret_cast<long long*>(smem + L::OFF_Q);   // (no query has been loaded)
+    const int n32 = (p.B + 31) / 32;
+    list_sums(p, sums, n32, L::THREADS / 32);
+    if (warp == 0) {
+      Share s{0, 0, 0, 0, 0, 0};
+      if (!find_share(p, sums, n32, s)) s.left = 0;
+      if (lane == 0) {
+        s_share[0] = s.g;
+        s_share[1] = s.hk;
+        s_share[2] = s.b;
+        s_share[3] = s.pair;
+        s_share[4] = s.off;
+        s_share[5] = s.left;
+      }
+    }
+    fence_proxy_async_smem();     // (at 16384 sequences the sums reach into the first stage of K)
+    __syncthreads();
+  }
+  Pieces pieces(Share{s_share[0], s_share[1], s_share[2], s_share[3], s_share[4], s_share[5]});
+  Piece piece;
+  uint32_t at = 0;      // steps of earlier pieces: ring positions of this piece's first
+  bool ok = true;
+  // tile X: score buffer u at [X*128 + u*64, +64) with P over its first 32 columns; O at [256 + X*128, +DH)
+
+  if (warp == 0) {
+    // ------------------------------ K and V, or their codes ------------------------------
+    uint32_t raw = 0;                       // blocks of codes requested so far
+    while (ok && pieces.next(p, piece)) {
+      const ChunkGroup& grp = p.grp[piece.g];
+      const int n = piece.n();
+      // Four lanes a step, a block of 16 keys each: rows of the pool (-1: no row of the pair sees any of the box's keys), and scales.
+      // Pages are asked for two batches ahead, scales one.
+      const int sub = lane & 3;
+      const int none = p.n_pages * p.Hkv * p.page_size;        // (behind the pool: TMA fills in zeros)
+      auto box_key = [&](int i) { return (piece.block(i) * STEP + sub * 16) / p.box * p.box; };
+      auto page_of = [&](int batch) -> int {
+        const int i = batch * BATCH + (lane >> 2);
+        if (i >= n) return -1;
+        const int key = box_key(i);
+        if (piece.unseen(p, key, p.box)) return -1;
+        const int page = p.block_table[size_t(piece.b) * p.max_pages + key / p.page_size];
+        return unsigned(page) < unsigned(p.n_pages) ? page : -2;
+      };
+      auto scales_of = [&](int batch, int page) -> uint32_t {  // K's and V's
+        const int i = batch * BATCH + (lane >> 2);
+        if (!BITS8 || i >= n || page < 0) return 0x7f7f;
+        const size_t block = (size_t(page) * p.Hkv + piece.hk) * (p.page_size / CACHE_BLOCK) + (piece.block(i) * STEP + sub * 16) % p.page_size / CACHE_BLOCK;
+        return grp.k_scale[block] | uint32_t(grp.v_scale[block]) << 8;
+      };
+      int page = page_of(0), page1 = page_of(1);
+      uint32_t scales = scales_of(0, page);
+      for (int batch = 0; batch * BATCH < n && ok; ++batch) {
+        const int page2 = page_of(batch + 2);
+        const uint32_t scales1 = scales_of(batch + 1, page1);
+        const int mine = batch * BATCH + (lane >> 2);
+        const int key = mine < n ? box_key(mine) : 0;
+        const int row = page >= 0 ? (page * p.Hkv + piece.hk) * p.page_size + key % p.page_size : none;
+        const bool issues = page != -1 && sub % (p.box / 16) == 0;
+        for (int i = batch * BATCH; i < min(n, (batch + 1) * BATCH) && ok; ++i) {
+          const bool load = issues && mine == i;
+          const uint32_t bytes = uint32_t(__popc(__ballot_sync(0xffffffffu, load))) * p.box * DH * (BITS8 ? 1 : 2);
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const CUtensorMap* const map = v ? &grp.map_v : &grp.map_k;
+            if constexpr (BITS8) {
+              const uint32_t s = raw % RS;
+              if (!warp_wait(&raw_empty[s], ((raw / RS) & 1) ^ 1, err)) { ok = false; break; }
+              if (mine == i) s_scale[s * 4 + sub] = uint8_t(v ? scales >> 8 : scales);
+              __syncwarp();
+              mbar_expect_tx_e(&raw_full[s], bytes, lane == 0);
+              __syncwarp();
+              tma_load_2d_e(smem + L::OFF_RAW + s * L::RAW_BYTES + sub * 16 * DH, map, &raw_full[s], 0, row, load);
+              ++raw;
+            } else {
+              const uint32_t j = at + i, s = j % KS;
+              uint64_t* const full = v ? &v_full[s] : &k_full[s];
+              if (!warp_wait(v ? &v_empty[s] : &k_empty[s], ((j / KS) & 1) ^ 1, err)) { ok = false; break; }
+              mbar_expect_tx_e(full, bytes, lane == 0);
+              __syncwarp();
+#pragma unroll
+              for (int h = 0; h < HALVES; ++h)
+                tma_load_2d_e(smem + (v ? L::OFF_V : L::OFF_K) + s * L::KV_BYTES + h * KV_HALF + sub * 16 * 128, map, full, h * 64, row, load);
+            }
+          }
+        }
+        page = page1;
+        page1 = page2;
+        scales = scales1;
+      }
+      at += n;
+    }
+    grid_dep_launch();
+  } else if (warp == 1 || warp == 2) {
+    // ------------------------------ MMA issuer of tile x ------------------------------
+    const uint32_t leader = elect_one();
+    constexpr uint32_t idesc_qk = umma_idesc_bf16(TILE, STEP, 0, 0);
+    constexpr uint32_t idesc_pv = umma_idesc_bf16(TILE, DH, 0, 1);
+    constexpr uint32_t hi = desc_hi_sw128(1024);
+    const uint32_t k_base = smem_u32(smem + L::OFF_K), v_base = smem_u32(smem + L::OFF_V);
+    const int x = warp - 1;
+    const uint32_t q_lo = desc_lo_sw128(smem_u32(smem + L::OFF_Q + x * L::Q_BYTES), 0);
+    const uint32_t tm_s = tmem_base + x * 128, tm_o = tmem_base + 256 + x * 128;
+    uint32_t it = 0;      // pieces so far
+    uint32_t done = 0;    // steps of earlier pieces in which this tile took part
+    while (ok && pieces.next(p, piece)) {
+      const int n = piece.n(), n_x = piece.n_of(x);
+      auto issue_s = [&](int i) {
+        const uint32_t u = (done + i) & 1, k_lo = desc_lo_sw128(k_base + (at + i) % KS * L::KV_BYTES, 0);
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ++ks)
+          umma_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, (ks / 4) * Q_HALF + (ks % 4) * 32), desc_lo_add(k_lo, (ks / 4) * KV_HALF + (ks % 4) * 32), hi, idesc_qk, ks != 0,
+                    leader);
+        umma_commit(&s_full[2 * x + u], leader);
+      };
+      // K of step i has come: scores, where the tile takes part, and the stage goes back
+      auto scores = [&](int i) -> bool {
+        if (!mbar_wait(&k_full[(at + i) % KS], ((at + i) / KS) & 1, err)) return false;
+        tc_fence_after_sync();
+        if (i < n_x) issue_s(i);
+        umma_commit(&k_empty[(at + i) % KS], leader);
+        if (i + 1 == max(n_x, 1)) umma_commit(q_empty, leader);   // no further score of this piece from this warp
+        return true;
+      };
+      if (!mbar_wait(q_full, it & 1, err)) { ok = false; break; }
+      tc_fence_after_sync();
+      for (int i = 0; i < 2 && i < n && ok; ++i) ok = scores(i);
+      for (int i = 0; i < n && ok; ++i) {
+        const uint32_t s = (at + i) % VS;
+        if (!mbar_wait(&v_full[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+        if (i < n_x) {
+          const uint32_t u = (done + i) & 1;
+          uint32_t add = i != 0;
+          if (piece.masked(p, piece.block(i))) {
+            if (!BITS8 && !mbar_wait(&v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+            // (the softmax threads have begun O with the rows that they add themselves)
+            if (i == 0) add = (s_bad[s * 4] | s_bad[s * 4 + 1] | s_bad[s * 4 + 2] | s_bad[s * 4 + 3]) != 0;
+          }
+          if (!mbar_wait(&p_ready[2 * x + u], ((done + i) >> 1) & 1, err)) { ok = false; break; }
+          tc_fence_after_sync();
+          const uint32_t v_lo = desc_lo_sw128(v_base + s * L::KV_BYTES, KV_HALF);
+#pragma unroll
+          for (int ks = 0; ks < STEP / 16; ++ks)
+            umma_ts_w(tm_o, tm_s + u * STEP + ks * 8, desc_lo_add(v_lo, ks * 2048), hi, idesc_pv, ks == 0 ? add : 1u, leader);
+          umma_commit(&pv_done[x], leader);
+          if (i + 1 == n_x) umma_commit(&o_done[x], leader);
+        }
+        umma_commit(&v_empty[s], leader);
+        if (i + 2 < n) ok = scores(i + 2);
+      }
+      at += n;
+      done += n_x;
+      ++it;
+    }
+  } else if (warp == 3) {
+    // ------------------------------ query rows; V blocks with masking ------------------------------
+    constexpr int CHUNKS = DH / 8, AT_ONCE = 32 / CHUNKS;       // 16-byte pieces of a row; rows per pass of the warp
+    const int g_inverse = 65536 / p.G + 1;                      // (in / G, exactly, for in < 128)
+    uint32_t it = 0;
+    while (ok && pieces.next(p, piece)) {
+      const ChunkGroup& grp = p.grp[piece.g];
+      if (!warp_wait(q_empty, (it & 1) ^ 1, err)) { ok = false; break; }
+      // (rows of the tiles behind the last one hold what they held: nothing of theirs is stored)
+      const long long row0 = (long long)piece.pair * 2 * TILE;
+      const int rows = int(min((long long)2 * TILE, (long long)piece.span.n * piece.R - row0));
+      const int chunk = lane % CHUNKS, first = lane / CHUNKS;
+      int token = int(div_places(row0 + first, piece.R)), in = int(row0 + first - (long long)token * piece.R);
+      auto source = [&]() {                                      // of the row at hand, and on to the next
+        const int member = in * g_inverse >> 16;
+        const size_t elem = (size_t(piece.span.row0 + token) * p.Hq + piece.hk * p.G + in - member * p.G) * DH + chunk * 8;
+        const uint8_t* const at = reinterpret_cast<const uint8_t*>(grp.q[member]) + (elem << (p.io_f32 ? 2 : 1));
+        for (in += AT_ONCE; in >= piece.R; in -= piece.R) ++token;
+        return at;
+      };
+      auto place = [&](int r) { return smem + L::OFF_Q + (r / TILE) * L::Q_BYTES + (chunk / 8) * Q_HALF + sw128_offset(r % TILE, chunk % 8); };
+      if (p.io_f32) {
+        constexpr int FLY = 4;
+        for (int r = first; r < rows; r += AT_ONCE * FLY) {
+          float4 v[FLY][2];
+#pragma unroll
+          for (int k = 0; k < FLY; ++k) {
+            if (r + k * AT_ONCE >= rows) break;
+            const float4* const src = reinterpret_cast<const float4*>(source());
+            v[k][0] = src[0];
+            v[k][1] = src[1];
+          }
+#pragma unroll
+          for (int k = 0; k < FLY; ++k) {
+            if (r + k * AT_ONCE >= rows) break;
+            *reinterpret_cast<uint4*>(place(r + k * AT_ONCE)) = make_uint4(pack_bf16(v[k][0].x, v[k][0].y), pack_bf16(v[k][0].z, v[k][0].w),
+                                                                          pack_bf16(v[k][1].x, v[k][1].y), pack_bf16(v[k][1].z, v[k][1].w));
+          }
+        }
+      } else {
+        for (int r = first; r < rows; r += AT_ONCE) cp_async16(smem_u32(place(r)), source(), 16);
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+      if constexpr (!BITS8) {
+        for (int i = 0; i < piece.n() && ok; ++i) {
+          const uint32_t s = (at + i) % VS;
+          ok = warp_wait(&v_full[s], ((at + i) / VS) & 1, err);
+          if (!ok) break;
+          const int block = piece.block(i);
+          if (piece.masked(p, block)) {
+            uint8_t* const v = smem + L::OFF_V + s * L::KV_BYTES;
+            unsigned long long bad = 0;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+              const int r = part * 32 + lane;
+              const bool dead = piece.unseen(p, block * STEP + r, 1);
+              uint32_t odd = 0;
+              if (!dead)
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) odd |= not_finite(*reinterpret_cast<const uint4*>(v + (c / 8) * KV_HALF + sw128_offset(r, c % 8)));
+              if (dead || odd != 0)
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) *reinterpret_cast<uint4*>(v + (c / 8) * KV_HALF + sw128_offset(r, c % 8)) = make_uint4(0, 0, 0, 0);
+              bad |= (unsigned long long)__ballot_sync(0xffffffffu, odd != 0) << (32 * part);
+            }
+            if (lane < 4) s_bad[s * 4 + lane] = lane == 0 ? bad : 0;
+            fence_proxy_async_smem();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&v_fixed[s]);
+        }
+      }
+      at += piece.n();
+      ++it;
+    }
+  } else if (warp < 12) {
+    // ------------------------------ softmax of tile x, and its rows of the outputs ------------------------------
+    const int x = (warp - 4) >> 2, quarter = warp & 3;
+    const int r = quarter * 32 + lane;   // row of the tile == TMEM lane
+    const uint32_t lane_sel = uint32_t(quarter * 32) << 16;
+    const uint32_t tm_s = tmem_base + x * 128 + lane_sel, tm_o = tmem_base + 256 + x * 128 + lane_sel;
+    const uint64_t c2 = pack_f2(p.scale_log2, p.scale_log2);
+    uint32_t done = 0, n_done = 0;       // steps of earlier pieces in which this tile took part; those pieces
+    while (ok && pieces.next(p, piece)) {
+      const long long n_rows = (long long)piece.span.n * piece.R, tile0 = ((long long)piece.pair * 2 + x) * TILE;
+      const bool there = tile0 + r < n_rows, any = tile0 + quarter * 32 < n_rows;      // (the same in the whole warp)
+      const int token = int(min((long long)piece.span.n - 1, div_places(tile0 + r, piece.R)));
+      const int pos = piece.span.pos0 + token;
+      const int pos_first = x == 0 ? piece.w.pos_first : piece.span.pos0 + int(min((long long)piece.span.n - 1, div_places(tile0, piece.R)));
+      const int pos_last = x == 0 ? piece.w.pos_last_a : piece.w.pos_last;
+      const int n_x = piece.n_of(x);
+      float m_used = -INFINITY;          // running maximum (log2 domain) that the exponentials are taken against
+      uint64_t l2 = 0ull, l2b = 0ull;
+      for (int i = 0; i < n_x; ++i) {
+        const uint32_t u = (done + i) & 1;
+        const int block = piece.block(i), key0 = block * STEP;
+        ok = warp_wait(&s_full[2 * x + u], ((done + i) >> 1) & 1, err);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t tm_su = tm_s + u * STEP;
+        bool rescale = false;
+        float alpha = 1.f;
+        unsigned long long seen = ~0ull;
+        if (any) {
+          uint32_t sv[STEP];
+          tmem_ld_x32(tm_su, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+          tmem_ld_x32(tm_su + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          tmem_ld_wait();
+          if (Piece::masked(p, block, pos_first, pos_last)) {
+            auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
+            seen = below(pos - key0 + 1);
+            if (p.window > 0) seen &= ~below(pos - p.window + 1 - key0) | below(p.sinks - key0);
+            const uint32_t lo = uint32_t(seen), up = uint32_t(seen >> 32);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              if ((lo >> k & 1) == 0) sv[k] = 0xff800000u;        // -inf
+              if ((up >> k & 1) == 0) sv[32 + k] = 0xff800000u;
+            }
+          }
+          float mp[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mp[k] = fmaxf(__uint_as_float(sv[2 * k]), __uint_as_float(sv[2 * k + 1]));
+#pragma unroll
+          for (int j = 8; j < STEP; j += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mp[k] = fmax3(mp[k], __uint_as_float(sv[j + 2 * k]), __uint_as_float(sv[j + 2 * k + 1]));
+          const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * p.scale_log2;
+          if (i == 0) {
+            m_used = m_step;
+          } else if (m_step > m_used + kRescaleBy) {
+            alpha = fast_exp2(m_used - m_step);
+            m_used = m_step;
+            l2 = fmul2(l2, pack_f2(alpha, alpha));
+            l2b = fmul2(l2b, pack_f2(alpha, alpha));
+            rescale = true;
+          }
+          const float nm = m_used == -INFINITY ? 0.f : -m_used;   // (a row that has seen nothing yet: all terms are 0)
+          const uint64_t nm2 = pack_f2(nm, nm);
+#pragma unroll
+          for (int g = 0; g < STEP / 32; ++g) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * k]), __uint_as_float(sv[g * 32 + 2 * k + 1])), c2, nm2);
+              const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
+              if (k & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
+              pk[k] = pack_bf16(f2_lo(e), f2_hi(e));
+            }
+            tmem_st_x16(tm_su + g * 16, pk);    // P as bf16 pairs over the first 32 columns of this score buffer
+          }
+        }
+        // O may still be receiving the last step's product: a rescale waits for it first.
+        bool behind = false;
+        auto wait_product = [&]() -> bool {
+          if (behind || i == 0) return true;
+          behind = true;
+          const bool wt = warp_wait(&pv_done[x], (done + i - 1) & 1, err);
+          tc_fence_after_sync();
+          return wt;
+        };
+        if (i > 0 && __any_sync(0xffffffffu, rescale)) {
+          if (!wait_product()) { ok = false; break; }
+#pragma unroll
+          for (int g = 0; g < DH / 32; ++g) {
+            uint32_t tmp[32];
+            tmem_ld_x32(tm_o + g * 32, tmp);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) tmp[k] = __float_as_uint(__uint_as_float(tmp[k]) * alpha);
+            tmem_st_x32(tm_o + g * 32, tmp);
+          }
+        }
+        tmem_st_wait();
+        if (piece.masked(p, block)) {
+          const uint32_t s = (at + i) % VS;
+          if (!warp_wait(BITS8 ? &v_full[s] : &v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+          const unsigned long long bad = s_bad[s * 4] | s_bad[s * 4 + 1] | s_bad[s * 4 + 2] | s_bad[s * 4 + 3];
+          if (bad != 0) {
+            if (!wait_product()) { ok = false; break; }
+            add_rows<DH, BITS8>(p, p.grp[piece.g], piece.b, piece.hk, key0, bad, any ? seen : 0ull, tm_su, tm_o, i == 0);
+          }
+        }
+        tc_fence_before_sync();
+        mbar_arrive(&p_ready[2 * x + u]);
+      }
+      if (!ok) break;
+      const float l_sum = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
+      if (n_x > 0) {
+        ok = warp_wait(&o_done[x], n_done & 1, err);
+        if (!ok) break;
+        tc_fence_after_sync();
+        ++n_done;
+      }
+      if (any) {
+        const ChunkGroup& grp = p.grp[piece.g];
+        const int in = int(tile0 + r - (long long)token * piece.R);
+        const int member = there ? in / p.G : 0;
+        const size_t head = size_t(piece.span.row0 + token) * p.Hq + piece.hk * p.G + (there ? in % p.G : 0);
+        const size_t part = size_t(piece.slot) * (2 * TILE) + x * TILE + r;
+        const float inv_l = l_sum == 0.f ? 0.f : 1.f / l_sum;
+        if (there) {
+          if (piece.whole)
+            grp.lse[member][head] = l_sum == 0.f ? -INFINITY : log_sum(m_used, l_sum);
+          else
+            *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m_used, l_sum);
+        }
+        if (n_x > 0) {
+#pragma unroll
+          for (int h = 0; h < DH / 32; ++h) {
+            uint32_t tmp[32];
+            tmem_ld_x32(tm_o + h * 32, tmp);
+            tmem_ld_wait();
+            if (there && !piece.whole) {
+              float* const dst = p.part_o + part * DH + h * 32;
+#pragma unroll
+              for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4*>(dst + k) = make_uint4(tmp[k], tmp[k + 1], tmp[k + 2], tmp[k + 3]);
+            } else if (there) {
+              uint32_t v[16];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) v[k] = pack_bf16(__uint_as_float(tmp[2 * k]) * inv_l, __uint_as_float(tmp[2 * k + 1]) * inv_l);
+              if (p.io_f32) {
+                float* const dst = reinterpret_cast<float*>(grp.o[member]) + head * DH + h * 32;
+#pragma unroll
+                for (int k = 0; k < 16; k += 2)
+                  *reinterpret_cast<uint4*>(dst + 2 * k) = make_uint4(v[k] << 16, v[k] & 0xffff0000u, v[k + 1] << 16, v[k + 1] & 0xffff0000u);
+              } else {
+                __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(grp.o[member]) + head * DH + h * 32;
+#pragma unroll
+                for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(dst + 2 * k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+              }
+            }
+            __syncwarp();
+          }
+        }
+      }
+      __syncwarp();
+      // (the next piece's first product waits for this warp's P, so O is free by then)
+      tc_fence_before_sync();
+      at += piece.n();
+      done += n_x;
+    }
+  } else if constexpr (BITS8) {
+    // ------------------------------ codes to bf16 ------------------------------
+    constexpr int PIECES = DH / 16;                       // 16-byte pieces of a row of codes
+    constexpr int PASSES = STEP * PIECES / 128;           // of the four warps; each 128 / PIECES rows
+    const int tid = threadIdx.x - 384, col = tid % PIECES;
+    uint32_t raw = 0;
+    while (ok && pieces.next(p, piece)) {
+      const int n = piece.n();
+      for (int i = 0; i < n && ok; ++i) {
+        const uint32_t j = at + i, s = j % KS;
+        const int block = piece.block(i);
+        const bool masked = piece.masked(p, block);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const uint32_t rs = raw % RS;
+          if (!warp_wait(&raw_full[rs], (raw / RS) & 1, err) || !warp_wait(v ? &v_empty[s] : &k_empty[s], ((j / KS) & 1) ^ 1, err)) { ok = false; break; }
+          uint4 codes[PASSES];
+          float power[PASSES];
+#pragma unroll
+          for (int k = 0; k < PASSES; ++k) {
+            const int row = (k * 128 + tid) / PIECES;
+            codes[k] = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + rs * L::RAW_BYTES + row * DH + col * 16);
+            power[k] = __uint_as_float(power_bits(exponent_of_byte(s_scale[rs * 4 + row / CACHE_BLOCK])));
+          }
+          mbar_arrive(&raw_empty[rs]);
+          uint8_t* const tile = smem + (v ? L::OFF_V : L::OFF_K) + s * L::KV_BYTES;
+          unsigned long long bad = 0;
+#pragma unroll
+          for (int k = 0; k < PASSES; ++k) {
+            const int row = (k * 128 + tid) / PIECES;
+            const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
+            uint4 half[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              half[e] = make_uint4(widen8(w[2 * e], power[k]), widen8(w[2 * e] >> 16, power[k]), widen8(w[2 * e + 1], power[k]), widen8(w[2 * e + 1] >> 16, power[k]));
+            if (v == 1 && masked) {
+              const bool dead = piece.unseen(p, block * STEP + row, 1);
+              const bool odd = !dead && (not_finite(half[0]) | not_finite(half[1])) != 0;
+              // the lanes of a row
+              const uint32_t of_row = __ballot_sync(0xffffffffu, odd) >> (lane / PIECES * PIECES) & ((1u << PIECES) - 1);
+              if (dead || of_row != 0) half[0] = half[1] = make_uint4(0, 0, 0, 0);
+              const uint32_t firsts = __ballot_sync(0xffffffffu, of_row != 0 && lane % PIECES == 0);
+#pragma unroll
+              for (int q = 0; q < 32 / PIECES; ++q)
+                if (firsts >> (q * PIECES) & 1) bad |= 1ull << ((k * 128 + tid - lane) / PIECES + q);
+            }
+            // (odd and even columns of a row take turns, so that the eight lanes of a phase hit different banks)
+            const int flip = (col >> 2) & 1;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int c = col * 2 + (e ^ flip);
+              *reinterpret_cast<uint4*>(tile + (c / 8) * KV_HALF + sw128_offset(row, c % 8)) = (e ^ flip) ? half[1] : half[0];
+            }
+          }
+          if (v == 1 && masked && lane == 0) s_bad[s * 4 + (tid >> 5)] = bad;
+          fence_proxy_async_smem();
+          __syncwarp();      // (lane 0's note is ahead of every lane's arrival by program order of its own)
+          mbar_arrive(v ? &v_full[s] : &k_full[s]);
+          ++raw;
+        }
+      }
+      at += n;
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// merge of the pieces of a unit: a warp per row, blockIdx.y a part of the unit's rows
+// ---------------------------------------------------------------------------------------------
+constexpr int MERGE_THREADS = 256, MERGE_PARTS = 8;
+template <int DH, int NG>
+__global__ void __launch_bounds__(MERGE_THREADS) chunk_merge_kernel(const __grid_constant__ ChunkParams<NG> p) {
+  constexpr int COLS = DH / 32;         // columns of a lane
+  grid_dep_launch();
+  grid_dep_wait();
+  const Merge m = p.merges[blockIdx.x];
+  if (m.w0 < 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const ChunkGroup& grp = p.grp[m.g];
+  const Span span = span_of(p, m.b);
+  const int R = p.members[m.g] * p.G;
+  const long long row0 = (long long)m.pair * 2 * TILE, n_rows = (long long)span.n * R;
+  for (int row = int(blockIdx.y) + MERGE_PARTS * warp; row < 2 * TILE; row += MERGE_PARTS * (MERGE_THREADS / 32)) {
+    if (row0 + row >= n_rows) continue;
+    float top = -INFINITY, sum = 0.f, acc[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) acc[c] = 0.f;
+    for (int w = m.w0; w <= m.w1; w += 32) {
+      // the lane's piece: maximum and sum
+      float pm = -INFINITY, pl = 0.f;
+      if (w + lane <= m.w1) {
+        const size_t part = size_t(2 * (w + lane) + (w + lane == m.w0 ? 1 : 0)) * (2 * TILE) + row;
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + part * 2);
+        pm = ml.x;
+        pl = ml.y;
+      }
+      float most = pm;
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+      most = fmaxf(top, most);
+      const float keep = top == -INFINITY ? 0.f : fast_exp2(top - most);
+      top = most;
+      sum *= keep;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) acc[c] *= keep;
+      const float weight = pm == -INFINITY ? 0.f : fast_exp2(pm - most);
+      float ws = weight * pl;
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) ws += __shfl_xor_sync(0xffffffffu, ws, d);
+      sum += ws;
+      const int n = min(32, m.w1 - w + 1);
+      constexpr int FLY = 4;
+      for (int i0 = 0; i0 < n; i0 += FLY) {
+        float held[FLY][COLS], f[FLY];
+#pragma unroll
+        for (int k = 0; k < FLY; ++k) {
+          const int i = i0 + k;
+          f[k] = __shfl_sync(0xffffffffu, weight, i & 31);
+          const float its = __shfl_sync(0xffffffffu, pm, i & 31);
+          if (i >= n || its == -INFINITY) {      // (a piece without keys for this tile has left no sums)
+            f[k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) held[k][c] = 0.f;
+            continue;
+          }
+          const size_t part = size_t(2 * (w + i) + (w + i == m.w0 ? 1 : 0)) * (2 * TILE) + row;
+          const float* const src = p.part_o + part * DH + lane * COLS;
+          if constexpr (COLS == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            held[k][0] = v.x, held[k][1] = v.y, held[k][2] = v.z, held[k][3] = v.w;
+          } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            held[k][0] = v.x, held[k][1] = v.y;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < FLY; ++k)
+#pragma unroll
+          for (int c = 0; c < COLS; ++c) acc[c] = fmaf(held[k][c], f[k], acc[c]);
+      }
+    }
+    const int token = int(div_places(row0 + row, R)), in = int(row0 + row - (long long)token * R), member = in / p.G;
+    const size_t head = size_t(span.row0 + token) * p.Hq + m.hk * p.G + in % p.G;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint32_t v[COLS / 2];
+#pragma unroll
+    for (int c = 0; c < COLS / 2; ++c) v[c] = pack_bf16(acc[2 * c] * inv, acc[2 * c + 1] * inv);
+    if (p.io_f32) {
+      float* const dst = reinterpret_cast<float*>(grp.o[member]) + head * DH + lane * COLS;
+#pragma unroll
+      for (int c = 0; c < COLS / 2; ++c) *reinterpret_cast<uint2*>(dst + 2 * c) = make_uint2(v[c] << 16, v[c] & 0xffff0000u);
+    } else {
+      uint32_t* const dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(grp.o[member]) + head * DH + lane * COLS);
+#pragma unroll
+      for (int c = 0; c < COLS / 2; ++c) dst[c] = v[c];
+    }
+    if (lane == 0) grp.lse[member][head] = sum == 0.f ? -INFINITY : log_sum(top, sum);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------
+size_t merge_bytes(int shares) { return align256(size_t(shares) * sizeof(Merge)); }
+size_t chunk_bytes(int shares, int dh) {
+  return merge_bytes(shares) + align256(size_t(shares) * 2 * (2 * TILE) * dh * 4) + align256(size_t(shares) * 2 * (2 * TILE) * 2 * 4);
+}
+// Most shares that the call's list can be cut into: no unit of `rows` a token walks more steps than the table is long.
+int shares_at_most(const kvp_decode_desc* d, int n_groups, int T) {
+  const long long steps = ((long long)d->max_pages * d->page_size + STEP - 1) / STEP + REST;
+  const long long units = ((long long)T * (CHUNK_MEMBERS * 16) / (2 * TILE) + std::min(T, d->B)) * d->Hkv * n_groups;
+  const long long most = units > (1ll << 40) / steps ? (1ll << 40) : units * steps;
+  return int(std::max(1ll, std::min((long long)sm_count(), most / LEAST_SHARE)));
+}
+
+int check_chunk(const kvp_decode_desc* d) {
+  int rc = d == nullptr ? KVP_ERR_INVALID_ARG : KVP_OK;
+  if (rc != KVP_OK) return rc;
+  kvp_decode_desc plain = *d;
+  plain.num_splits = 0;
+  rc = check_desc(&plain);
+  if (rc != KVP_OK) return rc;
+  // positions, rows of the pool and of the sums in shared memory are counted in 32 bits
+  if ((long long)d->max_pages * d->page_size > (1 << 30) || (long long)d->n_pages * d->Hkv * d->page_size > 0x7fffffffLL - STEP ||
+      d->Hq > (1 << 16) || d->B > (1 << 14))
+    return KVP_ERR_UNSUPPORTED;
+  return KVP_OK;
+}
+
+template <int DH, bool BITS8, int NG>
+cudaError_t launch_chunk(const ChunkParams<MANY_CHUNK_GROUPS>& all, int shares, cudaStream_t stream) {
+  using L = ChunkSmem<DH, BITS8>;
+  static thread_local ChunkParams<NG> p;
+  static_cast<ChunkSizes&>(p) = all;
+  std::copy(all.grp, all.grp + NG, p.grp);
+  cudaError_t e = allow_smem<chunk_kernel<DH, BITS8, NG>>(L::TOTAL);
+  if (e == cudaSuccess) e = launch_kernel(chunk_kernel<DH, BITS8, NG>, shares, L::THREADS, L::TOTAL, stream, 1, p);
+  if (e == cudaSuccess && shares > 1) e = launch_kernel(chunk_merge_kernel<DH, NG>, dim3(shares, MERGE_PARTS), MERGE_THREADS, 0, stream, 1, p);
+  return e;
+}
+template <int NG>
+cudaError_t launch_chunk(const ChunkParams<MANY_CHUNK_GROUPS>& p, int dh, bool bits8, int shares, cudaStream_t stream) {
+  return bits8 ? (dh == 128 ? launch_chunk<128, true, NG>(p, shares, stream) : launch_chunk<64, true, NG>(p, shares, stream))
+               : (dh == 128 ? launch_chunk<128, false, NG>(p, shares, stream) : launch_chunk<64, false, NG>(p, shares, stream));
+}
+
+}  // namespace
+
+int chunk_read_status() {
+  int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_chunk_status, sizeof(int)) != cudaSuccess) return -1;
+  if (v != 0) {
+    int zero = 0;
+    cudaMemcpyToSymbol(g_chunk_status, &zero, sizeof(int));
+  }
+  return v;
+}
+
+}  // namespace kvp
+
+using namespace kvp;
+
+extern "C" size_t kvp_attn_chunk_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor, int32_t T) {
+  if (check_chunk(d) != KVP_OK || donor == nullptr || T < 0) return 0;
+  return chunk_bytes(shares_at_most(d, std::min(d->L, MANY_CHUNK_GROUPS), T), d->dh);
+}
+
+extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float scale, int32_t window, int32_t sinks,
+                              const void* const* q, const void* const* k_cache, const void* const* v_cache, const uint8_t* const* k_scale,
+                              const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths, void* const* o, float* const* lse,
+                              int layer_begin, int layer_end, void* ws, size_t ws_bytes, kvp_stream_t stream_) {
+  int rc = check_chunk(d);
+  if (rc != KVP_OK) return rc;
+  if (donor == nullptr || q == nullptr || k_cache == nullptr || v_cache == nullptr || o == nullptr || lse == nullptr || block_table == nullptr ||
+      lengths == nullptr || (k_scale == nullptr) != (v_scale == nullptr))
+    return KVP_ERR_INVALID_ARG;
+  if (layer_begin < 0 || layer_end > d->L || layer_begin >= layer_end || T < 0 || (first == nullptr && T != d->B) || window < 0 || sinks < 0 ||
+      (window == 0 && sinks > 0) || !(scale >= 0.f && scale < INFINITY))
+    return KVP_ERR_INVALID_ARG;
+  for (int l = 0; l < d->L; ++l)
+    if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return KVP_ERR_BAD_DONOR;
+  if (T == 0) return KVP_OK;           // (tensors without rows have no memory)
+  const bool bits8 = k_scale != nullptr;
+  for (int l = layer_begin; l < layer_end; ++l) {
+    const int own = donor[l];
+    if (q[l] == nullptr || o[l] == nullptr || lse[l] == nullptr || k_cache[own] == nullptr || v_cache[own] == nullptr ||
+        (bits8 && (k_scale[own] == nullptr || v_scale[own] == nullptr)))
+      return KVP_ERR_INVALID_ARG;
+    if (!aligned16(q[l]) || !aligned16(o[l]) || !aligned16(k_cache[own]) || !aligned16(v_cache[own])) return KVP_ERR_UNSUPPORTED;
+  }
+  const int shares = shares_at_most(d, std::min(d->L, MANY_CHUNK_GROUPS), T);
+  if (ws == nullptr || ws_bytes < chunk_bytes(shares, d->dh)) return KVP_ERR_WORKSPACE;
+  if (!aligned16(ws)) return KVP_ERR_UNSUPPORTED;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  static thread_local ChunkParams<MANY_CHUNK_GROUPS> p;
+  p.block_table = block_table;
+  p.lengths = lengths;
+  p.first = first;
+  uint8_t* at = static_cast<uint8_t*>(ws);
+  p.merges = reinterpret_cast<Merge*>(at);
+  p.part_o = reinterpret_cast<float*>(at += merge_bytes(shares));
+  p.part_ml = reinterpret_cast<float*>(at += align256(size_t(shares) * 2 * (2 * TILE) * d->dh * 4));
+  p.B = d->B;
+  p.T = T;
+  p.Hq = d->Hq;
+  p.Hkv = d->Hkv;
+  p.G = d->Hq / d->Hkv;
+  p.page_size = d->page_size;
+  p.max_pages = d->max_pages;
+  p.n_pages = d->n_pages;
+  const int capacity = d->max_pages * d->page_size;
+  p.window = window < capacity ? window : 0;      // (nothing is further back)
+  p.sinks = std::min(sinks, capacity);
+  p.box = d->page_size % 64 == 0 ? 64 : d->page_size % 32 == 0 ? 32 : 16;
+  p.io_f32 = d->dtype == KVP_F32;
+  p.scale_log2 = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
+  // Layers that share a donor, as many as fit a tile's rows for a token.  Those with most layers first.
+  const int per = std::min(CHUNK_MEMBERS, TILE / p.G);
+  p.n_groups = p.n_kinds = 0;
+  int own = 0, l = layer_begin;
+  for (;;) {
+    // the next group
+    ChunkGroup& grp = p.grp[p.n_groups];
+    int n = 0;
+    for (; own < d->L && n == 0; n == 0 ? (++own, l = layer_begin) : 0) {
+      if (donor[own] != own) continue;
+      for (; l < layer_end && n < per; ++l) {
+        if (donor[l] != own) continue;
+        grp.q[n] = q[l];
+        grp.o[n] = o[l];
+        grp.lse[n] = lse[l];
+        ++n;
+      }
+      if (n > 0) break;
+    }
+    if (n > 0) {
+      for (int i = n; i < CHUNK_MEMBERS; ++i) {
+        grp.q[i] = grp.q[0];
+        grp.o[i] = grp.o[0];
+        grp.lse[i] = grp.lse[0];
+      }
+      grp.v_pool = v_cache[own];
+      grp.k_scale = bits8 ? k_scale[own] : nullptr;
+      grp.v_scale = bits8 ? v_scale[own] : nullptr;
+      const uint64_t dims[2] = {uint64_t(d->dh), uint64_t(d->n_pages) * d->Hkv * d->page_size};
+      const uint64_t strides[1] = {uint64_t(d->dh) * (bits8 ? 1 : 2)};
+      const uint32_t box[2] = {bits8 ? uint32_t(d->dh) : 64u, uint32_t(p.box)};
+      rc = make_tensor_map(&grp.map_k, k_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, !bits8);
+      if (rc == KVP_OK) rc = make_tensor_map(&grp.map_v, v_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, !bits8);
+      if (rc != KVP_OK) return rc;
+      const int g = p.n_groups++;
+      p.members[g] = n;
+      int kind = 0;
+      while (kind < p.n_kinds && p.kind_rows[kind] != n * p.G) ++kind;
+      if (kind == p.n_kinds) p.kind_rows[p.n_kinds++] = n * p.G;
+      p.kind[g] = kind;
+    }
+    if (p.n_groups == MANY_CHUNK_GROUPS || (n == 0 && p.n_groups > 0)) {
+      for (int g = p.n_groups; g < MANY_CHUNK_GROUPS; ++g) p.grp[g] = p.grp[0];   // no descriptor is left unset
+      timing_before(KVP_KERNEL_DECODE, stream);
+      const cudaError_t e = p.n_groups <= FEW_CHUNK_GROUPS ? launch_chunk<FEW_CHUNK_GROUPS>(p, d->dh, bits8, shares, stream)
+                                                           : launch_chunk<MANY_CHUNK_GROUPS>(p, d->dh, bits8, shares, stream);
+      timing_after(KVP_KERNEL_DECODE, stream);
+      if (e != cudaSuccess) return KVP_ERR_CUDA;
+      p.n_groups = p.n_kinds = 0;
+    }
+    if (n == 0) return KVP_OK;
+  }
+}

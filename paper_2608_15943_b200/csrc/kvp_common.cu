@@ -39,7 +39,9 @@ int make_tensor_map(CUtensorMap* out, const void* base, int elem_bytes, int rank
     estride[i] = 1;
     if (i + 1 < rank) gstride[i] = strides_bytes[i];
   }
-  const CUtensorMapDataType dt = elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  const CUtensorMapDataType dt = elem_bytes == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                 : elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
   const CUresult r = fn(out, dt, cuuint32_t(rank), const_cast<void*>(base), gdim, gstride, bdim, estride,
                         CU_TENSOR_MAP_INTERLEAVE_NONE,
                         swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
@@ -115,6 +117,9 @@ extern "C" int kvp_device_status(void) {
   if (v < 0) return KVP_ERR_CUDA;
   bad |= v;
   v = kvp::decode_read_status();
+  if (v < 0) return KVP_ERR_CUDA;
+  bad |= v;
+  v = kvp::chunk_read_status();
   if (v < 0) return KVP_ERR_CUDA;
   bad |= v;
   return bad ? KVP_ERR_TIMEOUT : KVP_OK;

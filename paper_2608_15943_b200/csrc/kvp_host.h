@@ -11,7 +11,7 @@
 
 namespace kvp {
 
-// Builds a tiled TMA descriptor over a row-major bf16/fp32 tensor of up to 4 dimensions.
+// Builds a tiled TMA descriptor over a row-major tensor of bytes, bf16 or fp32 of up to 4 dimensions.
 // dims[0] is the innermost (contiguous) extent in elements; strides_bytes[i] is the byte stride
 // of dims[i+1].  box[] is the tile copied per request.  swizzle128 selects the 128-byte swizzle
 // (the inner box extent must then span exactly 128 bytes).  Returns KVP_OK or KVP_ERR_CUDA.
@@ -79,6 +79,7 @@ int gemm_read_status();
 int attn_fwd_read_status();
 int attn_bwd_read_status();
 int decode_read_status();
+int chunk_read_status();
 
 int sm_count();
 

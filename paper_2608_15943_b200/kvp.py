@@ -34,7 +34,9 @@ EXPORTS = ["kvp_status_string", "kvp_device_status", "kvp_launch_count", "kvp_se
            "kvp_proj_fwd", "kvp_proj_bwd", "kvp_proj_bwd_range", "kvp_out_proj_fwd", "kvp_out_proj_bwd", "kvp_attn_fwd", "kvp_attn_bwd",
            "kvp_gemm", "kvp_rmsnorm", "kvp_rope", "kvp_swiglu", "kvp_add", "kvp_decode_workspace_bytes", "kvp_cache_append",
            "kvp_decode", "kvp_decode_static", "kvp_selftest_bounded_wait",
-           "kvp_cache_append_tokens", "kvp_decode8", "kvp_decode8_workspace_bytes"]
+           "kvp_cache_append_tokens", "kvp_decode8", "kvp_decode8_workspace_bytes",
+           "kvp_attn_chunk", "kvp_attn_chunk_workspace_bytes",
+           "kvp_pages_workspace_bytes", "kvp_pages_copy", "kvp_pages_fork", "kvp_pages_resize", "kvp_pages_trim", "kvp_pages_compact"]
 
 
 class KvpError(RuntimeError):
@@ -633,3 +635,142 @@ def decode8(desc, donor, q, k_cache, v_cache, k_scale, v_scale, block_table, len
     _check(lib.kvp_decode8(C.byref(desc), d, float(scale), _ptr_array(q, n), _ptr_array(k_cache, n), _ptr_array(v_cache, n), _ptr_array(k_scale, n),
                            _ptr_array(v_scale, n), block_table.data_ptr(), lengths.data_ptr(), _ptr_array(o, n), _ptr_array(lse, n), int(layer_begin), end, p,
                            size, stream), "kvp_decode8")
+
+
+# ------------------------------------------------------------------------------------------
+# attention of new tokens over the paged cache
+# ------------------------------------------------------------------------------------------
+lib.kvp_attn_chunk_workspace_bytes.restype = C.c_size_t
+lib.kvp_attn_chunk_workspace_bytes.argtypes = [C.POINTER(DecodeDesc), C.c_void_p, C.c_int32]
+lib.kvp_attn_chunk.restype = C.c_int
+lib.kvp_attn_chunk.argtypes = [C.POINTER(DecodeDesc), C.c_void_p, C.c_int32, C.c_void_p, C.c_float, C.c_int32, C.c_int32] + [_PP] * 5 + \
+    [C.c_void_p, C.c_void_p] + [_PP] * 2 + [C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+
+
+def attn_chunk_workspace_bytes(desc: DecodeDesc, donor, T: int) -> int:
+    """kvp_attn_chunk_workspace_bytes: enough for any layer range and for T rows or fewer."""
+    d, entries = _map(desc, donor)
+    return int(lib.kvp_attn_chunk_workspace_bytes(C.byref(desc), d, int(T))) if entries else 0
+
+
+def _fit_pools(desc, k_cache, v_cache, k_scale, v_scale, owners, device) -> None:
+    rows, held = desc.n_pages * desc.Hkv * desc.page_size, (torch.bfloat16,) if k_scale is None else _CODES
+    for what, ts, dtypes, numel in (("k_cache", k_cache, held, rows * desc.dh), ("v_cache", v_cache, held, rows * desc.dh),
+                                    ("k_scale", k_scale, _SCALES, rows // CACHE_BLOCK), ("v_scale", v_scale, _SCALES, rows // CACHE_BLOCK)):
+        if ts is not None:
+            _fit_layers(what, ts, dtypes, numel, owners, device)
+
+
+def attn_chunk(desc, donor, q, k_cache, v_cache, block_table, lengths, o, lse, ws, first=None, scale=0.0, window=0, sinks=0, k_scale=None, v_scale=None,
+               layer_begin=0, layer_end=None):
+    """kvp_attn_chunk: attention of the rows q[l] [T, Hq, dh] over the paged cache that their tokens are in already, into o[l] and the
+    log-sum-exp lse[l] [T, Hq].  Sequence b has rows first[b] .. first[b+1]-1 (int32 [B + 1]; None: one token each, T == B) at the
+    positions before lengths[b]; a row sees the tokens up to its own, with window > 0 the last `window` of them and the first `sinks`
+    alone.  With k_scale, v_scale the cache is the 8-bit one.  ws: attn_chunk_workspace_bytes.  Tensors are contiguous, of the
+    documented sizes, on the current device: ValueError otherwise."""
+    device, stream = _call_place()
+    end = desc.L if layer_end is None else int(layer_end)
+    layers, owners = _layer_range(desc, donor, int(layer_begin), end)
+    T = next((int(q[l].shape[0]) if q[l].dim() else 0 for l in layers if l < len(q) and q[l] is not None), 0)
+    if T == 0 and any(l >= len(ts) or ts[l] is None for ts in (q, o, lse) for l in layers):
+        _check(ERR_INVALID_ARG, "kvp_attn_chunk")     # (by their addresses the library cannot tell missing rows from none)
+    io = _io(desc)
+    for what, ts, dtypes, numel in (("q", q, io, T * desc.Hq * desc.dh), ("o", o, io, T * desc.Hq * desc.dh), ("lse", lse, (torch.float32,), T * desc.Hq)):
+        _fit_layers(what, ts, dtypes, numel, layers, device)
+    _fit_pools(desc, k_cache, v_cache, k_scale, v_scale, owners, device)
+    for what, t, numel in (("block_table", block_table, desc.B * desc.max_pages), ("lengths", lengths, desc.B), ("first", first, desc.B + 1)):
+        if t is not None:
+            _fit(what, t, _I32, numel, device)
+    if ws is not None:
+        _fit("ws", ws, (ws.dtype,), ws.numel(), device)
+    d, n = _map(desc, donor)
+    array = lambda ts: None if ts is None else _ptr_array(ts, n)
+    p, size = _ws(ws)
+    _check(lib.kvp_attn_chunk(C.byref(desc), d, T, _ptr(first), float(scale), int(window), int(sinks), _ptr_array(q, n), _ptr_array(k_cache, n),
+                              _ptr_array(v_cache, n), array(k_scale), array(v_scale), _ptr(block_table), _ptr(lengths), _ptr_array(o, n),
+                              _ptr_array(lse, n), int(layer_begin), end, p, size, stream), "kvp_attn_chunk")
+
+
+# ------------------------------------------------------------------------------------------
+# pages of the cache
+# ------------------------------------------------------------------------------------------
+_POOLS = [_PP] * 4
+lib.kvp_pages_workspace_bytes.restype = C.c_size_t
+lib.kvp_pages_workspace_bytes.argtypes = [C.POINTER(DecodeDesc)]
+lib.kvp_pages_copy.restype = C.c_int
+lib.kvp_pages_copy.argtypes = [C.POINTER(DecodeDesc), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p] + _POOLS + [C.c_void_p]
+lib.kvp_pages_fork.restype = C.c_int
+lib.kvp_pages_fork.argtypes = [C.POINTER(DecodeDesc)] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+lib.kvp_pages_resize.restype = C.c_int
+lib.kvp_pages_resize.argtypes = [C.POINTER(DecodeDesc)] + [C.c_void_p] * 7 + [C.c_size_t] + _POOLS + [C.c_void_p]
+lib.kvp_pages_trim.restype = C.c_int
+lib.kvp_pages_trim.argtypes = [C.POINTER(DecodeDesc), C.c_int32, C.c_int32] + [C.c_void_p] * 4
+lib.kvp_pages_compact.restype = C.c_int
+lib.kvp_pages_compact.argtypes = [C.POINTER(DecodeDesc)] + [C.c_void_p] * 6 + [C.c_size_t] + _POOLS + [C.c_void_p]
+
+
+def pages_workspace_bytes(desc: DecodeDesc) -> int:
+    """kvp_pages_workspace_bytes: enough for each of the calls below."""
+    return int(lib.kvp_pages_workspace_bytes(C.byref(desc)))
+
+
+def _fit_book(desc, device, ws=None, **tensors) -> None:
+    sizes = dict(block_table=desc.B * desc.max_pages, refs=desc.n_pages, lacking=1, used=1)
+    for what, t in tensors.items():
+        if t is not None:
+            _fit(what, t, _I32, sizes.get(what, desc.B), device)
+    if ws is not None:
+        _fit("ws", ws, (ws.dtype,), ws.numel(), device)
+
+
+def _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device):
+    _fit_pools(desc, k_cache, v_cache, k_scale, v_scale, _layer_range(desc, donor)[1], device)
+    d, n = _map(desc, donor)
+    return d, [None if ts is None else _ptr_array(ts, n) for ts in (k_cache, v_cache, k_scale, v_scale)]
+
+
+def pages_copy(desc, donor, src, dst, k_cache, v_cache, k_scale=None, v_scale=None):
+    """kvp_pages_copy: the pages src[i] go to dst[i] (int32, as many), in all owner layers.  No page may be the target of two, nor a
+    target and a source.  Tensors of these calls are contiguous, of the documented sizes, on the current device: ValueError otherwise."""
+    device, stream = _call_place()
+    n = src.numel()
+    _fit("src", src, _I32, n, device)
+    _fit("dst", dst, _I32, n, device)
+    d, pools = _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device)
+    _check(lib.kvp_pages_copy(C.byref(desc), d, n, _ptr(src), _ptr(dst), *pools, stream), "kvp_pages_copy")
+
+
+def pages_fork(desc, parent, refs, block_table, lengths, ws):
+    """kvp_pages_fork: row b goes on from what row parent[b] was (its own number: it stays; -1: it ends).  Pages are shared, none is
+    copied; refs, block_table and lengths are updated in place."""
+    device, stream = _call_place()
+    _fit_book(desc, device, ws, parent=parent, refs=refs, block_table=block_table, lengths=lengths)
+    p, size = _ws(ws)
+    _check(lib.kvp_pages_fork(C.byref(desc), _ptr(parent), _ptr(refs), _ptr(block_table), _ptr(lengths), p, size, stream), "kvp_pages_fork")
+
+
+def pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, ws, k_cache, v_cache, k_scale=None, v_scale=None):
+    """kvp_pages_resize: rows grow and shrink to new_lengths; a row that grows inside a shared page gets a copy of it.  lacking (int32
+    [1]) receives 0, or what is short (then nothing is changed): the pages lacking, -1 for a length out of range."""
+    device, stream = _call_place()
+    _fit_book(desc, device, ws, new_lengths=new_lengths, refs=refs, block_table=block_table, lengths=lengths, lacking=lacking)
+    d, pools = _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device)
+    p, size = _ws(ws)
+    _check(lib.kvp_pages_resize(C.byref(desc), d, _ptr(new_lengths), _ptr(refs), _ptr(block_table), _ptr(lengths), _ptr(lacking), p, size, *pools, stream),
+           "kvp_pages_resize")
+
+
+def pages_trim(desc, window, sinks, refs, block_table, lengths):
+    """kvp_pages_trim: frees the pages that no later token sees with this window and so many first tokens."""
+    device, stream = _call_place()
+    _fit_book(desc, device, refs=refs, block_table=block_table, lengths=lengths)
+    _check(lib.kvp_pages_trim(C.byref(desc), int(window), int(sinks), _ptr(refs), _ptr(block_table), _ptr(lengths), stream), "kvp_pages_trim")
+
+
+def pages_compact(desc, donor, refs, block_table, lengths, used, ws, k_cache, v_cache, k_scale=None, v_scale=None):
+    """kvp_pages_compact: the used pages become pages 0 .. used-1; used (int32 [1]) receives their number."""
+    device, stream = _call_place()
+    _fit_book(desc, device, ws, refs=refs, block_table=block_table, lengths=lengths, used=used)
+    d, pools = _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device)
+    p, size = _ws(ws)
+    _check(lib.kvp_pages_compact(C.byref(desc), d, _ptr(refs), _ptr(block_table), _ptr(lengths), _ptr(used), p, size, *pools, stream), "kvp_pages_compact")
