@@ -8,9 +8,12 @@
 // second kernel.  So one long context occupies the whole device, and prompts of any lengths leave no SM behind.
 //   warp 0        TMA producer: K and V blocks, page by page (8-bit cache: the codes into a ring of their own, and their scales)
 //   warps 1, 2    tcgen05.mma issuers, one per tile: S = Q K^T into one of two 64-column score buffers, O += P V with P from TMEM
-//   warp 3        gathers the query rows of the next unit, and looks through the V blocks that not every row sees in full
-//   warps 4-11    softmax, a warpgroup per tile, a thread per row; then O out of TMEM to the outputs or to the unit's partial sums
-//   warps 12-15   (8-bit cache only) codes times scales to bf16, which holds every such product exactly
+//   warp 3        lays out the CTA's pieces of units, and looks through the V blocks that not every row sees in full
+//   warps 4-11    softmax, a warpgroup per tile, a thread per row; then O out of TMEM to the outputs or to the unit's partial sums,
+//                 while the rows of the next piece come into shared memory.  Where a unit has one tile alone, both warpgroups have
+//                 it, take every other step each, and put their two sums together at the end.
+//   warps 12-19   (8-bit cache only) V's codes to f16, which holds them exactly.  K's are operands as they are; the scales are applied
+//                 to the scores and to the weights of V.
 // Masked places.  A score that a row does not see is -infinity before the maximum.  In V, rows that no row of the unit sees (slots
 // behind the sequence, freed pages before the window: anything may be there) are not read and are zeros in shared memory.  A
 // visible row of V with an infinity or NaN in it must reach the rows that see it and no other, which 0 * NaN in a matrix product
@@ -40,24 +43,37 @@ constexpr int REST = 3, LEAST_SHARE = 8;
 
 __device__ int g_chunk_status;
 
+constexpr int PIECES = 4, PIECES_BYTES = 640;       // the ring of pieces
+// The scales of a step of the 8-bit cache, a block of 16 keys each: K's and V's powers of two, and V's exponents.  A step's stay until
+// its product has been issued: K is asked for one step ahead of V at the most, and V's rings hold fewer steps than there are places.
+struct Scales {
+  float4 k, v, e;
+};
+constexpr int SCALES = 16;
+
 template <int DH, bool BITS8>
 struct ChunkSmem {
-  static constexpr int K_STAGES = BITS8 ? (DH == 128 ? 3 : 4) : (DH == 128 ? 5 : 8);
-  static constexpr int V_STAGES = K_STAGES;
-  static constexpr int RAW_STAGES = BITS8 ? (DH == 128 ? 8 : 16) : 0;
-  static constexpr int Q_BYTES = TILE * DH * 2, KV_BYTES = STEP * DH * 2, RAW_BYTES = STEP * DH;
+  static constexpr int K_STAGES = BITS8 ? (DH == 128 ? 6 : 8) : (DH == 128 ? 5 : 8);
+  static constexpr int V_STAGES = BITS8 ? 4 : K_STAGES;
+  static constexpr int RAW_STAGES = BITS8 ? (DH == 128 ? 6 : 8) : 0;                       // V's codes
+  static constexpr int Q_BYTES = TILE * DH * 2, V_BYTES = STEP * DH * 2, K_BYTES = BITS8 ? STEP * DH : V_BYTES, RAW_BYTES = STEP * DH;
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
-  static constexpr int OFF_V = OFF_K + K_STAGES * KV_BYTES;
-  static constexpr int OFF_RAW = OFF_V + V_STAGES * KV_BYTES;
+  static constexpr int OFF_V = OFF_K + K_STAGES * K_BYTES;
+  static constexpr int OFF_RAW = OFF_V + V_STAGES * V_BYTES;
   static constexpr int OFF_BAR = OFF_RAW + RAW_STAGES * RAW_BYTES;
-  static constexpr int OFF_BAD = OFF_BAR + 640;                 // [V_STAGES][4] rows of V that are left to the softmax threads
-  static constexpr int OFF_SCALE = OFF_BAD + V_STAGES * 32;     // [RAW_STAGES] four bytes each
-  static constexpr int OFF_SHARE = OFF_SCALE + RAW_STAGES * 4;
-  static constexpr int TOTAL = OFF_SHARE + 64 + 1024;
-  static constexpr int THREADS = BITS8 ? 512 : 384;
+  static constexpr int BARRIERS = 2 + 2 * K_STAGES + 3 * V_STAGES + 14 + 2 * PIECES + 2 * RAW_STAGES;
+  static constexpr int OFF_BAD = OFF_BAR + (BARRIERS + 2) / 2 * 16;   // [V_STAGES][4] rows of V that are left to the softmax threads
+  static constexpr int OFF_SCALE = OFF_BAD + V_STAGES * 32;     // [SCALES]
+  static constexpr int OFF_PIECES = OFF_SCALE + (BITS8 ? SCALES * int(sizeof(Scales)) : 0);
+  static constexpr int TOTAL = OFF_PIECES + PIECES_BYTES + 1024;      // room for the alignment
+  static constexpr int THREADS = BITS8 ? 640 : 384;
 };
 static_assert(ChunkSmem<128, false>::TOTAL <= 232448 && ChunkSmem<128, true>::TOTAL <= 232448, "shared memory of a CTA");
+// (two groups of warps convert every other step each, so that a stage always is the same group's)
+static_assert(ChunkSmem<128, true>::V_STAGES % 2 == 0 && ChunkSmem<64, true>::RAW_STAGES % 2 == 0 && ChunkSmem<128, true>::RAW_STAGES % 2 == 0 &&
+                  ChunkSmem<64, true>::RAW_STAGES + ChunkSmem<64, true>::V_STAGES + 1 < SCALES && ChunkSmem<128, true>::RAW_STAGES + ChunkSmem<128, true>::V_STAGES + 1 < SCALES,
+              "rings of the 8-bit cache");
 
 // A unit that more than one share holds, noted by the CTA of its second share
 struct Merge {
@@ -262,67 +278,99 @@ __device__ __forceinline__ bool find_share(const ChunkSizes& p, const long long*
   return there;
 }
 
-// A share's pieces, one after the other; every role walks them by itself.
+// A share's pieces, one after the other: what the roles need of them, laid out by warp 3 in a ring in shared memory.
 struct Piece {
-  int g, hk, b, pair, R;
-  Span span;
-  Walked w;
-  int c0, c1;            // steps of the unit
-  bool whole;            // the unit has no other piece
-  int slot;              // place of its partial sums
-  __device__ __forceinline__ int n() const { return c1 - c0; }
-  __device__ __forceinline__ int n_a() const { return max(0, min(c1, w.n_a) - c0); }
-  __device__ __forceinline__ bool has_b() const { return ((long long)pair * 2 + 1) * TILE < (long long)span.n * R; }
-  __device__ __forceinline__ int n_of(int x) const { return x == 0 ? n_a() : has_b() ? n() : 0; }
-  __device__ __forceinline__ int block(int i) const {       // of the piece's step i
-    const int c = c0 + i;
-    return c < w.sink_blocks ? c : w.from + c - w.sink_blocks;
-  }
-  // not every row of the pair sees all keys of the block
-  __device__ __forceinline__ bool masked(const ChunkSizes& p, int block) const { return masked(p, block, w.pos_first, w.pos_last); }
-  static __device__ __forceinline__ bool masked(const ChunkSizes& p, int block, int pos_first, int pos_last) {
-    const int key = block * STEP;
-    return key + STEP - 1 > pos_first || (p.window > 0 && pos_last - p.window >= key && key + STEP > p.sinks);
-  }
-  // no row of the pair sees any of n keys from `key` on
+  int n;                       // steps; 0: there are no more pieces
+  int g, hk, b;
+  int R, row0;                 // rows of a token; row of q of the sequence's first token
+  int pos0;                    // its position
+  int duo;                     // one tile: both halves of the CTA have its rows, and take every other step each
+  int n_x[2];                  // steps that each half takes
+  int rows[2];                 // rows of its tile
+  int token[2], in[2];         // the tile's first: its token, and which of the token's rows
+  int pos_first, pos_last;     // positions of the unit's rows
+  int sinks, at_sinks, at;     // step i is block at_sinks + i for i < sinks, at + i from there on
+  int2 clear, clear_x[2];      // steps i, x <= i < y, in which all rows (the half's rows) see every key
+  int whole, slot;             // the unit has no other piece; otherwise the place of its partial sums
+  __device__ __forceinline__ int block(int i) const { return (i < sinks ? at_sinks : at) + i; }
+  // no row of the unit sees any of n keys from `key` on
   __device__ __forceinline__ bool unseen(const ChunkSizes& p, int key, int n) const {
-    return key > w.pos_last || (p.window > 0 && key + n - 1 <= w.pos_first - p.window && key >= p.sinks);
+    return key > pos_last || (p.window > 0 && key + n - 1 <= pos_first - p.window && key >= p.sinks);
   }
 };
+static_assert(PIECES * sizeof(Piece) <= PIECES_BYTES && sizeof(Piece) % 8 == 0, "the ring of pieces");
+
 struct Pieces {
   int g, hk, b, pair, off, left;
   __device__ __forceinline__ explicit Pieces(const Share& s) : g(s.g), hk(s.hk), b(s.b), pair(s.pair), off(s.off), left(s.left) {}
-  __device__ __forceinline__ bool next(const ChunkSizes& p, Piece& out) {
+  // The next piece, by a warp together; lane 0 writes it down.
+  __device__ __forceinline__ void next(const ChunkSizes& p, Piece& out) {
+    const int lane = lane_id();
     while (left > 0) {
-      out.g = g;
-      out.hk = hk;
-      out.b = b;
-      out.pair = pair;
-      out.R = p.members[g] * p.G;
-      out.span = span_of(p, b);
-      const int pairs = pairs_of(out.span, out.R);
-      if (pair >= pairs) {                 // (a sequence without rows, or the last pair is done)
+      const int R = p.members[g] * p.G;
+      const Span span = span_of(p, b);
+      if (pair >= pairs_of(span, R)) {        // on to the next sequence that has rows
         pair = 0;
-        if (++b == p.B) {
-          b = 0;
-          if (++hk == p.Hkv) {
-            hk = 0;
-            ++g;
+        ++b;
+        for (;;) {
+          if (b >= p.B) {
+            b = 0;
+            if (++hk == p.Hkv) {
+              hk = 0;
+              ++g;
+            }
           }
+          const uint32_t some = __ballot_sync(0xffffffffu, b + lane < p.B && span_of(p, min(b + lane, p.B - 1)).n > 0);
+          b += some != 0 ? __ffs(some) - 1 : 32;
+          if (some != 0) break;
         }
         continue;
       }
-      out.w = walked(p, out.span, out.R, pair);
-      out.c0 = off;
-      out.c1 = min(out.w.n, off + left);
-      out.whole = off == 0 && out.c1 == out.w.n;
-      out.slot = 2 * int(blockIdx.x) + (off == 0 ? 1 : 0);
-      left -= min(left, out.w.n + REST - off);
+      const Walked w = walked(p, span, R, pair);
+      const int c0 = off, c1 = min(w.n, off + left);
+      const int now = pair;
+      left -= min(left, w.n + REST - off);
       off = 0;
       ++pair;
-      if (out.c0 < out.c1) return true;
+      if (c0 >= c1) continue;
+      if (lane == 0) {
+        const long long row = (long long)now * 2 * TILE, n_rows = (long long)span.n * R;
+        const bool duo = row + TILE >= n_rows;
+        auto clear = [&](int pos_first, int pos_last) {      // (blocks of first tokens count as masked)
+          const int begin = p.window > 0 && pos_last >= p.window ? (pos_last - p.window) / STEP + 1 : 0, end = (pos_first + 1) / STEP;
+          return make_int2(w.sink_blocks + max(begin - w.from, 0) - c0, w.sink_blocks + end - w.from - c0);
+        };
+        out.g = g;
+        out.hk = hk;
+        out.b = b;
+        out.R = R;
+        out.row0 = span.row0;
+        out.pos0 = span.pos0;
+        out.duo = duo;
+        for (int x = 0; x < 2; ++x) {
+          const long long first = row + (duo ? 0 : x * TILE);
+          out.rows[x] = int(min((long long)TILE, n_rows - first));
+          out.token[x] = int(div_places(first, R));
+          out.in[x] = int(first - (long long)out.token[x] * R);
+        }
+        const int n = c1 - c0;
+        out.n_x[0] = duo ? (n + 1) / 2 : max(0, min(c1, w.n_a) - c0);
+        out.n_x[1] = duo ? n / 2 : n;
+        out.pos_first = w.pos_first;
+        out.pos_last = w.pos_last;
+        out.sinks = w.sink_blocks - c0;
+        out.at_sinks = c0;
+        out.at = w.from - w.sink_blocks + c0;
+        out.clear = clear(w.pos_first, w.pos_last);
+        out.clear_x[0] = duo ? out.clear : clear(w.pos_first, w.pos_last_a);
+        out.clear_x[1] = duo ? out.clear : clear(span.pos0 + out.token[1], w.pos_last);
+        out.whole = c0 == 0 && c1 == w.n;
+        out.slot = 2 * int(blockIdx.x) + (c0 == 0 ? 1 : 0);
+        out.n = n;
+      }
+      return;
     }
-    return false;
+    if (lane == 0) out.n = 0;
   }
 };
 
@@ -334,17 +382,69 @@ __device__ __forceinline__ uint32_t tmem_ld_x1(uint32_t taddr) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
   return r;
 }
+__device__ __forceinline__ void tmem_st_x4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ float4 tmem_ld_x4(uint32_t taddr) {
+  uint32_t a, b, c, d;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(taddr) : "memory");
+  tmem_ld_wait();
+  return make_float4(__uint_as_float(a), __uint_as_float(b), __uint_as_float(c), __uint_as_float(d));
+}
 // A bounded wait of a whole warp: true in all lanes or in none (the roles that use warp-wide operations go on or leave together).
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); }
-// two e4m3 numbers times 2^e as bf16: exact, but for what is beyond its range
-__device__ __forceinline__ uint32_t widen8(uint32_t two, float power) {
-  const float2 f = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(two)));
-  return pack_bf16(f.x * power, f.y * power);
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t not_finite(uint32_t two) {   // of two bf16 numbers
-  return uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u);
+__device__ __forceinline__ uint32_t f32x4_to_e5m2(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return uint32_t(lo) | uint32_t(hi) << 16;
 }
+// of bf16 numbers
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u); }
 __device__ __forceinline__ uint32_t not_finite(const uint4& v) { return not_finite(v.x) | not_finite(v.y) | not_finite(v.z) | not_finite(v.w); }
+// Sixteen e4m3 numbers: whether one of them is NaN, and all times 2^-8 as f16.  The bits of a finite one, its exponent and mantissa
+// one place down from a half's upper byte, are that f16 number (subnormal ones too).  (The conversion instruction takes some
+// seven others, and NaN with it: decode's loop over drafts of 16 sequences 372 us with it for K and V.)
+__device__ __forceinline__ uint32_t any_nan(const uint4& c) {
+  const uint32_t m = 0x7f7f7f7fu, one = 0x01010101u;
+  return (((c.x & m) + one) | ((c.y & m) + one) | ((c.z & m) + one) | ((c.w & m) + one)) & 0x80808080u;
+}
+__device__ __forceinline__ uint32_t widen(uint32_t w, int upper) {
+  const uint32_t apart = __byte_perm(w, 0, upper ? 0x3424 : 0x1404);     // a code in the upper byte of each half
+  return (apart & 0x80008000u) | (apart >> 1 & 0x3f803f80u);
+}
+__device__ __forceinline__ void widen16(const uint4& c, uint4 (&out)[2]) {
+  out[0] = make_uint4(widen(c.x, 0), widen(c.x, 1), widen(c.y, 0), widen(c.y, 1));
+  out[1] = make_uint4(widen(c.z, 0), widen(c.z, 1), widen(c.w, 0), widen(c.w, 1));
+}
+__device__ __forceinline__ uint32_t nan_too(uint32_t two) {       // 480 * 2^-8 is what NaN's bits come out as
+  return two | ((two & 0x3f80u) == 0x3f80u ? 0x7f80u : 0) | ((two & 0x3f800000u) == 0x3f800000u ? 0x7f800000u : 0);
+}
+__device__ __forceinline__ void put_nan(uint4 (&out)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) out[i] = make_uint4(nan_too(out[i].x), nan_too(out[i].y), nan_too(out[i].z), nan_too(out[i].w));
+}
+// D[tmem] (+)= A[smem] * B[smem], 8-bit floating-point numbers
+__device__ __forceinline__ void umma8_ss_w(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+  asm volatile(
+      "{\n"
+      " .reg .pred p, q;\n"
+      " .reg .b64 da, db;\n"
+      " mov.b64 da, {%1, %3};\n"
+      " mov.b64 db, {%2, %3};\n"
+      " setp.ne.b32 p, %5, 0;\n"
+      " setp.ne.b32 q, %6, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+// upper word of the descriptor of a K-major tile of 64-byte rows with the 64-byte swizzle: 512 bytes between groups of eight rows
+constexpr uint32_t DESC_HI_SW64 = (512u >> 4) | (1u << 14) | (4u << 29);
 
 // O of this thread's row += p_j V_j for the keys `left` of a block, from the pool itself.  P is in TMEM by now, as the product takes
 // it; `fresh`: O holds nothing yet.  A warp together.
@@ -364,22 +464,24 @@ __device__ __noinline__ void add_rows(const ChunkSizes& p, const ChunkGroup& grp
       const int j = __ffsll(rest) - 1, key = key0 + j;
       const uint32_t two = tmem_ld_x1(tm_p + (j >> 1));
       tmem_ld_wait();
-      const float pj = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+      const float2 pf = f16x2_to_f32(two);
+      const float pj = BITS8 ? (j & 1 ? pf.y : pf.x) : __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
       const int page = p.block_table[size_t(b) * p.max_pages + key / p.page_size];
       const bool takes = unsigned(page) < unsigned(p.n_pages) && (seen >> j & 1) != 0;
       const size_t row = takes ? (size_t(page) * p.Hkv + hk) * p.page_size + key % p.page_size : 0;
-      float power = 1.f;
-      if (BITS8) power = __uint_as_float(power_bits(exponent_of_byte(grp.v_scale[row / CACHE_BLOCK])));
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        uint32_t v;
-        if (BITS8)
-          v = widen8(reinterpret_cast<const uint16_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i], power);
-        else
-          v = reinterpret_cast<const uint32_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i];
+        float2 v;
+        if (BITS8) {
+          v = f16x2_to_f32(e4m3x2_to_f16x2(reinterpret_cast<const uint16_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i]));
+          v.x *= 0.00390625f, v.y *= 0.00390625f;
+        } else {
+          const uint32_t bits = reinterpret_cast<const uint32_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i];
+          v = make_float2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u));
+        }
         if (takes) {
-          acc[2 * i] = __float_as_uint(fmaf(pj, __uint_as_float(v << 16), __uint_as_float(acc[2 * i])));
-          acc[2 * i + 1] = __float_as_uint(fmaf(pj, __uint_as_float(v & 0xffff0000u), __uint_as_float(acc[2 * i + 1])));
+          acc[2 * i] = __float_as_uint(fmaf(pj, v.x, __uint_as_float(acc[2 * i])));
+          acc[2 * i + 1] = __float_as_uint(fmaf(pj, v.y, __uint_as_float(acc[2 * i + 1])));
         }
       }
       __syncwarp();      // (the next load of TMEM is one of the whole warp)
@@ -400,51 +502,58 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* const q_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);
-  uint64_t* const q_empty = q_full + 1;         // 2 arrivals: both issuing warps are done with the query tiles
-  uint64_t* const k_full = q_empty + 1;         // [KS]
+  uint64_t* const q_full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR);   // [2] per tile: its rows have come (4 arrivals)
+  uint64_t* const k_full = q_full + 2;          // [KS]
   uint64_t* const k_empty = k_full + KS;        // [KS]
   uint64_t* const v_full = k_empty + KS;        // [VS]
   uint64_t* const v_empty = v_full + VS;        // [VS]
   uint64_t* const v_fixed = v_empty + VS;       // [VS] warp 3 has looked through the block (8 bits: the converting warps have, at v_full)
   uint64_t* const s_full = v_fixed + VS;        // [2][2] per tile and score buffer
-  uint64_t* const p_ready = s_full + 4;         // [2][2] (128 arrivals)
+  uint64_t* const p_ready = s_full + 4;         // [2][2] (4 arrivals)
   uint64_t* const pv_done = p_ready + 4;        // [2] one completion per step's product
   uint64_t* const o_done = pv_done + 2;         // [2] a piece's last product
-  uint64_t* const raw_full = o_done + 2;        // [RS]
-  uint64_t* const raw_empty = raw_full + RS;    // [RS] (128 arrivals)
-  static_assert((2 + 2 * KS + 3 * VS + 12 + 2 * RS) * 8 <= 632, "barriers");
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + 632);
+  uint64_t* const duo_ml = o_done + 2;          // the halves of a duo have left their rows' maxima and sums (8 arrivals),
+  uint64_t* const duo_free = duo_ml + 1;        // and have read each other's O (8 arrivals)
+  uint64_t* const piece_full = duo_free + 1;    // [PIECES]
+  uint64_t* const piece_empty = piece_full + PIECES;   // [PIECES] (an arrival of each warp that reads them)
+  uint64_t* const raw_full = piece_empty + PIECES;     // [RS]
+  uint64_t* const raw_empty = raw_full + RS;    // [RS] (4 arrivals)
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(q_full + L::BARRIERS);
+  Piece* const s_pieces = reinterpret_cast<Piece*>(smem + L::OFF_PIECES);
   unsigned long long* const s_bad = reinterpret_cast<unsigned long long*>(smem + L::OFF_BAD);
-  uint8_t* const s_scale = smem + L::OFF_SCALE;
-  int* const s_share = reinterpret_cast<int*>(smem + L::OFF_SHARE);
+  Scales* const s_scales = reinterpret_cast<Scales*>(smem + L::OFF_SCALE);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* const err = &g_chunk_status;
 
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 2);
+    mbar_init(duo_ml, 8);
+    mbar_init(duo_free, 8);
+    for (int i = 0; i < PIECES; ++i) {
+      mbar_init(&piece_full[i], 1);
+      mbar_init(&piece_empty[i], L::THREADS / 32 - 1);
+    }
     for (int i = 0; i < KS; ++i) {
-      mbar_init(&k_full[i], BITS8 ? 128 : 1);
+      mbar_init(&k_full[i], 1);
       mbar_init(&k_empty[i], 2);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(&v_full[i], BITS8 ? 128 : 1);
-      mbar_init(&v_empty[i], 2);
+      mbar_init(&v_full[i], BITS8 ? 4 : 1);
+      mbar_init(&v_empty[i], BITS8 ? 2 : 3);    // both issuing warps, and warp 3: nobody may fall a round of the ring behind
       mbar_init(&v_fixed[i], 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_ready[i], 128);
+      mbar_init(&p_ready[i], 4);
     }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 4);
       mbar_init(&pv_done[i], 1);
       mbar_init(&o_done[i], 1);
     }
     for (int i = 0; i < RS; ++i) {
       mbar_init(&raw_full[i], 1);
-      mbar_init(&raw_empty[i], 128);
+      mbar_init(&raw_empty[i], 4);
     }
     mbar_fence_init();
   }
@@ -457,54 +566,56 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   grid_dep_wait();
-  {
-    long long* const sums = reinterpret_cast<long long*>(smem + L::OFF_Q);   // (no query has been loaded)
-    const int n32 = (p.B + 31) / 32;
-    list_sums(p, sums, n32, L::THREADS / 32);
-    if (warp == 0) {
-      Share s{0, 0, 0, 0, 0, 0};
-      if (!find_share(p, sums, n32, s)) s.left = 0;
-      if (lane == 0) {
-        s_share[0] = s.g;
-        s_share[1] = s.hk;
-        s_share[2] = s.b;
-        s_share[3] = s.pair;
-        s_share[4] = s.off;
-        s_share[5] = s.left;
-      }
-    }
-    fence_proxy_async_smem();     // (at 16384 sequences the sums reach into the first stage of K)
-    __syncthreads();
-  }
-  Pieces pieces(Share{s_share[0], s_share[1], s_share[2], s_share[3], s_share[4], s_share[5]});
-  Piece piece;
+  long long* const sums = reinterpret_cast<long long*>(smem + L::OFF_Q);   // (no query has been loaded)
+  const int n32 = (p.B + 31) / 32;
+  list_sums(p, sums, n32, L::THREADS / 32);
+  Share share{0, 0, 0, 0, 0, 0};
+  if (warp == 3 && !find_share(p, sums, n32, share)) share.left = 0;
+  fence_proxy_async_smem();     // (at 16384 sequences the sums reach into the first stage of K)
+  __syncthreads();
   uint32_t at = 0;      // steps of earlier pieces: ring positions of this piece's first
+  uint32_t it = 0;      // pieces so far
   bool ok = true;
+  // The piece that the role is at; it stays in the ring until the role gives it back.
+  auto piece_at = [&](uint32_t i) -> const Piece* {
+    ok = ok && warp_wait(&piece_full[i % PIECES], (i / PIECES) & 1, err);
+    const Piece* const of = s_pieces + i % PIECES;
+    return ok && of->n > 0 ? of : nullptr;
+  };
+  auto give_back = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&piece_empty[it % PIECES]);
+    ++it;
+  };
   // tile X: score buffer u at [X*128 + u*64, +64) with P over its first 32 columns; O at [256 + X*128, +DH)
 
+  // (8-bit cache: 96 registers a thread at launch, 61440 in all, go to 128 x 64 here, 256 x 144 to the softmax, 256 x 64 to the conversion)
+  if (warp < 4) {
+    if constexpr (BITS8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  }
   if (warp == 0) {
     // ------------------------------ K and V, or their codes ------------------------------
-    uint32_t raw = 0;                       // blocks of codes requested so far
-    while (ok && pieces.next(p, piece)) {
-      const ChunkGroup& grp = p.grp[piece.g];
-      const int n = piece.n();
-      // Four lanes a step, a block of 16 keys each: rows of the pool (-1: no row of the pair sees any of the box's keys), and scales.
+    const uint32_t leader = elect_one();    // the whole warp runs the loop; one lane issues
+    while (const Piece* const piece = piece_at(it)) {
+      const ChunkGroup& grp = p.grp[piece->g];
+      const int n = piece->n, hk = piece->hk;
+      // Four lanes a step, a block of 16 keys each: rows of the pool (-1: no row of the unit sees any of the box's keys), and scales.
       // Pages are asked for two batches ahead, scales one.
       const int sub = lane & 3;
       const int none = p.n_pages * p.Hkv * p.page_size;        // (behind the pool: TMA fills in zeros)
-      auto box_key = [&](int i) { return (piece.block(i) * STEP + sub * 16) / p.box * p.box; };
+      auto box_key = [&](int i) { return (piece->block(i) * STEP + sub * 16) / p.box * p.box; };
       auto page_of = [&](int batch) -> int {
         const int i = batch * BATCH + (lane >> 2);
         if (i >= n) return -1;
         const int key = box_key(i);
-        if (piece.unseen(p, key, p.box)) return -1;
-        const int page = p.block_table[size_t(piece.b) * p.max_pages + key / p.page_size];
+        if (piece->unseen(p, key, p.box)) return -1;
+        const int page = p.block_table[size_t(piece->b) * p.max_pages + key / p.page_size];
         return unsigned(page) < unsigned(p.n_pages) ? page : -2;
       };
       auto scales_of = [&](int batch, int page) -> uint32_t {  // K's and V's
         const int i = batch * BATCH + (lane >> 2);
         if (!BITS8 || i >= n || page < 0) return 0x7f7f;
-        const size_t block = (size_t(page) * p.Hkv + piece.hk) * (p.page_size / CACHE_BLOCK) + (piece.block(i) * STEP + sub * 16) % p.page_size / CACHE_BLOCK;
+        const size_t block = (size_t(page) * p.Hkv + hk) * (p.page_size / CACHE_BLOCK) + (piece->block(i) * STEP + sub * 16) % p.page_size / CACHE_BLOCK;
         return grp.k_scale[block] | uint32_t(grp.v_scale[block]) << 8;
       };
       int page = page_of(0), page1 = page_of(1);
@@ -514,32 +625,37 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         const uint32_t scales1 = scales_of(batch + 1, page1);
         const int mine = batch * BATCH + (lane >> 2);
         const int key = mine < n ? box_key(mine) : 0;
-        const int row = page >= 0 ? (page * p.Hkv + piece.hk) * p.page_size + key % p.page_size : none;
-        const bool issues = page != -1 && sub % (p.box / 16) == 0;
+        const int row = page >= 0 ? (page * p.Hkv + hk) * p.page_size + key % p.page_size : none;
+        const uint32_t issues = __ballot_sync(0xffffffffu, page != -1 && sub % (p.box / 16) == 0);
         for (int i = batch * BATCH; i < min(n, (batch + 1) * BATCH) && ok; ++i) {
-          const bool load = issues && mine == i;
-          const uint32_t bytes = uint32_t(__popc(__ballot_sync(0xffffffffu, load))) * p.box * DH * (BITS8 ? 1 : 2);
+          const int lane0 = (i - batch * BATCH) * 4;
+          const uint32_t boxes = issues >> lane0 & 15;
+          const uint32_t bytes = uint32_t(__popc(boxes)) * p.box * DH * (BITS8 ? 1 : 2);
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
             const CUtensorMap* const map = v ? &grp.map_v : &grp.map_k;
+            const uint32_t j = at + i, ring = !v ? KS : BITS8 ? RS : VS, s = j % ring;
+            uint64_t* const full = !v ? &k_full[s] : BITS8 ? &raw_full[s] : &v_full[s];
+            if (!warp_wait(!v ? &k_empty[s] : BITS8 ? &raw_empty[s] : &v_empty[s], ((j / ring) & 1) ^ 1, err)) { ok = false; break; }
             if constexpr (BITS8) {
-              const uint32_t s = raw % RS;
-              if (!warp_wait(&raw_empty[s], ((raw / RS) & 1) ^ 1, err)) { ok = false; break; }
-              if (mine == i) s_scale[s * 4 + sub] = uint8_t(v ? scales >> 8 : scales);
+              if (!v && mine == i) {         // (ahead of K, which the scores wait for)
+                float* const of = reinterpret_cast<float*>(s_scales + j % SCALES) + sub;
+                of[0] = __uint_as_float(power_bits(exponent_of_byte(scales & 255)));
+                of[4] = __uint_as_float(power_bits(exponent_of_byte(scales >> 8)));
+                of[8] = float(exponent_of_byte(scales >> 8));
+              }
               __syncwarp();
-              mbar_expect_tx_e(&raw_full[s], bytes, lane == 0);
-              __syncwarp();
-              tma_load_2d_e(smem + L::OFF_RAW + s * L::RAW_BYTES + sub * 16 * DH, map, &raw_full[s], 0, row, load);
-              ++raw;
-            } else {
-              const uint32_t j = at + i, s = j % KS;
-              uint64_t* const full = v ? &v_full[s] : &k_full[s];
-              if (!warp_wait(v ? &v_empty[s] : &k_empty[s], ((j / KS) & 1) ^ 1, err)) { ok = false; break; }
-              mbar_expect_tx_e(full, bytes, lane == 0);
-              __syncwarp();
+            }
+            mbar_expect_tx_e(full, bytes, leader);
+            uint8_t* const tile = smem + (!v ? L::OFF_K + s * L::K_BYTES : BITS8 ? L::OFF_RAW + s * L::RAW_BYTES : L::OFF_V + s * L::V_BYTES);
+            for (int b = 0; b < 4; b += p.box / 16) {
+              const int y = __shfl_sync(0xffffffffu, row, lane0 + b);
+              if constexpr (BITS8) {
+                tma_load_2d_e(tile + b * 16 * DH, map, full, 0, y, leader & boxes >> b);
+              } else {
 #pragma unroll
-              for (int h = 0; h < HALVES; ++h)
-                tma_load_2d_e(smem + (v ? L::OFF_V : L::OFF_K) + s * L::KV_BYTES + h * KV_HALF + sub * 16 * 128, map, full, h * 64, row, load);
+                for (int h = 0; h < HALVES; ++h) tma_load_2d_e(tile + h * KV_HALF + b * 16 * 128, map, full, h * 64, y, leader & boxes >> b);
+              }
             }
           }
         }
@@ -548,129 +664,125 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         scales = scales1;
       }
       at += n;
+      give_back();
     }
     grid_dep_launch();
   } else if (warp == 1 || warp == 2) {
     // ------------------------------ MMA issuer of tile x ------------------------------
     const uint32_t leader = elect_one();
-    constexpr uint32_t idesc_qk = umma_idesc_bf16(TILE, STEP, 0, 0);
-    constexpr uint32_t idesc_pv = umma_idesc_bf16(TILE, DH, 0, 1);
+    // The types of A and B are in bits 7 and 10: bf16; 8-bit cache: P and V in f16, K in e4m3 with Q's two parts in e4m3 and e5m2.
+    constexpr uint32_t no_types = ~((1u << 7) | (1u << 10));
+    constexpr uint32_t idesc_qk = BITS8 ? umma_idesc_bf16(TILE, STEP, 0, 0) & no_types : umma_idesc_bf16(TILE, STEP, 0, 0);
+    constexpr uint32_t idesc_pv = BITS8 ? umma_idesc_bf16(TILE, DH, 0, 1) & no_types : umma_idesc_bf16(TILE, DH, 0, 1);
     constexpr uint32_t hi = desc_hi_sw128(1024);
+    constexpr uint32_t hi8 = DH == 128 ? hi : DESC_HI_SW64;        // rows of e4m3 numbers
     const uint32_t k_base = smem_u32(smem + L::OFF_K), v_base = smem_u32(smem + L::OFF_V);
     const int x = warp - 1;
     const uint32_t q_lo = desc_lo_sw128(smem_u32(smem + L::OFF_Q + x * L::Q_BYTES), 0);
     const uint32_t tm_s = tmem_base + x * 128, tm_o = tmem_base + 256 + x * 128;
-    uint32_t it = 0;      // pieces so far
-    uint32_t done = 0;    // steps of earlier pieces in which this tile took part
-    while (ok && pieces.next(p, piece)) {
-      const int n = piece.n(), n_x = piece.n_of(x);
-      auto issue_s = [&](int i) {
-        const uint32_t u = (done + i) & 1, k_lo = desc_lo_sw128(k_base + (at + i) % KS * L::KV_BYTES, 0);
-#pragma unroll
-        for (int ks = 0; ks < DH / 16; ++ks)
-          umma_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, (ks / 4) * Q_HALF + (ks % 4) * 32), desc_lo_add(k_lo, (ks / 4) * KV_HALF + (ks % 4) * 32), hi, idesc_qk, ks != 0,
-                    leader);
-        umma_commit(&s_full[2 * x + u], leader);
-      };
+    uint32_t done = 0, n_done = 0;    // steps of earlier pieces in which this tile took part; those pieces
+    while (const Piece* const piece = piece_at(it)) {
+      const int n = piece->n, n_x = piece->n_x[x];
+      const bool duo = piece->duo;
+      const int2 clear = piece->clear;
+      // (the tile's steps are i itself, or those of its parity)
+      auto takes = [&](int i) { return duo ? (i & 1) == x : i < n_x; };
+      auto own = [&](int i) { return done + (duo ? i >> 1 : i); };
       // K of step i has come: scores, where the tile takes part, and the stage goes back
       auto scores = [&](int i) -> bool {
-        if (!mbar_wait(&k_full[(at + i) % KS], ((at + i) / KS) & 1, err)) return false;
-        tc_fence_after_sync();
-        if (i < n_x) issue_s(i);
-        umma_commit(&k_empty[(at + i) % KS], leader);
-        if (i + 1 == max(n_x, 1)) umma_commit(q_empty, leader);   // no further score of this piece from this warp
+        const uint32_t s = (at + i) % KS;
+        if (!warp_wait(&k_full[s], ((at + i) / KS) & 1, err)) return false;
+        if (takes(i)) {
+          tc_fence_after_sync();
+          const uint32_t u = own(i) & 1, k_lo = desc_lo_sw128(k_base + s * L::K_BYTES, 0);
+          if constexpr (BITS8) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int ks = 0; ks < DH / 32; ++ks)
+                umma8_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, part * (TILE * DH) + ks * 32), desc_lo_add(k_lo, ks * 32), hi8, idesc_qk | (part << 7), (part | ks) != 0, leader);
+          } else {
+#pragma unroll
+            for (int ks = 0; ks < DH / 16; ++ks)
+              umma_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, (ks / 4) * Q_HALF + (ks % 4) * 32), desc_lo_add(k_lo, (ks / 4) * KV_HALF + (ks % 4) * 32), hi, idesc_qk, ks != 0,
+                        leader);
+          }
+          umma_commit(&s_full[2 * x + u], leader);
+          umma_commit(&k_empty[s], leader);
+        } else if (leader) {
+          mbar_arrive(&k_empty[s]);
+        }
         return true;
       };
-      if (!mbar_wait(q_full, it & 1, err)) { ok = false; break; }
+      if (n_x > 0 && !warp_wait(&q_full[x], n_done & 1, err)) { ok = false; break; }
       tc_fence_after_sync();
-      for (int i = 0; i < 2 && i < n && ok; ++i) ok = scores(i);
+      // Scores run ahead of the products: a buffer is free once the product of the tile's step before last has been issued.
+      const int ahead = duo ? (KS > 4 ? 4 : KS - 1) : 2;
+      for (int i = 0; i < ahead && i < n && ok; ++i) ok = scores(i);
       for (int i = 0; i < n && ok; ++i) {
         const uint32_t s = (at + i) % VS;
-        if (!mbar_wait(&v_full[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
-        if (i < n_x) {
-          const uint32_t u = (done + i) & 1;
-          uint32_t add = i != 0;
-          if (piece.masked(p, piece.block(i))) {
-            if (!BITS8 && !mbar_wait(&v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+        if (!warp_wait(&v_full[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+        if (takes(i)) {
+          const uint32_t k = own(i), u = k & 1;
+          uint32_t add = k != done;
+          if (i < clear.x || i >= clear.y) {
+            if (!BITS8 && !warp_wait(&v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
             // (the softmax threads have begun O with the rows that they add themselves)
-            if (i == 0) add = (s_bad[s * 4] | s_bad[s * 4 + 1] | s_bad[s * 4 + 2] | s_bad[s * 4 + 3]) != 0;
+            if (k == done) add = (s_bad[s * 4] | s_bad[s * 4 + 1] | s_bad[s * 4 + 2] | s_bad[s * 4 + 3]) != 0;
           }
-          if (!mbar_wait(&p_ready[2 * x + u], ((done + i) >> 1) & 1, err)) { ok = false; break; }
+          if (!warp_wait(&p_ready[2 * x + u], (k >> 1) & 1, err)) { ok = false; break; }
           tc_fence_after_sync();
-          const uint32_t v_lo = desc_lo_sw128(v_base + s * L::KV_BYTES, KV_HALF);
+          const uint32_t v_lo = desc_lo_sw128(v_base + s * L::V_BYTES, KV_HALF);
 #pragma unroll
           for (int ks = 0; ks < STEP / 16; ++ks)
             umma_ts_w(tm_o, tm_s + u * STEP + ks * 8, desc_lo_add(v_lo, ks * 2048), hi, idesc_pv, ks == 0 ? add : 1u, leader);
           umma_commit(&pv_done[x], leader);
-          if (i + 1 == n_x) umma_commit(&o_done[x], leader);
+          if (k + 1 == done + n_x) umma_commit(&o_done[x], leader);
+          umma_commit(&v_empty[s], leader);
+        } else if (leader) {
+          mbar_arrive(&v_empty[s]);
         }
-        umma_commit(&v_empty[s], leader);
-        if (i + 2 < n) ok = scores(i + 2);
+        if (i + ahead < n) ok = scores(i + ahead);
       }
       at += n;
       done += n_x;
-      ++it;
+      n_done += n_x > 0 ? 1 : 0;
+      give_back();
     }
   } else if (warp == 3) {
-    // ------------------------------ query rows; V blocks with masking ------------------------------
-    constexpr int CHUNKS = DH / 8, AT_ONCE = 32 / CHUNKS;       // 16-byte pieces of a row; rows per pass of the warp
-    const int g_inverse = 65536 / p.G + 1;                      // (in / G, exactly, for in < 128)
-    uint32_t it = 0;
-    while (ok && pieces.next(p, piece)) {
-      const ChunkGroup& grp = p.grp[piece.g];
-      if (!warp_wait(q_empty, (it & 1) ^ 1, err)) { ok = false; break; }
-      // (rows of the tiles behind the last one hold what they held: nothing of theirs is stored)
-      const long long row0 = (long long)piece.pair * 2 * TILE;
-      const int rows = int(min((long long)2 * TILE, (long long)piece.span.n * piece.R - row0));
-      const int chunk = lane % CHUNKS, first = lane / CHUNKS;
-      int token = int(div_places(row0 + first, piece.R)), in = int(row0 + first - (long long)token * piece.R);
-      auto source = [&]() {                                      // of the row at hand, and on to the next
-        const int member = in * g_inverse >> 16;
-        const size_t elem = (size_t(piece.span.row0 + token) * p.Hq + piece.hk * p.G + in - member * p.G) * DH + chunk * 8;
-        const uint8_t* const at = reinterpret_cast<const uint8_t*>(grp.q[member]) + (elem << (p.io_f32 ? 2 : 1));
-        for (in += AT_ONCE; in >= piece.R; in -= piece.R) ++token;
-        return at;
-      };
-      auto place = [&](int r) { return smem + L::OFF_Q + (r / TILE) * L::Q_BYTES + (chunk / 8) * Q_HALF + sw128_offset(r % TILE, chunk % 8); };
-      if (p.io_f32) {
-        constexpr int FLY = 4;
-        for (int r = first; r < rows; r += AT_ONCE * FLY) {
-          float4 v[FLY][2];
-#pragma unroll
-          for (int k = 0; k < FLY; ++k) {
-            if (r + k * AT_ONCE >= rows) break;
-            const float4* const src = reinterpret_cast<const float4*>(source());
-            v[k][0] = src[0];
-            v[k][1] = src[1];
-          }
-#pragma unroll
-          for (int k = 0; k < FLY; ++k) {
-            if (r + k * AT_ONCE >= rows) break;
-            *reinterpret_cast<uint4*>(place(r + k * AT_ONCE)) = make_uint4(pack_bf16(v[k][0].x, v[k][0].y), pack_bf16(v[k][0].z, v[k][0].w),
-                                                                          pack_bf16(v[k][1].x, v[k][1].y), pack_bf16(v[k][1].z, v[k][1].w));
-          }
-        }
-      } else {
-        for (int r = first; r < rows; r += AT_ONCE) cp_async16(smem_u32(place(r)), source(), 16);
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-      fence_proxy_async_smem();
+    // ------------------------------ the pieces; V blocks with masking ------------------------------
+    Pieces pieces(share);
+    // A piece is laid out one ahead of the one whose V blocks are looked through.
+    auto lay_out = [&](uint32_t i) {
+      ok = ok && warp_wait(&piece_empty[i % PIECES], ((i / PIECES) & 1) ^ 1, err);
+      if (!ok) return false;
+      Piece* const of = s_pieces + i % PIECES;
+      pieces.next(p, *of);
       __syncwarp();
-      if (lane == 0) mbar_arrive(q_full);
+      const bool some = of->n > 0;
+      if (lane == 0) mbar_arrive(&piece_full[i % PIECES]);
+      return some;
+    };
+    bool more = lay_out(0);
+    while (more) {
+      const Piece* const piece = s_pieces + it % PIECES;
+      const int n = piece->n;
+      more = lay_out(it + 1);
       if constexpr (!BITS8) {
-        for (int i = 0; i < piece.n() && ok; ++i) {
+        constexpr int CHUNKS = DH / 8;       // 16-byte pieces of a row
+        const int2 clear = piece->clear;
+        for (int i = 0; i < n && ok; ++i) {
           const uint32_t s = (at + i) % VS;
           ok = warp_wait(&v_full[s], ((at + i) / VS) & 1, err);
           if (!ok) break;
-          const int block = piece.block(i);
-          if (piece.masked(p, block)) {
-            uint8_t* const v = smem + L::OFF_V + s * L::KV_BYTES;
+          if (i < clear.x || i >= clear.y) {
+            const int block = piece->block(i);
+            uint8_t* const v = smem + L::OFF_V + s * L::V_BYTES;
             unsigned long long bad = 0;
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
               const int r = part * 32 + lane;
-              const bool dead = piece.unseen(p, block * STEP + r, 1);
+              const bool dead = piece->unseen(p, block * STEP + r, 1);
               uint32_t odd = 0;
               if (!dead)
 #pragma unroll
@@ -684,34 +796,111 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
             fence_proxy_async_smem();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(&v_fixed[s]);
+          if (lane == 0) {
+            mbar_arrive(&v_fixed[s]);
+            mbar_arrive(&v_empty[s]);
+          }
         }
+        at += n;
       }
-      at += piece.n();
       ++it;
     }
   } else if (warp < 12) {
     // ------------------------------ softmax of tile x, and its rows of the outputs ------------------------------
+    if constexpr (BITS8) asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     const int x = (warp - 4) >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;   // row of the tile == TMEM lane
     const uint32_t lane_sel = uint32_t(quarter * 32) << 16;
     const uint32_t tm_s = tmem_base + x * 128 + lane_sel, tm_o = tmem_base + 256 + x * 128 + lane_sel;
-    const uint64_t c2 = pack_f2(p.scale_log2, p.scale_log2);
-    uint32_t done = 0, n_done = 0;       // steps of earlier pieces in which this tile took part; those pieces
-    while (ok && pieces.next(p, piece)) {
-      const long long n_rows = (long long)piece.span.n * piece.R, tile0 = ((long long)piece.pair * 2 + x) * TILE;
-      const bool there = tile0 + r < n_rows, any = tile0 + quarter * 32 < n_rows;      // (the same in the whole warp)
-      const int token = int(min((long long)piece.span.n - 1, div_places(tile0 + r, piece.R)));
-      const int pos = piece.span.pos0 + token;
-      const int pos_first = x == 0 ? piece.w.pos_first : piece.span.pos0 + int(min((long long)piece.span.n - 1, div_places(tile0, piece.R)));
-      const int pos_last = x == 0 ? piece.w.pos_last_a : piece.w.pos_last;
-      const int n_x = piece.n_of(x);
+    float c_next = p.scale_log2;         // factor of the scores (8 bits: with what the thread's row has been multiplied by taken back)
+    uint32_t done = 0, n_done = 0, n_duo = 0;       // steps of earlier pieces in which this tile took part; those pieces; duos
+    // The thread's query row of a piece goes to its place: every product with the last one's has been seen to complete.
+    auto ask_q = [&](const Piece* of) {
+      if (of->n_x[x] == 0 || r >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
+      const int more = (of->in[x] + r) / of->R, in = of->in[x] + r - more * of->R;
+      const size_t elem = (size_t(of->row0 + of->token[x] + more) * p.Hq + of->hk * p.G + in % p.G) * DH;
+      const void* const q = p.grp[of->g].q[in / p.G];
+      uint8_t* const tile = smem + L::OFF_Q + x * L::Q_BYTES;
+      auto place = [&](int c) { return reinterpret_cast<uint4*>(tile + (c / 8) * Q_HALF + sw128_offset(r, c % 8)); };
+      auto eight = [&](int c) -> uint4 {               // as bf16
+        if (!p.io_f32) return reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(q) + elem)[c];
+        const float4* const src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(q) + elem) + 2 * c;
+        const float4 a = src[0], b = src[1];
+        return make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+      };
+      if constexpr (BITS8) {
+        // A number as the sum of two, e4m3 and e5m2, which both go into products with K as it is: a bf16 number's eight bits are four
+        // and three (what is left by rounding to four bits is eight steps of the eighth at the most).  By a power of two a row, the
+        // largest to 2^7: exact for all elements down to 2^-16 of it, and off by 2^-25 of the largest at most below that.
+        float most = 0.f;
+#pragma unroll 8
+        for (int c = 0; c < DH / 8; ++c) {
+          const uint4 v = eight(c);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t two = j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w;
+            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
+          }
+        }
+        const int up = min(max(7 + 127 - int(__float_as_uint(most) >> 23), -120), 120);
+        const float power = __uint_as_float(uint32_t(up + 127) << 23);
+        c_next = p.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
+#pragma unroll 2
+        for (int c = 0; c < DH / 16; ++c) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint4 v = eight(2 * c + e);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t a = j == 0 ? v.x : v.z, b = j == 0 ? v.y : v.w;
+              float f[4] = {__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] * power : NAN;
+              hi[2 * e + j] = f32x4_to_e4m3(f[0], f[1], f[2], f[3]);
+              const float2 r = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + j]))), t = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + j] >> 16)));
+              lo[2 * e + j] = f32x4_to_e5m2(f[0] - r.x, f[1] - r.y, f[2] - t.x, f[3] - t.y);
+            }
+          }
+          const uint32_t at8 = DH == 128 ? sw128_offset(r, c) : r * 64u + ((c ^ (r >> 1 & 3)) << 4);
+          *reinterpret_cast<uint4*>(tile + at8) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(tile + TILE * DH + at8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+      } else if (p.io_f32) {
+#pragma unroll 4
+        for (int c = 0; c < DH / 8; ++c) *place(c) = eight(c);
+      } else {
+        const __nv_bfloat16* const src = reinterpret_cast<const __nv_bfloat16*>(q) + elem;
+#pragma unroll
+        for (int c = 0; c < DH / 8; ++c) cp_async16(smem_u32(place(c)), src + c * 8, 16);
+      }
+      cp_async_commit();
+    };
+    auto give_q = [&](const Piece* of) {
+      if (of->n_x[x] == 0) return;
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[x]);
+    };
+    const Piece* piece = piece_at(0);
+    if (piece != nullptr) {
+      ask_q(piece);
+      give_q(piece);
+    }
+    while (piece != nullptr) {
+      const bool any = quarter * 32 < piece->rows[x];      // (the same in the whole warp)
+      const bool duo = piece->duo;
+      const int2 pair_clear = piece->clear, clear = piece->clear_x[x];
+      const int n_x = piece->n_x[x];
+      const float c_row = c_next;
       float m_used = -INFINITY;          // running maximum (log2 domain) that the exponentials are taken against
+      float o_used = -INFINITY;          // 8 bits: what O is in units of (log2, V's power with it)
       uint64_t l2 = 0ull, l2b = 0ull;
-      for (int i = 0; i < n_x; ++i) {
-        const uint32_t u = (done + i) & 1;
-        const int block = piece.block(i), key0 = block * STEP;
-        ok = warp_wait(&s_full[2 * x + u], ((done + i) >> 1) & 1, err);
+      for (int k = 0; k < n_x; ++k) {
+        const int i = duo ? 2 * k + x : k;
+        const uint32_t u = (done + k) & 1;
+        ok = warp_wait(&s_full[2 * x + u], ((done + k) >> 1) & 1, err);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t tm_su = tm_s + u * STEP;
@@ -723,127 +912,223 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           tmem_ld_x32(tm_su, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
           tmem_ld_x32(tm_su + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
           tmem_ld_wait();
-          if (Piece::masked(p, block, pos_first, pos_last)) {
+          if (i < clear.x || i >= clear.y) {
+            const int key0 = piece->block(i) * STEP;
+            const int pos = piece->pos0 + piece->token[x] + (piece->in[x] + min(r, piece->rows[x] - 1)) / piece->R;
             auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
             seen = below(pos - key0 + 1);
             if (p.window > 0) seen &= ~below(pos - p.window + 1 - key0) | below(p.sinks - key0);
             const uint32_t lo = uint32_t(seen), up = uint32_t(seen >> 32);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              if ((lo >> k & 1) == 0) sv[k] = 0xff800000u;        // -inf
-              if ((up >> k & 1) == 0) sv[32 + k] = 0xff800000u;
+            for (int j = 0; j < 32; ++j) {
+              if ((lo >> j & 1) == 0) sv[j] = 0xff800000u;        // -inf
+              if ((up >> j & 1) == 0) sv[32 + j] = 0xff800000u;
             }
           }
           float mp[4];
+          if constexpr (BITS8) {
+            // A score is its product times K's power, a weight of V the probability times V's: 2^(s + e), in f16, relative to
+            // o_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
+            // weight has 11 bits unless it is below 2^-21 of the largest.
+            const Scales& of = s_scales[(at + i) % SCALES];
+            const float4 kp = of.k, vp = of.v, ve = of.e;
+            // (not zero: a masked score is -infinity times this)
+            const float cg[4] = {fmaxf(c_row * kp.x, 1.1754944e-38f), fmaxf(c_row * kp.y, 1.1754944e-38f), fmaxf(c_row * kp.z, 1.1754944e-38f), fmaxf(c_row * kp.w, 1.1754944e-38f)};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mp[k] = fmaxf(__uint_as_float(sv[2 * k]), __uint_as_float(sv[2 * k + 1]));
+            for (int j = 0; j < 4; ++j) mp[j] = fmaxf(__uint_as_float(sv[16 * j]), __uint_as_float(sv[16 * j + 1]));
 #pragma unroll
-          for (int j = 8; j < STEP; j += 8)
+            for (int g = 2; g < 16; g += 2)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mp[k] = fmax3(mp[k], __uint_as_float(sv[j + 2 * k]), __uint_as_float(sv[j + 2 * k + 1]));
-          const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * p.scale_log2;
-          if (i == 0) {
-            m_used = m_step;
-          } else if (m_step > m_used + kRescaleBy) {
-            alpha = fast_exp2(m_used - m_step);
-            m_used = m_step;
-            l2 = fmul2(l2, pack_f2(alpha, alpha));
-            l2b = fmul2(l2b, pack_f2(alpha, alpha));
-            rescale = true;
-          }
-          const float nm = m_used == -INFINITY ? 0.f : -m_used;   // (a row that has seen nothing yet: all terms are 0)
-          const uint64_t nm2 = pack_f2(nm, nm);
+              for (int j = 0; j < 4; ++j) mp[j] = fmax3(mp[j], __uint_as_float(sv[16 * j + g]), __uint_as_float(sv[16 * j + g + 1]));
 #pragma unroll
-          for (int g = 0; g < STEP / 32; ++g) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * k]), __uint_as_float(sv[g * 32 + 2 * k + 1])), c2, nm2);
-              const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
-              if (k & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
-              pk[k] = pack_bf16(f2_lo(e), f2_hi(e));
+            for (int j = 0; j < 4; ++j) mp[j] *= cg[j];
+            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
+            const float o_step = fmaxf(fmaxf(mp[0] + ve.x, mp[1] + ve.y), fmaxf(mp[2] + ve.z, mp[3] + ve.w));
+            if (k == 0) {
+              m_used = m_step;
+              o_used = o_step - 7.f;
+            } else {
+              if (m_step > m_used + kRescaleBy) {
+                const float f = fast_exp2(m_used - m_step);
+                m_used = m_step;
+                l2 = fmul2(l2, pack_f2(f, f));
+                l2b = fmul2(l2b, pack_f2(f, f));
+              }
+              if (o_step > o_used + 15.f) {
+                alpha = fast_exp2(o_used - (o_step - 7.f));
+                o_used = o_step - 7.f;
+                rescale = true;
+              }
             }
-            tmem_st_x16(tm_su + g * 16, pk);    // P as bf16 pairs over the first 32 columns of this score buffer
+            const bool none = m_used == -INFINITY;                    // (a row that has seen nothing yet: all terms are 0)
+            const float nm = none ? 0.f : -m_used, unit = none ? 0.f : fast_exp2(m_used - o_used);
+            // (finite: scales of blocks that the row does not see are of any size, and its probabilities there 0)
+            constexpr float most = 3.4028235e38f;
+            const float fg[4] = {fminf(unit * vp.x, most), fminf(unit * vp.y, most), fminf(unit * vp.z, most), fminf(unit * vp.w, most)};
+            const uint64_t nm2 = pack_f2(nm, nm);
+#pragma unroll
+            for (int g = 0; g < STEP / 32; ++g) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int of16 = g * 2 + j / 8;
+                const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), pack_f2(cg[of16], cg[of16]), nm2);
+                const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
+                if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
+                const uint64_t w = fmul2(e, pack_f2(fg[of16], fg[of16]));
+                pk[j] = pack_f16(f2_lo(w), f2_hi(w));
+              }
+              tmem_st_x16(tm_su + g * 16, pk);
+            }
+          } else {
+            const uint64_t c2 = pack_f2(c_row, c_row);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mp[j] = fmaxf(__uint_as_float(sv[2 * j]), __uint_as_float(sv[2 * j + 1]));
+#pragma unroll
+            for (int g = 8; g < STEP; g += 8)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mp[j] = fmax3(mp[j], __uint_as_float(sv[g + 2 * j]), __uint_as_float(sv[g + 2 * j + 1]));
+            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * c_row;
+            if (k == 0) {
+              m_used = m_step;
+            } else if (m_step > m_used + kRescaleBy) {
+              alpha = fast_exp2(m_used - m_step);
+              m_used = m_step;
+              l2 = fmul2(l2, pack_f2(alpha, alpha));
+              l2b = fmul2(l2b, pack_f2(alpha, alpha));
+              rescale = true;
+            }
+            const float nm = m_used == -INFINITY ? 0.f : -m_used;     // (a row that has seen nothing yet: all terms are 0)
+            const uint64_t nm2 = pack_f2(nm, nm);
+#pragma unroll
+            for (int g = 0; g < STEP / 32; ++g) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), c2, nm2);
+                const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
+                if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
+                pk[j] = pack_bf16(f2_lo(e), f2_hi(e));
+              }
+              tmem_st_x16(tm_su + g * 16, pk);    // P as bf16 pairs over the first 32 columns of this score buffer
+            }
           }
         }
         // O may still be receiving the last step's product: a rescale waits for it first.
-        bool behind = false;
-        auto wait_product = [&]() -> bool {
-          if (behind || i == 0) return true;
-          behind = true;
-          const bool wt = warp_wait(&pv_done[x], (done + i - 1) & 1, err);
+        if (k > 0 && __any_sync(0xffffffffu, rescale)) {
+          if (!warp_wait(&pv_done[x], (done + k - 1) & 1, err)) { ok = false; break; }
           tc_fence_after_sync();
-          return wt;
-        };
-        if (i > 0 && __any_sync(0xffffffffu, rescale)) {
-          if (!wait_product()) { ok = false; break; }
 #pragma unroll
           for (int g = 0; g < DH / 32; ++g) {
             uint32_t tmp[32];
             tmem_ld_x32(tm_o + g * 32, tmp);
             tmem_ld_wait();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) tmp[k] = __float_as_uint(__uint_as_float(tmp[k]) * alpha);
+            for (int j = 0; j < 32; ++j) tmp[j] = __float_as_uint(__uint_as_float(tmp[j]) * alpha);
             tmem_st_x32(tm_o + g * 32, tmp);
           }
         }
         tmem_st_wait();
-        if (piece.masked(p, block)) {
+        if (i < pair_clear.x || i >= pair_clear.y) {
           const uint32_t s = (at + i) % VS;
-          if (!warp_wait(BITS8 ? &v_full[s] : &v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
+          // (V first: only then is v_fixed past the stage's last use)
+          if (!warp_wait(&v_full[s], ((at + i) / VS) & 1, err) || (!BITS8 && !warp_wait(&v_fixed[s], ((at + i) / VS) & 1, err))) { ok = false; break; }
           const unsigned long long bad = s_bad[s * 4] | s_bad[s * 4 + 1] | s_bad[s * 4 + 2] | s_bad[s * 4 + 3];
           if (bad != 0) {
-            if (!wait_product()) { ok = false; break; }
-            add_rows<DH, BITS8>(p, p.grp[piece.g], piece.b, piece.hk, key0, bad, any ? seen : 0ull, tm_su, tm_o, i == 0);
+            if (k > 0 && !warp_wait(&pv_done[x], (done + k - 1) & 1, err)) { ok = false; break; }
+            tc_fence_after_sync();
+            add_rows<DH, BITS8>(p, p.grp[piece->g], piece->b, piece->hk, piece->block(i) * STEP, bad, any ? seen : 0ull, tm_su, tm_o, k == 0);
           }
         }
         tc_fence_before_sync();
-        mbar_arrive(&p_ready[2 * x + u]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_ready[2 * x + u]);
       }
       if (!ok) break;
-      const float l_sum = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
+      const Piece* const next = piece_at(it + 1);
+      if (!ok) break;
+      if (next != nullptr) ask_q(next);
+      float m = m_used, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
       if (n_x > 0) {
-        ok = warp_wait(&o_done[x], n_done & 1, err);
-        if (!ok) break;
+        if (!warp_wait(&o_done[x], n_done & 1, err)) break;
         tc_fence_after_sync();
         ++n_done;
       }
+      // (8 bits: O is in units of its own, and V in shared memory 2^-8 of its codes)
+      const float unit = !BITS8 ? 1.f : m == -INFINITY ? 0.f : fast_exp2(o_used - m + 8.f);
+      float mine = unit, others = 0.f;
+      if (duo) {                           // the two halves' rows are the same ones; each puts half of the columns together
+        tmem_st_x4(tm_s, __float_as_uint(m), __float_as_uint(l), __float_as_uint(unit), 0);   // (over a score buffer: the next piece has not begun)
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(duo_ml);
+        if (!warp_wait(duo_ml, n_duo & 1, err)) break;
+        tc_fence_after_sync();
+        const float4 other = tmem_ld_x4(x == 0 ? tm_s + 128 : tm_s - 128);
+        const float top = fmaxf(m, other.x);
+        mine = m == -INFINITY ? 0.f : fast_exp2(m - top);
+        others = other.x == -INFINITY ? 0.f : fast_exp2(other.x - top);
+        l = l * mine + other.y * others;
+        m = top;
+        mine *= unit;
+        others *= other.z;
+      }
       if (any) {
-        const ChunkGroup& grp = p.grp[piece.g];
-        const int in = int(tile0 + r - (long long)token * piece.R);
+        const ChunkGroup& grp = p.grp[piece->g];
+        const bool there = r < piece->rows[x], whole = piece->whole;
+        const int more = (piece->in[x] + r) / piece->R, in = piece->in[x] + r - more * piece->R;
         const int member = there ? in / p.G : 0;
-        const size_t head = size_t(piece.span.row0 + token) * p.Hq + piece.hk * p.G + (there ? in % p.G : 0);
-        const size_t part = size_t(piece.slot) * (2 * TILE) + x * TILE + r;
-        const float inv_l = l_sum == 0.f ? 0.f : 1.f / l_sum;
-        if (there) {
-          if (piece.whole)
-            grp.lse[member][head] = l_sum == 0.f ? -INFINITY : log_sum(m_used, l_sum);
+        const size_t head = size_t(piece->row0 + piece->token[x] + more) * p.Hq + piece->hk * p.G + (there ? in % p.G : 0);
+        const size_t part = size_t(piece->slot) * (2 * TILE) + (duo ? 0 : x * TILE) + r;
+        const float inv_l = l == 0.f ? 0.f : 1.f / l;
+        if (there && !(duo && x == 1)) {
+          if (whole)
+            grp.lse[member][head] = l == 0.f ? -INFINITY : log_sum(m, l);
           else
-            *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m_used, l_sum);
+            *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m, l);
         }
-        if (n_x > 0) {
-#pragma unroll
-          for (int h = 0; h < DH / 32; ++h) {
+        const int h_end = duo && x == 0 ? DH / 64 : DH / 32, n_other = duo ? piece->n_x[x ^ 1] : 0;
+        if (duo || n_x > 0) {
+          for (int h = duo && x == 1 ? DH / 64 : 0; h < h_end; ++h) {
             uint32_t tmp[32];
-            tmem_ld_x32(tm_o + h * 32, tmp);
-            tmem_ld_wait();
-            if (there && !piece.whole) {
+            if (n_x > 0) {
+              tmem_ld_x32(tm_o + h * 32, tmp);
+              tmem_ld_wait();
+            }
+            if (duo || BITS8) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) tmp[j] = n_x > 0 ? __float_as_uint(__uint_as_float(tmp[j]) * mine) : 0;
+            }
+            if (duo) {
+              if (n_other > 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  uint32_t far[16];
+                  tmem_ld_x16((x == 0 ? tm_o + 128 : tm_o - 128) + h * 32 + e * 16, far);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) tmp[e * 16 + j] = __float_as_uint(fmaf(__uint_as_float(far[j]), others, __uint_as_float(tmp[e * 16 + j])));
+                }
+              }
+            }
+            if (there && !whole) {
               float* const dst = p.part_o + part * DH + h * 32;
 #pragma unroll
-              for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4*>(dst + k) = make_uint4(tmp[k], tmp[k + 1], tmp[k + 2], tmp[k + 3]);
+              for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4*>(dst + j) = make_uint4(tmp[j], tmp[j + 1], tmp[j + 2], tmp[j + 3]);
             } else if (there) {
               uint32_t v[16];
 #pragma unroll
-              for (int k = 0; k < 16; ++k) v[k] = pack_bf16(__uint_as_float(tmp[2 * k]) * inv_l, __uint_as_float(tmp[2 * k + 1]) * inv_l);
+              for (int j = 0; j < 16; ++j) v[j] = pack_bf16(__uint_as_float(tmp[2 * j]) * inv_l, __uint_as_float(tmp[2 * j + 1]) * inv_l);
               if (p.io_f32) {
                 float* const dst = reinterpret_cast<float*>(grp.o[member]) + head * DH + h * 32;
 #pragma unroll
-                for (int k = 0; k < 16; k += 2)
-                  *reinterpret_cast<uint4*>(dst + 2 * k) = make_uint4(v[k] << 16, v[k] & 0xffff0000u, v[k + 1] << 16, v[k + 1] & 0xffff0000u);
+                for (int j = 0; j < 16; j += 2)
+                  *reinterpret_cast<uint4*>(dst + 2 * j) = make_uint4(v[j] << 16, v[j] & 0xffff0000u, v[j + 1] << 16, v[j + 1] & 0xffff0000u);
               } else {
                 __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(grp.o[member]) + head * DH + h * 32;
 #pragma unroll
-                for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(dst + 2 * k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(dst + 2 * j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
               }
             }
             __syncwarp();
@@ -851,73 +1136,93 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         }
       }
       __syncwarp();
-      // (the next piece's first product waits for this warp's P, so O is free by then)
       tc_fence_before_sync();
-      at += piece.n();
+      if (duo) {
+        if (lane == 0) mbar_arrive(duo_free);
+        if (!warp_wait(duo_free, n_duo & 1, err)) break;
+        ++n_duo;
+      }
+      // (the next piece's first products wait for these warps' P, so O is free by then)
+      at += piece->n;
       done += n_x;
+      if (next != nullptr) give_q(next);
+      give_back();
+      piece = next;
     }
   } else if constexpr (BITS8) {
-    // ------------------------------ codes to bf16 ------------------------------
-    constexpr int PIECES = DH / 16;                       // 16-byte pieces of a row of codes
-    constexpr int PASSES = STEP * PIECES / 128;           // of the four warps; each 128 / PIECES rows
-    const int tid = threadIdx.x - 384, col = tid % PIECES;
-    uint32_t raw = 0;
-    while (ok && pieces.next(p, piece)) {
-      const int n = piece.n();
-      for (int i = 0; i < n && ok; ++i) {
-        const uint32_t j = at + i, s = j % KS;
-        const int block = piece.block(i);
-        const bool masked = piece.masked(p, block);
+    // ------------------------------ V's codes to f16, every other step each four warps ------------------------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    constexpr int CODES = DH / 16;                       // 16-byte pieces of a row of codes
+    constexpr int PASSES = STEP * CODES / 128;           // of the four warps; each 128 / CODES rows
+    const uint32_t group = (warp - 12) >> 2;
+    const int tid = threadIdx.x & 127, col = tid % CODES;
+    while (const Piece* const piece = piece_at(it)) {
+      const int n = piece->n;
+      const int2 clear = piece->clear;
+      for (int i = int((group ^ at) & 1); i < n && ok; i += 2) {
+        const uint32_t j = at + i, s = j % VS, rs = j % RS;
+        if (!warp_wait(&raw_full[rs], (j / RS) & 1, err) || !warp_wait(&v_empty[s], ((j / VS) & 1) ^ 1, err)) { ok = false; break; }
+        uint4 codes[PASSES];
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const uint32_t rs = raw % RS;
-          if (!warp_wait(&raw_full[rs], (raw / RS) & 1, err) || !warp_wait(v ? &v_empty[s] : &k_empty[s], ((j / KS) & 1) ^ 1, err)) { ok = false; break; }
-          uint4 codes[PASSES];
-          float power[PASSES];
+        for (int k = 0; k < PASSES; ++k)
+          codes[k] = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + rs * L::RAW_BYTES + (k * 128 + tid) / CODES * DH + col * 16);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&raw_empty[rs]);
+        uint8_t* const tile = smem + L::OFF_V + s * L::V_BYTES;
+        auto store = [&](int k, const uint4 (&half)[2]) {
+          const int row = (k * 128 + tid) / CODES;
+          // (odd and even columns of a row take turns, so that the eight lanes of a phase hit different banks)
+          const int flip = (col >> 2) & 1;
 #pragma unroll
-          for (int k = 0; k < PASSES; ++k) {
-            const int row = (k * 128 + tid) / PIECES;
-            codes[k] = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + rs * L::RAW_BYTES + row * DH + col * 16);
-            power[k] = __uint_as_float(power_bits(exponent_of_byte(s_scale[rs * 4 + row / CACHE_BLOCK])));
+          for (int h = 0; h < 2; ++h) {
+            const int c = col * 2 + (h ^ flip);
+            *reinterpret_cast<uint4*>(tile + (c / 8) * KV_HALF + sw128_offset(row, c % 8)) = (h ^ flip) ? half[1] : half[0];
           }
-          mbar_arrive(&raw_empty[rs]);
-          uint8_t* const tile = smem + (v ? L::OFF_V : L::OFF_K) + s * L::KV_BYTES;
-          unsigned long long bad = 0;
+        };
+        uint32_t nan = 0;
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) nan |= any_nan(codes[k]);
+        const bool masked = i < clear.x || i >= clear.y;
+        if (!masked && __all_sync(0xffffffffu, nan == 0)) {
 #pragma unroll
           for (int k = 0; k < PASSES; ++k) {
-            const int row = (k * 128 + tid) / PIECES;
-            const uint32_t w[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
             uint4 half[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              half[e] = make_uint4(widen8(w[2 * e], power[k]), widen8(w[2 * e] >> 16, power[k]), widen8(w[2 * e + 1], power[k]), widen8(w[2 * e + 1] >> 16, power[k]));
-            if (v == 1 && masked) {
-              const bool dead = piece.unseen(p, block * STEP + row, 1);
-              const bool odd = !dead && (not_finite(half[0]) | not_finite(half[1])) != 0;
-              // the lanes of a row
-              const uint32_t of_row = __ballot_sync(0xffffffffu, odd) >> (lane / PIECES * PIECES) & ((1u << PIECES) - 1);
-              if (dead || of_row != 0) half[0] = half[1] = make_uint4(0, 0, 0, 0);
-              const uint32_t firsts = __ballot_sync(0xffffffffu, of_row != 0 && lane % PIECES == 0);
-#pragma unroll
-              for (int q = 0; q < 32 / PIECES; ++q)
-                if (firsts >> (q * PIECES) & 1) bad |= 1ull << ((k * 128 + tid - lane) / PIECES + q);
-            }
-            // (odd and even columns of a row take turns, so that the eight lanes of a phase hit different banks)
-            const int flip = (col >> 2) & 1;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int c = col * 2 + (e ^ flip);
-              *reinterpret_cast<uint4*>(tile + (c / 8) * KV_HALF + sw128_offset(row, c % 8)) = (e ^ flip) ? half[1] : half[0];
-            }
+            widen16(codes[k], half);
+            store(k, half);
           }
-          if (v == 1 && masked && lane == 0) s_bad[s * 4 + (tid >> 5)] = bad;
-          fence_proxy_async_smem();
-          __syncwarp();      // (lane 0's note is ahead of every lane's arrival by program order of its own)
-          mbar_arrive(v ? &v_full[s] : &k_full[s]);
-          ++raw;
+        } else {
+          unsigned long long bad = 0;
+#pragma unroll 1
+          for (int k = 0; k < PASSES; ++k) {
+            uint4 some = codes[0];
+#pragma unroll
+            for (int q = 1; q < PASSES; ++q)
+              if (k == q) some = codes[q];
+            const int row = (k * 128 + tid) / CODES;
+            uint4 half[2];
+            widen16(some, half);
+            const bool dead = masked && piece->unseen(p, piece->block(i) * STEP + row, 1);
+            const bool odd = !dead && any_nan(some) != 0;
+            // the lanes of a row
+            const uint32_t of_row = __ballot_sync(0xffffffffu, odd) >> (lane / CODES * CODES) & ((1u << CODES) - 1);
+            if (dead || (masked && of_row != 0)) {
+              half[0] = half[1] = make_uint4(0, 0, 0, 0);
+            } else if (odd) {
+              put_nan(half);
+            }
+            const uint32_t firsts = __ballot_sync(0xffffffffu, masked && of_row != 0 && lane % CODES == 0);
+            for (int q = 0; q < 32 / CODES; ++q)
+              if (firsts >> (q * CODES) & 1) bad |= 1ull << ((k * 128 + tid - lane) / CODES + q);
+            store(k, half);
+          }
+          if (masked && lane == 0) s_bad[s * 4 + (tid >> 5)] = bad;
         }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&v_full[s]);
       }
       at += n;
+      give_back();
     }
   }
 
@@ -1059,6 +1364,13 @@ cudaError_t launch_chunk(const ChunkParams<MANY_CHUNK_GROUPS>& all, int shares, 
   static_cast<ChunkSizes&>(p) = all;
   std::copy(all.grp, all.grp + NG, p.grp);
   cudaError_t e = allow_smem<chunk_kernel<DH, BITS8, NG>>(L::TOTAL);
+  if (BITS8 && e == cudaSuccess) {     // the kernel hands registers from warp to warp: 96 a thread at launch, or it would wait for good
+    static const int regs = [] {
+      cudaFuncAttributes at;
+      return cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(chunk_kernel<DH, BITS8, NG>)) == cudaSuccess ? at.numRegs : 0;
+    }();
+    if (regs != 96) return cudaErrorInvalidConfiguration;
+  }
   if (e == cudaSuccess) e = launch_kernel(chunk_kernel<DH, BITS8, NG>, shares, L::THREADS, L::TOTAL, stream, 1, p);
   if (e == cudaSuccess && shares > 1) e = launch_kernel(chunk_merge_kernel<DH, NG>, dim3(shares, MERGE_PARTS), MERGE_THREADS, 0, stream, 1, p);
   return e;
@@ -1170,8 +1482,8 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
       const uint64_t dims[2] = {uint64_t(d->dh), uint64_t(d->n_pages) * d->Hkv * d->page_size};
       const uint64_t strides[1] = {uint64_t(d->dh) * (bits8 ? 1 : 2)};
       const uint32_t box[2] = {bits8 ? uint32_t(d->dh) : 64u, uint32_t(p.box)};
-      rc = make_tensor_map(&grp.map_k, k_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, !bits8);
-      if (rc == KVP_OK) rc = make_tensor_map(&grp.map_v, v_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, !bits8);
+      rc = make_tensor_map(&grp.map_k, k_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, bits8 && d->dh == 64 ? SWIZZLE_64 : SWIZZLE_128);
+      if (rc == KVP_OK) rc = make_tensor_map(&grp.map_v, v_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, bits8 ? SWIZZLE_0 : SWIZZLE_128);
       if (rc != KVP_OK) return rc;
       const int g = p.n_groups++;
       p.members[g] = n;

@@ -26,7 +26,7 @@ EncodeTiledFn encode_fn() {
 }  // namespace
 
 int make_tensor_map(CUtensorMap* out, const void* base, int elem_bytes, int rank, const uint64_t* dims,
-                    const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128) {
+                    const uint64_t* strides_bytes, const uint32_t* box, int swizzle) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return KVP_ERR_CUDA;
   cuuint64_t gdim[5];
@@ -44,7 +44,7 @@ int make_tensor_map(CUtensorMap* out, const void* base, int elem_bytes, int rank
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
   const CUresult r = fn(out, dt, cuuint32_t(rank), const_cast<void*>(base), gdim, gstride, bdim, estride,
                         CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                        swizzle == SWIZZLE_128 ? CU_TENSOR_MAP_SWIZZLE_128B : swizzle == SWIZZLE_64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? KVP_OK : KVP_ERR_CUDA;
 }

@@ -13,10 +13,11 @@ namespace kvp {
 
 // Builds a tiled TMA descriptor over a row-major tensor of bytes, bf16 or fp32 of up to 4 dimensions.
 // dims[0] is the innermost (contiguous) extent in elements; strides_bytes[i] is the byte stride
-// of dims[i+1].  box[] is the tile copied per request.  swizzle128 selects the 128-byte swizzle
-// (the inner box extent must then span exactly 128 bytes).  Returns KVP_OK or KVP_ERR_CUDA.
+// of dims[i+1].  box[] is the tile copied per request.  swizzle: SWIZZLE_128 or SWIZZLE_64
+// (the inner box extent must then span exactly as many bytes), or none.  Returns KVP_OK or KVP_ERR_CUDA.
+enum { SWIZZLE_0 = 0, SWIZZLE_128 = 1, SWIZZLE_64 = 2 };   // (true: the 128-byte one)
 int make_tensor_map(CUtensorMap* out, const void* base, int elem_bytes, int rank, const uint64_t* dims,
-                    const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128);
+                    const uint64_t* strides_bytes, const uint32_t* box, int swizzle);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
