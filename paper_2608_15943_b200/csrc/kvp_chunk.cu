@@ -1357,6 +1357,57 @@ int check_chunk(const kvp_decode_desc* d) {
   return KVP_OK;
 }
 
+// One token a sequence, few query rows: decode's kernels, on a table of the pages that the token sees.  Front pages of first tokens,
+// then those from the window's first on; the positions between the two parts are one run, in the last page of the front or the
+// first of the window (kvp_host.h).
+struct Ones {
+  const int32_t *block_table, *lengths;
+  int32_t *table, *shortened;              // [B, columns], [B]; null without a window
+  int4* seen;                              // [B]
+  int B, page_size, max_pages, columns, window, sinks;
+};
+constexpr int ONES_THREADS = 128;
+__global__ void __launch_bounds__(ONES_THREADS) ones_kernel(const __grid_constant__ Ones p) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int b = blockIdx.x, length = p.lengths[b];
+  const bool there = length > 0 && length <= p.max_pages * p.page_size;
+  int4 seen = make_int4(0, 0, there, 0);
+  if (p.table != nullptr) {
+    const int len = there ? length : 0;
+    const int from = max(0, len - p.window), front = min((p.sinks + p.page_size - 1) / p.page_size, from / p.page_size), left_out = from / p.page_size - front;
+    const int shorter = len - left_out * p.page_size;
+    if (p.sinks < from) {
+      seen.x = min(p.sinks, len);
+      seen.y = from - left_out * p.page_size;
+    }
+    const int n = (shorter + p.page_size - 1) / p.page_size;
+    for (int i = threadIdx.x; i < n; i += ONES_THREADS)
+      p.table[size_t(b) * p.columns + i] = p.block_table[size_t(b) * p.max_pages + (i < front ? i : i + left_out)];
+    if (n == 0 && threadIdx.x == 0) p.table[size_t(b) * p.columns] = 0;      // (looked at before the length)
+    if (threadIdx.x == 0) p.shortened[b] = shorter;
+  }
+  if (threadIdx.x == 0) p.seen[b] = seen;
+}
+// Columns of that table; they hold no more than the whole one has.
+int ones_columns(const kvp_decode_desc* d, int window, int sinks) {
+  return int(std::min((long long)d->max_pages, (long long)(sinks + d->page_size - 1) / d->page_size + ((long long)window + d->page_size - 2) / d->page_size + 1));
+}
+size_t ones_bytes(const kvp_decode_desc* d, const int32_t* donor, int columns, bool bits8) {
+  return align256(size_t(d->B) * sizeof(int4)) + align256(size_t(d->B) * 4) + align256(size_t(d->B) * columns * 4) +
+         (bits8 ? kvp_decode8_workspace_bytes(d, donor) : kvp_decode_workspace_bytes(d, donor));
+}
+// All layers of every donor group fit one pass of decode's.
+bool few_rows(const kvp_decode_desc* d, const int32_t* donor, int begin, int end) {
+  const int per = std::min(MAX_MEMBERS, 16 / (d->Hq / d->Hkv));
+  for (int own = 0; own < end; ++own) {
+    int n = 0;
+    for (int l = begin; l < end; ++l) n += donor[l] == own;
+    if (n > per) return false;
+  }
+  return true;
+}
+
 template <int DH, bool BITS8, int NG>
 cudaError_t launch_chunk(const ChunkParams<MANY_CHUNK_GROUPS>& all, int shares, cudaStream_t stream) {
   using L = ChunkSmem<DH, BITS8>;
@@ -1399,7 +1450,13 @@ using namespace kvp;
 
 extern "C" size_t kvp_attn_chunk_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor, int32_t T) {
   if (check_chunk(d) != KVP_OK || donor == nullptr || T < 0) return 0;
-  return chunk_bytes(shares_at_most(d, std::min(d->L, MANY_CHUNK_GROUPS), T), d->dh);
+  size_t bytes = chunk_bytes(shares_at_most(d, std::min(d->L, MANY_CHUNK_GROUPS), T), d->dh);
+  if (T >= d->B) {
+    kvp_decode_desc plain = *d;
+    plain.num_splits = 0;
+    bytes = std::max({bytes, ones_bytes(&plain, donor, d->max_pages, false), ones_bytes(&plain, donor, d->max_pages, true)});
+  }
+  return bytes;
 }
 
 extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float scale, int32_t window, int32_t sinks,
@@ -1418,17 +1475,40 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
     if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return KVP_ERR_BAD_DONOR;
   if (T == 0) return KVP_OK;           // (tensors without rows have no memory)
   const bool bits8 = k_scale != nullptr;
-  for (int l = layer_begin; l < layer_end; ++l) {
+  for (int l = layer_begin; l < layer_end; ++l) {     // all of them before anything is launched
     const int own = donor[l];
     if (q[l] == nullptr || o[l] == nullptr || lse[l] == nullptr || k_cache[own] == nullptr || v_cache[own] == nullptr ||
         (bits8 && (k_scale[own] == nullptr || v_scale[own] == nullptr)))
       return KVP_ERR_INVALID_ARG;
     if (!aligned16(q[l]) || !aligned16(o[l]) || !aligned16(k_cache[own]) || !aligned16(v_cache[own])) return KVP_ERR_UNSUPPORTED;
   }
+  if (ws != nullptr && !aligned16(ws)) return KVP_ERR_UNSUPPORTED;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  const int capacity = d->max_pages * d->page_size;
+  if (window >= capacity) window = 0;             // (nothing is further back)
+  sinks = window > 0 ? std::min(sinks, capacity) : 0;
+  if (first == nullptr && few_rows(d, donor, layer_begin, layer_end)) {
+    kvp_decode_desc ones = *d;
+    ones.num_splits = 0;
+    if (window > 0) ones.max_pages = ones_columns(d, window, sinks);
+    if (ws == nullptr || ws_bytes < ones_bytes(&ones, donor, ones.max_pages, bits8)) return KVP_ERR_WORKSPACE;
+    uint8_t* at = static_cast<uint8_t*>(ws);
+    Ones p{block_table, lengths, nullptr, nullptr, reinterpret_cast<int4*>(at), d->B, d->page_size, d->max_pages, ones.max_pages, window, sinks};
+    at += align256(size_t(d->B) * sizeof(int4));
+    if (window > 0) {
+      p.shortened = reinterpret_cast<int32_t*>(at);
+      p.table = reinterpret_cast<int32_t*>(at + align256(size_t(d->B) * 4));
+    }
+    at += align256(size_t(d->B) * 4) + align256(size_t(d->B) * ones.max_pages * 4);
+    if (launch_kernel(ones_kernel, d->B, ONES_THREADS, 0, stream, 1, p) != cudaSuccess) return KVP_ERR_CUDA;
+    const int32_t* const table = window > 0 ? p.table : block_table;
+    const int32_t* const shortened = window > 0 ? p.shortened : lengths;
+    const size_t left = ws_bytes - size_t(at - static_cast<uint8_t*>(ws));
+    return bits8 ? decode8_seen(&ones, donor, scale, q, k_cache, v_cache, k_scale, v_scale, table, shortened, p.seen, o, lse, layer_begin, layer_end, at, left, stream)
+                 : decode_seen(&ones, donor, scale, q, k_cache, v_cache, table, shortened, p.seen, o, lse, layer_begin, layer_end, at, left, stream);
+  }
   const int shares = shares_at_most(d, std::min(d->L, MANY_CHUNK_GROUPS), T);
   if (ws == nullptr || ws_bytes < chunk_bytes(shares, d->dh)) return KVP_ERR_WORKSPACE;
-  if (!aligned16(ws)) return KVP_ERR_UNSUPPORTED;
-  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   static thread_local ChunkParams<MANY_CHUNK_GROUPS> p;
   p.block_table = block_table;
   p.lengths = lengths;
@@ -1445,9 +1525,8 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
   p.page_size = d->page_size;
   p.max_pages = d->max_pages;
   p.n_pages = d->n_pages;
-  const int capacity = d->max_pages * d->page_size;
-  p.window = window < capacity ? window : 0;      // (nothing is further back)
-  p.sinks = std::min(sinks, capacity);
+  p.window = window;
+  p.sinks = sinks;
   p.box = d->page_size % 64 == 0 ? 64 : d->page_size % 32 == 0 ? 32 : 16;
   p.io_f32 = d->dtype == KVP_F32;
   p.scale_log2 = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;

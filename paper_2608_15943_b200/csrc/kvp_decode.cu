@@ -76,7 +76,8 @@ __device__ __forceinline__ uint32_t ring_off(int row, int chunk) {
   return uint32_t(row) * (DH * 2) + (uint32_t(chunk ^ (row & 7)) << 4);
 }
 
-template <int DH, int NG>
+// WINDOW: some positions of a sequence are not seen (p.seen).
+template <int DH, int NG, bool WINDOW>
 __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kernel(const __grid_constant__ DecParams<NG> p) {
   constexpr int ROW_BYTES = DH * 2;
   constexpr int CHUNKS = ROW_BYTES / 16;           // 16-byte chunks per row
@@ -98,6 +99,14 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
   struct Cursor {
     int grp, b, hk, gran, ng, len;
     int id;                                        // the unit's number, where units are dealt out
+    int2 hole;                                     // (WINDOW) tokens that are not seen
+    __device__ __forceinline__ bool sees(int token) const { return token < len && !(WINDOW && token >= hole.x && token < hole.y); }
+  };
+  auto look = [&](Cursor& x) {
+    if (WINDOW) {
+      const int4 of = p.seen[x.b];
+      x.hole = make_int2(of.x, of.y);
+    }
   };
   Cursor c;                                        // start of the block's next piece
   int todo;                                        // places of the block's share of the list still to do
@@ -110,6 +119,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
     x.gran = 0;
     x.len = clamped_length(p, x.b);
     x.ng = granules_of(x.len);
+    look(x);
   };
   bool by_units = p.by_units != 0;
   int rest = 0;                                    // places behind the granules of a unit
@@ -198,6 +208,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
       }
       x.len = clamped_length(p, x.b);
       x.ng = granules_of(x.len);
+      look(x);
     }
   };
   // The piece behind the one at x, of the `left` places of the block's share from x on; past the end: grp >= n_groups.
@@ -213,6 +224,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
     }
   };
 
+  if (!caller_splits && !by_units) look(c);
   if (c.gran >= c.ng && !caller_splits) {          // the share begins behind the granules of a unit
     next_piece(c, todo);
     if (c.grp >= p.n_groups) return;
@@ -261,7 +273,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
         const uint32_t off = ring_off<DH>(row, chunk);
         // Slots at or past the sequence length were never appended and may hold anything (a NaN there would
         // survive the zero probability in P V): they are filled with zeros instead of being read.
-        const uint32_t nbytes = f_tok + row < f.len ? 16u : 0u;
+        const uint32_t nbytes = f.sees(f_tok + row) ? 16u : 0u;
         cp_async16(dst + off, ksrc + size_t(idx) * 16, nbytes);
         cp_async16(dst + TILE_BYTES + off, vsrc + size_t(idx) * 16, nbytes);
       }
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
         for (int u = 0; u < 4; ++u) {
           const int tk = tok0 + nb * 8 + t * 2 + (u & 1);
           float x = sacc[nb][u] * p.scale_log2;
-          if (tk >= c.len) x = -INFINITY;
+          if (!c.sees(tk)) x = -INFINITY;
           sacc[nb][u] = x;
           mt[u >> 1] = fmaxf(mt[u >> 1], x);
         }
@@ -372,7 +384,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
         mt[h] = fmaxf(mt[h], __shfl_xor_sync(0xffffffffu, mt[h], 2));
         const float m_new = fmaxf(m_run[h], mt[h]), ref_new = fmaxf(falls ? m_new - REFERENCE_DROP : ref[h], mt[h]);
         alpha[h] = ref[h] == -INFINITY ? 0.f : fast_exp2(ref[h] - ref_new);
-        beta[h] = fast_exp2(ref_new - m_new);
+        beta[h] = WINDOW && m_new == -INFINITY ? 0.f : fast_exp2(ref_new - m_new);   // (nothing seen yet)
         l_run[h] *= m_run[h] == -INFINITY ? 0.f : fast_exp2(m_run[h] - m_new);
         m_run[h] = m_new;
         ref[h] = ref_new;
@@ -384,7 +396,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
         for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            pr[nb][u] = fast_exp2(sacc[nb][u] - ref[u >> 1]);
+            pr[nb][u] = fast_exp2(sacc[nb][u] - (WINDOW && ref[u >> 1] == -INFINITY ? 0.f : ref[u >> 1]));
             l_here[u >> 1] += pr[nb][u];
           }
 #pragma unroll
@@ -482,7 +494,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int row = g + 8 * h;
-        if (row < R) {
+        if (row < R && (!WINDOW || p.seen[here.b].z != 0)) {
           const int mem = row / G;
           const size_t head = size_t(here.b) * p.Hq + here.hk * G + row % G;
           const float inv = 1.f / l_run[h];
@@ -590,7 +602,7 @@ DealBy deal_by(int dh) { return {sm_count() * (dh == 128 ? DEC_CTAS_PER_SM<128> 
 int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                 const void* const* v_cache, const int32_t* block_table, const int32_t* lengths, void* const* o,
                 float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, size_t limit,
-                cudaStream_t stream);
+                const int4* seen, cudaStream_t stream);
 
 }  // namespace
 
@@ -653,26 +665,31 @@ extern "C" int kvp_cache_append(const kvp_decode_desc* d, const int32_t* donor, 
 namespace kvp {
 namespace {
 
-template <int DH, int NG>
+template <int DH, int NG, bool WINDOW>
 cudaError_t launch_decode(const DecParams<MAX_DEC_GROUPS>& all, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
   constexpr int smem = DEC_WARPS * DEC_STAGES * 2 * GRAN * DH * 2;
-  cudaError_t e = allow_smem<decode_kernel<DH, NG>>(smem);
+  cudaError_t e = allow_smem<decode_kernel<DH, NG, WINDOW>>(smem);
   if (e != cudaSuccess) return e;
   DecParams<NG> p;
   static_cast<DecSizes&>(p) = all;
   std::copy(all.grp, all.grp + all.n_groups, p.grp);
   timing_before(KVP_KERNEL_DECODE, stream);
-  e = launch_kernel(decode_kernel<DH, NG>, grid, DEC_THREADS, smem, stream, 1, p);
+  e = launch_kernel(decode_kernel<DH, NG, WINDOW>, grid, DEC_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
     e = launch_kernel(decode_combine_kernel<DH, false, DecParams<NG>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
 }
 
+template <int DH, int NG>
+cudaError_t launch_decode(const DecParams<MAX_DEC_GROUPS>& p, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
+  return p.seen != nullptr ? launch_decode<DH, NG, true>(p, grid, combine_grid, wpr, stream) : launch_decode<DH, NG, false>(p, grid, combine_grid, wpr, stream);
+}
+
 int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                 const void* const* v_cache, const int32_t* block_table, const int32_t* lengths, void* const* o,
                 float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, size_t limit,
-                cudaStream_t stream) {
+                const int4* seen, cudaStream_t stream) {
   int rc = check_desc(d);
   if (rc != KVP_OK) return rc;
   if (donor == nullptr || q == nullptr || k_cache == nullptr || v_cache == nullptr || block_table == nullptr ||
@@ -704,6 +721,7 @@ int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, con
   p.max_shares = sc_plan.max_shares;
   p.num_splits = d->num_splits;
   p.io_f32 = d->dtype == KVP_F32;
+  p.seen = seen;
   const float sc = scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale;
   p.scale_log2 = sc * 1.4426950408889634f;
 
@@ -752,12 +770,18 @@ int decode_impl(const kvp_decode_desc* d, const int32_t* donor, float scale, con
 }  // namespace
 }  // namespace kvp
 
+int kvp::decode_seen(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache, const void* const* v_cache,
+                     const int32_t* block_table, const int32_t* lengths, const int4* seen, void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws,
+                     size_t ws_bytes, cudaStream_t stream) {
+  return decode_impl(d, donor, scale, q, k_cache, v_cache, block_table, lengths, o, lse, layer_begin, layer_end, ws, ws_bytes, 0, seen, stream);
+}
+
 extern "C" int kvp_decode(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q,
                           const void* const* k_cache, const void* const* v_cache, const int32_t* block_table,
                           const int32_t* lengths, void* const* o, float* const* lse, int layer_begin, int layer_end,
                           void* ws, size_t ws_bytes, kvp_stream_t stream) {
   return decode_impl(d, donor, scale, q, k_cache, v_cache, block_table, lengths, o, lse, layer_begin, layer_end, ws,
-                     ws_bytes, 0, reinterpret_cast<cudaStream_t>(stream));
+                     ws_bytes, 0, nullptr, reinterpret_cast<cudaStream_t>(stream));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -815,6 +839,6 @@ extern "C" int kvp_decode_static(const kvp_decode_desc* d, const int32_t* donor,
   rc = static_scratch_address(&scratch);
   if (rc != KVP_OK) return rc;
   return decode_impl(d, donor, scale, q, k_cache, v_cache, block_table, lengths, o, lse, layer_begin, layer_end, scratch,
-                     size_t(KVP_DECODE_STATIC_SCRATCH_BYTES), size_t(KVP_DECODE_STATIC_SCRATCH_BYTES),
+                     size_t(KVP_DECODE_STATIC_SCRATCH_BYTES), size_t(KVP_DECODE_STATIC_SCRATCH_BYTES), nullptr,
                      reinterpret_cast<cudaStream_t>(stream));
 }

@@ -158,7 +158,8 @@ __device__ __forceinline__ uint32_t v_off(int row, int chunk) {
   return uint32_t(row >> 1) * 128 + (uint32_t((row & 1) << 2 | (chunk ^ (row >> 1 & 3))) << 4);
 }
 
-template <int DH, int NB, int NG>
+// WINDOW: some positions of a sequence are not seen (p.seen).
+template <int DH, int NB, int NG, bool WINDOW>
 __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
   constexpr int GRAN_BYTES = GRAN * DH, TILE_BYTES = 2 * GRAN_BYTES, SLOTS = D8_SLOTS<DH, NB>, DEPTH = SLOTS / 2;
   constexpr int CHUNKS = DH / 16;                  // 16-byte chunks of a row
@@ -178,6 +179,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   struct Cursor {
     int grp, b, hk, gran, ng, seen;                // seen: tokens of the sequence (0: none, in one granule)
     int id;                                        // the unit's number, where units are dealt out
+    int2 hole;                                     // (WINDOW) tokens that are not seen
+    __device__ __forceinline__ bool meets(int token, int n) const { return WINDOW && token < hole.y && token + n > hole.x; }
+    __device__ __forceinline__ bool skips(int token) const { return WINDOW && token >= hole.x && token < hole.y; }
   };
   Cursor c;
   int todo;                                        // places of the block's share of the list still to do
@@ -186,6 +190,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   auto set_length = [&](Cursor& x, int len) {
     x.seen = min(max(len, 0), cap);
     x.ng = granules_of(max(x.seen, 1));
+  };
+  auto look = [&](Cursor& x) {
+    if (WINDOW) {
+      const int4 of = p.seen[x.b];
+      x.hole = make_int2(of.x, of.y);
+    }
   };
   auto set_unit = [&](Cursor& x, int id) {
     x.id = id;
@@ -385,14 +395,17 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
           ++x.grp;
         }
         set_length(x, p.lengths[x.b]);
+        look(x);
       }
     } else if (by_units && !caller_splits && x.id + unit_step < units) {
       go_to_unit(x, x.id + unit_step);
+      look(x);
       left = x.ng;
     } else {
       x.grp = p.n_groups;
     }
   };
+  look(c);
   if (c.gran >= c.ng && !caller_splits) {          // the share begins behind the granules of a unit
     next_piece(c, todo);
     if (c.grp >= p.n_groups) return;
@@ -408,6 +421,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   const Dec8Group* f_grp = &p.grp[0];
   const int32_t* bt = nullptr;                     // block-table entry of the page the next step begins in,
   int in_page = 0, f_live = 0;                     // its granule there; tokens of the piece from there on
+  int f_at = 0;                                    // (WINDOW) its first token
   int page = 0;                                    // that entry, looked at when its step is asked for: a load ahead of it
   int slot_in = 0, slot_out = 0;                   // in pairs: K's tile and V's behind it
   auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
@@ -420,6 +434,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
     bt = p.block_table + size_t(f.b) * p.max_pages + col;
     in_page = gran - col * gran_per_page;
     f_live = min(f.seen, (f.gran + n) * GRAN) - gran * GRAN;
+    f_at = gran * GRAN;
     page = *bt;
   };
   // Scales of the steps in the ring: a lane has the byte of one granule (lane & 3: K's and V's of the first, of the second).
@@ -430,8 +445,10 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   // V's granules of the step whose K was asked for last, and how many tokens of it are to be read (-1: no step)
   const uint8_t *v_src0 = nullptr, *v_src1 = nullptr;
   int v_live = -1;
+  int v_at = 0;                                    // (WINDOW) its first token, and the tokens that are not seen
+  int2 v_hole = make_int2(0, 0);
   // the tile of a step: 32 rows in a run from src0, or (split) 16 from either
-  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool split, bool is_v) {
+  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool split, bool is_v, int at, int2 hole) {
     if (!split) {
 #pragma unroll
       for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
@@ -442,7 +459,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
 #pragma unroll
       for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
         const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
-        cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), (i < CP_PER_LANE ? src0 : src1) + i % CP_PER_LANE * 512, row < live ? 16u : 0u);
+        cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), (i < CP_PER_LANE ? src0 : src1) + i % CP_PER_LANE * 512,
+                   row < live && !(WINDOW && at + row >= hole.x && at + row < hole.y) ? 16u : 0u);
       }
     }
   };
@@ -460,13 +478,16 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       if (!in_a_row || f_live <= GRAN) block1 = f_live > GRAN ? block_of(bt[1]) : block0;
       scale = (lane & 1 ? f_grp->v_scale : f_grp->k_scale)[lane & 2 ? block1 : block0];
       const size_t at0 = block0 * GRAN_BYTES + lane * 16, at1 = block1 * GRAN_BYTES + lane * 16;
-      v_split = !in_a_row || f_live < STEP;
-      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, v_split, false);
+      v_split = !in_a_row || f_live < STEP || f.meets(f_at, STEP);
+      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, v_split, false, f_at, f.hole);
       v_src0 = f_grp->v_cache + at0;
       v_src1 = f_grp->v_cache + at1;
       v_live = max(f_live, 0);
+      v_at = f_at;
+      v_hole = f.hole;
       f_left -= team;
       f_live -= team * STEP;
+      f_at += team * STEP;
       in_page += team * 2;
       if (in_page >= gran_per_page && f_left > 0) {
         do {
@@ -480,7 +501,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   };
   auto issue_v = [&]() {
     if (v_live >= 0) {
-      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, v_split, true);
+      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, v_split, true, v_at, v_hole);
       if (++slot_in == DEPTH) slot_in = 0;
     }
     cp_async_commit();
@@ -603,6 +624,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       issue_k(scales[DEPTH - 1]);
       // ---- softmax: terms of the sum 2^(x - M), weights of V 2^(x - M) 2^(e - D) ----
       const int left = tokens - i * STEP;          // visible tokens from this step on
+      const int at = c.gran * GRAN + i * STEP;     // its first
+      const bool partly = c.meets(at, STEP);
       uint64_t factor[2][NB], x[2][NB][2];         // x - M
       float v_exp[2];
       uint64_t to_v[2][NB];                        // e - D
@@ -626,12 +649,12 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
                 x[m][nb][u] = pack_f2(__fadd_rn(__fmul_rn(s2[m][nb][0][2 * u], f2_lo(factor[m][nb])), f2_lo(minus_M[nb])),
                                       __fadd_rn(__fmul_rn(s2[m][nb][0][2 * u + 1], f2_hi(factor[m][nb])), f2_hi(minus_M[nb])));
         }
-        if (left < STEP) {
+        if (left < STEP || partly) {
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              if (m * GRAN + tok_g + 2 * u >= left) {
+              if (m * GRAN + tok_g + 2 * u >= left || c.skips(at + m * GRAN + tok_g + 2 * u)) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) x[m][nb][u] = pack_f2(-INFINITY, -INFINITY);
               }
@@ -667,7 +690,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
               y[m] = -INFINITY;
 #pragma unroll
               for (int u = 0; u < 2; ++u)
-                if (m * GRAN + tok_g + 2 * u < left) y[m] = fmaxf(y[m], s2[m][nb][0][2 * u + h] * (h ? f2_hi(factor[m][nb]) : f2_lo(factor[m][nb])));
+                if (m * GRAN + tok_g + 2 * u < left && !c.skips(at + m * GRAN + tok_g + 2 * u)) y[m] = fmaxf(y[m], s2[m][nb][0][2 * u + h] * (h ? f2_hi(factor[m][nb]) : f2_lo(factor[m][nb])));
             }
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
@@ -808,6 +831,8 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       }
     if (first_step != 0) {
       // (the piece's first warp alone goes on to store)
+    } else if (WINDOW && !caller_splits && from_start && to_end && p.seen[here.b].z == 0) {
+      // (the row of no sequence is left as it is)
     } else if (!caller_splits && from_start && to_end) {
       // ---- the whole unit: normalise and store; a lane has elements 16 m + g and 16 m + g + 8, of which lanes g and g ^ 1 make pairs ----
 #pragma unroll
@@ -876,20 +901,24 @@ int most_rows(const kvp_decode_desc* d, const SubGroup* subs, int n) {
   return rows;
 }
 
-template <int DH, int NB, int NG>
+template <int DH, int NB, int NG, bool WINDOW>
 cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& all, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
   constexpr int smem = D8_WARPS * D8_SLOTS<DH, NB> * STEP * DH;
-  cudaError_t e = allow_smem<decode8_kernel<DH, NB, NG>>(smem);
+  cudaError_t e = allow_smem<decode8_kernel<DH, NB, NG, WINDOW>>(smem);
   if (e != cudaSuccess) return e;
   Dec8Params<NG> p;
   static_cast<DecSizes&>(p) = all;
   std::copy(all.grp, all.grp + all.n_groups, p.grp);
   timing_before(KVP_KERNEL_DECODE, stream);
-  e = launch_kernel(decode8_kernel<DH, NB, NG>, grid, D8_THREADS, smem, stream, 1, p);
+  e = launch_kernel(decode8_kernel<DH, NB, NG, WINDOW>, grid, D8_THREADS, smem, stream, 1, p);
   timing_after(KVP_KERNEL_DECODE, stream);
   if (e == cudaSuccess && (p.num_splits > 0 || p.by_units == 0))   // whole units leave no pieces
     e = launch_kernel(decode_combine_kernel<DH, true, Dec8Params<NG>, Deal8<DH>>, combine_grid, COMBINE_THREADS, 0, stream, 1, p, wpr);
   return e;
+}
+template <int DH, int NB, int NG>
+cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& p, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
+  return p.seen != nullptr ? launch_decode8<DH, NB, NG, true>(p, grid, combine_grid, wpr, stream) : launch_decode8<DH, NB, NG, false>(p, grid, combine_grid, wpr, stream);
 }
 template <int DH, int NB>
 cudaError_t launch_decode8(const Dec8Params<MAX_DEC_GROUPS>& p, dim3 grid, dim3 combine_grid, int wpr, cudaStream_t stream) {
@@ -919,7 +948,14 @@ extern "C" size_t kvp_decode8_workspace_bytes(const kvp_decode_desc* d, const in
 extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache,
                            const void* const* v_cache, const uint8_t* const* k_scale, const uint8_t* const* v_scale, const int32_t* block_table,
                            const int32_t* lengths, void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes,
-                           kvp_stream_t stream_) {
+                           kvp_stream_t stream) {
+  return decode8_seen(d, donor, scale, q, k_cache, v_cache, k_scale, v_scale, block_table, lengths, nullptr, o, lse, layer_begin, layer_end, ws, ws_bytes,
+                      reinterpret_cast<cudaStream_t>(stream));
+}
+
+int kvp::decode8_seen(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache, const void* const* v_cache,
+                      const uint8_t* const* k_scale, const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths, const int4* seen,
+                      void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, cudaStream_t stream) {
   const int rc = check_desc8(d);
   if (rc != KVP_OK) return rc;
   if (donor == nullptr || q == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr || v_scale == nullptr ||
@@ -961,6 +997,7 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
   p.max_shares = plan.max_shares;
   p.num_splits = d->num_splits;
   p.io_f32 = d->dtype == KVP_F32;
+  p.seen = seen;
   p.scale_log2 = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
 
   for (int s0 = 0; s0 < n_sub; s0 += MAX_DEC_GROUPS) {
@@ -996,7 +1033,6 @@ extern "C" int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float
     const int wpr = unit_pieces > 8 ? 8 : 1;   // many pieces a unit: eight warps share those of a row
     const int rows_per_block = COMBINE_THREADS / 32 / wpr;
     const dim3 grid(static_cast<unsigned>(blocks)), cgrid(unsigned(units), (rows + rows_per_block - 1) / rows_per_block);
-    cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     const cudaError_t e = d->dh == 128 ? (plan.rows <= 8 ? launch_decode8<128, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<128, 2>(p, grid, cgrid, wpr, stream))
                                        : (plan.rows <= 8 ? launch_decode8<64, 1>(p, grid, cgrid, wpr, stream) : launch_decode8<64, 2>(p, grid, cgrid, wpr, stream));
     if (e != cudaSuccess) return KVP_ERR_CUDA;

@@ -29,6 +29,7 @@ struct DecSizes {
   int num_splits;              // > 0: the caller's split count instead; a block is one (unit, split)
   int io_f32;                  // queries are read and outputs written as fp32 (rounded to bf16 on load / widened on store)
   float scale_log2;
+  const int4* seen;            // [B], or null: under a window, the positions x <= j < y of the (shortened) sequence are not seen, and z: it has a row
 };
 
 __device__ __forceinline__ int clamp_length(const DecSizes& p, int len) { return min(max(len, 1), p.max_pages * p.page_size); }
@@ -215,6 +216,7 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
     if (warp % wpr != 0) return;
     for (int k = 1; k < wpr; ++k) merge(s_m[warp + k], s_l[warp + k], s_o[warp + k][lane % LANES]);
   }
+  if (p.seen != nullptr && p.seen[b].z == 0) return;   // (the row of no sequence is left as it is)
   if (row < R && lane < LANES) {
     const int mem = row / G;
     const size_t head = size_t(b) * p.Hq + hk * G + row % G;

@@ -74,6 +74,15 @@ struct BwdF32 {
   bool read_first;   // all inputs are read before any output is written
 };
 
+// kvp_decode and kvp_decode8 where some positions of a sequence are not seen: seen[b] (device) = (x, y, z): positions x <= j < y of
+// sequence b, which are neither read nor count; z == 0: it has no row, and nothing is written for it.
+int decode_seen(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache, const void* const* v_cache,
+                const int32_t* block_table, const int32_t* lengths, const int4* seen, void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws,
+                size_t ws_bytes, cudaStream_t stream);
+int decode8_seen(const kvp_decode_desc* d, const int32_t* donor, float scale, const void* const* q, const void* const* k_cache, const void* const* v_cache,
+                 const uint8_t* const* k_scale, const uint8_t* const* v_scale, const int32_t* block_table, const int32_t* lengths, const int4* seen,
+                 void* const* o, float* const* lse, int layer_begin, int layer_end, void* ws, size_t ws_bytes, cudaStream_t stream);
+
 void gemm_set_pair_mode(int mode);   // 0: single-CTA tiles only, 1: pairs where the caller prefers them, 2: pairs everywhere
 int gemm_pair_mode();
 int gemm_read_status();
