@@ -137,6 +137,27 @@ PyObject* bind_cache(PyObject*, PyObject* list) {
   Py_RETURN_NONE;
 }
 
+struct PagesLibrary {
+  decltype(&kvp_attn_chunk) attn_chunk;
+  decltype(&kvp_pages_copy) copy;
+  decltype(&kvp_pages_fork) fork;
+  decltype(&kvp_pages_resize) resize;
+  decltype(&kvp_pages_trim) trim;
+  decltype(&kvp_pages_compact) compact;
+} pages_lib;
+// bind_pages(addresses of the entry points that PagesLibrary lists)
+PyObject* bind_pages(PyObject*, PyObject* list) {
+  constexpr Py_ssize_t n = sizeof(PagesLibrary) / sizeof(void*);
+  if (!PyList_Check(list) || PyList_GET_SIZE(list) != n) return PyErr_Format(PyExc_ValueError, "%zd addresses", n);
+  void* at[n];
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    at[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  memcpy(&pages_lib, at, sizeof(pages_lib));
+  Py_RETURN_NONE;
+}
+
 // Element types of a tensor of the calls that look at their tensors.
 enum Kind { BF16, F32, I32, CODES, SCALES };
 bool is_kind(const at::Tensor& t, Kind k) {
@@ -578,13 +599,176 @@ ENTRY(decode8) {   // desc, donor, scale, q, k_cache, v_cache, k_scale, v_scale,
     return [=] { return cache_lib.decode8(d, donor, scale, q, kc, vc, ks, vs, table, lengths, o, lse, b, e, ws.p, ws.n, stream); };
   });
 }
+// A call's place: device (as Reader::device) and stream, its last arguments; what it says of the device is read ahead of the tensors.
+void read_device(Reader& r, PyObject* o, bool bound) {
+  r.ok = r.ok && bound;
+  r.device = r.ok && PyLong_CheckExact(o) ? int(PyLong_AsLong(o)) : -2;
+}
+// A workspace that is contiguous and on the call's device.
+Reader::Space space_of(Reader& r) {
+  if (r.ok && r.left > 0 && *r.a != Py_None && THPVariable_CheckExact(*r.a)) {
+    const at::Tensor& w = THPVariable_Unpack(*r.a);
+    r.ok = w.is_contiguous() && (r.device == -2 || (w.is_cuda() && w.get_device() == r.device));
+  }
+  return r.workspace();
+}
+const int32_t* int32_or_none(Reader& r, int64_t numel) {
+  if (r.left > 0 && *r.a == Py_None) {
+    r.next();
+    return nullptr;
+  }
+  return static_cast<const int32_t*>(r.one(I32, numel));
+}
+ENTRY(attn_chunk) {   // desc, donor, q, k_cache, v_cache, block_table, lengths, o, lse, ws, first, scale, window, sinks, k_scale, v_scale, layer_begin, layer_end or None, device, stream
+  return run(args, n, 20, [&](Reader& r) {
+    read_device(r, r.ok ? args[18] : Py_None, pages_lib.attn_chunk != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    r.ok = r.ok && r.entries == z.L && PyLong_CheckExact(args[16]) && (args[17] == Py_None || PyLong_CheckExact(args[17]));
+    const long begin = r.ok ? PyLong_AsLong(args[16]) : 0, end = r.ok && args[17] != Py_None ? PyLong_AsLong(args[17]) : z.L;
+    if (r.ok && (begin < 0 || begin >= end || end > z.L)) r.ok = false;   // (kvp.py's to refuse)
+    const int b = int(begin), e = int(end);
+    // the number of rows: of the first layer's queries
+    int64_t T = 0;
+    if (r.ok && PyList_CheckExact(*r.a) && PyList_GET_SIZE(*r.a) > b && THPVariable_CheckExact(PyList_GET_ITEM(*r.a, b))) {
+      const at::Tensor& q0 = THPVariable_Unpack(PyList_GET_ITEM(*r.a, b));
+      r.ok = q0.dim() > 0 && q0.size(0) > 0 && q0.size(0) <= INT32_MAX;   // (no rows, or missing ones: kvp.py's to tell)
+      T = r.ok ? q0.size(0) : 0;
+    } else {
+      r.ok = false;
+    }
+    const Kind io = z.dtype == KVP_F32 ? F32 : BF16;
+    const bool bits8 = r.ok && args[14] != Py_None;
+    const int64_t qs = T * z.Hq * z.dh, rows = int64_t(z.n_pages) * z.Hkv * z.page_size;
+    In q = r.layers_of<const void* const>(io, qs, donor, false, false, b, e);
+    In kc = r.layers_of<const void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true, false, b, e),
+       vc = r.layers_of<const void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true, false, b, e);
+    auto* table = static_cast<const int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<const int32_t*>(r.one(I32, z.B));
+    Out o = r.layers_of<void* const>(io, qs, donor, false, false, b, e);
+    OutF lse = r.layers_of<float* const>(F32, T * z.Hq, donor, false, false, b, e);
+    const Reader::Space ws = space_of(r);
+    const int32_t* first = int32_or_none(r, int64_t(z.B) + 1);
+    const float scale = float(r.real());
+    const long long window = r.integer(), sinks = r.integer();
+    r.ok = r.ok && window >= INT32_MIN && window <= INT32_MAX && sinks >= INT32_MIN && sinks <= INT32_MAX;
+    typedef const uint8_t* const* Scale;
+    Scale ks = r.layers_of<const uint8_t* const>(SCALES, rows / 16, donor, true, true, b, e), vs = r.layers_of<const uint8_t* const>(SCALES, rows / 16, donor, true, true, b, e);
+    r.next();
+    r.next();
+    r.next();
+    const kvp_stream_t stream = r.stream();
+    return [=] {
+      return pages_lib.attn_chunk(d, donor, int32_t(T), first, scale, int32_t(window), int32_t(sinks), q, kc, vc, ks, vs, table, lengths, o, lse, b, e, ws.p, ws.n, stream);
+    };
+  });
+}
+// The pools of a call on pages, and its last two arguments.
+struct PagePools {
+  Out k, v;
+  uint8_t* const* ks;
+  uint8_t* const* vs;
+  kvp_stream_t stream;
+  PagePools(Reader& r, const kvp_decode_desc& z, const int32_t* donor) {
+    const bool bits8 = r.ok && r.left > 2 && r.a[2] != Py_None;
+    const int64_t rows = int64_t(z.n_pages) * z.Hkv * z.page_size;
+    r.ok = r.ok && r.entries == z.L;
+    k = r.layers_of<void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true);
+    v = r.layers_of<void* const>(bits8 ? CODES : BF16, rows * z.dh, donor, true);
+    ks = r.layers_of<uint8_t* const>(SCALES, rows / 16, donor, true, true);
+    vs = r.layers_of<uint8_t* const>(SCALES, rows / 16, donor, true, true);
+    r.next();
+    stream = r.stream();
+  }
+};
+ENTRY(pages_copy) {   // desc, donor, src, dst, k_cache, v_cache, k_scale, v_scale, device, stream
+  return run(args, n, 10, [&](Reader& r) {
+    read_device(r, r.ok ? args[8] : Py_None, pages_lib.copy != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    int64_t count = 0;
+    r.ok = r.ok && THPVariable_CheckExact(args[2]);
+    if (r.ok) count = THPVariable_Unpack(args[2]).numel();
+    r.ok = r.ok && count <= INT32_MAX;
+    auto* src = static_cast<const int32_t*>(r.one(I32, count));
+    auto* dst = static_cast<const int32_t*>(r.one(I32, count));
+    const PagePools at(r, z, donor);
+    return [=] { return pages_lib.copy(d, donor, int32_t(count), src, dst, at.k, at.v, at.ks, at.vs, at.stream); };
+  });
+}
+ENTRY(pages_fork) {   // desc, parent, refs, block_table, lengths, ws, device, stream
+  return run(args, n, 8, [&](Reader& r) {
+    read_device(r, r.ok ? args[6] : Py_None, pages_lib.fork != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    auto* parent = static_cast<const int32_t*>(r.one(I32, z.B));
+    auto* refs = static_cast<int32_t*>(r.one(I32, z.n_pages));
+    auto* table = static_cast<int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<int32_t*>(r.one(I32, z.B));
+    const Reader::Space ws = space_of(r);
+    r.next();
+    const kvp_stream_t stream = r.stream();
+    return [=] { return pages_lib.fork(d, parent, refs, table, lengths, ws.p, ws.n, stream); };
+  });
+}
+ENTRY(pages_resize) {   // desc, donor, new_lengths, refs, block_table, lengths, lacking, ws, k_cache, v_cache, k_scale, v_scale, device, stream
+  return run(args, n, 14, [&](Reader& r) {
+    read_device(r, r.ok ? args[12] : Py_None, pages_lib.resize != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    auto* to = static_cast<const int32_t*>(r.one(I32, z.B));
+    auto* refs = static_cast<int32_t*>(r.one(I32, z.n_pages));
+    auto* table = static_cast<int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<int32_t*>(r.one(I32, z.B));
+    auto* lacking = static_cast<int32_t*>(r.one(I32, 1));
+    const Reader::Space ws = space_of(r);
+    const PagePools at(r, z, donor);
+    return [=] { return pages_lib.resize(d, donor, to, refs, table, lengths, lacking, ws.p, ws.n, at.k, at.v, at.ks, at.vs, at.stream); };
+  });
+}
+ENTRY(pages_trim) {   // desc, window, sinks, refs, block_table, lengths, device, stream
+  return run(args, n, 8, [&](Reader& r) {
+    read_device(r, r.ok ? args[6] : Py_None, pages_lib.trim != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    const long long window = r.integer(), sinks = r.integer();
+    r.ok = r.ok && window >= INT32_MIN && window <= INT32_MAX && sinks >= INT32_MIN && sinks <= INT32_MAX;
+    auto* refs = static_cast<int32_t*>(r.one(I32, z.n_pages));
+    auto* table = static_cast<int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<const int32_t*>(r.one(I32, z.B));
+    r.next();
+    const kvp_stream_t stream = r.stream();
+    return [=] { return pages_lib.trim(d, int32_t(window), int32_t(sinks), refs, table, lengths, stream); };
+  });
+}
+ENTRY(pages_compact) {   // desc, donor, refs, block_table, lengths, used, ws, k_cache, v_cache, k_scale, v_scale, device, stream
+  return run(args, n, 13, [&](Reader& r) {
+    read_device(r, r.ok ? args[11] : Py_None, pages_lib.compact != nullptr);
+    auto* d = r.structure<kvp_decode_desc>(desc_type);
+    auto* donor = r.donor_map();
+    const kvp_decode_desc z = r.ok ? *d : kvp_decode_desc{};
+    auto* refs = static_cast<int32_t*>(r.one(I32, z.n_pages));
+    auto* table = static_cast<int32_t*>(r.one(I32, int64_t(z.B) * z.max_pages));
+    auto* lengths = static_cast<const int32_t*>(r.one(I32, z.B));
+    auto* used = static_cast<int32_t*>(r.one(I32, 1));
+    const Reader::Space ws = space_of(r);
+    const PagePools at(r, z, donor);
+    return [=] { return pages_lib.compact(d, donor, refs, table, lengths, used, ws.p, ws.n, at.k, at.v, at.ks, at.vs, at.stream); };
+  });
+}
 #define METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(fn)), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {{"pointers", pointers, METH_VARARGS, nullptr}, {"donors", donors, METH_O, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr},
+                         {"bind_pages", bind_pages, METH_O, nullptr},
                          METHOD("gemm", gemm), METHOD("rmsnorm", rmsnorm), METHOD("rope", rope), METHOD("swiglu", zip<false>), METHOD("add", zip<true>),
                          METHOD("proj_fwd", proj_fwd), METHOD("proj_bwd", proj_bwd), METHOD("out_proj_fwd", out_proj_fwd), METHOD("out_proj_bwd", out_proj_bwd),
                          METHOD("attn_fwd", attn_fwd), METHOD("attn_bwd", attn_bwd), METHOD("cache_append", cache_append), METHOD("decode", decode),
                          METHOD("cache_append_tokens", cache_append_tokens), METHOD("decode8", decode8),
+                         METHOD("attn_chunk", attn_chunk), METHOD("pages_copy", pages_copy), METHOD("pages_fork", pages_fork), METHOD("pages_resize", pages_resize),
+                         METHOD("pages_trim", pages_trim), METHOD("pages_compact", pages_compact),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pack", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -669,6 +669,10 @@ def attn_chunk(desc, donor, q, k_cache, v_cache, block_table, lengths, o, lse, w
     alone.  With k_scale, v_scale the cache is the 8-bit one.  ws: attn_chunk_workspace_bytes.  Tensors are contiguous, of the
     documented sizes, on the current device: ValueError otherwise."""
     device, stream = _call_place()
+    status = _pack.attn_chunk(desc, donor, q, k_cache, v_cache, block_table, lengths, o, lse, ws, first, scale, window, sinks, k_scale, v_scale, layer_begin,
+                              layer_end, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_attn_chunk")
     end = desc.L if layer_end is None else int(layer_end)
     layers, owners = _layer_range(desc, donor, int(layer_begin), end)
     T = next((int(q[l].shape[0]) if q[l].dim() else 0 for l in layers if l < len(q) and q[l] is not None), 0)
@@ -733,6 +737,9 @@ def pages_copy(desc, donor, src, dst, k_cache, v_cache, k_scale=None, v_scale=No
     """kvp_pages_copy: the pages src[i] go to dst[i] (int32, as many), in all owner layers.  No page may be the target of two, nor a
     target and a source.  Tensors of these calls are contiguous, of the documented sizes, on the current device: ValueError otherwise."""
     device, stream = _call_place()
+    status = _pack.pages_copy(desc, donor, src, dst, k_cache, v_cache, k_scale, v_scale, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_pages_copy")
     n = src.numel()
     _fit("src", src, _I32, n, device)
     _fit("dst", dst, _I32, n, device)
@@ -744,6 +751,9 @@ def pages_fork(desc, parent, refs, block_table, lengths, ws):
     """kvp_pages_fork: row b goes on from what row parent[b] was (its own number: it stays; -1: it ends).  Pages are shared, none is
     copied; refs, block_table and lengths are updated in place."""
     device, stream = _call_place()
+    status = _pack.pages_fork(desc, parent, refs, block_table, lengths, ws, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_pages_fork")
     _fit_book(desc, device, ws, parent=parent, refs=refs, block_table=block_table, lengths=lengths)
     p, size = _ws(ws)
     _check(lib.kvp_pages_fork(C.byref(desc), _ptr(parent), _ptr(refs), _ptr(block_table), _ptr(lengths), p, size, stream), "kvp_pages_fork")
@@ -753,6 +763,9 @@ def pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, 
     """kvp_pages_resize: rows grow and shrink to new_lengths; a row that grows inside a shared page gets a copy of it.  lacking (int32
     [1]) receives 0, or what is short (then nothing is changed): the pages lacking, -1 for a length out of range."""
     device, stream = _call_place()
+    status = _pack.pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, ws, k_cache, v_cache, k_scale, v_scale, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_pages_resize")
     _fit_book(desc, device, ws, new_lengths=new_lengths, refs=refs, block_table=block_table, lengths=lengths, lacking=lacking)
     d, pools = _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device)
     p, size = _ws(ws)
@@ -763,6 +776,9 @@ def pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, 
 def pages_trim(desc, window, sinks, refs, block_table, lengths):
     """kvp_pages_trim: frees the pages that no later token sees with this window and so many first tokens."""
     device, stream = _call_place()
+    status = _pack.pages_trim(desc, window, sinks, refs, block_table, lengths, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_pages_trim")
     _fit_book(desc, device, refs=refs, block_table=block_table, lengths=lengths)
     _check(lib.kvp_pages_trim(C.byref(desc), int(window), int(sinks), _ptr(refs), _ptr(block_table), _ptr(lengths), stream), "kvp_pages_trim")
 
@@ -770,7 +786,13 @@ def pages_trim(desc, window, sinks, refs, block_table, lengths):
 def pages_compact(desc, donor, refs, block_table, lengths, used, ws, k_cache, v_cache, k_scale=None, v_scale=None):
     """kvp_pages_compact: the used pages become pages 0 .. used-1; used (int32 [1]) receives their number."""
     device, stream = _call_place()
+    status = _pack.pages_compact(desc, donor, refs, block_table, lengths, used, ws, k_cache, v_cache, k_scale, v_scale, device, stream)
+    if status is not NotImplemented:
+        return _check(status, "kvp_pages_compact")
     _fit_book(desc, device, ws, refs=refs, block_table=block_table, lengths=lengths, used=used)
     d, pools = _pool_arrays(desc, donor, k_cache, v_cache, k_scale, v_scale, device)
     p, size = _ws(ws)
     _check(lib.kvp_pages_compact(C.byref(desc), d, _ptr(refs), _ptr(block_table), _ptr(lengths), _ptr(used), p, size, *pools, stream), "kvp_pages_compact")
+
+
+_pack.bind_pages([C.cast(getattr(lib, "kvp_" + n), C.c_void_p).value for n in ("attn_chunk", "pages_copy", "pages_fork", "pages_resize", "pages_trim", "pages_compact")])

@@ -1,4 +1,5 @@
 """What the calls on new tokens and on pages refuse, before anything reaches the device; the pages' oracle by itself."""
+import ctypes as C
 import random
 import types
 
@@ -20,6 +21,16 @@ def kvp():
 def as_on_a_device(kvp, monkeypatch):
     """Tensors on the host pass the look at their device, and the call stops at the library's own checks."""
     monkeypatch.setattr(kvp, "_call_place", lambda: (-2, 0))
+
+
+NATIVE = ("attn_chunk", "pages_copy", "pages_fork", "pages_resize", "pages_trim", "pages_compact")
+
+
+@pytest.fixture(params=["native", "ctypes"], autouse=True)
+def path(request, kvp, monkeypatch):
+    """Both ways into the library: the native module, and what it leaves to the binding."""
+    if request.param == "ctypes":
+        monkeypatch.setattr(kvp, "_pack", types.SimpleNamespace(**{n: lambda *a: NotImplemented for n in NATIVE}))
 
 
 @pytest.fixture
@@ -226,3 +237,63 @@ def test_the_oracle_by_hand():
     book.trim(3, 0)
     assert book.table[0][:3] == [-1, -1, 1] and book.table[1][:2] == [-1, 3]
     assert book.compact() == 2 and book.table[0][2] == 1 and book.table[1][1] == 0
+
+
+# ---------------------------------------------------------------------------------------------
+# what both paths hand over
+# ---------------------------------------------------------------------------------------------
+FORMS = {"attn_chunk": "SDipfiiAAAAAppAAiiplp", "pages_copy": "SDippAAAAp", "pages_fork": "Sppppplp", "pages_resize": "SDppppp" + "pl" + "AAAAp", "pages_trim": "Siipppp",
+         "pages_compact": "SDpppp" + "pl" + "AAAAp"}
+TYPES = dict(i=C.c_int, l=C.c_size_t, f=C.c_float, p=C.c_void_p, S=C.c_void_p, D=C.c_void_p, A=C.c_void_p)
+
+
+def test_both_paths_hand_over_the_same(kvp, monkeypatch, request):
+    if torch.cuda.is_available() or "ctypes" in request.node.name:
+        pytest.skip("host tensors; both paths at once")
+    seen, keep = [], []
+    for name, form in FORMS.items():
+        def called(*args, name=name, form=form):
+            layers = C.cast(args[0], C.POINTER(C.c_int32))[0]
+            read = {"S": lambda v: C.string_at(v, C.sizeof(kvp.DecodeDesc)), "D": lambda v: C.string_at(v, 4 * layers), "A": lambda v: v and C.string_at(v, 8 * layers)}
+            seen.append([name] + [read.get(k, lambda v: v)(v) for k, v in zip(form, args)])
+            return 0
+        keep.append(C.CFUNCTYPE(C.c_int, *[TYPES[k] for k in form])(called))
+        monkeypatch.setattr(kvp.lib, "kvp_" + name, keep[-1])
+    real = kvp._pack
+    original = [C.cast(getattr(C.CDLL(kvp.LIB_PATH), "kvp_" + n), C.c_void_p).value for n in FORMS]
+    monkeypatch.setattr(kvp, "_call_place", lambda: (-2, 0x7f0000001238))
+    none = types.SimpleNamespace(**{n: lambda *a: NotImplemented for n in NATIVE})
+    real.bind_pages([C.cast(cb, C.c_void_p).value for cb in keep])
+    try:
+        calls = []
+        for over, kw in (({}, {}), (dict(bits8=True), dict(window=9, sinks=3)), (dict(dtype=torch.float32), dict(scale=0.25, layer_begin=1)), ({}, dict(layer_end=1, window=2))):
+            a = chunk_args(kvp, **over)
+            a.kw = kw
+            calls.append(lambda a=a: chunk(kvp, a))
+        a = chunk_args(kvp, T=3)
+        a.first = None
+        calls.append(lambda a=a: chunk(kvp, a))
+        for bits8 in (False, True):
+            a = pages_args(kvp)
+            if bits8:
+                b = chunk_args(kvp, bits8=True)
+                a.k, a.v, a.ks, a.vs = b.k, b.v, b.ks, b.vs
+            a.kw = dict(window=7, sinks=2)
+            calls += [lambda a=a, f=f: f(kvp, a) for f in CALLS.values()]
+        for call in calls:
+            del seen[:]
+            monkeypatch.setattr(kvp, "_pack", real)
+            call()
+            monkeypatch.setattr(kvp, "_pack", none)
+            call()
+            x, y = seen
+            assert len(x) == len(FORMS[x[0]]) + 1
+            for k, u, w in zip("." + FORMS[x[0]], x, y):
+                if k != "A":
+                    assert u == w, (x[0], k)
+                    continue
+                assert (u is None) == (w is None)
+                for i in range(0, len(u or b""), 8):          # (the native path hands over what the call looks at alone)
+                    assert u[i:i + 8] in (w[i:i + 8], bytes(8))
+    finally:
+        real.bind_pages(original)
