@@ -18,9 +18,11 @@
 // behind the sequence, freed pages before the window: anything may be there) are not read and are zeros in shared memory.  A
 // visible row of V with an infinity or NaN in it must reach the rows that see it and no other, which 0 * NaN in a matrix product
 // does not give: in blocks with any masking such rows are taken out, and the softmax threads add them to O by themselves.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kvp_cache8.cuh"
 #include "kvp_decode_list.cuh"
@@ -158,27 +160,40 @@ __device__ __forceinline__ Walked walked(const ChunkSizes& p, const Span& s, int
   w.n_a = min(w.sink_blocks, end_a) + max(0, end_a - w.from);
   return w;
 }
-// Places of the lane's sequence b (0 behind the last), a warp together.
-__device__ __forceinline__ long long places_of(const ChunkSizes& p, int b, int R) {
+// Of the lane's sequence b (nothing behind the last), a warp together: places, units of a KV head, steps of the longest.
+struct Listed {
+  long long places;
+  int pairs, longest;
+};
+__device__ __forceinline__ Listed listed(const ChunkSizes& p, int b, int R) {
   const int lane = lane_id();
   Span s{0, 0, 0};
   if (b < p.B) s = span_of(p, b);
-  const int pairs = pairs_of(s, R);
-  long long sum = 0;
-  const bool few = pairs <= 2;
+  Listed l{0, pairs_of(s, R), 0};
+  const bool few = l.pairs <= 2;
   if (few)
-    for (int i = 0; i < pairs; ++i) sum += walked(p, s, R, i).n + REST;
+    for (int i = 0; i < l.pairs; ++i) {
+      const int n = walked(p, s, R, i).n;
+      l.places += n + REST;
+      l.longest = max(l.longest, n);
+    }
   for (uint32_t left = __ballot_sync(0xffffffffu, !few); left != 0; left &= left - 1) {
     const int of = __ffs(left) - 1;
     const Span t{__shfl_sync(0xffffffffu, s.row0, of), __shfl_sync(0xffffffffu, s.n, of), __shfl_sync(0xffffffffu, s.pos0, of)};
-    const int n = __shfl_sync(0xffffffffu, pairs, of);
+    const int n = __shfl_sync(0xffffffffu, l.pairs, of);
     long long mine = 0;
-    for (int i = lane; i < n; i += 32) mine += walked(p, t, R, i).n + REST;
+    int longest = 0;
+    for (int i = lane; i < n; i += 32) {
+      const int steps = walked(p, t, R, i).n;
+      mine += steps + REST;
+      longest = max(longest, steps);
+    }
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-    if (lane == of) sum = mine;
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (lane == of) l.places = mine, l.longest = longest;
   }
-  return sum;
+  return l;
 }
 __device__ __forceinline__ long long warp_scan(long long v) {   // inclusive
 #pragma unroll
@@ -188,73 +203,212 @@ __device__ __forceinline__ long long warp_scan(long long v) {   // inclusive
   }
   return v;
 }
-// Where a share begins
+// What a CTA gets: whole units `first`, first + gridDim.x, ... below `rounds_end`, then a share of the list behind them.
 struct Share {
   int g, hk, b, pair;
   int off;           // places of the unit that belong to earlier shares
   int left;          // places of the share
+  long long rounds_end;
 };
-// Sums over 32 sequences each, then over all before them: sums[kind][i], i <= n32 = ceil(B / 32).  All warps of the block.
-__device__ __forceinline__ void list_sums(const ChunkSizes& p, long long* sums, int n32, int warps) {
-  const int warp = threadIdx.x >> 5, lane = lane_id();
-  for (int i = warp; i < n32 * p.n_kinds; i += warps) {
-    const int kind = i / n32, at = i % n32;
-    long long v = places_of(p, at * 32 + lane, p.kind_rows[kind]);
+// Sums over 32 sequences each, then over all before them, i <= n32 = ceil(B / 32): of places [kind][i], and of units [kind][i]; longest
+// unit of each 32.  All warps of the block.
+struct Sums {
+  long long *places, *units;
+  int* longest;
+  int n32;
+  __device__ __forceinline__ Sums(void* at, const ChunkSizes& p) : places(static_cast<long long*>(at)), n32((p.B + 31) / 32) {
+    units = places + p.n_kinds * (n32 + 1);
+    longest = reinterpret_cast<int*>(units + p.n_kinds * (n32 + 1));
+  }
+  __device__ __forceinline__ void* end(const ChunkSizes& p) const { return longest + (p.n_kinds * n32 + 1) / 2 * 2; }
+  __device__ __forceinline__ long long all_places(int kind) const { return places[kind * (n32 + 1) + n32]; }
+  __device__ __forceinline__ long long all_units(int kind) const { return units[kind * (n32 + 1) + n32]; }
+};
+__device__ __forceinline__ long long warp_sum(long long v) {
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if (lane == 0) sums[kind * (n32 + 1) + at] = v;
+  for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+__device__ __forceinline__ void list_sums(const ChunkSizes& p, const Sums& s, int warps) {
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+  for (int i = warp; i < s.n32 * p.n_kinds; i += warps) {
+    const int kind = i / s.n32, at = i % s.n32;
+    const Listed l = listed(p, at * 32 + lane, p.kind_rows[kind]);
+    const long long places = warp_sum(l.places), units = warp_sum(l.pairs);
+    const int longest = __reduce_max_sync(0xffffffffu, l.longest);
+    if (lane == 0) {
+      s.places[kind * (s.n32 + 1) + at] = places;
+      s.units[kind * (s.n32 + 1) + at] = units;
+      s.longest[i] = longest;
+    }
   }
   __syncthreads();
-  for (int kind = warp; kind < p.n_kinds; kind += warps) {
-    long long* const s = sums + kind * (n32 + 1);
+  for (int k = warp; k < 2 * p.n_kinds; k += warps) {
+    long long* const of = s.places + k * (s.n32 + 1);       // (units follow places)
     long long before = 0;
-    for (int i0 = 0; i0 < n32; i0 += 32) {
+    for (int i0 = 0; i0 < s.n32; i0 += 32) {
       const int i = i0 + lane;
-      const long long v = i < n32 ? s[i] : 0, up = warp_scan(v);
-      if (i < n32) s[i] = before + up - v;
+      const long long v = i < s.n32 ? of[i] : 0, up = warp_scan(v);
+      if (i < s.n32) of[i] = before + up - v;
       before += __shfl_sync(0xffffffffu, up, 31);
     }
     __syncwarp();
-    if (lane == 0) s[n32] = before;
+    if (lane == 0) of[s.n32] = before;
   }
   __syncthreads();
 }
-// The share of this CTA, by one warp; writes the note for the merge.  Returns false where there is none.
-__device__ __forceinline__ bool find_share(const ChunkSizes& p, const long long* sums, int n32, Share& out) {
+// the last of sums[0 .. n) that is at or below `at`, by a warp
+__device__ __forceinline__ int last_below(const long long* sums, int n, long long at) {
+  int i = 0;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const uint32_t below = __ballot_sync(0xffffffffu, i0 + lane_id() < n && sums[i0 + lane_id()] <= at);
+    if (below == 0) break;
+    i = i0 + 31 - __clz(below);
+  }
+  return i;
+}
+// How the list is dealt out.  Many units: whole, in rounds of one a CTA, so that CTAs that run together read the same keys at the same
+// time, out of L2; the last two rounds and what is left are cut into shares that even out what the rounds gave.  Not where a unit is longer
+// than an eighth of a CTA's work (what is left would not even that out), or where there are few: equal shares of the whole list.
+// (Pieces of prompts behind 2K to 8K tokens, read out of memory: 8.3 GB with equal shares of the list.)
+constexpr int ROUNDS_FROM = 4, ROUNDS_LEFT = 2;
+struct Deal {
+  long long rounds_end;        // units that are dealt out whole
+  long long base;              // their places
+  long long total;             // places behind them
+  int n;                       // shares of these
+  bool even;                   // all alike, or from places `begin` on
+  long long* begin;            // [n + 1]
+  __device__ __forceinline__ long long first(int w) const { return even ? Dealt(total, n).begin(w) : begin[w]; }
+  __device__ __forceinline__ int share_of(long long at) const { return even ? Dealt(total, n).share_of(at) : last_below(begin, n, at); }
+};
+// The unit, or the place, `at` of the list, by a warp: group, KV head, sequence; what is left is inside the sequence's.  `other`: the
+// places, or units, ahead of it.
+struct Found {
+  int g, hk, b;
+  long long left, other;
+};
+template <bool UNITS>
+__device__ __forceinline__ Found find(const ChunkSizes& p, const Sums& s, long long at) {
+  Found f{0, 0, 0, at, 0};
+  auto all = [&](int kind, bool units) { return units ? s.all_units(kind) : s.all_places(kind); };
+  for (;; ++f.g) {
+    const int kind = p.kind[f.g];
+    if (f.left < all(kind, UNITS) * p.Hkv) break;
+    f.left -= all(kind, UNITS) * p.Hkv;
+    f.other += all(kind, !UNITS) * p.Hkv;
+  }
+  const int kind = p.kind[f.g];
+  f.hk = int(div_places(f.left, all(kind, UNITS)));
+  f.left -= f.hk * all(kind, UNITS);
+  f.other += f.hk * all(kind, !UNITS);
+  const int row = kind * (s.n32 + 1), i = last_below((UNITS ? s.units : s.places) + row, s.n32, f.left);
+  f.left -= (UNITS ? s.units : s.places)[row + i];
+  f.other += (UNITS ? s.places : s.units)[row + i];
+  const Listed l = listed(p, i * 32 + lane_id(), p.kind_rows[kind]);
+  const long long mine = UNITS ? l.pairs : l.places, its = UNITS ? l.places : l.pairs, up = warp_scan(mine), up_its = warp_scan(its);
+  const int of = __ffs(__ballot_sync(0xffffffffu, up > f.left)) - 1;
+  f.left -= __shfl_sync(0xffffffffu, up - mine, of);
+  f.other += __shfl_sync(0xffffffffu, up_its - its, of);
+  f.b = i * 32 + of;
+  return f;
+}
+// By all warps of the block; `room` bytes of shared memory behind the sums.
+__device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int room, int warps) {
+  const int lane = lane_id(), warp = threadIdx.x >> 5, n = int(gridDim.x);
+  Deal d{0, 0, 0, 0, true, static_cast<long long*>(s.end(p))};
+  long long units = 0;
+  int longest = 0;
+  for (int g = 0; g < p.n_groups; ++g) {
+    d.total += s.all_places(p.kind[g]) * p.Hkv;
+    units += s.all_units(p.kind[g]) * p.Hkv;
+  }
+  for (int i = lane; i < s.n32 * p.n_kinds; i += 32) longest = max(longest, s.longest[i]);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (units >= (long long)ROUNDS_FROM * n && (long long)longest * 8 * n <= d.total) {
+    d.rounds_end = (div_places(units, n) - ROUNDS_LEFT) * n;
+    const Found f = find<true>(p, s, d.rounds_end);
+    const Span span = span_of(p, f.b);
+    const int R = p.members[f.g] * p.G;
+    long long before = 0;
+    for (int pair = lane; pair < int(f.left); pair += 32) before += walked(p, span, R, pair).n + REST;
+    d.base = f.other + warp_sum(before);
+    // what the rounds give each CTA, from the places of every unit of a KV head
+    int* const cost = reinterpret_cast<int*>(d.begin + n + 1);
+    long long all = 0;
+    for (int kind = 0; kind < p.n_kinds; ++kind) all += s.all_units(kind);
+    if (all * 4 + (n + 1) * 8 <= room) {
+      for (int kind = 0, at = 0; kind < p.n_kinds; at += int(s.all_units(kind)), ++kind) {
+        const int rows = p.kind_rows[kind];
+        for (int i = warp; i < s.n32; i += warps) {
+          const Span mine = i * 32 + lane < p.B ? span_of(p, i * 32 + lane) : Span{0, 0, 0};
+          const int pairs = pairs_of(mine, rows);
+          const int to = at + int(s.units[kind * (s.n32 + 1) + i] + warp_scan(pairs) - pairs);
+          const bool few = pairs <= 2;
+          if (few)
+            for (int pair = 0; pair < pairs; ++pair) cost[to + pair] = walked(p, mine, rows, pair).n + REST;
+          for (uint32_t left = __ballot_sync(0xffffffffu, !few); left != 0; left &= left - 1) {
+            const int of = __ffs(left) - 1;
+            const Span t{__shfl_sync(0xffffffffu, mine.row0, of), __shfl_sync(0xffffffffu, mine.n, of), __shfl_sync(0xffffffffu, mine.pos0, of)};
+            const int many = __shfl_sync(0xffffffffu, pairs, of), from = __shfl_sync(0xffffffffu, to, of);
+            for (int pair = lane; pair < many; pair += 32) cost[from + pair] = walked(p, t, rows, pair).n + REST;
+          }
+        }
+      }
+      __syncthreads();
+      if (int(threadIdx.x) < n) {
+        long long mine = 0, in = threadIdx.x;                  // unit of the KV head `g`, hk
+        int g = 0, hk = 0, at = 0;
+        for (long long u = threadIdx.x; u < d.rounds_end; u += n, in += n) {
+          while (in >= s.all_units(p.kind[g])) {
+            in -= s.all_units(p.kind[g]);
+            if (++hk == p.Hkv) {
+              hk = 0;
+              ++g;
+              at = 0;
+              for (int kind = 0; kind < p.kind[g]; ++kind) at += int(s.all_units(kind));
+            }
+          }
+          mine += cost[at + in];
+        }
+        d.begin[threadIdx.x] = max(0ll, div_places(d.total, n) - mine);
+      }
+      __syncthreads();
+      if (warp == 0) {                                         // sums, then in proportion: they come to what is left
+        long long sum = 0;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+          const long long v = i0 + lane < n ? d.begin[i0 + lane] : 0, up = warp_scan(v);
+          __syncwarp();
+          if (i0 + lane < n) d.begin[i0 + lane] = sum + up - v;
+          sum += __shfl_sync(0xffffffffu, up, 31);
+        }
+        __syncwarp();
+        const double part = sum > 0 ? double(d.total - d.base) / double(sum) : 0.;
+        for (int i = lane; i < n; i += 32) d.begin[i] = min(d.total - d.base, (long long)(double(d.begin[i]) * part));
+        if (lane == 0) d.begin[n] = d.total - d.base;
+      }
+      d.even = false;
+      __syncthreads();
+    }
+  }
+  d.total -= d.base;
+  d.n = d.even ? int(min((long long)n, max(d.total > 0 ? 1ll : 0ll, d.total / LEAST_SHARE))) : n;
+  return d;
+}
+// The share of this CTA, by one warp; writes the note for the merge.
+__device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, const Deal& d) {
   const int lane = lane_id(), w = int(blockIdx.x);
-  long long total = 0;
-  for (int g = 0; g < p.n_groups; ++g) total += sums[p.kind[g] * (n32 + 1) + n32] * p.Hkv;
-  const int n = int(min((long long)gridDim.x, max(total > 0 ? 1ll : 0ll, total / LEAST_SHARE)));
+  Share out{0, 0, 0, 0, 0, 0, d.rounds_end};
   Merge note{0, 0, 0, 0, -1, -1, {0, 0}};
-  bool there = w < n;
-  if (there) {
-    const Dealt dealt(total, n);
-    long long at = dealt.begin(w);
-    int g = 0;
-    for (;; ++g) {
-      const long long of_group = sums[p.kind[g] * (n32 + 1) + n32] * p.Hkv;
-      if (at < of_group) break;
-      at -= of_group;
-    }
-    const long long* const s = sums + p.kind[g] * (n32 + 1);
-    const int R = p.kind_rows[p.kind[g]];
-    out.g = g;
-    out.hk = int(div_places(at, s[n32]));
-    at -= out.hk * s[n32];
-    // the last 32 sequences that begin at or before it, then the sequence
-    int i = 0;
-    for (int i0 = 0; i0 < n32; i0 += 32) {
-      const uint32_t before = __ballot_sync(0xffffffffu, i0 + lane < n32 && s[i0 + lane] <= at);
-      if (before == 0) break;
-      i = i0 + 31 - __clz(before);
-    }
-    at -= s[i];
-    const long long mine = places_of(p, i * 32 + lane, R), up = warp_scan(mine);
-    const int of = __ffs(__ballot_sync(0xffffffffu, up > at)) - 1;
-    at -= __shfl_sync(0xffffffffu, up - mine, of);
-    out.b = i * 32 + of;
-    const Span span = span_of(p, out.b);
-    const int pairs = pairs_of(span, R);
+  const long long begin = w < d.n ? d.first(w) : 0, size = w < d.n ? (w + 1 < d.n ? d.first(w + 1) : d.total) - begin : 0;
+  if (size > 0) {
+    const Found f = find<false>(p, s, d.base + begin);
+    out.g = f.g;
+    out.hk = f.hk;
+    out.b = f.b;
+    long long at = f.left;
+    const Span span = span_of(p, f.b);
+    const int R = p.members[f.g] * p.G, pairs = pairs_of(span, R);
     for (int pair0 = 0;; pair0 += 32) {
       const int pair = pair0 + lane;
       const long long cost = pair < pairs ? walked(p, span, R, pair).n + REST : 0, sum = warp_scan(cost);
@@ -269,13 +423,21 @@ __device__ __forceinline__ bool find_share(const ChunkSizes& p, const long long*
       break;
     }
     out.off = int(at);
-    out.left = int(dealt.size(w));
+    out.left = int(size);
+    // the unit goes on from an earlier share: the first that begins inside it notes it
     const int steps = walked(p, span, R, out.pair).n;
-    if (w > 0 && out.off > 0 && out.off < steps && dealt.begin(w) - out.off >= dealt.begin(w - 1))
-      note = Merge{out.g, out.hk, out.b, out.pair, w - 1, dealt.share_of(dealt.begin(w) - out.off + steps - 1), {0, 0}};
+    if (out.off > 0 && out.off < steps) {
+      const int w0 = d.share_of(begin - out.off);
+      int second = w0 + 1;                 // (shares may be empty)
+      while (d.first(second) == d.first(w0)) ++second;
+      if (d.first(second) == begin && second == w) note = Merge{out.g, out.hk, out.b, out.pair, w0, d.share_of(begin - out.off + steps - 1), {0, 0}};
+    }
   }
+  // (an empty share may lie between two of a unit's)
+  if (size == 0 && w < d.n)
+    for (int row = lane; row < 2 * TILE; row += 32) *reinterpret_cast<float2*>(p.part_ml + (size_t(2 * w) * (2 * TILE) + row) * 2) = make_float2(-INFINITY, 0.f);
   if (lane == 0) p.merges[w] = note;
-  return there;
+  return out;
 }
 
 // A share's pieces, one after the other: what the roles need of them, laid out by warp 3 in a ring in shared memory.
@@ -301,29 +463,59 @@ struct Piece {
 static_assert(PIECES * sizeof(Piece) <= PIECES_BYTES && sizeof(Piece) % 8 == 0, "the ring of pieces");
 
 struct Pieces {
+  Share share;                 // where the share begins
   int g, hk, b, pair, off, left;
-  __device__ __forceinline__ explicit Pieces(const Share& s) : g(s.g), hk(s.hk), b(s.b), pair(s.pair), off(s.off), left(s.left) {}
+  long long unit;              // the next of the whole ones; from rounds_end on: the share's
+  __device__ __forceinline__ explicit Pieces(const Share& s) : share(s), g(0), hk(0), b(0), pair(0), off(0), left(0), unit(blockIdx.x) {}
+  // k units further on, by a warp together
+  __device__ __forceinline__ void advance(const ChunkSizes& p, long long k) {
+    k += pair;
+    for (;;) {
+      const int pairs = b + lane_id() < p.B ? pairs_of(span_of(p, b + lane_id()), p.members[g] * p.G) : 0;
+      const long long up = warp_scan(pairs);
+      const uint32_t hit = __ballot_sync(0xffffffffu, up > k);
+      if (hit != 0) {
+        const int of = __ffs(hit) - 1;
+        pair = int(k - __shfl_sync(0xffffffffu, up - pairs, of));
+        b += of;
+        return;
+      }
+      k -= __shfl_sync(0xffffffffu, up, 31);
+      b += 32;
+      if (b >= p.B) {
+        b = 0;
+        if (++hk == p.Hkv) {
+          hk = 0;
+          ++g;
+        }
+      }
+    }
+  }
   // The next piece, by a warp together; lane 0 writes it down.
   __device__ __forceinline__ void next(const ChunkSizes& p, Piece& out) {
     const int lane = lane_id();
-    while (left > 0) {
+    for (;;) {
+      if (unit < share.rounds_end) {          // a whole unit, a round behind the last one
+        advance(p, unit == blockIdx.x ? unit : (long long)gridDim.x);
+        unit += gridDim.x;
+        off = 0;
+        left = INT_MAX;
+      } else if (share.left >= 0) {           // on to the share
+        g = share.g;
+        hk = share.hk;
+        b = share.b;
+        pair = share.pair;
+        off = share.off;
+        left = share.left;
+        share.left = -1;
+        unit = LLONG_MAX;
+      }
+      if (left <= 0) break;
+      const bool in_rounds = unit != LLONG_MAX;
       const int R = p.members[g] * p.G;
       const Span span = span_of(p, b);
-      if (pair >= pairs_of(span, R)) {        // on to the next sequence that has rows
-        pair = 0;
-        ++b;
-        for (;;) {
-          if (b >= p.B) {
-            b = 0;
-            if (++hk == p.Hkv) {
-              hk = 0;
-              ++g;
-            }
-          }
-          const uint32_t some = __ballot_sync(0xffffffffu, b + lane < p.B && span_of(p, min(b + lane, p.B - 1)).n > 0);
-          b += some != 0 ? __ffs(some) - 1 : 32;
-          if (some != 0) break;
-        }
+      if (!in_rounds && pair >= pairs_of(span, R)) {        // on to the next sequence that has rows
+        advance(p, 0);
         continue;
       }
       const Walked w = walked(p, span, R, pair);
@@ -332,6 +524,7 @@ struct Pieces {
       left -= min(left, w.n + REST - off);
       off = 0;
       ++pair;
+      if (in_rounds) pair = now;              // (the place that the next round is counted from)
       if (c0 >= c1) continue;
       if (lane == 0) {
         const long long row = (long long)now * 2 * TILE, n_rows = (long long)span.n * R;
@@ -391,6 +584,10 @@ __device__ __forceinline__ float4 tmem_ld_x4(uint32_t taddr) {
   tmem_ld_wait();
   return make_float4(__uint_as_float(a), __uint_as_float(b), __uint_as_float(c), __uint_as_float(d));
 }
+// A number that is the same in the whole warp, so that the compiler knows it: what follows from it stays in uniform registers, from
+// which tensor and copy instructions take their operands (moved there one by one, they cost the issuing warps half their time).
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ int2 uniform(int2 v) { return make_int2(uniform(v.x), uniform(v.y)); }
 // A bounded wait of a whole warp: true in all lanes or in none (the roles that use warp-wide operations go on or leave together).
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -491,6 +688,12 @@ __device__ __noinline__ void add_rows(const ChunkSizes& p, const ChunkGroup& grp
   tmem_st_wait();
 }
 
+// Steps that scores run ahead of the products with P: a score buffer is free once the product of its tile's step before last has been issued.
+template <int KS>
+__device__ __forceinline__ int scores_ahead(bool duo) {
+  static_assert(KS > 2, "");
+  return !duo ? 2 : KS > 4 ? 4 : KS - 1;
+}
 // ---------------------------------------------------------------------------------------------
 // the kernel
 // ---------------------------------------------------------------------------------------------
@@ -523,7 +726,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
   unsigned long long* const s_bad = reinterpret_cast<unsigned long long*>(smem + L::OFF_BAD);
   Scales* const s_scales = reinterpret_cast<Scales*>(smem + L::OFF_SCALE);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   int* const err = &g_chunk_status;
 
   if (threadIdx.x == 0) {
@@ -564,14 +767,16 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t tmem_base = uniform(*tmem_slot);
   grid_dep_wait();
-  long long* const sums = reinterpret_cast<long long*>(smem + L::OFF_Q);   // (no query has been loaded)
-  const int n32 = (p.B + 31) / 32;
-  list_sums(p, sums, n32, L::THREADS / 32);
-  Share share{0, 0, 0, 0, 0, 0};
-  if (warp == 3 && !find_share(p, sums, n32, share)) share.left = 0;
-  fence_proxy_async_smem();     // (at 16384 sequences the sums reach into the first stage of K)
+  const Sums sums(smem + L::OFF_Q, p);          // (no query, K or V has been loaded)
+  list_sums(p, sums, L::THREADS / 32);
+  Share share{0, 0, 0, 0, 0, 0, 0};
+  {
+    const Deal deal = deal_out(p, sums, L::OFF_BAR - L::OFF_Q - int(static_cast<uint8_t*>(sums.end(p)) - (smem + L::OFF_Q)), L::THREADS / 32);
+    if (warp == 3) share = find_share(p, sums, deal);
+  }
+  fence_proxy_async_smem();     // (at 16384 sequences the sums reach into K's stages)
   __syncthreads();
   uint32_t at = 0;      // steps of earlier pieces: ring positions of this piece's first
   uint32_t it = 0;      // pieces so far
@@ -580,7 +785,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
   auto piece_at = [&](uint32_t i) -> const Piece* {
     ok = ok && warp_wait(&piece_full[i % PIECES], (i / PIECES) & 1, err);
     const Piece* const of = s_pieces + i % PIECES;
-    return ok && of->n > 0 ? of : nullptr;
+    return ok && uniform(of->n) > 0 ? of : nullptr;
   };
   auto give_back = [&]() {
     __syncwarp();
@@ -597,12 +802,12 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     // ------------------------------ K and V, or their codes ------------------------------
     const uint32_t leader = elect_one();    // the whole warp runs the loop; one lane issues
     while (const Piece* const piece = piece_at(it)) {
-      const ChunkGroup& grp = p.grp[piece->g];
-      const int n = piece->n, hk = piece->hk;
+      const ChunkGroup& grp = p.grp[uniform(piece->g)];
+      const int n = uniform(piece->n), hk = uniform(piece->hk);
       // Four lanes a step, a block of 16 keys each: rows of the pool (-1: no row of the unit sees any of the box's keys), and scales.
       // Pages are asked for two batches ahead, scales one.
       const int sub = lane & 3;
-      const int none = p.n_pages * p.Hkv * p.page_size;        // (behind the pool: TMA fills in zeros)
+      const int none = p.n_pages * p.Hkv * p.page_size, per_box = p.box / 16;        // (behind the pool: TMA fills in zeros)
       auto box_key = [&](int i) { return (piece->block(i) * STEP + sub * 16) / p.box * p.box; };
       auto page_of = [&](int batch) -> int {
         const int i = batch * BATCH + (lane >> 2);
@@ -612,56 +817,84 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         const int page = p.block_table[size_t(piece->b) * p.max_pages + key / p.page_size];
         return unsigned(page) < unsigned(p.n_pages) ? page : -2;
       };
+      auto row_of = [&](int batch, int page) -> int {
+        const int i = batch * BATCH + (lane >> 2);
+        return page >= 0 ? (page * p.Hkv + hk) * p.page_size + box_key(i) % p.page_size : none;
+      };
+      auto boxes_of = [&](int page) -> uint32_t { return __ballot_sync(0xffffffffu, page != -1 && sub % per_box == 0); };
       auto scales_of = [&](int batch, int page) -> uint32_t {  // K's and V's
         const int i = batch * BATCH + (lane >> 2);
         if (!BITS8 || i >= n || page < 0) return 0x7f7f;
         const size_t block = (size_t(page) * p.Hkv + hk) * (p.page_size / CACHE_BLOCK) + (piece->block(i) * STEP + sub * 16) % p.page_size / CACHE_BLOCK;
         return grp.k_scale[block] | uint32_t(grp.v_scale[block]) << 8;
       };
-      int page = page_of(0), page1 = page_of(1);
-      uint32_t scales = scales_of(0, page);
-      for (int batch = 0; batch * BATCH < n && ok; ++batch) {
-        const int page2 = page_of(batch + 2);
-        const uint32_t scales1 = scales_of(batch + 1, page1);
-        const int mine = batch * BATCH + (lane >> 2);
-        const int key = mine < n ? box_key(mine) : 0;
-        const int row = page >= 0 ? (page * p.Hkv + hk) * p.page_size + key % p.page_size : none;
-        const uint32_t issues = __ballot_sync(0xffffffffu, page != -1 && sub % (p.box / 16) == 0);
-        for (int i = batch * BATCH; i < min(n, (batch + 1) * BATCH) && ok; ++i) {
-          const int lane0 = (i - batch * BATCH) * 4;
-          const uint32_t boxes = issues >> lane0 & 15;
-          const uint32_t bytes = uint32_t(__popc(boxes)) * p.box * DH * (BITS8 ? 1 : 2);
+      // K or V of a step, whose pages are in lanes lane0 .. lane0 + 3
+      auto load = [&](int i, int row, uint32_t boxes, auto is_v) -> bool {
+        constexpr bool v = decltype(is_v)::value;
+        constexpr uint32_t ring = !v ? KS : BITS8 ? RS : VS;
+        const uint32_t j = at + i, s = j % ring, lane0 = (i % BATCH) * 4;
+        uint64_t* const full = !v ? &k_full[s] : BITS8 ? &raw_full[s] : &v_full[s];
+        if (!warp_wait(!v ? &k_empty[s] : BITS8 ? &raw_empty[s] : &v_empty[s], ((j / ring) & 1) ^ 1, err)) return false;
+        boxes = boxes >> lane0 & 15;
+        if constexpr (BITS8) __syncwarp();           // (the scales are written)
+        mbar_expect_tx_e(full, uint32_t(__popc(boxes)) * p.box * DH * (BITS8 ? 1 : 2), leader);
+        uint8_t* const tile = smem + (!v ? L::OFF_K + s * L::K_BYTES : BITS8 ? L::OFF_RAW + s * L::RAW_BYTES : L::OFF_V + s * L::V_BYTES);
+        const CUtensorMap* const map = v ? &grp.map_v : &grp.map_k;
+        for (int b = 0; b < 4; b += per_box) {
+          const int y = __shfl_sync(0xffffffffu, row, lane0 + b);
+          if constexpr (BITS8) {
+            tma_load_2d_e(tile + b * 16 * DH, map, full, 0, y, leader & boxes >> b);
+          } else {
 #pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const CUtensorMap* const map = v ? &grp.map_v : &grp.map_k;
-            const uint32_t j = at + i, ring = !v ? KS : BITS8 ? RS : VS, s = j % ring;
-            uint64_t* const full = !v ? &k_full[s] : BITS8 ? &raw_full[s] : &v_full[s];
-            if (!warp_wait(!v ? &k_empty[s] : BITS8 ? &raw_empty[s] : &v_empty[s], ((j / ring) & 1) ^ 1, err)) { ok = false; break; }
-            if constexpr (BITS8) {
-              if (!v && mine == i) {         // (ahead of K, which the scores wait for)
-                float* const of = reinterpret_cast<float*>(s_scales + j % SCALES) + sub;
-                of[0] = __uint_as_float(power_bits(exponent_of_byte(scales & 255)));
-                of[4] = __uint_as_float(power_bits(exponent_of_byte(scales >> 8)));
-                of[8] = float(exponent_of_byte(scales >> 8));
-              }
-              __syncwarp();
-            }
-            mbar_expect_tx_e(full, bytes, leader);
-            uint8_t* const tile = smem + (!v ? L::OFF_K + s * L::K_BYTES : BITS8 ? L::OFF_RAW + s * L::RAW_BYTES : L::OFF_V + s * L::V_BYTES);
-            for (int b = 0; b < 4; b += p.box / 16) {
-              const int y = __shfl_sync(0xffffffffu, row, lane0 + b);
-              if constexpr (BITS8) {
-                tma_load_2d_e(tile + b * 16 * DH, map, full, 0, y, leader & boxes >> b);
-              } else {
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h) tma_load_2d_e(tile + h * KV_HALF + b * 16 * 128, map, full, h * 64, y, leader & boxes >> b);
-              }
-            }
+            for (int h = 0; h < HALVES; ++h) tma_load_2d_e(tile + h * KV_HALF + b * 16 * 128, map, full, h * 64, y, leader & boxes >> b);
           }
         }
-        page = page1;
-        page1 = page2;
-        scales = scales1;
+        return true;
+      };
+      constexpr std::false_type is_k;
+      constexpr std::true_type is_v;
+      if constexpr (BITS8) {
+        // K and V side by side: V's way is the longer one.
+        int page = page_of(0), page1 = page_of(1);
+        uint32_t scales = scales_of(0, page);
+        for (int batch = 0; batch * BATCH < n && ok; ++batch) {
+          const int page2 = page_of(batch + 2);
+          const uint32_t scales1 = scales_of(batch + 1, page1);
+          const int mine = batch * BATCH + (lane >> 2), row = row_of(batch, page);
+          const uint32_t boxes = boxes_of(page);
+          for (int i = batch * BATCH; i < min(n, (batch + 1) * BATCH) && ok; ++i) {
+            if (mine == i) {               // (ahead of K, which the scores wait for)
+              float* const of = reinterpret_cast<float*>(s_scales + (at + i) % SCALES) + sub;
+              of[0] = __uint_as_float(power_bits(exponent_of_byte(scales & 255)));
+              of[4] = __uint_as_float(power_bits(exponent_of_byte(scales >> 8)));
+              of[8] = float(exponent_of_byte(scales >> 8));
+            }
+            ok = load(i, row, boxes, is_k) && load(i, row, boxes, is_v);
+          }
+          page = page1;
+          page1 = page2;
+          scales = scales1;
+        }
+      } else {
+        // K as far ahead of V as the scores run ahead of the products: both rings are then full of what is to come.
+        const int ahead = scores_ahead<KS>(uniform(piece->duo) != 0);
+        int page1 = page_of(0), page2 = page_of(1), row0 = none, row1 = row_of(0, page1);
+        uint32_t boxes0 = 0, boxes1 = boxes_of(page1);
+        for (int i = 0; i < ahead && i < n && ok; ++i) ok = load(i, row1, boxes1, is_k);
+        for (int batch = 0; batch * BATCH < n && ok; ++batch) {
+          const int page3 = page_of(batch + 2);
+          row0 = row1;
+          boxes0 = boxes1;
+          row1 = row_of(batch + 1, page2);
+          boxes1 = boxes_of(page2);
+          const int end = (batch + 1) * BATCH;
+          for (int i = batch * BATCH; i < min(n, end) && ok; ++i) {
+            const bool next = i + ahead >= end;
+            if (i + ahead < n) ok = load(i + ahead, next ? row1 : row0, next ? boxes1 : boxes0, is_k);
+            ok = ok && load(i, row0, boxes0, is_v);
+          }
+          page2 = page3;
+        }
       }
       at += n;
       give_back();
@@ -682,48 +915,55 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     const uint32_t tm_s = tmem_base + x * 128, tm_o = tmem_base + 256 + x * 128;
     uint32_t done = 0, n_done = 0;    // steps of earlier pieces in which this tile took part; those pieces
     while (const Piece* const piece = piece_at(it)) {
-      const int n = piece->n, n_x = piece->n_x[x];
-      const bool duo = piece->duo;
-      const int2 clear = piece->clear;
+      const int n = uniform(piece->n), n_x = uniform(piece->n_x[x]);
+      const bool duo = uniform(piece->duo) != 0;
+      const int2 clear = uniform(piece->clear);
       // (the tile's steps are i itself, or those of its parity)
       auto takes = [&](int i) { return duo ? (i & 1) == x : i < n_x; };
       auto own = [&](int i) { return done + (duo ? i >> 1 : i); };
-      // K of step i has come: scores, where the tile takes part, and the stage goes back
-      auto scores = [&](int i) -> bool {
-        const uint32_t s = (at + i) % KS;
-        if (!warp_wait(&k_full[s], ((at + i) / KS) & 1, err)) return false;
-        if (takes(i)) {
-          tc_fence_after_sync();
-          const uint32_t u = own(i) & 1, k_lo = desc_lo_sw128(k_base + s * L::K_BYTES, 0);
-          if constexpr (BITS8) {
+      auto k_come = [&](int i) -> bool { return warp_wait(&k_full[(at + i) % KS], ((at + i) / KS) & 1, err); };
+      // K of step i has come: scores, where the tile takes part
+      auto scores = [&](int i) {
+        if (!takes(i)) return;
+        const uint32_t u = own(i) & 1, k_lo = desc_lo_sw128(k_base + (at + i) % KS * L::K_BYTES, 0);
+        if constexpr (BITS8) {
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < 2; ++part)
 #pragma unroll
-              for (int ks = 0; ks < DH / 32; ++ks)
-                umma8_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, part * (TILE * DH) + ks * 32), desc_lo_add(k_lo, ks * 32), hi8, idesc_qk | (part << 7), (part | ks) != 0, leader);
-          } else {
+            for (int ks = 0; ks < DH / 32; ++ks)
+              umma8_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, part * (TILE * DH) + ks * 32), desc_lo_add(k_lo, ks * 32), hi8, idesc_qk | (part << 7), (part | ks) != 0, leader);
+        } else {
 #pragma unroll
-            for (int ks = 0; ks < DH / 16; ++ks)
-              umma_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, (ks / 4) * Q_HALF + (ks % 4) * 32), desc_lo_add(k_lo, (ks / 4) * KV_HALF + (ks % 4) * 32), hi, idesc_qk, ks != 0,
-                        leader);
-          }
-          umma_commit(&s_full[2 * x + u], leader);
-          umma_commit(&k_empty[s], leader);
-        } else if (leader) {
-          mbar_arrive(&k_empty[s]);
+          for (int ks = 0; ks < DH / 16; ++ks)
+            umma_ss_w(tm_s + u * STEP, desc_lo_add(q_lo, (ks / 4) * Q_HALF + (ks % 4) * 32), desc_lo_add(k_lo, (ks / 4) * KV_HALF + (ks % 4) * 32), hi, idesc_qk, ks != 0,
+                      leader);
         }
-        return true;
+        umma_commit(&s_full[2 * x + u], leader);
+      };
+      // stages go back: behind this warp's products with them, or at once where it has none
+      auto release = [&](uint64_t* bar, bool taken) {
+        if (taken)
+          umma_commit(bar, leader);
+        else if (leader)
+          mbar_arrive(bar);
       };
       if (n_x > 0 && !warp_wait(&q_full[x], n_done & 1, err)) { ok = false; break; }
-      tc_fence_after_sync();
-      // Scores run ahead of the products: a buffer is free once the product of the tile's step before last has been issued.
-      const int ahead = duo ? (KS > 4 ? 4 : KS - 1) : 2;
-      for (int i = 0; i < ahead && i < n && ok; ++i) ok = scores(i);
+      const int ahead = scores_ahead<KS>(duo);
+      for (int i = 0; i < ahead && i < n && ok; ++i) {
+        ok = k_come(i);
+        if (!ok) break;
+        tc_fence_after_sync();
+        scores(i);
+        release(&k_empty[(at + i) % KS], takes(i));
+      }
       for (int i = 0; i < n && ok; ++i) {
+        // (everything that the products and the next scores wait for ahead of P, which comes last)
         const uint32_t s = (at + i) % VS;
-        if (!warp_wait(&v_full[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
-        if (takes(i)) {
-          const uint32_t k = own(i), u = k & 1;
+        const bool further = i + ahead < n;
+        if (!warp_wait(&v_full[s], ((at + i) / VS) & 1, err) || (further && !k_come(i + ahead))) { ok = false; break; }
+        const bool mine = takes(i);
+        if (mine) {
+          const uint32_t k = own(i), u = k & 1, v_lo = desc_lo_sw128(v_base + s * L::V_BYTES, KV_HALF);
           uint32_t add = k != done;
           if (i < clear.x || i >= clear.y) {
             if (!BITS8 && !warp_wait(&v_fixed[s], ((at + i) / VS) & 1, err)) { ok = false; break; }
@@ -732,17 +972,18 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           }
           if (!warp_wait(&p_ready[2 * x + u], (k >> 1) & 1, err)) { ok = false; break; }
           tc_fence_after_sync();
-          const uint32_t v_lo = desc_lo_sw128(v_base + s * L::V_BYTES, KV_HALF);
 #pragma unroll
           for (int ks = 0; ks < STEP / 16; ++ks)
             umma_ts_w(tm_o, tm_s + u * STEP + ks * 8, desc_lo_add(v_lo, ks * 2048), hi, idesc_pv, ks == 0 ? add : 1u, leader);
           umma_commit(&pv_done[x], leader);
           if (k + 1 == done + n_x) umma_commit(&o_done[x], leader);
-          umma_commit(&v_empty[s], leader);
-        } else if (leader) {
-          mbar_arrive(&v_empty[s]);
         }
-        if (i + ahead < n) ok = scores(i + ahead);
+        if (further) {
+          if (!mine) tc_fence_after_sync();
+          scores(i + ahead);
+          release(&k_empty[(at + i + ahead) % KS], takes(i + ahead));
+        }
+        release(&v_empty[s], mine);
       }
       at += n;
       done += n_x;
@@ -759,18 +1000,18 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       Piece* const of = s_pieces + i % PIECES;
       pieces.next(p, *of);
       __syncwarp();
-      const bool some = of->n > 0;
+      const bool some = uniform(of->n) > 0;
       if (lane == 0) mbar_arrive(&piece_full[i % PIECES]);
       return some;
     };
     bool more = lay_out(0);
     while (more) {
       const Piece* const piece = s_pieces + it % PIECES;
-      const int n = piece->n;
+      const int n = uniform(piece->n);
       more = lay_out(it + 1);
       if constexpr (!BITS8) {
         constexpr int CHUNKS = DH / 8;       // 16-byte pieces of a row
-        const int2 clear = piece->clear;
+        const int2 clear = uniform(piece->clear);
         for (int i = 0; i < n && ok; ++i) {
           const uint32_t s = (at + i) % VS;
           ok = warp_wait(&v_full[s], ((at + i) / VS) & 1, err);
@@ -890,9 +1131,9 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     }
     while (piece != nullptr) {
       const bool any = quarter * 32 < piece->rows[x];      // (the same in the whole warp)
-      const bool duo = piece->duo;
-      const int2 pair_clear = piece->clear, clear = piece->clear_x[x];
-      const int n_x = piece->n_x[x];
+      const bool duo = uniform(piece->duo) != 0;
+      const int2 pair_clear = uniform(piece->clear), clear = uniform(piece->clear_x[x]);
+      const int n_x = uniform(piece->n_x[x]);
       const float c_row = c_next;
       float m_used = -INFINITY;          // running maximum (log2 domain) that the exponentials are taken against
       float o_used = -INFINITY;          // 8 bits: what O is in units of (log2, V's power with it)
@@ -1143,7 +1384,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         ++n_duo;
       }
       // (the next piece's first products wait for these warps' P, so O is free by then)
-      at += piece->n;
+      at += uniform(piece->n);
       done += n_x;
       if (next != nullptr) give_q(next);
       give_back();
@@ -1157,8 +1398,8 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     const uint32_t group = (warp - 12) >> 2;
     const int tid = threadIdx.x & 127, col = tid % CODES;
     while (const Piece* const piece = piece_at(it)) {
-      const int n = piece->n;
-      const int2 clear = piece->clear;
+      const int n = uniform(piece->n);
+      const int2 clear = uniform(piece->clear);
       for (int i = int((group ^ at) & 1); i < n && ok; i += 2) {
         const uint32_t j = at + i, s = j % VS, rs = j % RS;
         if (!warp_wait(&raw_full[rs], (j / RS) & 1, err) || !warp_wait(&v_empty[s], ((j / VS) & 1) ^ 1, err)) { ok = false; break; }

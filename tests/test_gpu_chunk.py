@@ -411,6 +411,23 @@ def test_another_stream_and_captured_graphs(kvp):
             x.check(o, l)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("donor,lens,new,Hq,Hkv,dh,page,window", [
+    ([0], [700, 650, 600, 900, 300, 1000, 60, 640], [600] * 4 + [300, 600, 60, 600], 32, 8, 64, 16, 0),
+    ([0, 1, 1], [500 + 40 * (i % 7) for i in range(12)], [200 + 30 * (i % 5) for i in range(12)], 12, 6, 128, 48, 0),       # of two kinds
+    ([0], [100 + i % 50 for i in range(130)], [1 + i % 3 for i in range(130)], 10, 5, 64, 16, 0),                           # a step or two each
+    ([0, 0], [1500, 1800, 40, 2000], [1500, 1700, 40, 900], 16, 8, 64, 32, 100),
+    ([0], [4000] + [200] * 20, [4000] + [200] * 20, 8, 8, 64, 64, 0),                                                       # one far longer than the others
+    ([0], [6000, 9000, 100], [6000, 2000, 100], 8, 8, 64, 64, 0),
+])
+def test_many_units(kvp, donor, lens, new, Hq, Hkv, dh, page, window, bits):
+    """Units dealt out in rounds, and the shares behind them, which even out what the rounds gave: of different sizes, some empty."""
+    c = Case(kvp, donor, lens, new, Hq, Hkv, dh, page, bits, window, 5 if window else 0)
+    (o, lse), (o2, lse2) = c.run(), c.run()
+    c.check(o, lse)
+    assert all(torch.equal(x, y) for x, y in zip(o + lse, o2 + lse2))
+
+
 def test_smaller_calls_in_the_workspace_of_a_large_one(kvp):
     c = Case(kvp, [0, 1], [900, 40], [60, 3], 8, 2, 64, 16)
     ws = Guarded().empty((kvp.attn_chunk_workspace_bytes(c.desc, c.donor, 5000),), torch.uint8, 0xff)
