@@ -84,6 +84,14 @@ struct Merge {
   int pad[2];
 };
 
+// Rows of a token, and what divides by them: row / n is the upper word of 2 row * mul, shifted (mul: 2^(31 + shift) / n rounded up, n <=
+// 2^shift; exact below 2^31).  The set-up of every call walks through some dozen such quotients ahead of its first load.
+struct Rows {
+  int n, shift;
+  uint32_t mul;
+  __device__ __forceinline__ int token(int row) const { return int(__umulhi(uint32_t(row) * 2, mul) >> shift); }
+};
+
 struct ChunkSizes {
   const int32_t *block_table, *lengths, *first;
   Merge* merges;                           // [shares]
@@ -93,7 +101,8 @@ struct ChunkSizes {
   int n_groups;
   int members[MANY_CHUNK_GROUPS];
   int kind[MANY_CHUNK_GROUPS];             // groups of as many members have the same list: its number
-  int n_kinds, kind_rows[CHUNK_MEMBERS];   // rows of a token in each
+  int n_kinds;
+  Rows rows[CHUNK_MEMBERS];                // of each list
   int window, sinks;                       // window 0: none
   int box;                                 // keys of a TMA box: 64, 32 or 16
   int io_f32;
@@ -145,11 +154,11 @@ struct Walked {
   int sink_blocks, from;                 // blocks of first tokens, then blocks from `from` on
   int n, n_a;                            // steps, and those of tile A
 };
-__device__ __forceinline__ int pairs_of(const Span& s, int R) { return int((uint32_t(s.n) * uint64_t(R) + 2 * TILE - 1) / (2 * TILE)); }
-__device__ __forceinline__ Walked walked(const ChunkSizes& p, const Span& s, int R, int pair) {
+__device__ __forceinline__ int pairs_of(const Span& s, const Rows& R) { return (s.n * R.n + 2 * TILE - 1) / (2 * TILE); }
+__device__ __forceinline__ Walked walked(const ChunkSizes& p, const Span& s, const Rows& R, int pair) {
   Walked w;
-  const long long row0 = (long long)pair * 2 * TILE;
-  auto token = [&](long long row) { return int(min((long long)s.n - 1, div_places(row, R))); };
+  const int row0 = pair * 2 * TILE;
+  auto token = [&](int row) { return min(s.n - 1, R.token(row)); };
   w.pos_first = s.pos0 + token(row0);
   w.pos_last_a = s.pos0 + token(row0 + TILE - 1);
   w.pos_last = s.pos0 + token(row0 + 2 * TILE - 1);
@@ -165,7 +174,7 @@ struct Listed {
   long long places;
   int pairs, longest;
 };
-__device__ __forceinline__ Listed listed(const ChunkSizes& p, int b, int R) {
+__device__ __forceinline__ Listed listed(const ChunkSizes& p, int b, const Rows& R) {
   const int lane = lane_id();
   Span s{0, 0, 0};
   if (b < p.B) s = span_of(p, b);
@@ -233,7 +242,7 @@ __device__ __forceinline__ void list_sums(const ChunkSizes& p, const Sums& s, in
   const int warp = threadIdx.x >> 5, lane = lane_id();
   for (int i = warp; i < s.n32 * p.n_kinds; i += warps) {
     const int kind = i / s.n32, at = i % s.n32;
-    const Listed l = listed(p, at * 32 + lane, p.kind_rows[kind]);
+    const Listed l = listed(p, at * 32 + lane, p.rows[kind]);
     const long long places = warp_sum(l.places), units = warp_sum(l.pairs);
     const int longest = __reduce_max_sync(0xffffffffu, l.longest);
     if (lane == 0) {
@@ -271,7 +280,8 @@ __device__ __forceinline__ int last_below(const long long* sums, int n, long lon
 // time, out of L2; the last two rounds and what is left are cut into shares that even out what the rounds gave.  Not where a unit is longer
 // than an eighth of a CTA's work (what is left would not even that out), or where there are few: equal shares of the whole list.
 // (Pieces of prompts behind 2K to 8K tokens, read out of memory: 8.3 GB with equal shares of the list.)
-constexpr int ROUNDS_FROM = 4, ROUNDS_LEFT = 2;
+// Few and short units: whole, one a CTA.
+constexpr int ROUNDS_FROM = 4, ROUNDS_LEFT = 2, WHOLE_UP_TO = 8;
 struct Deal {
   long long rounds_end;        // units that are dealt out whole
   long long base;              // their places
@@ -305,7 +315,7 @@ __device__ __forceinline__ Found find(const ChunkSizes& p, const Sums& s, long l
   const int row = kind * (s.n32 + 1), i = last_below((UNITS ? s.units : s.places) + row, s.n32, f.left);
   f.left -= (UNITS ? s.units : s.places)[row + i];
   f.other += (UNITS ? s.places : s.units)[row + i];
-  const Listed l = listed(p, i * 32 + lane_id(), p.kind_rows[kind]);
+  const Listed l = listed(p, i * 32 + lane_id(), p.rows[kind]);
   const long long mine = UNITS ? l.pairs : l.places, its = UNITS ? l.places : l.pairs, up = warp_scan(mine), up_its = warp_scan(its);
   const int of = __ffs(__ballot_sync(0xffffffffu, up > f.left)) - 1;
   f.left -= __shfl_sync(0xffffffffu, up - mine, of);
@@ -325,11 +335,14 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
   }
   for (int i = lane; i < s.n32 * p.n_kinds; i += 32) longest = max(longest, s.longest[i]);
   longest = __reduce_max_sync(0xffffffffu, longest);
-  if (units >= (long long)ROUNDS_FROM * n && (long long)longest * 8 * n <= d.total) {
+  if (units <= n && longest <= div_places(d.total, n) + WHOLE_UP_TO) {
+    d.rounds_end = units;
+    d.base = d.total;
+  } else if (units >= (long long)ROUNDS_FROM * n && (long long)longest * 8 * n <= d.total) {
     d.rounds_end = (div_places(units, n) - ROUNDS_LEFT) * n;
     const Found f = find<true>(p, s, d.rounds_end);
     const Span span = span_of(p, f.b);
-    const int R = p.members[f.g] * p.G;
+    const Rows R = p.rows[p.kind[f.g]];
     long long before = 0;
     for (int pair = lane; pair < int(f.left); pair += 32) before += walked(p, span, R, pair).n + REST;
     d.base = f.other + warp_sum(before);
@@ -339,7 +352,7 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
     for (int kind = 0; kind < p.n_kinds; ++kind) all += s.all_units(kind);
     if (all * 4 + (n + 1) * 8 <= room) {
       for (int kind = 0, at = 0; kind < p.n_kinds; at += int(s.all_units(kind)), ++kind) {
-        const int rows = p.kind_rows[kind];
+        const Rows rows = p.rows[kind];
         for (int i = warp; i < s.n32; i += warps) {
           const Span mine = i * 32 + lane < p.B ? span_of(p, i * 32 + lane) : Span{0, 0, 0};
           const int pairs = pairs_of(mine, rows);
@@ -408,7 +421,8 @@ __device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, 
     out.b = f.b;
     long long at = f.left;
     const Span span = span_of(p, f.b);
-    const int R = p.members[f.g] * p.G, pairs = pairs_of(span, R);
+    const Rows R = p.rows[p.kind[f.g]];
+    const int pairs = pairs_of(span, R);
     for (int pair0 = 0;; pair0 += 32) {
       const int pair = pair0 + lane;
       const long long cost = pair < pairs ? walked(p, span, R, pair).n + REST : 0, sum = warp_scan(cost);
@@ -471,7 +485,7 @@ struct Pieces {
   __device__ __forceinline__ void advance(const ChunkSizes& p, long long k) {
     k += pair;
     for (;;) {
-      const int pairs = b + lane_id() < p.B ? pairs_of(span_of(p, b + lane_id()), p.members[g] * p.G) : 0;
+      const int pairs = b + lane_id() < p.B ? pairs_of(span_of(p, b + lane_id()), p.rows[p.kind[g]]) : 0;
       const long long up = warp_scan(pairs);
       const uint32_t hit = __ballot_sync(0xffffffffu, up > k);
       if (hit != 0) {
@@ -512,7 +526,7 @@ struct Pieces {
       }
       if (left <= 0) break;
       const bool in_rounds = unit != LLONG_MAX;
-      const int R = p.members[g] * p.G;
+      const Rows R = p.rows[p.kind[g]];
       const Span span = span_of(p, b);
       if (!in_rounds && pair >= pairs_of(span, R)) {        // on to the next sequence that has rows
         advance(p, 0);
@@ -527,7 +541,7 @@ struct Pieces {
       if (in_rounds) pair = now;              // (the place that the next round is counted from)
       if (c0 >= c1) continue;
       if (lane == 0) {
-        const long long row = (long long)now * 2 * TILE, n_rows = (long long)span.n * R;
+        const int row = now * 2 * TILE, n_rows = span.n * R.n;
         const bool duo = row + TILE >= n_rows;
         auto clear = [&](int pos_first, int pos_last) {      // (blocks of first tokens count as masked)
           const int begin = p.window > 0 && pos_last >= p.window ? (pos_last - p.window) / STEP + 1 : 0, end = (pos_first + 1) / STEP;
@@ -536,15 +550,15 @@ struct Pieces {
         out.g = g;
         out.hk = hk;
         out.b = b;
-        out.R = R;
+        out.R = R.n;
         out.row0 = span.row0;
         out.pos0 = span.pos0;
         out.duo = duo;
         for (int x = 0; x < 2; ++x) {
-          const long long first = row + (duo ? 0 : x * TILE);
-          out.rows[x] = int(min((long long)TILE, n_rows - first));
-          out.token[x] = int(div_places(first, R));
-          out.in[x] = int(first - (long long)out.token[x] * R);
+          const int first = row + (duo ? 0 : x * TILE);
+          out.rows[x] = min(TILE, n_rows - first);
+          out.token[x] = R.token(first);
+          out.in[x] = first - out.token[x] * R.n;
         }
         const int n = c1 - c0;
         out.n_x[0] = duo ? (n + 1) / 2 : max(0, min(c1, w.n_a) - c0);
@@ -599,6 +613,21 @@ __device__ __forceinline__ uint32_t f32x4_to_e5m2(float a, float b, float c, flo
   asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
   asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
   return uint32_t(lo) | uint32_t(hi) << 16;
+}
+// Lane t of a quad holds four 16-byte parts of its row: of the parts t of the quad's four rows, row j's comes to v[4 j].
+__device__ __forceinline__ void swap_in_quads(uint32_t* v, int t) {
+#pragma unroll
+  for (int bit = 1; bit <= 2; bit *= 2)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (c & bit) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t &a = v[4 * c + i], &b = v[4 * (c | bit) + i];
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, t & bit ? a : b, bit);
+        if (t & bit) a = got; else b = got;
+      }
+    }
 }
 // of bf16 numbers
 __device__ __forceinline__ uint32_t not_finite(uint32_t two) { return uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u); }
@@ -1055,65 +1084,88 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     const uint32_t tm_s = tmem_base + x * 128 + lane_sel, tm_o = tmem_base + 256 + x * 128 + lane_sel;
     float c_next = p.scale_log2;         // factor of the scores (8 bits: with what the thread's row has been multiplied by taken back)
     uint32_t done = 0, n_done = 0, n_duo = 0;       // steps of earlier pieces in which this tile took part; those pieces; duos
-    // The thread's query row of a piece goes to its place: every product with the last one's has been seen to complete.
+    // The warp's query rows of a piece go to their places: every product with the last one's has been seen to complete.  Four lanes a row,
+    // and four rows one after the other: a row a lane, its 16-byte parts were as many lines each (3200 cycles a piece, and its output
+    // the same way 5400).
+    const int t = lane & 3, quad = lane & ~3;
+    auto of_row = [&](const void* own, int j) {            // row quad + j's
+      return reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), quad + j));
+    };
     auto ask_q = [&](const Piece* of) {
-      if (of->n_x[x] == 0 || r >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
-      const int more = (of->in[x] + r) / of->R, in = of->in[x] + r - more * of->R;
-      const size_t elem = (size_t(of->row0 + of->token[x] + more) * p.Hq + of->hk * p.G + in % p.G) * DH;
-      const void* const q = p.grp[of->g].q[in / p.G];
+      if (of->n_x[x] == 0 || quarter * 32 >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
+      const void* own = nullptr;
+      if (r < of->rows[x]) {
+        const int more = (of->in[x] + r) / of->R, in = of->in[x] + r - more * of->R;
+        const size_t elem = (size_t(of->row0 + of->token[x] + more) * p.Hq + of->hk * p.G + in % p.G) * DH;
+        own = static_cast<const uint8_t*>(p.grp[of->g].q[in / p.G]) + elem * (p.io_f32 ? 4 : 2);
+      }
       uint8_t* const tile = smem + L::OFF_Q + x * L::Q_BYTES;
-      auto place = [&](int c) { return reinterpret_cast<uint4*>(tile + (c / 8) * Q_HALF + sw128_offset(r, c % 8)); };
-      auto eight = [&](int c) -> uint4 {               // as bf16
-        if (!p.io_f32) return reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(q) + elem)[c];
-        const float4* const src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(q) + elem) + 2 * c;
+      auto eight = [&](const uint8_t* row, int c) -> uint4 {               // as bf16
+        if (!p.io_f32) return reinterpret_cast<const uint4*>(row)[c];
+        const float4* const src = reinterpret_cast<const float4*>(row) + 2 * c;
         const float4 a = src[0], b = src[1];
         return make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
       };
-      if constexpr (BITS8) {
-        // A number as the sum of two, e4m3 and e5m2, which both go into products with K as it is: a bf16 number's eight bits are four
-        // and three (what is left by rounding to four bits is eight steps of the eighth at the most).  By a power of two a row, the
-        // largest to 2^7: exact for all elements down to 2^-16 of it, and off by 2^-25 of the largest at most below that.
-        float most = 0.f;
-#pragma unroll 8
-        for (int c = 0; c < DH / 8; ++c) {
-          const uint4 v = eight(c);
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j) {
+        const uint8_t* const row = of_row(own, j);
+        const int at_row = quarter * 32 + quad + j;
+        if constexpr (BITS8) {
+          // A number as the sum of two, e4m3 and e5m2, which both go into products with K as it is: a bf16 number's eight bits are
+          // four and three (what is left by rounding to four bits is eight steps of the eighth at the most).  By a power of two a
+          // row, the largest to 2^7: exact for all elements down to 2^-16 of it, and off by 2^-25 of the largest at most below that.
+          uint4 v[DH / 64][2];
+          float most = 0.f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t two = j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w;
-            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
-          }
-        }
-        const int up = min(max(7 + 127 - int(__float_as_uint(most) >> 23), -120), 120);
-        const float power = __uint_as_float(uint32_t(up + 127) << 23);
-        c_next = p.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
-#pragma unroll 2
-        for (int c = 0; c < DH / 16; ++c) {
-          uint32_t hi[4], lo[4];
+          for (int c = 0; c < DH / 64; ++c)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint4 v = eight(2 * c + e);
+            for (int e = 0; e < 2; ++e) {
+              v[c][e] = row != nullptr ? eight(row, 2 * (4 * c + t) + e) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t a = j == 0 ? v.x : v.z, b = j == 0 ? v.y : v.w;
-              float f[4] = {__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t two = i == 0 ? v[c][e].x : i == 1 ? v[c][e].y : i == 2 ? v[c][e].z : v[c][e].w;
+                most = fmaxf(most, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
+              }
+            }
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+          const int up = min(max(7 + 127 - int(__float_as_uint(most) >> 23), -120), 120);
+          const float power = __uint_as_float(uint32_t(up + 127) << 23);
+          if (t == j) c_next = p.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
+          if (row != nullptr) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) f[i] = fabsf(f[i]) < INFINITY ? f[i] * power : NAN;
-              hi[2 * e + j] = f32x4_to_e4m3(f[0], f[1], f[2], f[3]);
-              const float2 r = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + j]))), t = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + j] >> 16)));
-              lo[2 * e + j] = f32x4_to_e5m2(f[0] - r.x, f[1] - r.y, f[2] - t.x, f[3] - t.y);
+            for (int c = 0; c < DH / 64; ++c) {
+              uint32_t hi[4], lo[4];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const uint32_t a = i == 0 ? v[c][e].x : v[c][e].z, b = i == 0 ? v[c][e].y : v[c][e].w;
+                  float f[4] = {__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) f[k] = fabsf(f[k]) < INFINITY ? f[k] * power : NAN;
+                  hi[2 * e + i] = f32x4_to_e4m3(f[0], f[1], f[2], f[3]);
+                  const float2 y = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + i]))), z = f16x2_to_f32(e4m3x2_to_f16x2(uint16_t(hi[2 * e + i] >> 16)));
+                  lo[2 * e + i] = f32x4_to_e5m2(f[0] - y.x, f[1] - y.y, f[2] - z.x, f[3] - z.y);
+                }
+              }
+              const int part = 4 * c + t;
+              const uint32_t at8 = DH == 128 ? sw128_offset(at_row, part) : at_row * 64u + ((part ^ (at_row >> 1 & 3)) << 4);
+              *reinterpret_cast<uint4*>(tile + at8) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+              *reinterpret_cast<uint4*>(tile + TILE * DH + at8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
           }
-          const uint32_t at8 = DH == 128 ? sw128_offset(r, c) : r * 64u + ((c ^ (r >> 1 & 3)) << 4);
-          *reinterpret_cast<uint4*>(tile + at8) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(tile + TILE * DH + at8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        }
-      } else if (p.io_f32) {
-#pragma unroll 4
-        for (int c = 0; c < DH / 8; ++c) *place(c) = eight(c);
-      } else {
-        const __nv_bfloat16* const src = reinterpret_cast<const __nv_bfloat16*>(q) + elem;
+        } else if (row != nullptr) {
 #pragma unroll
-        for (int c = 0; c < DH / 8; ++c) cp_async16(smem_u32(place(c)), src + c * 8, 16);
+          for (int c4 = 0; c4 < DH / 8; c4 += 4) {
+            const int c = c4 + t;
+            uint8_t* const place = tile + (c / 8) * Q_HALF + sw128_offset(at_row, c % 8);
+            if (p.io_f32)
+              *reinterpret_cast<uint4*>(place) = eight(row, c);
+            else
+              cp_async16(smem_u32(place), row + c * 16, 16);
+          }
+        }
       }
       cp_async_commit();
     };
@@ -1315,6 +1367,8 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         mine *= unit;
         others *= other.z;
       }
+      // (the next piece's first scores run beside what is left of this one; those of a duo are over the halves' notes)
+      if (!duo && next != nullptr) give_q(next);
       if (any) {
         const ChunkGroup& grp = p.grp[piece->g];
         const bool there = r < piece->rows[x], whole = piece->whole;
@@ -1329,6 +1383,12 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           else
             *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m, l);
         }
+        void* own = nullptr;
+        if (there)
+          own = !whole ? static_cast<void*>(p.part_o + part * DH) : static_cast<uint8_t*>(grp.o[member]) + head * DH * (p.io_f32 ? 4 : 2);
+        uint8_t* rows[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rows[j] = of_row(own, j);
         const int h_end = duo && x == 0 ? DH / 64 : DH / 32, n_other = duo ? piece->n_x[x ^ 1] : 0;
         if (duo || n_x > 0) {
           for (int h = duo && x == 1 ? DH / 64 : 0; h < h_end; ++h) {
@@ -1353,23 +1413,30 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
                 }
               }
             }
-            if (there && !whole) {
-              float* const dst = p.part_o + part * DH + h * 32;
+            if (!whole) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4*>(dst + j) = make_uint4(tmp[j], tmp[j + 1], tmp[j + 2], tmp[j + 3]);
-            } else if (there) {
+              for (int e = 0; e < 2; ++e) {
+                swap_in_quads(&tmp[16 * e], t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (rows[j] != nullptr)
+                    *reinterpret_cast<uint4*>(rows[j] + (h * 32 + e * 16 + t * 4) * 4) = make_uint4(tmp[16 * e + 4 * j], tmp[16 * e + 4 * j + 1], tmp[16 * e + 4 * j + 2], tmp[16 * e + 4 * j + 3]);
+              }
+            } else {
               uint32_t v[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) v[j] = pack_bf16(__uint_as_float(tmp[2 * j]) * inv_l, __uint_as_float(tmp[2 * j + 1]) * inv_l);
-              if (p.io_f32) {
-                float* const dst = reinterpret_cast<float*>(grp.o[member]) + head * DH + h * 32;
+              swap_in_quads(v, t);
 #pragma unroll
-                for (int j = 0; j < 16; j += 2)
-                  *reinterpret_cast<uint4*>(dst + 2 * j) = make_uint4(v[j] << 16, v[j] & 0xffff0000u, v[j + 1] << 16, v[j + 1] & 0xffff0000u);
-              } else {
-                __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(grp.o[member]) + head * DH + h * 32;
-#pragma unroll
-                for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(dst + 2 * j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+              for (int j = 0; j < 4; ++j) {
+                if (rows[j] == nullptr) continue;
+                if (p.io_f32) {
+                  uint4* const dst = reinterpret_cast<uint4*>(rows[j] + (h * 32 + t * 8) * 4);
+                  dst[0] = make_uint4(v[4 * j] << 16, v[4 * j] & 0xffff0000u, v[4 * j + 1] << 16, v[4 * j + 1] & 0xffff0000u);
+                  dst[1] = make_uint4(v[4 * j + 2] << 16, v[4 * j + 2] & 0xffff0000u, v[4 * j + 3] << 16, v[4 * j + 3] & 0xffff0000u);
+                } else {
+                  *reinterpret_cast<uint4*>(rows[j] + (h * 32 + t * 8) * 2) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                }
               }
             }
             __syncwarp();
@@ -1386,7 +1453,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       // (the next piece's first products wait for these warps' P, so O is free by then)
       at += uniform(piece->n);
       done += n_x;
-      if (next != nullptr) give_q(next);
+      if (duo && next != nullptr) give_q(next);
       give_back();
       piece = next;
     }
@@ -1489,8 +1556,8 @@ __global__ void __launch_bounds__(MERGE_THREADS) chunk_merge_kernel(const __grid
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const ChunkGroup& grp = p.grp[m.g];
   const Span span = span_of(p, m.b);
-  const int R = p.members[m.g] * p.G;
-  const long long row0 = (long long)m.pair * 2 * TILE, n_rows = (long long)span.n * R;
+  const Rows R = p.rows[p.kind[m.g]];
+  const int row0 = m.pair * 2 * TILE, n_rows = span.n * R.n;
   for (int row = int(blockIdx.y) + MERGE_PARTS * warp; row < 2 * TILE; row += MERGE_PARTS * (MERGE_THREADS / 32)) {
     if (row0 + row >= n_rows) continue;
     float top = -INFINITY, sum = 0.f, acc[COLS];
@@ -1550,7 +1617,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) chunk_merge_kernel(const __grid
           for (int c = 0; c < COLS; ++c) acc[c] = fmaf(held[k][c], f[k], acc[c]);
       }
     }
-    const int token = int(div_places(row0 + row, R)), in = int(row0 + row - (long long)token * R), member = in / p.G;
+    const int token = R.token(row0 + row), in = row0 + row - token * R.n, member = in / p.G;
     const size_t head = size_t(span.row0 + token) * p.Hq + m.hk * p.G + in % p.G;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     uint32_t v[COLS / 2];
@@ -1584,6 +1651,12 @@ int shares_at_most(const kvp_decode_desc* d, int n_groups, int T) {
   return int(std::max(1ll, std::min((long long)sm_count(), most / LEAST_SHARE)));
 }
 
+Rows rows_of_token(int n) {
+  Rows r{n, 0, 0};
+  while (1 << r.shift < n) ++r.shift;
+  r.mul = uint32_t(((uint64_t(1) << (31 + r.shift)) + n - 1) / n);
+  return r;
+}
 int check_chunk(const kvp_decode_desc* d) {
   int rc = d == nullptr ? KVP_ERR_INVALID_ARG : KVP_OK;
   if (rc != KVP_OK) return rc;
@@ -1714,6 +1787,7 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
     return KVP_ERR_INVALID_ARG;
   for (int l = 0; l < d->L; ++l)
     if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return KVP_ERR_BAD_DONOR;
+  if (T >= 1 << 24) return KVP_ERR_UNSUPPORTED;      // rows, a tile's at most for a token, are counted in 31 bits
   if (T == 0) return KVP_OK;           // (tensors without rows have no memory)
   const bool bits8 = k_scale != nullptr;
   for (int l = layer_begin; l < layer_end; ++l) {     // all of them before anything is launched
@@ -1808,8 +1882,8 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
       const int g = p.n_groups++;
       p.members[g] = n;
       int kind = 0;
-      while (kind < p.n_kinds && p.kind_rows[kind] != n * p.G) ++kind;
-      if (kind == p.n_kinds) p.kind_rows[p.n_kinds++] = n * p.G;
+      while (kind < p.n_kinds && p.rows[kind].n != n * p.G) ++kind;
+      if (kind == p.n_kinds) p.rows[p.n_kinds++] = rows_of_token(n * p.G);
       p.kind[g] = kind;
     }
     if (p.n_groups == MANY_CHUNK_GROUPS || (n == 0 && p.n_groups > 0)) {
