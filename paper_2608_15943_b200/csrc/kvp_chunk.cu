@@ -102,7 +102,7 @@ struct ChunkSizes {
   int members[MANY_CHUNK_GROUPS];
   int kind[MANY_CHUNK_GROUPS];             // groups of as many members have the same list: its number
   int n_kinds;
-  Rows rows[CHUNK_MEMBERS];                // of each list
+  Rows rows[CHUNK_MEMBERS], heads;         // of each list; G, the query heads of a KV head, the same way
   int window, sinks;                       // window 0: none
   int box;                                 // keys of a TMA box: 64, 32 or 16
   int io_f32;
@@ -458,7 +458,7 @@ __device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, 
 struct Piece {
   int n;                       // steps; 0: there are no more pieces
   int g, hk, b;
-  int R, row0;                 // rows of a token; row of q of the sequence's first token
+  int row0;                    // row of q of the sequence's first token
   int pos0;                    // its position
   int duo;                     // one tile: both halves of the CTA have its rows, and take every other step each
   int n_x[2];                  // steps that each half takes
@@ -467,7 +467,7 @@ struct Piece {
   int pos_first, pos_last;     // positions of the unit's rows
   int sinks, at_sinks, at;     // step i is block at_sinks + i for i < sinks, at + i from there on
   int2 clear, clear_x[2];      // steps i, x <= i < y, in which all rows (the half's rows) see every key
-  int whole, slot;             // the unit has no other piece; otherwise the place of its partial sums
+  int whole, slot, pad;        // the unit has no other piece; otherwise the place of its partial sums
   __device__ __forceinline__ int block(int i) const { return (i < sinks ? at_sinks : at) + i; }
   // no row of the unit sees any of n keys from `key` on
   __device__ __forceinline__ bool unseen(const ChunkSizes& p, int key, int n) const {
@@ -550,7 +550,6 @@ struct Pieces {
         out.g = g;
         out.hk = hk;
         out.b = b;
-        out.R = R.n;
         out.row0 = span.row0;
         out.pos0 = span.pos0;
         out.duo = duo;
@@ -1095,9 +1094,10 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       if (of->n_x[x] == 0 || quarter * 32 >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
       const void* own = nullptr;
       if (r < of->rows[x]) {
-        const int more = (of->in[x] + r) / of->R, in = of->in[x] + r - more * of->R;
-        const size_t elem = (size_t(of->row0 + of->token[x] + more) * p.Hq + of->hk * p.G + in % p.G) * DH;
-        own = static_cast<const uint8_t*>(p.grp[of->g].q[in / p.G]) + elem * (p.io_f32 ? 4 : 2);
+        const Rows R = p.rows[p.kind[of->g]];
+        const int more = R.token(of->in[x] + r), in = of->in[x] + r - more * R.n, member = p.heads.token(in);
+        const size_t elem = (size_t(of->row0 + of->token[x] + more) * p.Hq + of->hk * p.G + in - member * p.G) * DH;
+        own = static_cast<const uint8_t*>(p.grp[of->g].q[member]) + elem * (p.io_f32 ? 4 : 2);
       }
       uint8_t* const tile = smem + L::OFF_Q + x * L::Q_BYTES;
       auto eight = [&](const uint8_t* row, int c) -> uint4 {               // as bf16
@@ -1207,7 +1207,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           tmem_ld_wait();
           if (i < clear.x || i >= clear.y) {
             const int key0 = piece->block(i) * STEP;
-            const int pos = piece->pos0 + piece->token[x] + (piece->in[x] + min(r, piece->rows[x] - 1)) / piece->R;
+            const int pos = piece->pos0 + piece->token[x] + p.rows[p.kind[piece->g]].token(piece->in[x] + min(r, piece->rows[x] - 1));
             auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
             seen = below(pos - key0 + 1);
             if (p.window > 0) seen &= ~below(pos - p.window + 1 - key0) | below(p.sinks - key0);
@@ -1372,9 +1372,9 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       if (any) {
         const ChunkGroup& grp = p.grp[piece->g];
         const bool there = r < piece->rows[x], whole = piece->whole;
-        const int more = (piece->in[x] + r) / piece->R, in = piece->in[x] + r - more * piece->R;
-        const int member = there ? in / p.G : 0;
-        const size_t head = size_t(piece->row0 + piece->token[x] + more) * p.Hq + piece->hk * p.G + (there ? in % p.G : 0);
+        const Rows R = p.rows[p.kind[piece->g]];
+        const int more = R.token(piece->in[x] + r), in = piece->in[x] + r - more * R.n, member = p.heads.token(in);
+        const size_t head = size_t(piece->row0 + piece->token[x] + more) * p.Hq + piece->hk * p.G + in - member * p.G;
         const size_t part = size_t(piece->slot) * (2 * TILE) + (duo ? 0 : x * TILE) + r;
         const float inv_l = l == 0.f ? 0.f : 1.f / l;
         if (there && !(duo && x == 1)) {
@@ -1617,8 +1617,8 @@ __global__ void __launch_bounds__(MERGE_THREADS) chunk_merge_kernel(const __grid
           for (int c = 0; c < COLS; ++c) acc[c] = fmaf(held[k][c], f[k], acc[c]);
       }
     }
-    const int token = R.token(row0 + row), in = row0 + row - token * R.n, member = in / p.G;
-    const size_t head = size_t(span.row0 + token) * p.Hq + m.hk * p.G + in % p.G;
+    const int token = R.token(row0 + row), in = row0 + row - token * R.n, member = p.heads.token(in);
+    const size_t head = size_t(span.row0 + token) * p.Hq + m.hk * p.G + in - member * p.G;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     uint32_t v[COLS / 2];
 #pragma unroll
@@ -1837,6 +1837,7 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
   p.Hq = d->Hq;
   p.Hkv = d->Hkv;
   p.G = d->Hq / d->Hkv;
+  p.heads = rows_of_token(p.G);
   p.page_size = d->page_size;
   p.max_pages = d->max_pages;
   p.n_pages = d->n_pages;
