@@ -45,7 +45,7 @@ constexpr int REST = 3, LEAST_SHARE = 8;
 
 __device__ int g_chunk_status;
 
-constexpr int PIECES = 4, PIECES_BYTES = 640;       // the ring of pieces
+constexpr int PIECES = 4, PIECES_BYTES = 512;       // the ring of pieces
 // The scales of a step of the 8-bit cache, a block of 16 keys each: K's and V's powers of two, and V's exponents.  A step's stay until
 // its product has been issued: K is asked for one step ahead of V at the most, and V's rings hold fewer steps than there are places.
 struct Scales {
@@ -467,7 +467,7 @@ struct Piece {
   int pos_first, pos_last;     // positions of the unit's rows
   int sinks, at_sinks, at;     // step i is block at_sinks + i for i < sinks, at + i from there on
   int2 clear, clear_x[2];      // steps i, x <= i < y, in which all rows (the half's rows) see every key
-  int whole, slot, pad;        // the unit has no other piece; otherwise the place of its partial sums
+  int whole, slot;             // the unit has no other piece; otherwise the place of its partial sums
   __device__ __forceinline__ int block(int i) const { return (i < sinks ? at_sinks : at) + i; }
   // no row of the unit sees any of n keys from `key` on
   __device__ __forceinline__ bool unseen(const ChunkSizes& p, int key, int n) const {
