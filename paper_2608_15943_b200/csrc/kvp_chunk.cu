@@ -460,7 +460,8 @@ struct Piece {
   int g, hk, b;
   int row0;                    // row of q of the sequence's first token
   int pos0;                    // its position
-  int duo;                     // one tile: both halves of the CTA have its rows, and take every other step each
+  int duo;                     // one tile: both halves of the CTA have its rows, and take every other step each; 2: rows of half a tile,
+                               // in its second half for half 1, so that softmax works on all four quarters of the SM
   int n_x[2];                  // steps that each half takes
   int rows[2];                 // rows of its tile
   int token[2], in[2];         // the tile's first: its token, and which of the token's rows
@@ -552,7 +553,7 @@ struct Pieces {
         out.b = b;
         out.row0 = span.row0;
         out.pos0 = span.pos0;
-        out.duo = duo;
+        out.duo = !duo ? 0 : n_rows - row <= TILE / 2 ? 2 : 1;
         for (int x = 0; x < 2; ++x) {
           const int first = row + (duo ? 0 : x * TILE);
           out.rows[x] = min(TILE, n_rows - first);
@@ -638,13 +639,13 @@ __device__ __forceinline__ uint32_t any_nan(const uint4& c) {
   const uint32_t m = 0x7f7f7f7fu, one = 0x01010101u;
   return (((c.x & m) + one) | ((c.y & m) + one) | ((c.z & m) + one) | ((c.w & m) + one)) & 0x80808080u;
 }
-__device__ __forceinline__ uint32_t widen(uint32_t w, int upper) {
-  const uint32_t apart = __byte_perm(w, 0, upper ? 0x3424 : 0x1404);     // a code in the upper byte of each half
-  return (apart & 0x80008000u) | (apart >> 1 & 0x3f803f80u);
-}
+// Of four columns' codes the even ones in one word and the odd ones in the other, which takes no permutation of bytes: so columns 4 i
+// + 1 and 4 i + 2 are in each other's place, and whoever reads O puts them back.
 __device__ __forceinline__ void widen16(const uint4& c, uint4 (&out)[2]) {
-  out[0] = make_uint4(widen(c.x, 0), widen(c.x, 1), widen(c.y, 0), widen(c.y, 1));
-  out[1] = make_uint4(widen(c.z, 0), widen(c.z, 1), widen(c.w, 0), widen(c.w, 1));
+  auto even = [](uint32_t w) { return (w << 8 & 0x80008000u) | (w << 7 & 0x3f803f80u); };
+  auto odd = [](uint32_t w) { return (w & 0x80008000u) | (w >> 1 & 0x3f803f80u); };
+  out[0] = make_uint4(even(c.x), odd(c.x), even(c.y), odd(c.y));
+  out[1] = make_uint4(even(c.z), odd(c.z), even(c.w), odd(c.w));
 }
 __device__ __forceinline__ uint32_t nan_too(uint32_t two) {       // 480 * 2^-8 is what NaN's bits come out as
   return two | ((two & 0x3f80u) == 0x3f80u ? 0x7f80u : 0) | ((two & 0x3f800000u) == 0x3f800000u ? 0x7f800000u : 0);
@@ -704,9 +705,10 @@ __device__ __noinline__ void add_rows(const ChunkSizes& p, const ChunkGroup& grp
           const uint32_t bits = reinterpret_cast<const uint32_t*>(grp.v_pool)[(row * DH + h * 32) / 2 + i];
           v = make_float2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u));
         }
+        const int at0 = !BITS8 ? 2 * i : i / 2 * 4 + (i & 1), at1 = at0 + (BITS8 ? 2 : 1);        // (as widen16 leaves the columns)
         if (takes) {
-          acc[2 * i] = __float_as_uint(fmaf(pj, v.x, __uint_as_float(acc[2 * i])));
-          acc[2 * i + 1] = __float_as_uint(fmaf(pj, v.y, __uint_as_float(acc[2 * i + 1])));
+          acc[at0] = __float_as_uint(fmaf(pj, v.x, __uint_as_float(acc[at0])));
+          acc[at1] = __float_as_uint(fmaf(pj, v.y, __uint_as_float(acc[at1])));
         }
       }
       __syncwarp();      // (the next load of TMEM is one of the whole warp)
@@ -1078,7 +1080,8 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     // ------------------------------ softmax of tile x, and its rows of the outputs ------------------------------
     if constexpr (BITS8) asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     const int x = (warp - 4) >> 2, quarter = warp & 3;
-    const int r = quarter * 32 + lane;   // row of the tile == TMEM lane
+    // the warp's first row of a piece, at its TMEM lanes (below 0: none)
+    auto first_row = [&](const Piece* of) { return quarter * 32 - (of->duo == 2 && x == 1 ? TILE / 2 : 0); };
     const uint32_t lane_sel = uint32_t(quarter * 32) << 16;
     const uint32_t tm_s = tmem_base + x * 128 + lane_sel, tm_o = tmem_base + 256 + x * 128 + lane_sel;
     float c_next = p.scale_log2;         // factor of the scores (8 bits: with what the thread's row has been multiplied by taken back)
@@ -1091,7 +1094,8 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       return reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), quad + j));
     };
     auto ask_q = [&](const Piece* of) {
-      if (of->n_x[x] == 0 || quarter * 32 >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
+      const int r0 = uniform(first_row(of)), r = r0 + lane;
+      if (of->n_x[x] == 0 || r0 < 0 || r0 >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
       const void* own = nullptr;
       if (r < of->rows[x]) {
         const Rows R = p.rows[p.kind[of->g]];
@@ -1182,8 +1186,9 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       give_q(piece);
     }
     while (piece != nullptr) {
-      const bool any = quarter * 32 < piece->rows[x];      // (the same in the whole warp)
-      const bool duo = uniform(piece->duo) != 0;
+      const int r0 = uniform(first_row(piece)), r = r0 + lane;
+      const bool any = r0 >= 0 && r0 < piece->rows[x];      // (the same in the whole warp)
+      const bool duo = uniform(piece->duo) != 0, apart = uniform(piece->duo) == 2;
       const int2 pair_clear = uniform(piece->clear), clear = uniform(piece->clear_x[x]);
       const int n_x = uniform(piece->n_x[x]);
       const float c_row = c_next;
@@ -1204,6 +1209,9 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           uint32_t sv[STEP];
           tmem_ld_x32(tm_su, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
           tmem_ld_x32(tm_su + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          const Scales& of = s_scales[BITS8 ? (at + i) % SCALES : 0];
+          float4 kp, ve;
+          if constexpr (BITS8) kp = of.k, ve = of.e;      // (on their way beside the scores)
           tmem_ld_wait();
           if (i < clear.x || i >= clear.y) {
             const int key0 = piece->block(i) * STEP;
@@ -1223,8 +1231,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
             // A score is its product times K's power, a weight of V the probability times V's: 2^(s + e), in f16, relative to
             // o_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
             // weight has 11 bits unless it is below 2^-21 of the largest.
-            const Scales& of = s_scales[(at + i) % SCALES];
-            const float4 kp = of.k, vp = of.v, ve = of.e;
+            const float4 vp = of.v;
             // (not zero: a masked score is -infinity times this)
             const float cg[4] = {fmaxf(c_row * kp.x, 1.1754944e-38f), fmaxf(c_row * kp.y, 1.1754944e-38f), fmaxf(c_row * kp.z, 1.1754944e-38f), fmaxf(c_row * kp.w, 1.1754944e-38f)};
 #pragma unroll
@@ -1340,7 +1347,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       if (!ok) break;
       const Piece* const next = piece_at(it + 1);
       if (!ok) break;
-      if (next != nullptr) ask_q(next);
+      if (next != nullptr && !apart) ask_q(next);
       float m = m_used, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
       if (n_x > 0) {
         if (!warp_wait(&o_done[x], n_done & 1, err)) break;
@@ -1350,15 +1357,31 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       // (8 bits: O is in units of its own, and V in shared memory 2^-8 of its codes)
       const float unit = !BITS8 ? 1.f : m == -INFINITY ? 0.f : fast_exp2(o_used - m + 8.f);
       float mine = unit, others = 0.f;
-      if (duo) {                           // the two halves' rows are the same ones; each puts half of the columns together
-        tmem_st_x4(tm_s, __float_as_uint(m), __float_as_uint(l), __float_as_uint(unit), 0);   // (over a score buffer: the next piece has not begun)
-        tmem_st_wait();
+      // A duo's halves have the same rows, and each puts half of the columns together.  Maxima and sums are exchanged, and O read, by way
+      // of TMEM (over a score buffer: the next piece has not begun); where the rows are at other lanes, by the room of the queries.
+      auto shared_row = [&](int y) { return smem + L::OFF_Q + y * L::Q_BYTES + r * (DH * 2); };       // of half y: DH / 2 columns that it leaves to the other
+      auto shared_ml = [&](int y) { return reinterpret_cast<float4*>(smem + L::OFF_Q + y * L::Q_BYTES + TILE / 2 * (DH * 2)) + r; };
+      if (duo) {
+        if (!apart) {
+          tmem_st_x4(tm_s, __float_as_uint(m), __float_as_uint(l), __float_as_uint(unit), 0);
+          tmem_st_wait();
+        } else if (any) {
+          *shared_ml(x) = make_float4(m, l, unit, 0.f);
+          for (int h = 0; h < DH / 64 && n_x > 0; ++h) {
+            uint32_t tmp[32];
+            tmem_ld_x32(tm_o + ((x ^ 1) * (DH / 64) + h) * 32, tmp);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<uint4*>(shared_row(x) + (((h * 8 + j) ^ (r & 7)) << 4)) = make_uint4(tmp[4 * j], tmp[4 * j + 1], tmp[4 * j + 2], tmp[4 * j + 3]);
+          }
+        }
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(duo_ml);
         if (!warp_wait(duo_ml, n_duo & 1, err)) break;
         tc_fence_after_sync();
-        const float4 other = tmem_ld_x4(x == 0 ? tm_s + 128 : tm_s - 128);
+        const float4 other = !apart ? tmem_ld_x4(x == 0 ? tm_s + 128 : tm_s - 128) : any ? *shared_ml(x ^ 1) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
         const float top = fmaxf(m, other.x);
         mine = m == -INFINITY ? 0.f : fast_exp2(m - top);
         others = other.x == -INFINITY ? 0.f : fast_exp2(other.x - top);
@@ -1406,11 +1429,28 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                   uint32_t far[16];
-                  tmem_ld_x16((x == 0 ? tm_o + 128 : tm_o - 128) + h * 32 + e * 16, far);
-                  tmem_ld_wait();
+                  if (!apart) {
+                    tmem_ld_x16((x == 0 ? tm_o + 128 : tm_o - 128) + h * 32 + e * 16, far);
+                    tmem_ld_wait();
+                  } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                      const int c = (h - x * (DH / 64)) * 8 + e * 4 + j;
+                      const uint4 v = *reinterpret_cast<const uint4*>(shared_row(x ^ 1) + ((c ^ (r & 7)) << 4));
+                      far[4 * j] = v.x, far[4 * j + 1] = v.y, far[4 * j + 2] = v.z, far[4 * j + 3] = v.w;
+                    }
+                  }
 #pragma unroll
                   for (int j = 0; j < 16; ++j) tmp[e * 16 + j] = __float_as_uint(fmaf(__uint_as_float(far[j]), others, __uint_as_float(tmp[e * 16 + j])));
                 }
+              }
+            }
+            if constexpr (BITS8) {
+#pragma unroll
+              for (int j = 1; j < 32; j += 4) {
+                const uint32_t other = tmp[j];
+                tmp[j] = tmp[j + 1];
+                tmp[j + 1] = other;
               }
             }
             if (!whole) {
@@ -1453,6 +1493,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       // (the next piece's first products wait for these warps' P, so O is free by then)
       at += uniform(piece->n);
       done += n_x;
+      if (next != nullptr && apart) ask_q(next);
       if (duo && next != nullptr) give_q(next);
       give_back();
       piece = next;
@@ -1463,7 +1504,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     constexpr int CODES = DH / 16;                       // 16-byte pieces of a row of codes
     constexpr int PASSES = STEP * CODES / 128;           // of the four warps; each 128 / CODES rows
     const uint32_t group = (warp - 12) >> 2;
-    const int tid = threadIdx.x & 127, col = tid % CODES;
+    const int tid = threadIdx.x & 127, col = tid % CODES, flip = (col >> 2) & 1;
     while (const Piece* const piece = piece_at(it)) {
       const int n = uniform(piece->n);
       const int2 clear = uniform(piece->clear);
@@ -1472,19 +1513,21 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         if (!warp_wait(&raw_full[rs], (j / RS) & 1, err) || !warp_wait(&v_empty[s], ((j / VS) & 1) ^ 1, err)) { ok = false; break; }
         uint4 codes[PASSES];
 #pragma unroll
-        for (int k = 0; k < PASSES; ++k)
-          codes[k] = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + rs * L::RAW_BYTES + (k * 128 + tid) / CODES * DH + col * 16);
+        for (int k = 0; k < PASSES; ++k) {
+          // (the half of a column of codes that is stored first; the eight lanes of a phase of stores hit different banks that way)
+          const uint8_t* const raw = smem + L::OFF_RAW + rs * L::RAW_BYTES + (k * 128 + tid) / CODES * DH + col * 16;
+          const uint2 a = *reinterpret_cast<const uint2*>(raw + flip * 8), b = *reinterpret_cast<const uint2*>(raw + (flip ^ 1) * 8);
+          codes[k] = make_uint4(a.x, a.y, b.x, b.y);
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(&raw_empty[rs]);
         uint8_t* const tile = smem + L::OFF_V + s * L::V_BYTES;
         auto store = [&](int k, const uint4 (&half)[2]) {
           const int row = (k * 128 + tid) / CODES;
-          // (odd and even columns of a row take turns, so that the eight lanes of a phase hit different banks)
-          const int flip = (col >> 2) & 1;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int c = col * 2 + (h ^ flip);
-            *reinterpret_cast<uint4*>(tile + (c / 8) * KV_HALF + sw128_offset(row, c % 8)) = (h ^ flip) ? half[1] : half[0];
+            *reinterpret_cast<uint4*>(tile + (c / 8) * KV_HALF + sw128_offset(row, c % 8)) = half[h];
           }
         };
         uint32_t nan = 0;
