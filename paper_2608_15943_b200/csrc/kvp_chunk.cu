@@ -442,9 +442,8 @@ __device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, 
     const int steps = walked(p, span, R, out.pair).n;
     if (out.off > 0 && out.off < steps) {
       const int w0 = d.share_of(begin - out.off);
-      int second = w0 + 1;                 // (shares may be empty)
-      while (d.first(second) == d.first(w0)) ++second;
-      if (d.first(second) == begin && second == w) note = Merge{out.g, out.hk, out.b, out.pair, w0, d.share_of(begin - out.off + steps - 1), {0, 0}};
+      // (the next one may be empty, and then begins where the first that is not does)
+      if (d.first(w0 + 1) == begin) note = Merge{out.g, out.hk, out.b, out.pair, w0, d.share_of(begin - out.off + steps - 1), {0, 0}};
     }
   }
   // (an empty share may lie between two of a unit's)

@@ -62,6 +62,20 @@ def test_rows_around_halves_of_tiles(kvp, new, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("donor,lens,new,Hq,Hkv", [
+    ([0, 0], [1843, 181, 1452, 2063, 1986], [539, 118, 849, 226, 684], 128, 16),
+    ([0], [2371, 1671, 830, 2609, 634, 1004, 1534, 582, 2695, 1720, 1016], [836, 513, 746, 638, 487, 332, 888, 119, 865, 69, 491], 256, 16),
+    ([0, 0, 0, 0], [1571, 545, 314, 2191, 480], [555, 227, 125, 418, 369], 256, 16),
+    ([0, 0], [2079, 2204, 1238, 567, 2314, 708], [898, 579, 482, 73, 604, 263], 128, 16),
+])
+def test_units_over_shares_without_places(kvp, donor, lens, new, Hq, Hkv, bits):
+    """A unit goes from a share over one that has been left nothing, the second of its shares, into a third."""
+    c = Case(kvp, donor, lens, new, Hq, Hkv, 64, 16, bits)
+    o, lse = c.run()
+    c.check(o, lse, layers=[0, len(donor) - 1])
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("one_each", [True, False])
 def test_windows_of_any_size(kvp, bits, one_each):
     """A window that reaches behind every token is none; more first tokens than there are tokens."""
