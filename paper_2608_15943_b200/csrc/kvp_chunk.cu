@@ -628,9 +628,6 @@ __device__ __forceinline__ void swap_in_quads(uint32_t* v, int t) {
       }
     }
 }
-// of bf16 numbers
-__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return uint32_t((two & 0x7f80u) == 0x7f80u) | uint32_t((two & 0x7f800000u) == 0x7f800000u); }
-__device__ __forceinline__ uint32_t not_finite(const uint4& v) { return not_finite(v.x) | not_finite(v.y) | not_finite(v.z) | not_finite(v.w); }
 // Sixteen e4m3 numbers: whether one of them is NaN, and all times 2^-8 as f16.  The bits of a finite one, its exponent and mantissa
 // one place down from a half's upper byte, are that f16 number (subnormal ones too).  (The conversion instruction takes some
 // seven others, and NaN with it: decode's loop over drafts of 16 sequences 372 us with it for K and V.)
@@ -1037,13 +1034,16 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     while (more) {
       const Piece* const piece = s_pieces + it % PIECES;
       const int n = uniform(piece->n);
-      more = lay_out(it + 1);
+      // (behind the first steps of a long piece, whose blocks may have masks that its products wait for)
+      const int lay_at = !BITS8 && n > 8 ? 2 : 0;
+      if (lay_at == 0) more = lay_out(it + 1);
       if constexpr (!BITS8) {
         constexpr int CHUNKS = DH / 8;       // 16-byte pieces of a row
         const int2 clear = uniform(piece->clear);
         for (int i = 0; i < n && ok; ++i) {
           const uint32_t s = (at + i) % VS;
-          ok = warp_wait(&v_full[s], ((at + i) / VS) & 1, err);
+          if (lay_at > 0 && i == lay_at) more = lay_out(it + 1);
+          ok = ok && warp_wait(&v_full[s], ((at + i) / VS) & 1, err);
           if (!ok) break;
           if (i < clear.x || i >= clear.y) {
             const int block = piece->block(i);
@@ -1053,14 +1053,20 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
             for (int part = 0; part < 2; ++part) {
               const int r = part * 32 + lane;
               const bool dead = piece->unseen(p, block * STEP + r, 1);
-              uint32_t odd = 0;
+              uint32_t most = 0;               // largest magnitudes, as bits
               if (!dead)
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) odd |= not_finite(*reinterpret_cast<const uint4*>(v + (c / 8) * KV_HALF + sw128_offset(r, c % 8)));
-              if (dead || odd != 0)
+                for (int c = 0; c < CHUNKS; ++c) {
+                  const uint4 w = *reinterpret_cast<const uint4*>(v + (c / 8) * KV_HALF + sw128_offset(r, c % 8));
+                  constexpr uint32_t no_sign = 0x7fff7fffu;
+                  most = __vimax3_s16x2(most, w.x & no_sign, w.y & no_sign);
+                  most = __vimax3_s16x2(most, w.z & no_sign, w.w & no_sign);
+                }
+              const bool odd = (most & 0xffffu) >= 0x7f80u || most >= 0x7f800000u;
+              if (dead || odd)
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) *reinterpret_cast<uint4*>(v + (c / 8) * KV_HALF + sw128_offset(r, c % 8)) = make_uint4(0, 0, 0, 0);
-              bad |= (unsigned long long)__ballot_sync(0xffffffffu, odd != 0) << (32 * part);
+              bad |= (unsigned long long)__ballot_sync(0xffffffffu, odd) << (32 * part);
             }
             if (lane < 4) s_bad[s * 4 + lane] = lane == 0 ? bad : 0;
             fence_proxy_async_smem();
@@ -1073,6 +1079,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         }
         at += n;
       }
+      more = more && ok;
       ++it;
     }
   } else if (warp < 12) {
