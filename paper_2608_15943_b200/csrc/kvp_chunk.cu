@@ -1095,13 +1095,24 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     // The warp's query rows of a piece go to their places: every product with the last one's has been seen to complete.  Four lanes a row,
     // and four rows one after the other: a row a lane, its 16-byte parts were as many lines each (3200 cycles a piece, and its output
     // the same way 5400).
+    // Rows that a tile has not are zeros, and their products then take little of the power that bounds large calls.
+    bool clean = false;                  // all of the warp's are zeros
     const int t = lane & 3, quad = lane & ~3;
     auto of_row = [&](const void* own, int j) {            // row quad + j's
       return reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), quad + j));
     };
     auto ask_q = [&](const Piece* of) {
       const int r0 = uniform(first_row(of)), r = r0 + lane;
-      if (of->n_x[x] == 0 || r0 < 0 || r0 >= of->rows[x]) return;     // (what is there stays: nothing of it is stored)
+      if (of->n_x[x] == 0) return;
+      if (r0 < 0 || r0 >= of->rows[x]) {
+        for (int i = lane; !clean && i < 32 * DH / 8; i += 32) {
+          const int row = quarter * 32 + i / (DH / 8), c = i % (DH / 8);
+          *reinterpret_cast<uint4*>(smem + L::OFF_Q + x * L::Q_BYTES + (BITS8 ? quarter * 32 * DH + (c & 1) * (TILE * DH) + i / 2 * 16 : (c / 8) * Q_HALF + sw128_offset(row, c % 8))) = make_uint4(0, 0, 0, 0);
+        }
+        clean = true;
+        return;
+      }
+      clean = false;
       const void* own = nullptr;
       if (r < of->rows[x]) {
         const Rows R = p.rows[p.kind[of->g]];
@@ -1142,7 +1153,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           const int up = min(max(7 + 127 - int(__float_as_uint(most) >> 23), -120), 120);
           const float power = __uint_as_float(uint32_t(up + 127) << 23);
           if (t == j) c_next = p.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
-          if (row != nullptr) {
+          {
 #pragma unroll
             for (int c = 0; c < DH / 64; ++c) {
               uint32_t hi[4], lo[4];
@@ -1165,12 +1176,14 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               *reinterpret_cast<uint4*>(tile + TILE * DH + at8) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
           }
-        } else if (row != nullptr) {
+        } else {
 #pragma unroll
           for (int c4 = 0; c4 < DH / 8; c4 += 4) {
             const int c = c4 + t;
             uint8_t* const place = tile + (c / 8) * Q_HALF + sw128_offset(at_row, c % 8);
-            if (p.io_f32)
+            if (row == nullptr)
+              *reinterpret_cast<uint4*>(place) = make_uint4(0, 0, 0, 0);
+            else if (p.io_f32)
               *reinterpret_cast<uint4*>(place) = eight(row, c);
             else
               cp_async16(smem_u32(place), row + c * 16, 16);
@@ -1499,6 +1512,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       // (the next piece's first products wait for these warps' P, so O is free by then)
       at += uniform(piece->n);
       done += n_x;
+      if (apart) clean = false;
       if (next != nullptr && apart) ask_q(next);
       if (duo && next != nullptr) give_q(next);
       give_back();
