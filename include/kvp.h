@@ -357,13 +357,16 @@ int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, con
  * Rows at positions outside [0, max_pages*page_size) and rows outside all sequences are left out: nothing of theirs is written.
  * Slots at and behind a sequence's length, and tokens that no row of the call sees (pages freed by kvp_pages_trim with the same
  * window among them), are not relied on: they may hold anything.  What a row does not see has no part in its result, infinite or not.
- *   k_cache[l], v_cache[l]  as kvp_decode where k_scale and v_scale are NULL, as kvp_decode8 otherwise; numbers of the 8-bit cache
- *   are taken as bf16 (infinite beyond its range).  A page number outside [0, n_pages) stands for a page of zeros.
- * scale == 0 means 1/sqrt(dh); it is not negative.  P is rounded to bf16 for the second product, sums are fp32: |V| is to stay below
- * 2^100.  A row whose scores are all -infinity has output 0 and LSE -infinity.
+ *   k_cache[l], v_cache[l]  as kvp_decode where k_scale and v_scale are NULL, as kvp_decode8 otherwise.  A page number outside
+ *   [0, n_pages) stands for a page of zeros.
+ * scale == 0 means 1/sqrt(dh); it is not negative.  KVP_F32 queries are rounded to bf16; infinities and NaN in a row of them reach the
+ * outputs of that row alone.  P is rounded to bf16 for the second product, and over the 8-bit cache to 11 bits (f16; below 2^-21 of a row's
+ * largest weight, P times V's scale, to 2^-32 of it).  The 8-bit cache's numbers and scales are taken as they are; in the scores with
+ * them, a query element of less than 2^-16 of its row's largest may be off by 2^-25 of that.  Sums are fp32: |V| is to stay below 2^100.
+ * A row whose scores are all -infinity has output 0 and LSE -infinity.
  * A call cuts the work by the lengths of the whole batch: equal calls give equal bits, and a sequence's last bits (fp32 summation
  * order) depend on the other sequences and the layer range.  dtype and the rest of d as for kvp_decode, num_splits is not read;
- * max_pages*page_size <= 2^30, B <= 16384, n_pages*Hkv*page_size < 2^31 - 64.
+ * max_pages*page_size <= 2^30, B <= 16384, T < 2^24, n_pages*Hkv*page_size < 2^31 - 64.
  * Workspace: kvp_attn_chunk_workspace_bytes(d, donor, T), 16-byte aligned; enough for any layer range and any smaller T. */
 size_t kvp_attn_chunk_workspace_bytes(const kvp_decode_desc* d, const int32_t* donor, int32_t T);
 int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, int32_t T, const int32_t* first, float scale, int32_t window,

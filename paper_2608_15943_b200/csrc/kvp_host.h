@@ -11,11 +11,11 @@
 
 namespace kvp {
 
+enum { SWIZZLE_0 = 0, SWIZZLE_128 = 1, SWIZZLE_64 = 2 };   // (callers may give a bool: true is the 128-byte one)
 // Builds a tiled TMA descriptor over a row-major tensor of bytes, bf16 or fp32 of up to 4 dimensions.
 // dims[0] is the innermost (contiguous) extent in elements; strides_bytes[i] is the byte stride
 // of dims[i+1].  box[] is the tile copied per request.  swizzle: SWIZZLE_128 or SWIZZLE_64
 // (the inner box extent must then span exactly as many bytes), or none.  Returns KVP_OK or KVP_ERR_CUDA.
-enum { SWIZZLE_0 = 0, SWIZZLE_128 = 1, SWIZZLE_64 = 2 };   // (true: the 128-byte one)
 int make_tensor_map(CUtensorMap* out, const void* base, int elem_bytes, int rank, const uint64_t* dims,
                     const uint64_t* strides_bytes, const uint32_t* box, int swizzle);
 

@@ -130,6 +130,13 @@ def test_scales_come_in_pairs_and_alignment(kvp, as_on_a_device):
     assert e.value.status == UNSUPPORTED
 
 
+def test_more_rows_than_are_counted(kvp):
+    some = (C.c_void_p * 1)(256)
+    d = kvp.DecodeDesc(1, 1, 4, 2, 64, 16, 4, 12, 0, kvp.BF16)
+    call = lambda T: kvp.lib.kvp_attn_chunk(C.byref(d), (C.c_int32 * 1)(0), T, 256, 0.0, 0, 0, some, some, some, None, None, 256, 256, some, some, 0, 1, None, 0, None)
+    assert call(1 << 24) == UNSUPPORTED and call((1 << 31) - 1) == UNSUPPORTED and call((1 << 24) - 1) == WORKSPACE
+
+
 def test_no_rows_are_no_work(kvp, as_on_a_device):
     a = chunk_args(kvp, T=0)
     chunk(kvp, a)
