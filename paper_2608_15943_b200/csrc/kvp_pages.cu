@@ -4,8 +4,10 @@
 //
 // Bookkeeping is one cluster of up to eight blocks a call, which meets between the phases that read and those that write: what
 // a call decides is decided from the state before it, and free pages are ranked by prefix sums over the pages, lowest first, so
-// results are the same from run to run.  Bound: latency, of three to five trips to L2 with a cluster barrier behind each.
-// Pages that move are listed in the workspace, and a second launch copies them in all layers: bound by HBM.
+// results are the same from run to run.  Bound: latency, of three to five trips to L2 with a cluster barrier behind each.  Books that
+// the threads of one block can keep in registers are read once instead.  Pages that move are listed in the workspace, and a second
+// launch copies them in all layers: bound by HBM (100 MB read and written in 32 us, at the rate of a plain copy), past the other
+// numbers in L2.
 #include <algorithm>
 
 #include "kvp_cache8.h"
@@ -267,6 +269,190 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_kernel(const __grid_co
 }
 
 // ---------------------------------------------------------------------------------------------
+// the same for small books: one block, whose threads keep what they have read
+// ---------------------------------------------------------------------------------------------
+// Every number is read once, as many as the threads have at a time, and what is decided stays in registers and shared memory: one chain
+// of loads instead of one for each phase (32 rows of 25 places, two resizes with what they copy, from a graph: 16.4 -> 10.8 us; 64 rows of
+// 24, a fork and two resizes 57 -> 49).
+constexpr int FEW_PAGES = 8, FEW_PLACES = 4;      // of a thread: pages, and places of the table
+__global__ void __launch_bounds__(BOOK_THREADS, 1) fork_few_kernel(const __grid_constant__ Book p, const int32_t* parent) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int lane = lane_id(), per_row = (p.max_pages + 31) / 32, items = p.B * per_row;
+  int row[FEW_PLACES], place[FEW_PLACES], from[FEW_PLACES], length[FEW_PLACES], had[FEW_PLACES], have[FEW_PLACES], before[FEW_PLACES], after[FEW_PLACES];
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    const int w = u * BOOK_WARPS + int(threadIdx.x >> 5);
+    row[u] = w < items ? w / per_row : -1;
+    place[u] = w % per_row * 32 + lane;
+    from[u] = row[u] >= 0 ? parent[row[u]] : 0;
+    if (from[u] == row[u] || from[u] < -1 || from[u] >= p.B) row[u] = -1;
+  }
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    length[u] = row[u] >= 0 && from[u] >= 0 ? p.lengths[from[u]] : 0;
+    had[u] = row[u] >= 0 ? p.places(p.lengths[row[u]]) : 0;
+    have[u] = p.places(length[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    before[u] = place[u] < had[u] ? p.at(row[u], place[u]) : -1;
+    after[u] = place[u] < have[u] ? p.at(from[u], place[u]) : -1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    if (row[u] < 0) continue;
+    if (place[u] == 0) p.lengths[row[u]] = length[u];
+    if (place[u] < max(had[u], have[u])) p.at(row[u], place[u]) = after[u];
+    if (before[u] == after[u]) continue;
+    if (p.is_page(before[u])) atomicSub(p.refs + before[u], 1);
+    if (p.is_page(after[u])) atomicAdd(p.refs + after[u], 1);
+  }
+}
+__global__ void __launch_bounds__(BOOK_THREADS, 1) resize_few_kernel(const __grid_constant__ Book p, const __grid_constant__ BookSpace ws, const int32_t* to, int32_t* lacking) {
+  __shared__ int s_need[BOOK_THREADS + 1], s_copies[BOOK_THREADS + 1], s_had[BOOK_THREADS], s_have[BOOK_THREADS];   // first new page and copy of each row
+  __shared__ __align__(16) int s_end[BOOK_THREADS];
+  __shared__ unsigned long long s_warp[32];
+  grid_dep_launch();
+  grid_dep_wait();
+  const int tid = int(threadIdx.x), each = (p.n_pages + BOOK_THREADS - 1) / BOOK_THREADS, lane = lane_id();
+  uint32_t free = 0;                     // of the thread's pages, tid * each + u
+#pragma unroll
+  for (int u = 0; u < FEW_PAGES; ++u)
+    if (u < each && tid * each + u < p.n_pages && p.refs[tid * each + u] == 0) free |= 1u << u;
+  const bool is_row = tid < p.B;
+  const int length = is_row ? p.lengths[tid] : 0, longer = is_row ? to[tid] : 0, had = p.places(length), have = p.places(longer);
+  int end = is_row && longer > length && length > 0 && length % p.page_size != 0 && had > 0 ? p.at(tid, had - 1) : -1;
+  if (!p.is_page(end)) end = -1;
+  const int held = end >= 0 ? p.refs[end] : 0;
+  s_had[tid] = had;
+  s_have[tid] = have;
+  s_end[tid] = is_row ? end : -1;
+  const bool bad = __syncthreads_or(longer < 0 || longer > (long long)p.max_pages * p.page_size) != 0;
+  bool copies = false;
+  if (held > 1) {
+    int growing = 0, lowest = tid;
+    for (int i = (p.B - 1) / 4; i >= 0; --i) {
+      const int4 of = reinterpret_cast<const int4*>(s_end)[i];
+      growing += (of.x == end) + (of.y == end) + (of.z == end) + (of.w == end);
+      lowest = min(lowest, of.x == end ? 4 * i : of.y == end ? 4 * i + 1 : of.z == end ? 4 * i + 2 : of.w == end ? 4 * i + 3 : lowest);
+    }
+    copies = growing != held || lowest != tid;
+  }
+  // new pages, copies and free pages ahead of the thread's, 20 bits each (none is above FEW_PAGES * BOOK_THREADS)
+  const unsigned long long mine = (unsigned long long)(max(0, have - had) + copies) | (unsigned long long)copies << 20 | (unsigned long long)__popc(free) << 40;
+  unsigned long long total;
+  const unsigned long long ahead = block_scan(mine, s_warp, total);
+  constexpr uint32_t LOW = (1u << 20) - 1;
+  const int need = int(total & LOW), n_free = int(total >> 40);
+  s_need[tid] = int(ahead & LOW);
+  s_copies[tid] = int(ahead >> 20 & LOW);
+  if (tid == 0) {
+    s_need[BOOK_THREADS] = need;
+    s_copies[BOOK_THREADS] = int(total >> 20 & LOW);
+  }
+  const int short_of = bad ? -1 : max(0, need - n_free);
+  if (tid == 0) {
+    *lacking = short_of;
+    *ws.n_copies = short_of != 0 ? 0 : int(total >> 20 & LOW);
+  }
+  if (short_of != 0) return;             // (the same in all threads)
+  __syncthreads();
+  for (int k = int(ahead >> 40); free != 0 && k < need; free &= free - 1, ++k) {
+    const int page = tid * each + __ffs(free) - 1;
+    int lo = 0, hi = p.B - 1;            // last row that begins at or before k
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (s_need[mid] <= k) lo = mid; else hi = mid - 1;
+    }
+    const int i = k - s_need[lo], its_copies = s_copies[lo + 1] - s_copies[lo];
+    if (i < its_copies) {
+      ws.src[s_copies[lo]] = s_end[lo];
+      ws.dst[s_copies[lo]] = page;
+    }
+    p.at(lo, s_had[lo] + i - its_copies) = page;
+    p.refs[page] = 1;
+  }
+  if (copies) atomicSub(p.refs + end, 1);
+  if (is_row) p.lengths[tid] = longer;
+  // (what a row gives up is at other places and of other pages than what the others get)
+  for (int row = tid >> 5; row < p.B; row += BOOK_WARPS)
+    for (int place = s_have[row] + lane; place < s_had[row]; place += 32) {
+      const int page = p.at(row, place);
+      if (p.is_page(page)) atomicSub(p.refs + page, 1);
+      p.at(row, place) = -1;
+    }
+}
+__global__ void __launch_bounds__(BOOK_THREADS, 1) compact_few_kernel(const __grid_constant__ Book p, const __grid_constant__ BookSpace ws, int32_t* used_out) {
+  __shared__ uint16_t s_hole[FEW_PAGES * BOOK_THREADS / 2], s_to[FEW_PAGES * BOOK_THREADS];    // holes by rank; new numbers of the pages that move
+  __shared__ unsigned long long s_warp[32];
+  __shared__ int s_below;
+  grid_dep_launch();
+  grid_dep_wait();
+  const int tid = int(threadIdx.x), each = (p.n_pages + BOOK_THREADS - 1) / BOOK_THREADS, lane = lane_id();
+  const int per_row = (p.max_pages + 31) / 32, items = p.B * per_row;
+  int refs[FEW_PAGES], named[FEW_PLACES];
+#pragma unroll
+  for (int u = 0; u < FEW_PAGES; ++u) refs[u] = u < each && tid * each + u < p.n_pages ? p.refs[tid * each + u] : 0;
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    const int w = u * BOOK_WARPS + (tid >> 5), row = w / per_row, place = w % per_row * 32 + lane;
+    named[u] = w < items && place < p.places(p.lengths[row]) ? p.at(row, place) : -1;
+  }
+  int mine = 0;
+#pragma unroll
+  for (int u = 0; u < FEW_PAGES; ++u) mine += refs[u] != 0;
+  unsigned long long total;
+  const int ahead = int(block_scan(mine, s_warp, total)), used = int(total);
+  // Holes are the free pages below `used`, movers the used ones at or above it: as many.  A page's rank among either follows from
+  // the number of used pages below it.
+  if (tid == 0 && used == p.n_pages) s_below = used;
+  for (int u = 0, before = ahead; u < each; ++u) {
+    const int page = tid * each + u;
+    if (page >= p.n_pages) break;
+    int r = 0;
+#pragma unroll
+    for (int k = 0; k < FEW_PAGES; ++k) r = k == u ? refs[k] : r;
+    if (page == used) s_below = before;
+    if (page < used && r == 0) s_hole[page - before] = uint16_t(page);
+    if (page >= used) s_to[page] = 0xffff;
+    before += r != 0;
+  }
+  __syncthreads();
+  const int below = s_below;             // used pages below `used`
+  if (tid == 0) {
+    *used_out = used;
+    *ws.n_copies = used - below;
+  }
+  if (used == below) return;             // (the same in all threads)
+  for (int u = 0, before = ahead; u < each; ++u) {
+    const int page = tid * each + u;
+    if (page >= p.n_pages) break;
+    int r = 0;
+#pragma unroll
+    for (int k = 0; k < FEW_PAGES; ++k) r = k == u ? refs[k] : r;
+    if (page >= used && r != 0) {
+      const int rank = before - below, to = s_hole[rank];
+      s_to[page] = uint16_t(to);
+      ws.src[rank] = page;
+      ws.dst[rank] = to;
+      p.refs[to] = r;
+      p.refs[page] = 0;
+    }
+    before += r != 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < FEW_PLACES; ++u) {
+    if (named[u] < used || named[u] >= p.n_pages || s_to[named[u]] == 0xffff) continue;
+    const int w = u * BOOK_WARPS + (tid >> 5);
+    p.at(w / per_row, w % per_row * 32 + lane) = s_to[named[u]];
+  }
+}
+static_assert(FEW_PAGES * BOOK_THREADS < 0xffff && FEW_PLACES * BOOK_WARPS <= BOOK_THREADS, "numbers of pages in 16 bits; a thread a row");
+
+// ---------------------------------------------------------------------------------------------
 // trim: places that no later token sees
 // ---------------------------------------------------------------------------------------------
 constexpr int TRIM_THREADS = 256;
@@ -377,12 +563,12 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_pages_kernel(const __grid_c
 #pragma unroll
     for (int u = 0; u < COPY_FLY; ++u) {
       const uint32_t off = piece * COPY_CHUNK + (u * COPY_THREADS + threadIdx.x) * 16;
-      if (off < p.page_bytes) held[u] = *reinterpret_cast<const uint4*>(src + off);
+      if (off < p.page_bytes) held[u] = __ldcs(reinterpret_cast<const uint4*>(src + off));
     }
 #pragma unroll
     for (int u = 0; u < COPY_FLY; ++u) {
       const uint32_t off = piece * COPY_CHUNK + (u * COPY_THREADS + threadIdx.x) * 16;
-      if (off < p.page_bytes) *reinterpret_cast<uint4*>(dst + off) = held[u];
+      if (off < p.page_bytes) __stcs(reinterpret_cast<uint4*>(dst + off), held[u]);
     }
     uint8_t* const scales = which & 1 ? at.v_scale : at.k_scale;
     if (piece == 0 && scales != nullptr)
@@ -459,6 +645,10 @@ int book_blocks(const kvp_decode_desc* d) {
   const long long work = (long long)d->B * d->max_pages + d->n_pages;
   return work <= 8 * BOOK_THREADS ? 1 : BOOK_BLOCKS;
 }
+// Rows, pages and places that one block's threads can keep
+bool few(const kvp_decode_desc* d) {
+  return d->n_pages <= FEW_PAGES * BOOK_THREADS && (long long)d->B * ((d->max_pages + 31) / 32) <= FEW_PLACES * BOOK_WARPS;
+}
 
 }  // namespace
 }  // namespace kvp
@@ -487,8 +677,9 @@ int kvp_pages_fork(const kvp_decode_desc* d, const int32_t* parent, int32_t* ref
   rc = check_space(d, ws, ws_bytes);
   if (rc != KVP_OK) return rc;
   const int blocks = book_blocks(d);
-  const cudaError_t e = launch_kernel(fork_kernel, blocks, BOOK_THREADS, 0, reinterpret_cast<cudaStream_t>(stream), blocks, book_of(d, refs, block_table, lengths),
-                                      book_space(d, ws), parent);
+  const Book book = book_of(d, refs, block_table, lengths);
+  const cudaError_t e = few(d) ? launch_kernel(fork_few_kernel, 1, BOOK_THREADS, 0, reinterpret_cast<cudaStream_t>(stream), 1, book, parent)
+                               : launch_kernel(fork_kernel, blocks, BOOK_THREADS, 0, reinterpret_cast<cudaStream_t>(stream), blocks, book, book_space(d, ws), parent);
   return e == cudaSuccess ? KVP_OK : KVP_ERR_CUDA;
 }
 
@@ -506,7 +697,9 @@ int kvp_pages_resize(const kvp_decode_desc* d, const int32_t* donor, const int32
   const BookSpace space = book_space(d, ws);
   const int blocks = book_blocks(d), smem = (d->B + 1) * 8 + d->B * 4;
   if (allow_smem<resize_kernel>((MOST_ROWS + 1) * 8 + MOST_ROWS * 4) != cudaSuccess) return KVP_ERR_CUDA;
-  const cudaError_t e = launch_kernel(resize_kernel, blocks, BOOK_THREADS, smem, stream, blocks, book_of(d, refs, block_table, lengths), space, new_lengths, lacking);
+  const Book book = book_of(d, refs, block_table, lengths);
+  const cudaError_t e = few(d) ? launch_kernel(resize_few_kernel, 1, BOOK_THREADS, 0, stream, 1, book, space, new_lengths, lacking)
+                               : launch_kernel(resize_kernel, blocks, BOOK_THREADS, smem, stream, blocks, book, space, new_lengths, lacking);
   if (e != cudaSuccess) return KVP_ERR_CUDA;
   return copy_pages(d, donor, space.src, space.dst, space.n_copies, d->B, k_cache, v_cache, k_scale, v_scale, stream);
 }
@@ -532,7 +725,9 @@ int kvp_pages_compact(const kvp_decode_desc* d, const int32_t* donor, int32_t* r
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   const BookSpace space = book_space(d, ws);
   const int blocks = book_blocks(d);
-  const cudaError_t e = launch_kernel(compact_kernel, blocks, BOOK_THREADS, 0, stream, blocks, book_of(d, refs, block_table, const_cast<int32_t*>(lengths)), space, used);
+  const Book book = book_of(d, refs, block_table, const_cast<int32_t*>(lengths));
+  const cudaError_t e = few(d) ? launch_kernel(compact_few_kernel, 1, BOOK_THREADS, 0, stream, 1, book, space, used)
+                               : launch_kernel(compact_kernel, blocks, BOOK_THREADS, 0, stream, blocks, book, space, used);
   if (e != cudaSuccess) return KVP_ERR_CUDA;
   return copy_pages(d, donor, space.src, space.dst, space.n_copies, d->n_pages, k_cache, v_cache, k_scale, v_scale, stream);
 }
