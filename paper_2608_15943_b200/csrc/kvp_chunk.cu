@@ -277,8 +277,9 @@ __device__ __forceinline__ int last_below(const long long* sums, int n, long lon
   return i;
 }
 // How the list is dealt out.  Many units: whole, in rounds of one a CTA, so that CTAs that run together read the same keys at the same
-// time, out of L2; the last two rounds and what is left are cut into shares that even out what the rounds gave.  Not where a unit is longer
-// than an eighth of a CTA's work (what is left would not even that out), or where there are few: equal shares of the whole list.
+// time, out of L2; as many as give no CTA more than a fair part, and not the last two.  What is left is cut into shares that even out
+// what the rounds gave.  Not where a unit is longer than an eighth of a CTA's work (what is left would not even that out), or where
+// there are few: equal shares of the whole list.
 // (Pieces of prompts behind 2K to 8K tokens, read out of memory: 8.3 GB with equal shares of the list.)
 // Few and short units: whole, one a CTA.
 constexpr int ROUNDS_FROM = 4, ROUNDS_LEFT = 2, WHOLE_UP_TO = 8;
@@ -292,34 +293,26 @@ struct Deal {
   __device__ __forceinline__ long long first(int w) const { return even ? Dealt(total, n).begin(w) : begin[w]; }
   __device__ __forceinline__ int share_of(long long at) const { return even ? Dealt(total, n).share_of(at) : last_below(begin, n, at); }
 };
-// The unit, or the place, `at` of the list, by a warp: group, KV head, sequence; what is left is inside the sequence's.  `other`: the
-// places, or units, ahead of it.
+// The place `at` of the list, by a warp: group, KV head, sequence; what is left is inside the sequence's.
 struct Found {
   int g, hk, b;
-  long long left, other;
+  long long left;
 };
-template <bool UNITS>
 __device__ __forceinline__ Found find(const ChunkSizes& p, const Sums& s, long long at) {
-  Found f{0, 0, 0, at, 0};
-  auto all = [&](int kind, bool units) { return units ? s.all_units(kind) : s.all_places(kind); };
+  Found f{0, 0, 0, at};
   for (;; ++f.g) {
-    const int kind = p.kind[f.g];
-    if (f.left < all(kind, UNITS) * p.Hkv) break;
-    f.left -= all(kind, UNITS) * p.Hkv;
-    f.other += all(kind, !UNITS) * p.Hkv;
+    const long long group = s.all_places(p.kind[f.g]) * p.Hkv;
+    if (f.left < group) break;
+    f.left -= group;
   }
   const int kind = p.kind[f.g];
-  f.hk = int(div_places(f.left, all(kind, UNITS)));
-  f.left -= f.hk * all(kind, UNITS);
-  f.other += f.hk * all(kind, !UNITS);
-  const int row = kind * (s.n32 + 1), i = last_below((UNITS ? s.units : s.places) + row, s.n32, f.left);
-  f.left -= (UNITS ? s.units : s.places)[row + i];
-  f.other += (UNITS ? s.places : s.units)[row + i];
-  const Listed l = listed(p, i * 32 + lane_id(), p.rows[kind]);
-  const long long mine = UNITS ? l.pairs : l.places, its = UNITS ? l.places : l.pairs, up = warp_scan(mine), up_its = warp_scan(its);
+  f.hk = int(div_places(f.left, s.all_places(kind)));
+  f.left -= f.hk * s.all_places(kind);
+  const int row = kind * (s.n32 + 1), i = last_below(s.places + row, s.n32, f.left);
+  f.left -= s.places[row + i];
+  const long long mine = listed(p, i * 32 + lane_id(), p.rows[kind]).places, up = warp_scan(mine);
   const int of = __ffs(__ballot_sync(0xffffffffu, up > f.left)) - 1;
   f.left -= __shfl_sync(0xffffffffu, up - mine, of);
-  f.other += __shfl_sync(0xffffffffu, up_its - its, of);
   f.b = i * 32 + of;
   return f;
 }
@@ -339,18 +332,11 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
     d.rounds_end = units;
     d.base = d.total;
   } else if (units >= (long long)ROUNDS_FROM * n && (long long)longest * 8 * n <= d.total) {
-    d.rounds_end = (div_places(units, n) - ROUNDS_LEFT) * n;
-    const Found f = find<true>(p, s, d.rounds_end);
-    const Span span = span_of(p, f.b);
-    const Rows R = p.rows[p.kind[f.g]];
-    long long before = 0;
-    for (int pair = lane; pair < int(f.left); pair += 32) before += walked(p, span, R, pair).n + REST;
-    d.base = f.other + warp_sum(before);
     // what the rounds give each CTA, from the places of every unit of a KV head
     int* const cost = reinterpret_cast<int*>(d.begin + n + 1);
     long long all = 0;
     for (int kind = 0; kind < p.n_kinds; ++kind) all += s.all_units(kind);
-    if (all * 4 + (n + 1) * 8 <= room) {
+    if ((all + 1) * 4 + (n + 1) * 8 <= room) {
       for (int kind = 0, at = 0; kind < p.n_kinds; at += int(s.all_units(kind)), ++kind) {
         const Rows rows = p.rows[kind];
         for (int i = warp; i < s.n32; i += warps) {
@@ -368,11 +354,15 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
           }
         }
       }
+      int* const rounds = cost + all;
+      if (threadIdx.x == 0) *rounds = int(div_places(units, n)) - ROUNDS_LEFT;
       __syncthreads();
-      if (int(threadIdx.x) < n) {
+      // the CTA's places in the first `most` rounds, as long as they are no more than a fair part of all
+      const long long fair = div_places(d.total, n);
+      auto take = [&](int most, int& taken) {
         long long mine = 0, in = threadIdx.x;                  // unit of the KV head `g`, hk
         int g = 0, hk = 0, at = 0;
-        for (long long u = threadIdx.x; u < d.rounds_end; u += n, in += n) {
+        for (taken = 0; taken < most; ++taken, in += n) {
           while (in >= s.all_units(p.kind[g])) {
             in -= s.all_units(p.kind[g]);
             if (++hk == p.Hkv) {
@@ -382,10 +372,20 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
               for (int kind = 0; kind < p.kind[g]; ++kind) at += int(s.all_units(kind));
             }
           }
+          if (mine + cost[at + in] > fair) break;
           mine += cost[at + in];
         }
-        d.begin[threadIdx.x] = max(0ll, div_places(d.total, n) - mine);
+        return mine;
+      };
+      const bool is_cta = int(threadIdx.x) < n;
+      int taken = 0;
+      if (is_cta) {
+        take(int(div_places(units, n)) - ROUNDS_LEFT, taken);
+        atomicMin(rounds, taken);
       }
+      __syncthreads();
+      d.rounds_end = (long long)*rounds * n;
+      if (is_cta) d.begin[threadIdx.x] = fair - take(*rounds, taken);
       __syncthreads();
       if (warp == 0) {                                         // sums, then in proportion: they come to what is left
         long long sum = 0;
@@ -396,12 +396,14 @@ __device__ __forceinline__ Deal deal_out(const ChunkSizes& p, const Sums& s, int
           sum += __shfl_sync(0xffffffffu, up, 31);
         }
         __syncwarp();
-        const double part = sum > 0 ? double(d.total - d.base) / double(sum) : 0.;
-        for (int i = lane; i < n; i += 32) d.begin[i] = min(d.total - d.base, (long long)(double(d.begin[i]) * part));
-        if (lane == 0) d.begin[n] = d.total - d.base;
+        const long long left = sum + (d.total - n * fair);
+        const double part = sum > 0 ? double(left) / double(sum) : 0.;
+        for (int i = lane; i < n; i += 32) d.begin[i] = min(left, (long long)(double(d.begin[i]) * part));
+        if (lane == 0) d.begin[n] = left;
       }
       d.even = false;
       __syncthreads();
+      d.base = d.total - d.begin[n];
     }
   }
   d.total -= d.base;
@@ -415,7 +417,7 @@ __device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, 
   Merge note{0, 0, 0, 0, -1, -1, {0, 0}};
   const long long begin = w < d.n ? d.first(w) : 0, size = w < d.n ? (w + 1 < d.n ? d.first(w + 1) : d.total) - begin : 0;
   if (size > 0) {
-    const Found f = find<false>(p, s, d.base + begin);
+    const Found f = find(p, s, d.base + begin);
     out.g = f.g;
     out.hk = f.hk;
     out.b = f.b;
