@@ -4,8 +4,9 @@
 // The query rows of a sequence and KV head are laid out token by token: the G heads of a token in each of the layers that
 // share the donor.  128 of them are a tile, two tiles a unit; a unit walks the cached keys that any of its rows sees, 64 a step,
 // and each K/V block that it brings in serves both tiles, all heads and all layers.  The steps of all units form one list, which the
-// CTAs (one an SM) cut into equal shares from the lengths on the device; a unit that ends up in several shares is merged by a
-// second kernel.  So one long context occupies the whole device, and prompts of any lengths leave no SM behind.
+// CTAs (one an SM) deal out among themselves from the lengths on the device: whole units in rounds where there are many, equal shares
+// of the list where there are few; a unit that ends up in several shares is merged by a second kernel.  So one long context
+// occupies the whole device, and prompts of any lengths leave no SM behind.
 //   warp 0        TMA producer: K and V blocks, page by page (8-bit cache: the codes into a ring of their own, and their scales)
 //   warps 1, 2    tcgen05.mma issuers, one per tile: S = Q K^T into one of two 64-column score buffers, O += P V with P from TMEM
 //   warp 3        lays out the CTA's pieces of units, and looks through the V blocks that not every row sees in full
@@ -14,6 +15,13 @@
 //                 it, take every other step each, and put their two sums together at the end.
 //   warps 12-19   (8-bit cache only) V's codes to f16, which holds them exactly.  K's are operands as they are; the scales are applied
 //                 to the scores and to the weights of V.
+// What bounds it.  Drafts (2-8 tokens of 16 sequences of 4K-16K, 16 to 64 rows a unit): memory in bf16, 226 us, 5.8 TB/s; over the
+// 8-bit cache, 245 us, the chain of a step (scores out of TMEM, maximum, exponentials and weights, P, product; some 3300 cycles for
+// every other step of each half), beside the conversion of V on the same schedulers.  Prompts: the 1000 W of the board (1.67 to 1.8 GHz; 1100
+// TFLOP/s over 64K tokens, 71% of a burst of 15.5 ms); ahead of it the exponentials (1024 of 1800 cycles a step of two tiles) and the
+// products of 64 columns, which read Q again for each (1280).  Heads of 64 over 8 bits: the chain, 2800 cycles a step at full clock.
+// Left out: a quarter of the exponentials as polynomials on the multipliers (no faster in bf16, registers spill in 8 bits);
+// turns for the two tiles' exponentials (5 to 15% slower); the next piece's queries asked for ahead of the last step (5% slower).
 // Masked places.  A score that a row does not see is -infinity before the maximum.  In V, rows that no row of the unit sees (slots
 // behind the sequence, freed pages before the window: anything may be there) are not read and are zeros in shared memory.  A
 // visible row of V with an infinity or NaN in it must reach the rows that see it and no other, which 0 * NaN in a matrix product
@@ -40,8 +48,9 @@ constexpr int MANY_CHUNK_GROUPS = 16, FEW_CHUNK_GROUPS = 4;
 constexpr uint32_t Q_HALF = TILE * 128;   // one [128 rows x 128 B] block of Q
 constexpr uint32_t KV_HALF = STEP * 128;
 constexpr float kRescaleBy = 8.0f;        // log2: O is rescaled when the maximum has moved by more
-// Places of the list behind the steps of a unit, for its start and its merge; least places of a share.
-constexpr int REST = 3, LEAST_SHARE = 8;
+// Places of the list behind the steps of a unit, for its start, its output and its merge, 8900 cycles where a step of two tiles takes 1800
+// (3: drafts and prompts under a window 1% slower; 8: short prompts 1%); least places of a share.
+constexpr int REST = 6, LEAST_SHARE = 8;
 
 __device__ int g_chunk_status;
 
