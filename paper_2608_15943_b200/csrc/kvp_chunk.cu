@@ -1747,7 +1747,9 @@ int check_chunk(const kvp_decode_desc* d) {
 
 // One token a sequence, few query rows: decode's kernels, on a table of the pages that the token sees.  Front pages of first tokens,
 // then those from the window's first on; the positions between the two parts are one run, in the last page of the front or the
-// first of the window (kvp_host.h).
+// first of the window (kvp_host.h).  Those kernels bring in rows of 16 queries where a tile here has 128: 32 sequences of 16K-32K
+// under a window of 4096, two groups of 16 rows, 600 us on the list above and 493 so (6.5 TB/s); 58 of 1-3000 in 8 bits under
+// 1000, 6 rows, 155 and 37.
 struct Ones {
   const int32_t *block_table, *lengths;
   int32_t *table, *shortened;              // [B, columns], [B]; null without a window
