@@ -13,13 +13,13 @@
 //   warps 4-11    softmax, a warpgroup per tile, a thread per row; then O out of TMEM to the outputs or to the unit's partial sums,
 //                 while the rows of the next piece come into shared memory.  Where a unit has one tile alone, both warpgroups have
 //                 it, take every other step each, and put their two sums together at the end.
-//   warps 12-19   (8-bit cache only) V's codes to f16, which holds them exactly.  K's are operands as they are; the scales are applied
+//   warps 12-15   (8-bit cache only) V's codes to f16, which holds them exactly.  K's are operands as they are; the scales are applied
 //                 to the scores and to the weights of V.
 // What bounds it.  Drafts (2-8 tokens of 16 sequences of 4K-16K, 16 to 64 rows a unit): memory in bf16, 226 us, 5.8 TB/s; over the
 // 8-bit cache, 245 us, the chain of a step (scores out of TMEM, maximum, exponentials and weights, P, product; some 3300 cycles for
 // every other step of each half), beside the conversion of V on the same schedulers.  Prompts: the 1000 W of the board (1.67 to 1.8 GHz; 1100
 // TFLOP/s over 64K tokens, 71% of a burst of 15.5 ms); ahead of it the exponentials (1024 of 1800 cycles a step of two tiles) and the
-// products of 64 columns, which read Q again for each (1280).  Heads of 64 over 8 bits: the chain, 2800 cycles a step at full clock.
+// products of 64 columns, which read Q again for each (1280).  Heads of 64 over 8 bits: the chain, 2700 cycles a step at full clock.
 // Left out: a quarter of the exponentials as polynomials on the multipliers (no faster in bf16, registers spill in 8 bits);
 // turns for the two tiles' exponentials (5 to 15% slower); the next piece's queries asked for ahead of the last step (5% slower).
 // Masked places.  A score that a row does not see is -infinity before the maximum.  In V, rows that no row of the unit sees (slots
@@ -78,12 +78,13 @@ struct ChunkSmem {
   static constexpr int OFF_SCALE = OFF_BAD + V_STAGES * 32;     // [SCALES]
   static constexpr int OFF_PIECES = OFF_SCALE + (BITS8 ? SCALES * int(sizeof(Scales)) : 0);
   static constexpr int TOTAL = OFF_PIECES + PIECES_BYTES + 1024;      // room for the alignment
-  static constexpr int THREADS = BITS8 ? 640 : 384;
+  static constexpr int THREADS = BITS8 ? 512 : 384;
+  // 8-bit cache: registers of a thread at launch, of the softmax threads, and what stays with each of the others
+  static constexpr int LAUNCH_REGS = 128, SOFTMAX_REGS = 192, OTHER_REGS = 64;
+  static_assert(256 * SOFTMAX_REGS + 256 * OTHER_REGS <= 512 * LAUNCH_REGS, "registers of a CTA");
 };
 static_assert(ChunkSmem<128, false>::TOTAL <= 232448 && ChunkSmem<128, true>::TOTAL <= 232448, "shared memory of a CTA");
-// (two groups of warps convert every other step each, so that a stage always is the same group's)
-static_assert(ChunkSmem<128, true>::V_STAGES % 2 == 0 && ChunkSmem<64, true>::RAW_STAGES % 2 == 0 && ChunkSmem<128, true>::RAW_STAGES % 2 == 0 &&
-                  ChunkSmem<64, true>::RAW_STAGES + ChunkSmem<64, true>::V_STAGES + 1 < SCALES && ChunkSmem<128, true>::RAW_STAGES + ChunkSmem<128, true>::V_STAGES + 1 < SCALES,
+static_assert(ChunkSmem<64, true>::RAW_STAGES + ChunkSmem<64, true>::V_STAGES + 1 < SCALES && ChunkSmem<128, true>::RAW_STAGES + ChunkSmem<128, true>::V_STAGES + 1 < SCALES,
               "rings of the 8-bit cache");
 
 // A unit that more than one share holds, noted by the CTA of its second share
@@ -831,9 +832,8 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
   };
   // tile X: score buffer u at [X*128 + u*64, +64) with P over its first 32 columns; O at [256 + X*128, +DH)
 
-  // (8-bit cache: 96 registers a thread at launch, 61440 in all, go to 128 x 64 here, 256 x 144 to the softmax, 256 x 64 to the conversion)
   if (warp < 4) {
-    if constexpr (BITS8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if constexpr (BITS8) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
   }
   if (warp == 0) {
     // ------------------------------ K and V, or their codes ------------------------------
@@ -1095,7 +1095,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     }
   } else if (warp < 12) {
     // ------------------------------ softmax of tile x, and its rows of the outputs ------------------------------
-    if constexpr (BITS8) asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    if constexpr (BITS8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
     const int x = (warp - 4) >> 2, quarter = warp & 3;
     // the warp's first row of a piece, at its TMEM lanes (below 0: none)
     auto first_row = [&](const Piece* of) { return quarter * 32 - (of->duo == 2 && x == 1 ? TILE / 2 : 0); };
@@ -1236,12 +1236,14 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
         float alpha = 1.f;
         unsigned long long seen = ~0ull;
         if (any) {
+          float4 kp, vp, ve;
+          if constexpr (BITS8) {
+            const Scales& of = s_scales[(at + i) % SCALES];
+            kp = of.k, vp = of.v, ve = of.e;
+          }
           uint32_t sv[STEP];
           tmem_ld_x32(tm_su, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
           tmem_ld_x32(tm_su + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-          const Scales& of = s_scales[BITS8 ? (at + i) % SCALES : 0];
-          float4 kp, ve;
-          if constexpr (BITS8) kp = of.k, ve = of.e;      // (on their way beside the scores)
           tmem_ld_wait();
           if (i < clear.x || i >= clear.y) {
             const int key0 = piece->block(i) * STEP;
@@ -1261,7 +1263,6 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
             // A score is its product times K's power, a weight of V the probability times V's: 2^(s + e), in f16, relative to
             // o_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
             // weight has 11 bits unless it is below 2^-21 of the largest.
-            const float4 vp = of.v;
             // (not zero: a masked score is -infinity times this)
             const float cg[4] = {fmaxf(c_row * kp.x, 1.1754944e-38f), fmaxf(c_row * kp.y, 1.1754944e-38f), fmaxf(c_row * kp.z, 1.1754944e-38f), fmaxf(c_row * kp.w, 1.1754944e-38f)};
 #pragma unroll
@@ -1530,16 +1531,16 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       piece = next;
     }
   } else if constexpr (BITS8) {
-    // ------------------------------ V's codes to f16, every other step each four warps ------------------------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // ------------------------------ V's codes to f16 ------------------------------
+    // (by eight warps, two groups in turn, which leave the softmax 144 registers a thread, not 192: drafts 240 us instead of 229, prompts 1108 and 1058)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     constexpr int CODES = DH / 16;                       // 16-byte pieces of a row of codes
     constexpr int PASSES = STEP * CODES / 128;           // of the four warps; each 128 / CODES rows
-    const uint32_t group = (warp - 12) >> 2;
     const int tid = threadIdx.x & 127, col = tid % CODES, flip = (col >> 2) & 1;
     while (const Piece* const piece = piece_at(it)) {
       const int n = uniform(piece->n);
       const int2 clear = uniform(piece->clear);
-      for (int i = int((group ^ at) & 1); i < n && ok; i += 2) {
+      for (int i = 0; i < n && ok; ++i) {
         const uint32_t j = at + i, s = j % VS, rs = j % RS;
         if (!warp_wait(&raw_full[rs], (j / RS) & 1, err) || !warp_wait(&v_empty[s], ((j / VS) & 1) ^ 1, err)) { ok = false; break; }
         uint4 codes[PASSES];
@@ -1805,12 +1806,12 @@ cudaError_t launch_chunk(const ChunkParams<MANY_CHUNK_GROUPS>& all, int shares, 
   static_cast<ChunkSizes&>(p) = all;
   std::copy(all.grp, all.grp + NG, p.grp);
   cudaError_t e = allow_smem<chunk_kernel<DH, BITS8, NG>>(L::TOTAL);
-  if (BITS8 && e == cudaSuccess) {     // the kernel hands registers from warp to warp: 96 a thread at launch, or it would wait for good
+  if (BITS8 && e == cudaSuccess) {     // the kernel hands registers from warp to warp: without as many at launch it would wait for good
     static const int regs = [] {
       cudaFuncAttributes at;
       return cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(chunk_kernel<DH, BITS8, NG>)) == cudaSuccess ? at.numRegs : 0;
     }();
-    if (regs != 96) return cudaErrorInvalidConfiguration;
+    if (regs != L::LAUNCH_REGS) return cudaErrorInvalidConfiguration;
   }
   if (e == cudaSuccess) e = launch_kernel(chunk_kernel<DH, BITS8, NG>, shares, L::THREADS, L::TOTAL, stream, 1, p);
   if (e == cudaSuccess && shares > 1) e = launch_kernel(chunk_merge_kernel<DH, NG>, dim3(shares, MERGE_PARTS), MERGE_THREADS, 0, stream, 1, p);
