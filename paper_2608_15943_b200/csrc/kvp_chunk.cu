@@ -109,8 +109,7 @@ struct ChunkSizes {
   float* part_ml;                          // [2 * shares][256][2]
   int B, T, Hq, Hkv, G, page_size, max_pages, n_pages;
   int n_groups;
-  int members[MANY_CHUNK_GROUPS];
-  int kind[MANY_CHUNK_GROUPS];             // groups of as many members have the same list: its number
+  int kind[MANY_CHUNK_GROUPS];             // groups of as many layers have the same list: its number
   int n_kinds;
   Rows rows[CHUNK_MEMBERS], heads;         // of each list; G, the query heads of a KV head, the same way
   int window, sinks;                       // window 0: none
@@ -1958,7 +1957,6 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
       if (rc == KVP_OK) rc = make_tensor_map(&grp.map_v, v_cache[own], bits8 ? 1 : 2, 2, dims, strides, box, bits8 ? SWIZZLE_0 : SWIZZLE_128);
       if (rc != KVP_OK) return rc;
       const int g = p.n_groups++;
-      p.members[g] = n;
       int kind = 0;
       while (kind < p.n_kinds && p.rows[kind].n != n * p.G) ++kind;
       if (kind == p.n_kinds) p.rows[p.n_kinds++] = rows_of_token(n * p.G);
