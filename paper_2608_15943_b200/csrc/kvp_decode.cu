@@ -76,7 +76,7 @@ __device__ __forceinline__ uint32_t ring_off(int row, int chunk) {
   return uint32_t(row) * (DH * 2) + (uint32_t(chunk ^ (row & 7)) << 4);
 }
 
-// WINDOW: some positions of a sequence are not seen (p.seen).
+// WINDOW: some positions of a sequence are not seen (p.seen), and a number outside the pool stands for a page of zeros.
 template <int DH, int NG, bool WINDOW>
 __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kernel(const __grid_constant__ DecParams<NG> p) {
   constexpr int ROW_BYTES = DH * 2;
@@ -239,9 +239,11 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
   const int32_t* bt = nullptr;                     // block-table entry of the page the next granule is in,
   int in_page = 0, f_tok = 0;                      // its place there, and its first token
   size_t page_elem = 0;                            // offset of this KV head's block of that page
+  bool is_page = true;                             // (WINDOW) it is one of the pool
   int stage_in = 0;
   auto enter_page = [&]() {
-    const int page = min(max(*bt, 0), p.n_pages - 1);
+    const int entry = *bt, page = min(max(entry, 0), p.n_pages - 1);
+    is_page = !WINDOW || entry == page;
     page_elem = (size_t(page) * p.Hkv + f.hk) * p.page_size;
   };
   auto enter_piece = [&]() {
@@ -266,16 +268,21 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
       const uint8_t* ksrc = kbase + at;
       const uint8_t* vsrc = vbase + at;
       const uint32_t dst = ring_u32 + stage_in * STAGE_BYTES;
+      if (!is_page) {                             // (apart: with the test in every copy, 32 sequences of 16K-32K under a window take 553 us, not 520)
+#pragma unroll 1
+        for (int i = lane; i < STAGE_BYTES / 16; i += 32) cp_async16(dst + i * 16, kbase, 0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < CP_PER_LANE; ++i) {
-        const int idx = i * 32 + lane;          // 16-byte chunk index inside the contiguous granule
-        const int row = idx / CHUNKS, chunk = idx % CHUNKS;
-        const uint32_t off = ring_off<DH>(row, chunk);
-        // Slots at or past the sequence length were never appended and may hold anything (a NaN there would
-        // survive the zero probability in P V): they are filled with zeros instead of being read.
-        const uint32_t nbytes = f.sees(f_tok + row) ? 16u : 0u;
-        cp_async16(dst + off, ksrc + size_t(idx) * 16, nbytes);
-        cp_async16(dst + TILE_BYTES + off, vsrc + size_t(idx) * 16, nbytes);
+        for (int i = 0; i < CP_PER_LANE; ++i) {
+          const int idx = i * 32 + lane;          // 16-byte chunk index inside the contiguous granule
+          const int row = idx / CHUNKS, chunk = idx % CHUNKS;
+          const uint32_t off = ring_off<DH>(row, chunk);
+          // Slots at or past the sequence length were never appended and may hold anything (a NaN there would
+          // survive the zero probability in P V): they are filled with zeros instead of being read.
+          const uint32_t nbytes = f.sees(f_tok + row) ? 16u : 0u;
+          cp_async16(dst + off, ksrc + size_t(idx) * 16, nbytes);
+          cp_async16(dst + TILE_BYTES + off, vsrc + size_t(idx) * 16, nbytes);
+        }
       }
       if (++stage_in == STAGES) stage_in = 0;
       f_left -= DEC_WARPS;

@@ -158,7 +158,7 @@ __device__ __forceinline__ uint32_t v_off(int row, int chunk) {
   return uint32_t(row >> 1) * 128 + (uint32_t((row & 1) << 2 | (chunk ^ (row >> 1 & 3))) << 4);
 }
 
-// WINDOW: some positions of a sequence are not seen (p.seen).
+// WINDOW: some positions of a sequence are not seen (p.seen), and a number outside the pool stands for a page of zeros.
 template <int DH, int NB, int NG, bool WINDOW>
 __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(const __grid_constant__ Dec8Params<NG> p) {
   constexpr int GRAN_BYTES = GRAN * DH, TILE_BYTES = 2 * GRAN_BYTES, SLOTS = D8_SLOTS<DH, NB>, DEPTH = SLOTS / 2;
@@ -424,6 +424,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   int f_at = 0;                                    // (WINDOW) its first token
   int page = 0;                                    // that entry, looked at when its step is asked for: a load ahead of it
   int slot_in = 0, slot_out = 0;                   // in pairs: K's tile and V's behind it
+  auto is_page = [&](int page) { return !WINDOW || unsigned(page) < unsigned(p.n_pages); };
   auto block_of = [&](int page) { return (size_t(min(max(page, 0), p.n_pages - 1)) * p.Hkv + f.hk) * gran_per_page; };
   auto enter_piece = [&]() {
     const int n = min(f_todo, f.ng - f.gran);
@@ -447,8 +448,9 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   int v_live = -1;
   int v_at = 0;                                    // (WINDOW) its first token, and the tokens that are not seen
   int2 v_hole = make_int2(0, 0);
+  bool v_there0 = true, v_there1 = true;           // (WINDOW) the granules' pages are of the pool
   // the tile of a step: 32 rows in a run from src0, or (split) 16 from either
-  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool split, bool is_v, int at, int2 hole) {
+  auto copy_tile = [&](uint32_t dst, const uint8_t* src0, const uint8_t* src1, int live, bool split, bool is_v, int at, int2 hole, bool there0, bool there1) {
     if (!split) {
 #pragma unroll
       for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
@@ -460,7 +462,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       for (int i = 0; i < 2 * CP_PER_LANE; ++i) {
         const int idx = i * 32 + lane, row = idx / CHUNKS, chunk = idx % CHUNKS;
         cp_async16(dst + (is_v ? v_off<DH>(row, chunk) : k_off<DH>(row, chunk)), (i < CP_PER_LANE ? src0 : src1) + i % CP_PER_LANE * 512,
-                   row < live && !(WINDOW && at + row >= hole.x && at + row < hole.y) ? 16u : 0u);
+                   row < live && (i < CP_PER_LANE ? there0 : there1) && !(WINDOW && at + row >= hole.x && at + row < hole.y) ? 16u : 0u);
       }
     }
   };
@@ -475,11 +477,17 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
       const size_t block0 = block_of(page) + in_page;
       const bool in_a_row = in_page + 1 < gran_per_page;
       size_t block1 = block0 + 1;
-      if (!in_a_row || f_live <= GRAN) block1 = f_live > GRAN ? block_of(bt[1]) : block0;
-      scale = (lane & 1 ? f_grp->v_scale : f_grp->k_scale)[lane & 2 ? block1 : block0];
+      v_there0 = v_there1 = is_page(page);
+      if (!in_a_row || f_live <= GRAN) {
+        const int page1 = f_live > GRAN ? bt[1] : page;
+        block1 = f_live > GRAN ? block_of(page1) : block0;
+        v_there1 = is_page(page1);
+      }
+      scale = 0;                                   // (no page: the smallest powers, so that a zero of V raises no reference)
+      if (lane & 2 ? v_there1 : v_there0) scale = (lane & 1 ? f_grp->v_scale : f_grp->k_scale)[lane & 2 ? block1 : block0];
       const size_t at0 = block0 * GRAN_BYTES + lane * 16, at1 = block1 * GRAN_BYTES + lane * 16;
-      v_split = !in_a_row || f_live < STEP || f.meets(f_at, STEP);
-      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, v_split, false, f_at, f.hole);
+      v_split = !in_a_row || f_live < STEP || !v_there0 || f.meets(f_at, STEP);
+      copy_tile(ring + slot_in * 2 * TILE_BYTES, f_grp->k_cache + at0, f_grp->k_cache + at1, f_live, v_split, false, f_at, f.hole, v_there0, v_there1);
       v_src0 = f_grp->v_cache + at0;
       v_src1 = f_grp->v_cache + at1;
       v_live = max(f_live, 0);
@@ -501,7 +509,7 @@ __global__ void __launch_bounds__(D8_THREADS, D8_CTAS<DH, NB>) decode8_kernel(co
   };
   auto issue_v = [&]() {
     if (v_live >= 0) {
-      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, v_split, true, v_at, v_hole);
+      copy_tile(ring + (slot_in * 2 + 1) * TILE_BYTES, v_src0, v_src1, v_live, v_split, true, v_at, v_hole, v_there0, v_there1);
       if (++slot_in == DEPTH) slot_in = 0;
     }
     cp_async_commit();

@@ -29,7 +29,8 @@ struct DecSizes {
   int num_splits;              // > 0: the caller's split count instead; a block is one (unit, split)
   int io_f32;                  // queries are read and outputs written as fp32 (rounded to bf16 on load / widened on store)
   float scale_log2;
-  const int4* seen;            // [B], or null: under a window, the positions x <= j < y of the (shortened) sequence are not seen, and z: it has a row
+  const int4* seen;            // [B], or null: under a window, the positions x <= j < y of the (shortened) sequence are not seen, and z: it has a row;
+                               // with it a number outside the pool stands for a page of zeros (without: it is taken as the nearest that is one)
 };
 
 __device__ __forceinline__ int clamp_length(const DecSizes& p, int len) { return min(max(len, 1), p.max_pages * p.page_size); }
