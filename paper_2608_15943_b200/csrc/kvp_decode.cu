@@ -504,7 +504,8 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
         if (row < R && (!WINDOW || p.seen[here.b].z != 0)) {
           const int mem = row / G;
           const size_t head = size_t(here.b) * p.Hq + here.hk * G + row % G;
-          const float inv = 1.f / l_run[h];
+          const bool none = WINDOW && l_run[h] == 0.f;    // (scores that are all -infinity)
+          const float inv = none ? 0.f : 1.f / l_run[h];
 #pragma unroll
           for (int n = 0; n < NBLK; ++n) {
             const uint32_t v = pack_bf16(oacc[n][2 * h] * inv, oacc[n][2 * h + 1] * inv);   // rounded to bf16 either way: one set of results
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
             else
               *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(grp.o[mem]) + at) = v;
           }
-          if (t == 0) grp.lse[mem][head] = log_sum(m_run[h], l_run[h]);
+          if (t == 0) grp.lse[mem][head] = none ? -INFINITY : log_sum(m_run[h], l_run[h]);
         }
       }
     } else {

@@ -109,7 +109,8 @@ struct EvenDeal : Dealt {
 // `wpr` of them share a row of a unit (one where a unit has few pieces, eight where it has many), each lane four
 // columns.  Bound: latency; the pieces are in L2.
 constexpr int COMBINE_THREADS = 256;
-// EMPTY: there may be units without a token, whose pieces have no sum: output 0, LSE -infinity.
+// EMPTY: there may be units without a token, whose pieces have no sum: output 0, LSE -infinity.  (With p.seen any cache's rows may have
+// none: all of a row's scores are -infinity.)
 template <int DH, bool EMPTY, typename Params, typename Deal = EvenDeal<DH>>
 __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const __grid_constant__ Params p, int wpr) {
   constexpr int LANES = DH / 4;               // lanes per piece and row
@@ -221,14 +222,15 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
   if (row < R && lane < LANES) {
     const int mem = row / G;
     const size_t head = size_t(b) * p.Hq + hk * G + row % G;
-    const float inv = EMPTY && l == 0.f ? 0.f : 1.f / l;
+    const bool none = (EMPTY || p.seen != nullptr) && l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
     const uint2 v = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));   // rounded to bf16 either way
     if (p.io_f32)
       *reinterpret_cast<float4*>(reinterpret_cast<float*>(grp.o[mem]) + head * DH + col) =
           make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
     else
       *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(grp.o[mem]) + head * DH + col) = v;
-    if (lane == 0) grp.lse[mem][head] = EMPTY && l == 0.f ? -INFINITY : log_sum(m, l);
+    if (lane == 0) grp.lse[mem][head] = none ? -INFINITY : log_sum(m, l);
   }
 }
 
