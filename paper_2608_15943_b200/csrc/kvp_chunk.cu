@@ -860,7 +860,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       auto boxes_of = [&](int page) -> uint32_t { return __ballot_sync(0xffffffffu, page != -1 && sub % per_box == 0); };
       auto scales_of = [&](int batch, int page) -> uint32_t {  // K's and V's
         const int i = batch * BATCH + (lane >> 2);
-        if (!BITS8 || i >= n || page < 0) return 0x7f7f;
+        if (!BITS8 || i >= n || page < 0) return 0x7f;         // (V's the smallest: the zeros of a missing page raise no reference of the weights)
         const size_t block = (size_t(page) * p.Hkv + hk) * (p.page_size / CACHE_BLOCK) + (piece->block(i) * STEP + sub * 16) % p.page_size / CACHE_BLOCK;
         return grp.k_scale[block] | uint32_t(grp.v_scale[block]) << 8;
       };

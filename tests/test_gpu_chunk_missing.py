@@ -45,3 +45,17 @@ def test_rows_of_a_chunk(kvp, bits):
     c = Case(kvp, [0, 0, 2], [300, 90, 1000], [70, 90, 3], 4, 2, 64, 16, bits, freed=False)
     take_out(c, [(0, 0), (0, 15), (0, 18), (1, 0), (1, 1), (2, 5), (2, 62)] + [(2, i) for i in range(20, 50)])
     c.check(*c.run())
+
+
+@pytest.mark.parametrize("one_each", [True, False])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("power", [-100, -40, 0, 60])
+def test_small_scales_beside_a_missing_page(kvp, power, dh, one_each):
+    """The zeros of a missing page take no bits from values of any size: V's scales around 2^power in the 8-bit cache."""
+    lens = [90, 300, 7000]
+    c = Case(kvp, [0, 0], lens, [1] * 3 if one_each else [1, 80, 3], 4, 2, dh, 32, 8, one_each=one_each, freed=False)
+    g = torch.Generator().manual_seed(11)
+    for x in c.scales[1]:
+        x.copy_(torch.randint(127 + power, 130 + power, x.shape, generator=g, dtype=torch.uint8))
+    take_out(c, [(0, 0), (1, 2), (1, 9)] + [(2, i) for i in range(0, 219, 4)])
+    c.check(*c.run())
