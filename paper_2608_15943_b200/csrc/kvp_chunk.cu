@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "kvp_cache8.cuh"
+#include "kvp_chunk_rows.h"
 #include "kvp_decode_list.cuh"
 #include "kvp_host.h"
 #include "kvp_sm100.cuh"
@@ -40,7 +41,7 @@
 namespace kvp {
 namespace {
 
-constexpr int TILE = 128;                 // query rows of a tile (TMEM lanes)
+constexpr int TILE = CHUNK_TILE;          // query rows of a tile (TMEM lanes)
 constexpr int STEP = 64;                  // keys per step
 constexpr int BATCH = 8;                  // steps whose pages the producer's lanes hold: four blocks of 16 keys a step
 constexpr int CHUNK_MEMBERS = 8;          // layers of a donor group in one tile
@@ -92,14 +93,6 @@ struct Merge {
   int g, hk, b, pair;
   int w0, w1;                              // its shares (w0 < 0: nothing to merge)
   int pad[2];
-};
-
-// Rows of a token, and what divides by them: row / n is the upper word of 2 row * mul, shifted (mul: 2^(31 + shift) / n rounded up, n <=
-// 2^shift; exact below 2^31).  The set-up of every call walks through some dozen such quotients ahead of its first load.
-struct Rows {
-  int n, shift;
-  uint32_t mul;
-  __device__ __forceinline__ int token(int row) const { return int(__umulhi(uint32_t(row) * 2, mul) >> shift); }
 };
 
 struct ChunkSizes {
@@ -163,7 +156,7 @@ struct Walked {
   int sink_blocks, from;                 // blocks of first tokens, then blocks from `from` on
   int n, n_a;                            // steps, and those of tile A
 };
-__device__ __forceinline__ int pairs_of(const Span& s, const Rows& R) { return (s.n * R.n + 2 * TILE - 1) / (2 * TILE); }
+__device__ __forceinline__ int pairs_of(const Span& s, const Rows& R) { return units_of_rows(s.n * R.n); }
 __device__ __forceinline__ Walked walked(const ChunkSizes& p, const Span& s, const Rows& R, int pair) {
   Walked w;
   const int row0 = pair * 2 * TILE;
@@ -448,7 +441,7 @@ __device__ __forceinline__ Share find_share(const ChunkSizes& p, const Sums& s, 
       break;
     }
     out.off = int(at);
-    out.left = int(size);
+    out.left = int(size);                  // (2^31 steps of a CTA would take most of an hour)
     // the unit goes on from an earlier share: the first that begins inside it notes it
     const int steps = walked(p, span, R, out.pair).n;
     if (out.off > 0 && out.off < steps) {
@@ -1725,12 +1718,6 @@ int shares_at_most(const kvp_decode_desc* d, int n_groups, int T) {
   return int(std::max(1ll, std::min((long long)sm_count(), most / LEAST_SHARE)));
 }
 
-Rows rows_of_token(int n) {
-  Rows r{n, 0, 0};
-  while (1 << r.shift < n) ++r.shift;
-  r.mul = uint32_t(((uint64_t(1) << (31 + r.shift)) + n - 1) / n);
-  return r;
-}
 int check_chunk(const kvp_decode_desc* d) {
   int rc = d == nullptr ? KVP_ERR_INVALID_ARG : KVP_OK;
   if (rc != KVP_OK) return rc;
@@ -1863,7 +1850,7 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
     return KVP_ERR_INVALID_ARG;
   for (int l = 0; l < d->L; ++l)
     if (donor[l] < 0 || donor[l] > l || donor[donor[l]] != donor[l]) return KVP_ERR_BAD_DONOR;
-  if (T >= 1 << 24) return KVP_ERR_UNSUPPORTED;      // rows, a tile's at most for a token, are counted in 31 bits
+  if (T > CHUNK_MOST_TOKENS) return KVP_ERR_UNSUPPORTED;
   if (T == 0) return KVP_OK;           // (tensors without rows have no memory)
   const bool bits8 = k_scale != nullptr;
   for (int l = layer_begin; l < layer_end; ++l) {     // all of them before anything is launched
