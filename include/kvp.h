@@ -362,7 +362,7 @@ int kvp_decode8(const kvp_decode_desc* d, const int32_t* donor, float scale, con
  * scale == 0 means 1/sqrt(dh); it is not negative.  KVP_F32 queries are rounded to bf16; infinities and NaN in a row of them reach the
  * outputs of that row alone.  P is rounded to bf16 for the second product, and over the 8-bit cache to 11 bits (f16; below 2^-21 of a row's
  * largest weight, P times V's scale, to 2^-32 of it).  The 8-bit cache's numbers and scales are taken as they are; in the scores with
- * them, a query element of less than 2^-16 of its row's largest may be off by 2^-25 of that.  Sums are fp32: |V| is to stay below 2^100.
+ * them, a query element of less than 2^-13 of its row's largest may be off by 2^-21 of that.  Sums are fp32: |V| is to stay below 2^100.
  * A row whose scores are all -infinity has output 0 and LSE -infinity.
  * A call cuts the work by the lengths of the whole batch: equal calls give equal bits, and a sequence's last bits (fp32 summation
  * order) depend on the other sequences and the layer range.  dtype and the rest of d as for kvp_decode, num_splits is not read;
