@@ -395,11 +395,14 @@ int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, int32_t T, co
  *   kvp_pages_resize   row b has length new_lengths[b] (DEVICE int32 [B]) from now on.  A row that grows gets pages; a row that shrinks
  *                      gives up those behind its new length.  A row that grows inside a partly filled page with refs > 1 gets a
  *                      copy of it, so that an append changes no other row's tokens; only if all who hold the page grow, the lowest
- *                      of them keeps it.  New pages go to the rows in order, a copy's before those behind it.
+ *                      of them keeps it.  New pages go to the rows in order, a copy's before those behind it.  A row that grows
+ *                      inside a place without a page (kvp_pages_trim freed it before the row shrank into it) gets one there; the slots
+ *                      in front of its new tokens may hold anything.
  *                      lacking: DEVICE int32 [1], 0; or the number of pages that are lacking, or -1 where a new length is outside
  *                      [0, max_pages*page_size]: then nothing is changed.
  *   kvp_pages_trim     frees the pages that no token from position lengths[b] on sees, with window >= 1 and sinks as in
- *                      kvp_attn_chunk: those whose tokens are all below lengths[b] - window + 1 and at or above sinks.
+ *                      kvp_attn_chunk: those whose tokens are all below lengths[b] - window + 1 and at or above sinks.  (Tokens
+ *                      are gone with them for good, for a row that shrinks afterwards too.)
  *   kvp_pages_compact  moves the used pages with the highest numbers, in order, into the free ones below the number of used pages,
  *                      and renames them in the table, so that pages 0 .. used-1 are the used ones.  used: DEVICE int32 [1]. */
 size_t kvp_pages_workspace_bytes(const kvp_decode_desc* d);

@@ -50,16 +50,18 @@ class Book:
         if any(not 0 <= n <= self.max_pages * self.page for n in to):
             return -1
         free = [p for p in range(self.n_pages) if self.refs[p] == 0]
-        grows_in = []
+        grows_in, gaps = [], []                           # the page that a row grows in; whether there is none in that place
         for b, n in enumerate(self.lengths):
-            p = self.table[b][self.places(n) - 1] if n % self.page and to[b] > n else -1
+            inside = n % self.page and to[b] > n
+            p = self.table[b][self.places(n) - 1] if inside else -1
             grows_in.append(p if 0 <= p < self.n_pages else -1)
+            gaps.append(bool(inside) and grows_in[b] < 0)
         takes = []
         for b, p in enumerate(grows_in):
             growing = [c for c, q in enumerate(grows_in) if q == p]
             keeps = len(growing) == self.refs[p] and growing[0] == b
             takes.append(p >= 0 and self.refs[p] > 1 and not keeps)
-        need = sum(takes) + sum(max(0, self.places(m) - self.places(n)) for n, m in zip(self.lengths, to))
+        need = sum(takes) + sum(gaps) + sum(max(0, self.places(m) - self.places(n)) for n, m in zip(self.lengths, to))
         if need > len(free):
             return need - len(free)
         was = list(self.content)
@@ -70,7 +72,7 @@ class Book:
                 self.content[p], self.refs[p] = was[grows_in[b]], 1
                 self.refs[grows_in[b]] -= 1
                 self.table[b][had - 1] = p
-            for i in range(had, have):
+            for i in range(had - gaps[b], have):
                 p = free.pop(0)
                 self.refs[p], self.table[b][i] = 1, p
             for i in range(have, had):

@@ -154,17 +154,23 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) fork_kernel(const __grid_cons
 // ---------------------------------------------------------------------------------------------
 // resize: rows grow (a page that is shared is copied first) and shrink
 // ---------------------------------------------------------------------------------------------
+constexpr int STAYS = -1, GAP = -2;   // of a row, in the place of the page that it grows in: it does not grow in one; it grows in a place without
+                                      // one (freed behind a window before the row shrank into it), and gets one there
 struct Resized {            // one row, from the state before the call
   int had, have;            // places
-  int end;                  // page that the row grows in, or -1
+  int end;                  // page that the row grows in, or one of the above
 };
+__device__ __forceinline__ int grows_in(const Book& p, int row, int length, int longer, int had) {
+  if (longer <= length || length <= 0 || length % p.page_size == 0 || had <= 0) return STAYS;
+  const int page = p.at(row, had - 1);
+  return p.is_page(page) ? page : GAP;
+}
 __device__ __forceinline__ Resized resized(const Book& p, const int32_t* to, int row) {
   const int length = p.lengths[row], longer = to[row];
   Resized r;
   r.had = p.places(length);
   r.have = p.places(longer);
-  r.end = longer > length && length > 0 && length % p.page_size != 0 && r.had > 0 ? p.at(row, r.had - 1) : -1;
-  if (!p.is_page(r.end)) r.end = -1;
+  r.end = grows_in(p, row, length, longer, r.had);
   return r;
 }
 __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_kernel(const __grid_constant__ Book p, const __grid_constant__ BookSpace ws, const int32_t* to, int32_t* lacking) {
@@ -201,7 +207,7 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_kernel(const __grid_co
         copies = growing != held || lowest != row;
       }
     }
-    ws.rows[row] = max(0, r.have - r.had);
+    ws.rows[row] = max(0, r.have - r.had) + (r.end == GAP);
     ws.rows[p.B + row] = copies;
   }
   const Slice slice(p.n_pages);
@@ -244,13 +250,13 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_kernel(const __grid_co
       if ((long long)(s_begin[mid] & PAGES) <= k) lo = mid; else hi = mid - 1;
     }
     const int i = int(k - (long long)(s_begin[lo] & PAGES)), copies = int((s_begin[lo + 1] >> COPY_BIT) - (s_begin[lo] >> COPY_BIT));
-    const int had = p.places(p.lengths[lo]);
+    const int from = p.places(p.lengths[lo]) - copies - (s_end[lo] == GAP);       // place of its first
     if (i < copies) {
       const int at = int(s_begin[lo] >> COPY_BIT);
       ws.src[at] = s_end[lo];
       ws.dst[at] = page;
     }
-    p.at(lo, had + i - copies) = page;
+    p.at(lo, from + i) = page;
     p.refs[page] = 1;
   }
   cluster_sync_all();
@@ -323,12 +329,11 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_few_kernel(const __gri
     if (u < each && tid * each + u < p.n_pages && p.refs[tid * each + u] == 0) free |= 1u << u;
   const bool is_row = tid < p.B;
   const int length = is_row ? p.lengths[tid] : 0, longer = is_row ? to[tid] : 0, had = p.places(length), have = p.places(longer);
-  int end = is_row && longer > length && length > 0 && length % p.page_size != 0 && had > 0 ? p.at(tid, had - 1) : -1;
-  if (!p.is_page(end)) end = -1;
+  const int end = is_row ? grows_in(p, tid, length, longer, had) : STAYS;
   const int held = end >= 0 ? p.refs[end] : 0;
   s_had[tid] = had;
   s_have[tid] = have;
-  s_end[tid] = is_row ? end : -1;
+  s_end[tid] = end;
   const bool bad = __syncthreads_or(longer < 0 || longer > (long long)p.max_pages * p.page_size) != 0;
   bool copies = false;
   if (held > 1) {
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_few_kernel(const __gri
     copies = growing != held || lowest != tid;
   }
   // new pages, copies and free pages ahead of the thread's, 20 bits each (none is above FEW_PAGES * BOOK_THREADS)
-  const unsigned long long mine = (unsigned long long)(max(0, have - had) + copies) | (unsigned long long)copies << 20 | (unsigned long long)__popc(free) << 40;
+  const unsigned long long mine = (unsigned long long)(max(0, have - had) + copies + (end == GAP)) | (unsigned long long)copies << 20 | (unsigned long long)__popc(free) << 40;
   unsigned long long total;
   const unsigned long long ahead = block_scan(mine, s_warp, total);
   constexpr uint32_t LOW = (1u << 20) - 1;
@@ -371,7 +376,7 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_few_kernel(const __gri
       ws.src[s_copies[lo]] = s_end[lo];
       ws.dst[s_copies[lo]] = page;
     }
-    p.at(lo, s_had[lo] + i - its_copies) = page;
+    p.at(lo, s_had[lo] - its_copies - (s_end[lo] == GAP) + i) = page;
     p.refs[page] = 1;
   }
   if (copies) atomicSub(p.refs + end, 1);
