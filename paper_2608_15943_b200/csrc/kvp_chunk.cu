@@ -108,7 +108,7 @@ struct ChunkSizes {
   int window, sinks;                       // window 0: none
   int box;                                 // keys of a TMA box: 64, 32 or 16
   int io_f32;
-  float scale_log2;
+  float scale, scale_power;                // of the products, for powers of 2: the two together; 8 bits: the second is a power of two, the first 1 to 2
 };
 struct ChunkGroup {
   CUtensorMap map_k, map_v;
@@ -1093,7 +1093,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
     auto first_row = [&](const Piece* of) { return quarter * 32 - (of->duo == 2 && x == 1 ? TILE / 2 : 0); };
     const uint32_t lane_sel = uint32_t(quarter * 32) << 16;
     const uint32_t tm_s = tmem_base + x * 128 + lane_sel, tm_o = tmem_base + 256 + x * 128 + lane_sel;
-    float c_next = p.scale_log2;         // factor of the scores (8 bits: with what the thread's row has been multiplied by taken back)
+    float c_next = 1.f;                  // 8 bits: a power of two, which takes back what the thread's row has been multiplied by
     uint32_t done = 0, n_done = 0, n_duo = 0;       // steps of earlier pieces in which this tile took part; those pieces; duos
     // The warp's query rows of a piece go to their places: every product with the last one's has been seen to complete.  Four lanes a row,
     // and four rows one after the other: a row a lane, its 16-byte parts were as many lines each (3200 cycles a piece, and its output
@@ -1157,7 +1157,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
           const int up = min(max(7 + 127 - int(__float_as_uint(most) >> 23), -120), 120);
           const float power = __uint_as_float(uint32_t(up + 127) << 23);
-          if (t == j) c_next = p.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
+          if (t == j) c_next = p.scale_power * __uint_as_float(uint32_t(127 - up) << 23);
           {
 #pragma unroll
             for (int c = 0; c < DH / 64; ++c) {
@@ -1216,8 +1216,11 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       const int2 pair_clear = uniform(piece->clear), clear = uniform(piece->clear_x[x]);
       const int n_x = uniform(piece->n_x[x]);
       const float c_row = c_next;
-      float m_used = -INFINITY;          // running maximum (log2 domain) that the exponentials are taken against
-      float o_used = -INFINITY;          // 8 bits: what O is in units of (log2, V's power with it)
+      // Running maximum of the products that the exponentials are taken against.  A product's difference to it is formed first and scaled
+      // then: that of the largest is 0, of whatever size it is.  (Scaled and subtracted in one operation, the largest of 2^34 comes out up to
+      // 2^10 above or below the rounded maximum.)
+      float m_used = -INFINITY;
+      float d_used = -INFINITY;          // 8 bits: what O is in units of, relative to the maximum (log2; of the size of V's powers)
       uint64_t l2 = 0ull, l2b = 0ull;
       for (int k = 0; k < n_x; ++k) {
         const int i = duo ? 2 * k + x : k;
@@ -1255,7 +1258,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
           float mp[4];
           if constexpr (BITS8) {
             // A score is its product times K's power, a weight of V the probability times V's: 2^(s + e), in f16, relative to
-            // o_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
+            // the maximum and d_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
             // weight has 11 bits unless it is below 2^-21 of the largest.
             // (not zero: a masked score is -infinity times this)
             const float cg[4] = {fmaxf(c_row * kp.x, 1.1754944e-38f), fmaxf(c_row * kp.y, 1.1754944e-38f), fmaxf(c_row * kp.z, 1.1754944e-38f), fmaxf(c_row * kp.w, 1.1754944e-38f)};
@@ -1268,29 +1271,30 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
 #pragma unroll
             for (int j = 0; j < 4; ++j) mp[j] *= cg[j];
             const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
-            const float o_step = fmaxf(fmaxf(mp[0] + ve.x, mp[1] + ve.y), fmaxf(mp[2] + ve.z, mp[3] + ve.w));
             if (k == 0) {
               m_used = m_step;
-              o_used = o_step - 7.f;
-            } else {
-              if (m_step > m_used + kRescaleBy) {
-                const float f = fast_exp2(m_used - m_step);
-                m_used = m_step;
-                l2 = fmul2(l2, pack_f2(f, f));
-                l2b = fmul2(l2b, pack_f2(f, f));
-              }
-              if (o_step > o_used + 15.f) {
-                alpha = fast_exp2(o_used - (o_step - 7.f));
-                o_used = o_step - 7.f;
-                rescale = true;
-              }
+            } else if ((m_step - m_used) * p.scale > kRescaleBy) {
+              const float rise = (m_step - m_used) * p.scale, f = fast_exp2(-rise);
+              m_used = m_step;
+              d_used -= rise;
+              l2 = fmul2(l2, pack_f2(f, f));
+              l2b = fmul2(l2b, pack_f2(f, f));
             }
             const bool none = m_used == -INFINITY;                    // (a row that has seen nothing yet: all terms are 0)
-            const float nm = none ? 0.f : -m_used, unit = none ? 0.f : fast_exp2(m_used - o_used);
+            const float nm = none ? 0.f : -m_used;
+            const float d_step = fmaxf(fmaxf(fmaf(mp[0] + nm, p.scale, ve.x), fmaf(mp[1] + nm, p.scale, ve.y)), fmaxf(fmaf(mp[2] + nm, p.scale, ve.z), fmaf(mp[3] + nm, p.scale, ve.w)));
+            if (k == 0) {
+              d_used = d_step - 7.f;
+            } else if (d_step > d_used + 15.f) {
+              alpha = fast_exp2(d_used - (d_step - 7.f));
+              d_used = d_step - 7.f;
+              rescale = true;
+            }
+            const float unit = none ? 0.f : fast_exp2(-d_used);
             // (finite: scales of blocks that the row does not see are of any size, and its probabilities there 0)
             constexpr float most = 3.4028235e38f;
             const float fg[4] = {fminf(unit * vp.x, most), fminf(unit * vp.y, most), fminf(unit * vp.z, most), fminf(unit * vp.w, most)};
-            const uint64_t nm2 = pack_f2(nm, nm);
+            const uint64_t nm2 = pack_f2(nm, nm), c2 = pack_f2(p.scale, p.scale);
 #pragma unroll
             for (int g = 0; g < STEP / 32; ++g) {
               uint32_t pk[16];
@@ -1298,7 +1302,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               for (int j = 0; j < 16; ++j) {
                 const int of16 = g * 2 + j / 8;
                 const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), pack_f2(cg[of16], cg[of16]), nm2);
-                const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
+                const uint64_t x2 = fmul2(e2, c2), e = pack_f2(fast_exp2(f2_lo(x2)), fast_exp2(f2_hi(x2)));
                 if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
                 const uint64_t w = fmul2(e, pack_f2(fg[of16], fg[of16]));
                 pk[j] = pack_f16(f2_lo(w), f2_hi(w));
@@ -1306,18 +1310,18 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               tmem_st_x16(tm_su + g * 16, pk);
             }
           } else {
-            const uint64_t c2 = pack_f2(c_row, c_row);
+            const uint64_t c2 = pack_f2(p.scale, p.scale);
 #pragma unroll
             for (int j = 0; j < 4; ++j) mp[j] = fmaxf(__uint_as_float(sv[2 * j]), __uint_as_float(sv[2 * j + 1]));
 #pragma unroll
             for (int g = 8; g < STEP; g += 8)
 #pragma unroll
               for (int j = 0; j < 4; ++j) mp[j] = fmax3(mp[j], __uint_as_float(sv[g + 2 * j]), __uint_as_float(sv[g + 2 * j + 1]));
-            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * c_row;
+            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
             if (k == 0) {
               m_used = m_step;
-            } else if (m_step > m_used + kRescaleBy) {
-              alpha = fast_exp2(m_used - m_step);
+            } else if ((m_step - m_used) * p.scale > kRescaleBy) {
+              alpha = fast_exp2((m_used - m_step) * p.scale);
               m_used = m_step;
               l2 = fmul2(l2, pack_f2(alpha, alpha));
               l2b = fmul2(l2b, pack_f2(alpha, alpha));
@@ -1330,7 +1334,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               uint32_t pk[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), c2, nm2);
+                const uint64_t e2 = fmul2(fadd2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), nm2), c2);
                 const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
                 if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
                 pk[j] = pack_bf16(f2_lo(e), f2_hi(e));
@@ -1373,14 +1377,14 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       const Piece* const next = piece_at(it + 1);
       if (!ok) break;
       if (next != nullptr && !apart) ask_q(next);
-      float m = m_used, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
+      float m = m_used * p.scale, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
       if (n_x > 0) {
         if (!warp_wait(&o_done[x], n_done & 1, err)) break;
         tc_fence_after_sync();
         ++n_done;
       }
       // (8 bits: O is in units of its own, and V in shared memory 2^-8 of its codes)
-      const float unit = !BITS8 ? 1.f : m == -INFINITY ? 0.f : fast_exp2(o_used - m + 8.f);
+      const float unit = !BITS8 ? 1.f : m == -INFINITY ? 0.f : fast_exp2(d_used + 8.f);
       float mine = unit, others = 0.f;
       // A duo's halves have the same rows, and each puts half of the columns together.  Maxima and sums are exchanged, and O read, by way
       // of TMEM (over a score buffer: the next piece has not begun); where the rows are at other lanes, by the room of the queries.
@@ -1910,7 +1914,13 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
   p.sinks = sinks;
   p.box = d->page_size % 64 == 0 ? 64 : d->page_size % 32 == 0 ? 32 : 16;
   p.io_f32 = d->dtype == KVP_F32;
-  p.scale_log2 = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
+  p.scale = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
+  p.scale_power = 1.f;
+  if (bits8) {
+    int e;
+    p.scale = 2.f * frexpf(p.scale, &e);
+    p.scale_power = ldexpf(1.f, e - 1);
+  }
   // Layers that share a donor, as many as fit a tile's rows for a token.  Those with most layers first.
   const int per = std::min(CHUNK_MEMBERS, TILE / p.G);
   p.n_groups = p.n_kinds = 0;
