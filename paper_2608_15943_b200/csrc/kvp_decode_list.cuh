@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
       }
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u) {
-        if (ml[u].x == -INFINITY) continue;   // an empty split
+        if (ml[u].y == 0.f) continue;         // an empty split (scores that are all NaN leave no maximum either, but a sum of NaN)
         const float mn = fmaxf(m, ml[u].x);
         const float fa = m == -INFINITY ? 0.f : fast_exp2(m - mn), fb = fast_exp2(ml[u].x - mn);
         acc.x = acc.x * fa + o[u].x * fb;
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(COMBINE_THREADS) decode_combine_kernel(const _
     }
   }
   auto merge = [&](float om, float ol, const float4& oo) {
-    if (om == -INFINITY) return;
+    if (ol == 0.f) return;
     const float mn = fmaxf(m, om);
     const float fa = m == -INFINITY ? 0.f : fast_exp2(m - mn), fb = fast_exp2(om - mn);
     acc.x = acc.x * fa + oo.x * fb;
