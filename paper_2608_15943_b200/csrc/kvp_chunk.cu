@@ -26,6 +26,7 @@
 // behind the sequence, freed pages before the window: anything may be there) are not read and are zeros in shared memory.  A
 // visible row of V with an infinity or NaN in it must reach the rows that see it and no other, which 0 * NaN in a matrix product
 // does not give: in blocks with any masking such rows are taken out, and the softmax threads add them to O by themselves.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -49,6 +50,11 @@ constexpr int MANY_CHUNK_GROUPS = 16, FEW_CHUNK_GROUPS = 4;
 constexpr uint32_t Q_HALF = TILE * 128;   // one [128 rows x 128 B] block of Q
 constexpr uint32_t KV_HALF = STEP * 128;
 constexpr float kRescaleBy = 8.0f;        // log2: O is rescaled when the maximum has moved by more
+// A product is scaled and the (rounded) maximum taken off in one operation, which is exact until its end: the largest score comes out as
+// what the maximum was rounded by, and from 2^31 on that is more than exponents hold.  So rows with a maximum beyond FAR, where scores are 1/2
+// and more apart, and off by more than that, are scaled by the power of two in the scale alone, of which the difference to the largest is
+// exact.  (Difference first and scaled then, for every row: prompts under a window 2220 -> 2270 us.  A branch for such rows: 2350.)
+constexpr float FAR = 8388608.f;
 // Places of the list behind the steps of a unit, for its start, its output and its merge, 8900 cycles where a step of two tiles takes 1800
 // (3: drafts and prompts under a window 1% slower; 8: short prompts 1%); least places of a share.
 constexpr int REST = 6, LEAST_SHARE = 8;
@@ -108,7 +114,7 @@ struct ChunkSizes {
   int window, sinks;                       // window 0: none
   int box;                                 // keys of a TMA box: 64, 32 or 16
   int io_f32;
-  float scale, scale_power;                // of the products, for powers of 2: the two together; 8 bits: the second is a power of two, the first 1 to 2
+  float scale, scale_power, scale_rest;    // of the products, for powers of 2: a power of two times 1 to 2
 };
 struct ChunkGroup {
   CUtensorMap map_k, map_v;
@@ -1216,11 +1222,19 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       const int2 pair_clear = uniform(piece->clear), clear = uniform(piece->clear_x[x]);
       const int n_x = uniform(piece->n_x[x]);
       const float c_row = c_next;
-      // Running maximum of the products that the exponentials are taken against.  A product's difference to it is formed first and scaled
-      // then: that of the largest is 0, of whatever size it is.  (Scaled and subtracted in one operation, the largest of 2^34 comes out up to
-      // 2^10 above or below the rounded maximum.)
-      float m_used = -INFINITY;
+      float m_used = -INFINITY;          // running maximum (log2 domain) that the exponentials are taken against,
+      float c_used = 0.f, nm = 0.f;      // the factor of the scores (8 bits: beside K's powers), what is added to them,
+      float limit = 0.f;                 // and how far above it a score moves it (log2)
       float d_used = -INFINITY;          // 8 bits: what O is in units of, relative to the maximum (log2; of the size of V's powers)
+      const float c_all = BITS8 ? p.scale_rest : p.scale, c_far = BITS8 ? 1.f : p.scale_power;
+      auto refer_to = [&](float largest) {                      // (8 bits: in units of powers of two)
+        const float c = fabsf(largest * c_all) > FAR ? c_far : c_all;
+        const bool none = largest == -INFINITY;                 // (a row that has seen nothing yet: all terms are 0)
+        m_used = largest * c_all;
+        c_used = BITS8 ? c_row * c : c;
+        nm = none ? 0.f : -(largest * c);
+        limit = none ? -FLT_MAX : kRescaleBy;
+      };
       uint64_t l2 = 0ull, l2b = 0ull;
       for (int k = 0; k < n_x; ++k) {
         const int i = duo ? 2 * k + x : k;
@@ -1260,29 +1274,37 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
             // A score is its product times K's power, a weight of V the probability times V's: 2^(s + e), in f16, relative to
             // the maximum and d_used, which rises (and O falls) where a weight would leave f16's upper range.  So scales cost no rounding, and a
             // weight has 11 bits unless it is below 2^-21 of the largest.
-            // (not zero: a masked score is -infinity times this)
-            const float cg[4] = {fmaxf(c_row * kp.x, 1.1754944e-38f), fmaxf(c_row * kp.y, 1.1754944e-38f), fmaxf(c_row * kp.z, 1.1754944e-38f), fmaxf(c_row * kp.w, 1.1754944e-38f)};
 #pragma unroll
             for (int j = 0; j < 4; ++j) mp[j] = fmaxf(__uint_as_float(sv[16 * j]), __uint_as_float(sv[16 * j + 1]));
 #pragma unroll
             for (int g = 2; g < 16; g += 2)
 #pragma unroll
               for (int j = 0; j < 4; ++j) mp[j] = fmax3(mp[j], __uint_as_float(sv[16 * j + g]), __uint_as_float(sv[16 * j + g + 1]));
+            const float k4[4] = {kp.x, kp.y, kp.z, kp.w};
+            float cg[4], x4[4];          // factors of the blocks' scores (not zero: a masked score is -infinity times this), their largest
+            auto scaled = [&]() {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mp[j] *= cg[j];
-            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
-            if (k == 0) {
-              m_used = m_step;
-            } else if ((m_step - m_used) * p.scale > kRescaleBy) {
-              const float rise = (m_step - m_used) * p.scale, f = fast_exp2(-rise);
-              m_used = m_step;
-              d_used -= rise;
-              l2 = fmul2(l2, pack_f2(f, f));
-              l2b = fmul2(l2b, pack_f2(f, f));
+              for (int j = 0; j < 4; ++j) {
+                cg[j] = fmaxf(c_used * k4[j], FLT_MIN);
+                x4[j] = fmaf(mp[j], cg[j], nm);
+              }
+              return fmaxf(fmaxf(x4[0], x4[1]), fmaxf(x4[2], x4[3]));
+            };
+            if (k == 0 || scaled() > limit) {
+              float largest = -INFINITY;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) largest = fmaxf(largest, mp[j] * fmaxf(c_row * k4[j], FLT_MIN));
+              const float m_before = m_used;
+              refer_to(largest);
+              scaled();
+              if (k > 0) {
+                const float rise = m_used - m_before, f = fast_exp2(-rise);
+                d_used -= rise;
+                l2 = fmul2(l2, pack_f2(f, f));
+                l2b = fmul2(l2b, pack_f2(f, f));
+              }
             }
-            const bool none = m_used == -INFINITY;                    // (a row that has seen nothing yet: all terms are 0)
-            const float nm = none ? 0.f : -m_used;
-            const float d_step = fmaxf(fmaxf(fmaf(mp[0] + nm, p.scale, ve.x), fmaf(mp[1] + nm, p.scale, ve.y)), fmaxf(fmaf(mp[2] + nm, p.scale, ve.z), fmaf(mp[3] + nm, p.scale, ve.w)));
+            const float d_step = fmaxf(fmaxf(x4[0] + ve.x, x4[1] + ve.y), fmaxf(x4[2] + ve.z, x4[3] + ve.w));
             if (k == 0) {
               d_used = d_step - 7.f;
             } else if (d_step > d_used + 15.f) {
@@ -1290,11 +1312,11 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               d_used = d_step - 7.f;
               rescale = true;
             }
-            const float unit = none ? 0.f : fast_exp2(-d_used);
+            const float unit = m_used == -INFINITY ? 0.f : fast_exp2(-d_used);
             // (finite: scales of blocks that the row does not see are of any size, and its probabilities there 0)
             constexpr float most = 3.4028235e38f;
             const float fg[4] = {fminf(unit * vp.x, most), fminf(unit * vp.y, most), fminf(unit * vp.z, most), fminf(unit * vp.w, most)};
-            const uint64_t nm2 = pack_f2(nm, nm), c2 = pack_f2(p.scale, p.scale);
+            const uint64_t nm2 = pack_f2(nm, nm);
 #pragma unroll
             for (int g = 0; g < STEP / 32; ++g) {
               uint32_t pk[16];
@@ -1302,7 +1324,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               for (int j = 0; j < 16; ++j) {
                 const int of16 = g * 2 + j / 8;
                 const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), pack_f2(cg[of16], cg[of16]), nm2);
-                const uint64_t x2 = fmul2(e2, c2), e = pack_f2(fast_exp2(f2_lo(x2)), fast_exp2(f2_hi(x2)));
+                const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
                 if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
                 const uint64_t w = fmul2(e, pack_f2(fg[of16], fg[of16]));
                 pk[j] = pack_f16(f2_lo(w), f2_hi(w));
@@ -1310,31 +1332,31 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
               tmem_st_x16(tm_su + g * 16, pk);
             }
           } else {
-            const uint64_t c2 = pack_f2(p.scale, p.scale);
 #pragma unroll
             for (int j = 0; j < 4; ++j) mp[j] = fmaxf(__uint_as_float(sv[2 * j]), __uint_as_float(sv[2 * j + 1]));
 #pragma unroll
             for (int g = 8; g < STEP; g += 8)
 #pragma unroll
               for (int j = 0; j < 4; ++j) mp[j] = fmax3(mp[j], __uint_as_float(sv[g + 2 * j]), __uint_as_float(sv[g + 2 * j + 1]));
-            const float m_step = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
+            const float largest = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3]));
             if (k == 0) {
-              m_used = m_step;
-            } else if ((m_step - m_used) * p.scale > kRescaleBy) {
-              alpha = fast_exp2((m_used - m_step) * p.scale);
-              m_used = m_step;
+              refer_to(largest);
+            } else if (fmaf(largest, c_used, nm) > limit) {
+              const float m_before = m_used;
+              refer_to(largest);
+              alpha = fast_exp2(m_before - m_used);
               l2 = fmul2(l2, pack_f2(alpha, alpha));
               l2b = fmul2(l2b, pack_f2(alpha, alpha));
               rescale = true;
             }
-            const float nm = m_used == -INFINITY ? 0.f : -m_used;     // (a row that has seen nothing yet: all terms are 0)
+            const uint64_t c2 = pack_f2(c_used, c_used);
             const uint64_t nm2 = pack_f2(nm, nm);
 #pragma unroll
             for (int g = 0; g < STEP / 32; ++g) {
               uint32_t pk[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                const uint64_t e2 = fmul2(fadd2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), nm2), c2);
+                const uint64_t e2 = ffma2(pack_f2(__uint_as_float(sv[g * 32 + 2 * j]), __uint_as_float(sv[g * 32 + 2 * j + 1])), c2, nm2);
                 const uint64_t e = pack_f2(fast_exp2(f2_lo(e2)), fast_exp2(f2_hi(e2)));
                 if (j & 1) l2b = fadd2(l2b, e); else l2 = fadd2(l2, e);
                 pk[j] = pack_bf16(f2_lo(e), f2_hi(e));
@@ -1377,7 +1399,7 @@ __global__ void __launch_bounds__(ChunkSmem<DH, BITS8>::THREADS, 1) chunk_kernel
       const Piece* const next = piece_at(it + 1);
       if (!ok) break;
       if (next != nullptr && !apart) ask_q(next);
-      float m = m_used * p.scale, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
+      float m = m_used, l = (f2_lo(l2) + f2_hi(l2)) + (f2_lo(l2b) + f2_hi(l2b));
       if (n_x > 0) {
         if (!warp_wait(&o_done[x], n_done & 1, err)) break;
         tc_fence_after_sync();
@@ -1915,12 +1937,9 @@ extern "C" int kvp_attn_chunk(const kvp_decode_desc* d, const int32_t* donor, in
   p.box = d->page_size % 64 == 0 ? 64 : d->page_size % 32 == 0 ? 32 : 16;
   p.io_f32 = d->dtype == KVP_F32;
   p.scale = (scale == 0.f ? 1.f / sqrtf(float(d->dh)) : scale) * 1.4426950408889634f;
-  p.scale_power = 1.f;
-  if (bits8) {
-    int e;
-    p.scale = 2.f * frexpf(p.scale, &e);
-    p.scale_power = ldexpf(1.f, e - 1);
-  }
+  int two_to;
+  p.scale_rest = 2.f * frexpf(p.scale, &two_to);
+  p.scale_power = ldexpf(1.f, two_to - 1);
   // Layers that share a donor, as many as fit a tile's rows for a token.  Those with most layers first.
   const int per = std::min(CHUNK_MEMBERS, TILE / p.G);
   p.n_groups = p.n_kinds = 0;
