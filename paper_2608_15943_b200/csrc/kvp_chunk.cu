@@ -15,10 +15,10 @@
 //                 it, take every other step each, and put their two sums together at the end.
 //   warps 12-15   (8-bit cache only) V's codes to f16, which holds them exactly.  K's are operands as they are; the scales are applied
 //                 to the scores and to the weights of V.
-// What bounds it.  Drafts (2-8 tokens of 16 sequences of 4K-16K, 16 to 64 rows a unit): memory in bf16, 226 us, 5.8 TB/s; over the
-// 8-bit cache, 245 us, the chain of a step (scores out of TMEM, maximum, exponentials and weights, P, product; some 3300 cycles for
-// every other step of each half), beside the conversion of V on the same schedulers.  Prompts: the 1000 W of the board (1.67 to 1.8 GHz; 1100
-// TFLOP/s over 64K tokens, 71% of a burst of 15.5 ms); ahead of it the exponentials (1024 of 1800 cycles a step of two tiles) and the
+// What bounds it.  Drafts (2-8 tokens of 16 sequences of 4K-16K, 16 to 64 rows a unit): memory in bf16, 228 us, 5.8 TB/s; over the
+// 8-bit cache, 243 us, the chain of a step (scores out of TMEM, maximum, exponentials and weights, P, product; some 2900 cycles for
+// every other step of each half), beside the conversion of V on the same schedulers.  Prompts: the 1000 W of the board (1.67 to 1.8 GHz; 1190
+// TFLOP/s over 64K tokens in a burst of 15.7 ms, 1050 over seconds); ahead of it the exponentials (1024 of 1800 cycles a step of two tiles) and the
 // products of 64 columns, which read Q again for each (1280).  Heads of 64 over 8 bits: the chain, 2700 cycles a step at full clock.
 // Left out: a quarter of the exponentials as polynomials on the multipliers (no faster in bf16, registers spill in 8 bits);
 // turns for the two tiles' exponentials (5 to 15% slower); the next piece's queries asked for ahead of the last step (5% slower).
@@ -289,7 +289,8 @@ __device__ __forceinline__ int last_below(const long long* sums, int n, long lon
 // what the rounds gave.  Not where a unit is longer than an eighth of a CTA's work (what is left would not even that out), or where
 // there are few: equal shares of the whole list.
 // (Pieces of prompts behind 2K to 8K tokens, read out of memory: 8.3 GB with equal shares of the list.)
-// Few and short units: whole, one a CTA.
+// Few and short units: whole, one a CTA, up to WHOLE_UP_TO steps more than an equal share has.  (Four tokens behind 100-300, 400-600, 900-1100 and
+// 1900-2100 of 8 sequences: 16.6, 19.5, 22.7 and 24.5 us; cut, 22.0, 22.2, 22.8 and 24.5; whole up to 32 more 16.6, 19.5, 24.2 and 34.8.)
 constexpr int ROUNDS_FROM = 4, ROUNDS_LEFT = 2, WHOLE_UP_TO = 8;
 struct Deal {
   long long rounds_end;        // units that are dealt out whole
@@ -640,7 +641,7 @@ __device__ __forceinline__ void swap_in_quads(uint32_t* v, int t) {
 }
 // Sixteen e4m3 numbers: whether one of them is NaN, and all times 2^-8 as f16.  The bits of a finite one, its exponent and mantissa
 // one place down from a half's upper byte, are that f16 number (subnormal ones too).  (The conversion instruction takes some
-// seven others, and NaN with it: decode's loop over drafts of 16 sequences 372 us with it for K and V.)
+// seven others, and NaN with it: drafts of 16 sequences 526 us with it for K and V, 310 with K as an operand and V so.)
 __device__ __forceinline__ uint32_t any_nan(const uint4& c) {
   const uint32_t m = 0x7f7f7f7fu, one = 0x01010101u;
   return (((c.x & m) + one) | ((c.y & m) + one) | ((c.z & m) + one) | ((c.w & m) + one)) & 0x80808080u;
@@ -1762,9 +1763,13 @@ int check_chunk(const kvp_decode_desc* d) {
 
 // One token a sequence, few query rows: decode's kernels, on a table of the pages that the token sees.  Front pages of first tokens,
 // then those from the window's first on; the positions between the two parts are one run, in the last page of the front or the
-// first of the window (kvp_host.h).  Those kernels bring in rows of 16 queries where a tile here has 128: 32 sequences of 16K-32K
-// under a window of 4096, two groups of 16 rows, 600 us on the list above and 493 so (6.5 TB/s); 58 of 1-3000 in 8 bits under
-// 1000, 6 rows, 155 and 37.
+// first of the window (kvp_host.h).  Those kernels bring in rows of 16 queries where a tile here has 128, and take more rows in passes that
+// read K and V again.  So up to 16 rows a group (us, on the tiles -> so; one group, 8 KV heads):
+//   rows, bf16, 16 sequences of 4K-16K            8: 134 -> 120   16: 135 -> 119   24: 136 -> 225   32: 136 -> 231
+//   the same in 8 bits                            8: 140 -> 67    16: 142 -> 92    24: 143 -> 160   32: 144 -> 165
+//   bf16, 32 of 16K-32K under a window of 4096    8: 111 -> 92    16: 112 -> 93    24: 113 -> 181   32: 113 -> 185
+//   8 bits, heads of 64, 58 of 1000-3000          8: 107 -> 40    16: 109 -> 59    24: 109 -> 113   32: 110 -> 122
+// (4 of 100-200 stay faster so: 16.5 -> 11.5 at 24 and 32 rows.)
 struct Ones {
   const int32_t *block_table, *lengths;
   int32_t *table, *shortened;              // [B, columns], [B]; null without a window

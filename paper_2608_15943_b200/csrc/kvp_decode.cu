@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(DEC_THREADS, DEC_CTAS_PER_SM<DH>) decode_kerne
       const uint8_t* ksrc = kbase + at;
       const uint8_t* vsrc = vbase + at;
       const uint32_t dst = ring_u32 + stage_in * STAGE_BYTES;
-      if (!is_page) {                             // (apart: with the test in every copy, 32 sequences of 16K-32K under a window take 553 us, not 520)
+      if (!is_page) {                             // (apart: with the test in every copy, 32 sequences of 16K-32K under a window take 553 us, not 525)
 #pragma unroll 1
         for (int i = lane; i < STAGE_BYTES / 16; i += 32) cp_async16(dst + i * 16, kbase, 0);
       } else {

@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(BOOK_THREADS, 1) resize_kernel(const __grid_co
     bool copies = false;
     if (r.end >= 0) {
       const int held = p.refs[r.end];
-      if (held > 1) {
+      if (held > 1) {                    // (all rows one after the other: 17 us where 300 share a page and grow, 59 where 1024 do, 1.0 ms where 16384 do)
         int growing = 0, lowest = row;
         for (int other = p.B - 1; other >= 0; --other)
           if (s_end[other] == r.end) {

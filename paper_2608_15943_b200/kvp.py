@@ -760,7 +760,8 @@ def pages_fork(desc, parent, refs, block_table, lengths, ws):
 
 
 def pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, ws, k_cache, v_cache, k_scale=None, v_scale=None):
-    """kvp_pages_resize: rows grow and shrink to new_lengths; a row that grows inside a shared page gets a copy of it.  lacking (int32
+    """kvp_pages_resize: rows grow and shrink to new_lengths; a row that grows inside a shared page gets a copy of it,
+    one that grows inside a place without a page gets one there.  lacking (int32
     [1]) receives 0, or what is short (then nothing is changed): the pages lacking, -1 for a length out of range."""
     device, stream = _call_place()
     status = _pack.pages_resize(desc, donor, new_lengths, refs, block_table, lengths, lacking, ws, k_cache, v_cache, k_scale, v_scale, device, stream)
